@@ -353,6 +353,99 @@ fk_status fk_golden_scores(const void *A, int32_t dtype, int32_t n_q_heads, int3
 fk_status fk_golden_trace(const float *alpha, int32_t n_kv_heads, int32_t T, int32_t budget,
                           int32_t interval, int32_t *kept, void *stream);
 
+/*
+ * ---- The prompt's side: a paged cache, attention of chunks over it, accumulated weights, compression ----
+ *
+ * A prompt is longer than any budget.  Until it is compressed (Section 4.3: once, before decoding) its pairs lie in pages of a pool that
+ * all sequences share:
+ *   K, V        [n_pages][n_kv_heads][page_size][head_dim]  dtype
+ *   page_table  [batch][max_pages] int32   page i of sequence b holds its positions i * page_size .. (i + 1) * page_size - 1
+ *   kv_len      [batch] int32              pairs of every sequence, those of the current chunk among them
+ *   q_start     [batch + 1] int32          tokens q_start[b] .. q_start[b + 1] - 1 of the call are sequence b's chunk (of any length, 0 too);
+ *                                          ascending; tokens outside of all chunks are not touched
+ * Token i of a chunk of c tokens has position p = kv_len[b] - c + i.  Its queries see the pairs j <= p; with window > 0 only those with
+ * j > p - window or j < n_sink (a sliding window, and first tokens that stay visible).  A page_table entry outside [0, n_pages) is a hole:
+ * nothing is stored there and nobody sees its pairs.  kv_len is taken as at most max_pages * page_size; tokens at negative positions are not
+ * stored and see nothing.  Values of pairs that a query does not see, infinities and NaN among them, do not reach its results.
+ * n_tokens is the number of tokens that q, out, stats, k_new and v_new hold.  max_chunk and max_len bound the chunks' and the sequences'
+ * lengths; they only size the launch, results are right beyond them too.
+ */
+typedef struct {
+    int32_t batch;      /* sequences */
+    int32_t n_q_heads;  /* query heads per token */
+    int32_t n_kv_heads; /* KV heads; group size g = n_q_heads / n_kv_heads <= 8 */
+    int32_t head_dim;   /* 64 or 128 */
+    int32_t page_size;  /* pairs per page: a power of two, 16 to 1024 */
+    int32_t n_pages;    /* pages of the pool */
+    int32_t max_pages;  /* entries per row of the page table; max_pages * page_size < 2^24 */
+    int32_t dtype;      /* fk_dtype of q, K, V, out */
+} fk_paged_desc;
+
+/* The new pairs join the cache: K and V of token i of sequence b's chunk, k_new / v_new [n_tokens][n_kv_heads][head_dim], are stored at
+ * their position.  Two sequences may share pages that no chunk of the call is stored to. */
+fk_status fk_paged_append(const fk_paged_desc *desc, void *K, void *V, const int32_t *page_table, const int32_t *kv_len,
+                          const int32_t *q_start, int32_t n_tokens, const void *k_new, const void *v_new, void *stream);
+
+/*
+ * Attention of every chunk over its sequence's pairs (the chunk's own are in the cache: fk_paged_append first), single tokens included:
+ *   out[t][hq][:] = sum_j 2^(s_j - M) V_j / L,  s_j = log2(e) * softmax_scale * <q[t][hq], K_j>,  M = max_j s_j,  L = sum_j 2^(s_j - M)
+ * over the pairs j that the query sees.  q, out: [n_tokens][n_q_heads][head_dim]; stats (may be NULL): [n_tokens][n_q_heads][2] fp32, M and L.  A query
+ * that sees nothing gets zeros and (-inf, 0).  fp32 accumulation; bf16: the weights are rounded to bf16 before they meet V, L is the sum of
+ * the unrounded ones.  workspace: fk_paged_attn_workspace bytes, no initialisation required; calls sharing it must not overlap in time.
+ */
+size_t fk_paged_attn_workspace(const fk_paged_desc *desc, int32_t n_tokens, int32_t max_chunk, int32_t max_len);
+fk_status fk_paged_attn(const fk_paged_desc *desc, const void *q, const void *K, const void *V, const int32_t *page_table,
+                        const int32_t *kv_len, const int32_t *q_start, int32_t n_tokens, int32_t max_chunk, int32_t max_len,
+                        int32_t window, int32_t n_sink, float softmax_scale, void *out, float *stats, void *workspace,
+                        size_t workspace_bytes, void *stream);
+
+/*
+ * The attention weight that every pair received from the chunks' queries, summed over the group's query heads:
+ *   acc[b][h][j] = (j older than the chunk ? acc[b][h][j] : 0) + sum_{t in chunk, t sees j} sum_{hq in group h} 2^(s_j - M) / L
+ * with the M and L that fk_paged_attn gave in stats for the same q, view and scale.  acc: [batch][n_kv_heads][max_pages * page_size] fp32,
+ * the layout of fk_select_keep's scores for a cache of that capacity; slots from kv_len on, and rows of sequences without a chunk, are not
+ * written.  The order of the sums is fixed: equal calls give equal bits.  workspace as for fk_paged_attn.
+ */
+size_t fk_paged_weights_workspace(const fk_paged_desc *desc, int32_t n_tokens, int32_t max_chunk, int32_t max_len);
+fk_status fk_paged_weights(const fk_paged_desc *desc, const void *q, const void *K, const int32_t *page_table, const int32_t *kv_len,
+                           const int32_t *q_start, int32_t n_tokens, int32_t max_chunk, int32_t max_len, int32_t window, int32_t n_sink,
+                           float softmax_scale, const float *stats, float *acc, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * Compression of the prompts into the rows of a budgeted cache (`rows`: same batch, heads, head_dim and dtype): slot j of row (b, h) receives
+ * the pair at position keep_idx[b][h][j], j < min(kv_len[b], budget) - K, V, the position into pos, its accumulated weight into acc_rows -
+ * and len[b][h] = min(kv_len[b], budget).  keep_idx: [batch][n_kv_heads][budget], as fk_select_keep writes it on acc; an entry outside
+ * [0, kv_len[b]) or in a hole leaves its slot as it is.  acc and acc_rows [batch][n_kv_heads][rows->capacity] may both be NULL.  The rows must
+ * not share memory with the pool.
+ */
+fk_status fk_paged_compress(const fk_paged_desc *desc, const void *K, const void *V, const int32_t *page_table, const int32_t *kv_len,
+                            const float *acc, const int32_t *keep_idx, int32_t budget, const fk_cache_desc *rows, void *K_rows,
+                            void *V_rows, int32_t *pos, int32_t *len, float *acc_rows, void *stream);
+
+/*
+ * ---- Eviction by accumulated attention weight ----
+ *
+ * The score that learned ones are compared with: the attention weight a pair has received so far.  Device state, owned by the caller:
+ * acc [batch][n_kv_heads][capacity] fp32, in the layout of fk_select_keep's scores, so that an event is fk_select_keep on acc, then
+ * fk_compact_acc.
+ */
+
+/* Bytes of workspace fk_decode_step_acc needs (0 on bad args); no initialisation required. */
+size_t fk_decode_step_acc_workspace(const fk_cache_desc *desc);
+
+/*
+ * fk_decode_step that also adds the step's attention weights (softmax over the retained set including the new pair, fp32 weights from the
+ * unrounded exponentials), summed over the group's query heads, to acc; the slot of the new pair starts from zero.  Other arguments and
+ * results as fk_decode_step.  Calls sharing a workspace must not overlap in time.
+ */
+fk_status fk_decode_step_acc(const fk_cache_desc *desc, const void *q, void *K, void *V, int32_t *pos, int32_t *len,
+                             const void *k_new, const void *v_new, const int32_t *pos_new, int32_t max_len,
+                             float softmax_scale, float *acc, void *out, void *workspace, size_t workspace_bytes, void *stream);
+
+/* fk_compact that moves the accumulated weights with K, V and pos.  Other arguments and results as fk_compact. */
+fk_status fk_compact_acc(const fk_cache_desc *desc, void *K, void *V, int32_t *pos, float *acc, int32_t *len,
+                         const int32_t *keep_idx, int32_t budget, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -22,12 +22,17 @@ FK_F32, FK_BF16 = 0, 1
 SYMBOLS = ["fk_status_string", "fk_version", "fk_append", "fk_decode_attn_workspace", "fk_decode_attn", "fk_decode_step", "fk_decode_step_packed", "fk_decode_window",
            "fk_decode_step_static", "fk_score_kv", "fk_select_keep", "fk_select_keep_workspace", "fk_select_keep_ws", "fk_select_keep_sampled", "fk_compact", "fk_decode_step_feat_workspace",
            "fk_decode_step_feat", "fk_decode_window_feat", "fk_score_kv_feat", "fk_compact_feat", "fk_golden_steps", "fk_golden_scores",
-           "fk_golden_trace", "fk_stream_read"]
+           "fk_golden_trace", "fk_paged_append", "fk_paged_attn_workspace", "fk_paged_attn", "fk_paged_weights_workspace", "fk_paged_weights",
+           "fk_paged_compress", "fk_decode_step_acc_workspace", "fk_decode_step_acc", "fk_compact_acc", "fk_stream_read"]
 
 
 class fk_cache_desc(ctypes.Structure):
     _fields_ = [("batch", ctypes.c_int32), ("n_q_heads", ctypes.c_int32), ("n_kv_heads", ctypes.c_int32),
                 ("head_dim", ctypes.c_int32), ("capacity", ctypes.c_int32), ("dtype", ctypes.c_int32), ("flags", ctypes.c_int32)]
+
+
+class fk_paged_desc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("batch", "n_q_heads", "n_kv_heads", "head_dim", "page_size", "n_pages", "max_pages", "dtype")]
 
 
 class fk_scorer(ctypes.Structure):
@@ -83,6 +88,16 @@ def lib() -> ctypes.CDLL:
         L.fk_golden_steps.restype, L.fk_golden_steps.argtypes = i32, [i32, i32, i32]
         L.fk_golden_scores.restype, L.fk_golden_scores.argtypes = ctypes.c_int, [vp, i32, i32, i32, i32, ctypes.c_int64, i32, i32, vp, vp, vp]
         L.fk_golden_trace.restype, L.fk_golden_trace.argtypes = ctypes.c_int, [vp, i32, i32, i32, i32, vp, vp]
+        pp = ctypes.POINTER(fk_paged_desc)
+        L.fk_paged_append.restype, L.fk_paged_append.argtypes = ctypes.c_int, [pp, vp, vp, vp, vp, vp, i32, vp, vp, vp]
+        L.fk_paged_attn_workspace.restype, L.fk_paged_attn_workspace.argtypes = sz, [pp, i32, i32, i32]
+        L.fk_paged_attn.restype, L.fk_paged_attn.argtypes = ctypes.c_int, [pp, vp, vp, vp, vp, vp, vp, i32, i32, i32, i32, i32, f32, vp, vp, vp, sz, vp]
+        L.fk_paged_weights_workspace.restype, L.fk_paged_weights_workspace.argtypes = sz, [pp, i32, i32, i32]
+        L.fk_paged_weights.restype, L.fk_paged_weights.argtypes = ctypes.c_int, [pp, vp, vp, vp, vp, vp, i32, i32, i32, i32, i32, f32, vp, vp, vp, sz, vp]
+        L.fk_paged_compress.restype, L.fk_paged_compress.argtypes = ctypes.c_int, [pp, vp, vp, vp, vp, vp, vp, i32, dp, vp, vp, vp, vp, vp, vp]
+        L.fk_decode_step_acc_workspace.restype, L.fk_decode_step_acc_workspace.argtypes = sz, [dp]
+        L.fk_decode_step_acc.restype, L.fk_decode_step_acc.argtypes = ctypes.c_int, [dp, vp, vp, vp, vp, vp, vp, vp, vp, i32, f32, vp, vp, vp, sz, vp]
+        L.fk_compact_acc.restype, L.fk_compact_acc.argtypes = ctypes.c_int, [dp, vp, vp, vp, vp, vp, vp, i32, vp]
         L.fk_stream_read.restype, L.fk_stream_read.argtypes = ctypes.c_int, [vp, sz, vp, vp]
         _lib = L
     return _lib
@@ -343,6 +358,93 @@ def fk_golden_trace(alpha, T: int, budget: int, interval: int, kept, stream=None
     """alpha [n_kv_heads, M, T] fp32; kept [n_kv_heads, M, budget] int32."""
     _call("fk_golden_trace", _ptr(alpha), int(alpha.shape[0]), int(T), int(budget), int(interval), _ptr(kept),
                                  _stream(stream))
+
+
+@dataclass
+class PagedDesc:
+    batch: int
+    n_q_heads: int
+    n_kv_heads: int
+    head_dim: int
+    page_size: int  # a power of two, 16 to 1024
+    n_pages: int  # pages of the pool
+    max_pages: int  # entries per row of the page table
+    dtype: str  # 'f32' | 'bf16'
+
+    def c(self) -> fk_paged_desc:
+        return fk_paged_desc(self.batch, self.n_q_heads, self.n_kv_heads, self.head_dim, self.page_size, self.n_pages, self.max_pages,
+                             FK_F32 if self.dtype == "f32" else FK_BF16)
+
+
+def fk_paged_append(desc: PagedDesc, K, V, page_table, kv_len, q_start, k_new, v_new, stream=None) -> None:
+    """K, V [n_pages, n_kv_heads, page_size, D]; k_new, v_new [n_tokens, n_kv_heads, D]; kv_len counts the chunks already."""
+    _call("fk_paged_append", ctypes.byref(desc.c()), _ptr(K), _ptr(V), _ptr(page_table), _ptr(kv_len), _ptr(q_start), int(k_new.shape[0]), _ptr(k_new),
+          _ptr(v_new), _stream(stream))
+
+
+def fk_paged_attn_workspace(desc: PagedDesc, n_tokens: int, max_chunk: int, max_len: int) -> int:
+    return int(lib().fk_paged_attn_workspace(ctypes.byref(desc.c()), int(n_tokens), int(max_chunk), int(max_len)))
+
+
+def new_paged_attn_workspace(desc: PagedDesc, n_tokens: int, max_chunk: int, max_len: int) -> "torch.Tensor":
+    return torch.empty(max(fk_paged_attn_workspace(desc, n_tokens, max_chunk, max_len), 16), dtype=torch.uint8, device="cuda")
+
+
+def fk_paged_attn(desc: PagedDesc, q, K, V, page_table, kv_len, q_start, max_chunk: int, max_len: int, window: int, n_sink: int,
+                  softmax_scale: float, out, stats, workspace, stream=None) -> None:
+    """Attention of the chunks q [n_tokens, n_q_heads, D] over the paged cache; window 0: every pair up to the query's own is visible.
+    stats [n_tokens, n_q_heads, 2] fp32 or None."""
+    nbytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    _call("fk_paged_attn", ctypes.byref(desc.c()), _ptr(q), _ptr(K), _ptr(V), _ptr(page_table), _ptr(kv_len), _ptr(q_start), int(q.shape[0]),
+          int(max_chunk), int(max_len), int(window), int(n_sink), float(softmax_scale), _ptr(out), _ptr(stats), _ptr(workspace), nbytes, _stream(stream))
+
+
+def fk_paged_weights_workspace(desc: PagedDesc, n_tokens: int, max_chunk: int, max_len: int) -> int:
+    return int(lib().fk_paged_weights_workspace(ctypes.byref(desc.c()), int(n_tokens), int(max_chunk), int(max_len)))
+
+
+def new_paged_weights_workspace(desc: PagedDesc, n_tokens: int, max_chunk: int, max_len: int) -> "torch.Tensor":
+    return torch.empty(max(fk_paged_weights_workspace(desc, n_tokens, max_chunk, max_len), 16), dtype=torch.uint8, device="cuda")
+
+
+def fk_paged_weights(desc: PagedDesc, q, K, page_table, kv_len, q_start, max_chunk: int, max_len: int, window: int, n_sink: int,
+                     softmax_scale: float, stats, acc, workspace, stream=None) -> None:
+    """The weights that the pairs received from the chunks, added to acc [batch, n_kv_heads, max_pages * page_size]; stats from fk_paged_attn."""
+    nbytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    _call("fk_paged_weights", ctypes.byref(desc.c()), _ptr(q), _ptr(K), _ptr(page_table), _ptr(kv_len), _ptr(q_start), int(q.shape[0]), int(max_chunk),
+          int(max_len), int(window), int(n_sink), float(softmax_scale), _ptr(stats), _ptr(acc), _ptr(workspace), nbytes, _stream(stream))
+
+
+def fk_paged_compress(desc: PagedDesc, K, V, page_table, kv_len, acc, keep_idx, budget: int, rows: CacheDesc, K_rows, V_rows, pos, length,
+                      acc_rows, stream=None) -> None:
+    """The kept pairs of the prompts move from their pages into the rows of a budgeted cache; acc and acc_rows may both be None."""
+    _call("fk_paged_compress", ctypes.byref(desc.c()), _ptr(K), _ptr(V), _ptr(page_table), _ptr(kv_len), _ptr(acc), _ptr(keep_idx), int(budget),
+          ctypes.byref(rows.c()), _ptr(K_rows), _ptr(V_rows), _ptr(pos), _ptr(length), _ptr(acc_rows), _stream(stream))
+
+
+def new_acc(desc: CacheDesc) -> "torch.Tensor":
+    """Zero accumulated weights [batch, n_kv_heads, capacity] fp32, in the layout of fk_select_keep's scores."""
+    return torch.zeros((desc.batch, desc.n_kv_heads, desc.capacity), dtype=torch.float32, device="cuda")
+
+
+def fk_decode_step_acc_workspace(desc: CacheDesc) -> int:
+    return int(lib().fk_decode_step_acc_workspace(ctypes.byref(desc.c())))
+
+
+def new_acc_workspace(desc: CacheDesc) -> "torch.Tensor":
+    return torch.empty(max(fk_decode_step_acc_workspace(desc), 16), dtype=torch.uint8, device="cuda")
+
+
+def fk_decode_step_acc(desc: CacheDesc, q, K, V, pos, length, k_new, v_new, pos_new, max_len: int, softmax_scale: float, acc, out, workspace,
+                       stream=None) -> None:
+    """fk_decode_step that also adds the step's attention weights to acc."""
+    nbytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    _call("fk_decode_step_acc", ctypes.byref(desc.c()), _ptr(q), _ptr(K), _ptr(V), _ptr(pos), _ptr(length), _ptr(k_new), _ptr(v_new), _ptr(pos_new),
+          int(max_len), float(softmax_scale), _ptr(acc), _ptr(out), _ptr(workspace), nbytes, _stream(stream))
+
+
+def fk_compact_acc(desc: CacheDesc, K, V, pos, acc, length, keep_idx, budget: int, stream=None) -> None:
+    _call("fk_compact_acc", ctypes.byref(desc.c()), _ptr(K), _ptr(V), _ptr(pos), _ptr(acc), _ptr(length), _ptr(keep_idx), int(budget), _stream(stream))
 
 
 def fk_stream_read(src, sink, stream=None) -> None:

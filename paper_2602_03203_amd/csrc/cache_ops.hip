@@ -1,4 +1,5 @@
-// fk_append, fk_compact and fk_compact_feat: the calls that rewrite the cache (and the attention-feature state).
+// fk_append, fk_compact, fk_compact_feat and fk_compact_acc: the calls that rewrite the cache (and the attention-feature state, the accumulated
+// weights).
 #include "fk_common.h"
 
 namespace fk {
@@ -93,7 +94,8 @@ __device__ __forceinline__ void feat_roll(float4* __restrict__ feat, int row, in
 // [tT, (t+1)T); a source of any later tile is >= (t+1)T, and every source of tile t or of an
 // earlier tile has already been read, so no live source is overwritten.  What does not move is neither
 // read nor written, but for slot 0 in its place where there are few workgroups.
-// grid.x = row, grid.y = tensor * slices + slice (K slices, then V slices), last y = pos; Q4 > 0: the attention features before them
+// grid.x = row, grid.y = tensor * slices + slice (K slices, then V slices), then pos, then, where there are any, the accumulated weights; Q4 > 0: the
+// attention features before them
 // ---------------------------------------------------------------------------------------
 static constexpr int kSliceChunks = 8;  // 16-byte chunks per column slice
 typedef unsigned int u32x4_t __attribute__((ext_vector_type(4)));
@@ -108,7 +110,7 @@ __global__ __launch_bounds__(kCompactThreads) __attribute__((amdgpu_waves_per_eu
                                                                   int32_t* __restrict__ pos, float4* __restrict__ feat,
                                                                   int32_t* __restrict__ len,
                                                                   const int32_t* __restrict__ keep,
-                                                                  int cap, int budget, int chunks) {
+                                                                  int cap, int budget, int chunks, int32_t* __restrict__ acc) {
     const int row = blockIdx.x, part = (int)blockIdx.y - (Q4 > 0);
     if constexpr (Q4 > 0) {
         if (part < 0) {
@@ -122,9 +124,9 @@ __global__ __launch_bounds__(kCompactThreads) __attribute__((amdgpu_waves_per_eu
     const int n = cap;
     const int32_t* kp = keep + (size_t)row * budget;
     const int slices = chunks / kSliceChunks;
-    if (part == 2 * slices) {
-        if (Q4 == 0 && threadIdx.x == 0 && len[row] > budget) len[row] = budget;
-        int32_t* p = pos + (size_t)row * cap;
+    if (part >= 2 * slices) {   // the positions; one workgroup further, with acc, the accumulated weights (four bytes a slot as well)
+        if (Q4 == 0 && part == 2 * slices && threadIdx.x == 0 && len[row] > budget) len[row] = budget;
+        int32_t* p = (part == 2 * slices ? pos : acc) + (size_t)row * cap;
         for (int base = 0; base < budget; base += kCompactThreads * U) {
             int32_t val[U];
             int src[U];
@@ -325,7 +327,22 @@ extern "C" fk_status fk_compact(const fk_cache_desc* desc, void* K, void* V, int
     const int rows = desc->batch * desc->n_kv_heads;
     hipStream_t st = (hipStream_t)stream;
     hipLaunchKernelGGL(compact_kernel_for<0>(rows * 2ll * (chunks / kSliceChunks), rows, budget, desc->capacity), dim3(rows, 2 * (chunks / kSliceChunks) + 1), dim3(kCompactThreads), 0, st, (uint4*)K, (uint4*)V,
-                       pos, nullptr, len, keep_idx, desc->capacity, budget, chunks);
+                       pos, nullptr, len, keep_idx, desc->capacity, budget, chunks, nullptr);
+    return launch_status();
+}
+
+extern "C" fk_status fk_compact_acc(const fk_cache_desc* desc, void* K, void* V, int32_t* pos, float* acc, int32_t* len,
+                                    const int32_t* keep_idx, int32_t budget, void* stream) {
+    fk_status s = check_desc(desc);
+    if (s != FK_OK) return s;
+    if (!K || !V || !pos || !acc || !len || !keep_idx) return FK_ERR_INVALID_ARG;
+    if (budget <= 0 || budget > desc->capacity) return FK_ERR_INVALID_ARG;
+    if (!aligned16(K) || !aligned16(V) || !aligned16(acc)) return FK_ERR_INVALID_ARG;
+    const int chunks = desc->head_dim * (desc->dtype == FK_F32 ? 4 : 2) / 16;
+    const int rows = desc->batch * desc->n_kv_heads;
+    hipLaunchKernelGGL(compact_kernel_for<0>(rows * 2ll * (chunks / kSliceChunks), rows, budget, desc->capacity), dim3(rows, 2 * (chunks / kSliceChunks) + 2),
+                       dim3(kCompactThreads), 0, (hipStream_t)stream, (uint4*)K, (uint4*)V, pos, nullptr, len, keep_idx, desc->capacity, budget, chunks,
+                       reinterpret_cast<int32_t*>(acc));
     return launch_status();
 }
 
@@ -343,6 +360,6 @@ extern "C" fk_status fk_compact_feat(const fk_cache_desc* desc, void* K, void* V
     const long long workgroups = rows * 2ll * (chunks / kSliceChunks);
     const auto kern = g <= 4 ? compact_kernel_for<1>(workgroups, rows, budget, desc->capacity) : compact_kernel_for<2>(workgroups, rows, budget, desc->capacity);
     hipLaunchKernelGGL(kern, dim3(rows, 2 * (chunks / kSliceChunks) + 2), dim3(kCompactThreads), 0, st, (uint4*)K, (uint4*)V, pos,
-                       (float4*)feat, len, keep_idx, desc->capacity, budget, chunks);
+                       (float4*)feat, len, keep_idx, desc->capacity, budget, chunks, nullptr);
     return launch_status();
 }
