@@ -14,6 +14,26 @@ struct PagedParams {
     bool negate;
 };
 
+// A value that is the same for every lane, in a scalar register.  (Opaque first: the builtin is dropped where the compiler knows as much; it then
+// keeps what integer divisions gave, and all that follows from it, in vector registers: page numbers by vector loads, branches by exec masks, 60
+// registers more.)
+__device__ __forceinline__ int scalar(int x) {
+    asm volatile("" : "+v"(x));
+    return __builtin_amdgcn_readfirstlane(x);
+}
+
+template <typename T> __device__ __forceinline__ const T* scalar_ptr(const T* p) {
+    const uint64_t x = reinterpret_cast<uint64_t>(p);
+    const uint32_t lo = (uint32_t)scalar((int)(uint32_t)x), hi = (uint32_t)scalar((int)(uint32_t)(x >> 32));
+    return reinterpret_cast<const T*>((uint64_t)hi << 32 | lo);
+}
+
+// An element of an array that nothing writes during the launch, at an index that is the same for a whole wavefront: a scalar load.  (Vector loads
+// return in order: waiting for a page number would mean waiting for all pairs sent for before it.)
+__device__ __forceinline__ int load_uniform(const int32_t* p, int i) {
+    return ((const __attribute__((address_space(4))) int32_t*)p)[i];
+}
+
 // Tokens of sequence b in the packed buffers, and its pairs; whatever the arrays hold, inside the buffers.
 __device__ __forceinline__ int chunk_begin(const PagedParams& P, int b) { return min(max(P.q_start[b], 0), P.n_tokens); }
 __device__ __forceinline__ int chunk_end(const PagedParams& P, int b, int begin) { return min(max(P.q_start[b + 1], begin), P.n_tokens); }
@@ -33,6 +53,98 @@ __device__ __forceinline__ int sequence_of(const PagedParams& P, int t) {
 }
 
 __device__ __forceinline__ bool sees(const PagedParams& P, int p, int j) { return j <= p && (j > p - P.window || j < P.sink); }
+
+// ---- tiles of query rows --------------------------------------------------------------------------------------------
+// The queries of a (chunk, KV head) are rows: row r is head r % g of token r / g.  A tile is TM of them.  `slot` counts the places of a launch:
+// either place i of sequence b is slot i * batch + b (spread == false; a sequence has `per_seq` places, whose workgroups take every
+// per_seq-th of its tiles), or the slots are dealt to the tiles there are, sequence after sequence (`places` of them).  A sequence's last
+// tiles come first: they see the most.
+struct TileGrid {
+    bool spread;
+    int places;     // slots in all
+    int per_seq;
+    int least, most;   // rows of the chunks that the launch takes: least <= nq * g <= most
+};
+
+struct TileOf {
+    int b, begin, nq, n, first;   // sequence, its first token, tokens, pairs, position of the first token
+    int tile, step;               // tiles tile, tile - step, .. >= 0
+    bool one;                     // no more tiles than places: each has its own
+};
+
+__device__ __forceinline__ bool chunk_of(const PagedParams& P, const TileGrid& G, int b, TileOf& t, int tm, int& tiles) {
+    t.b = b;
+    t.begin = chunk_begin(P, b);
+    t.nq = chunk_end(P, b, t.begin) - t.begin;
+    const int rows = t.nq * P.g;
+    tiles = rows >= G.least && rows <= G.most ? (rows + tm - 1) / tm : 0;
+    return tiles > 0;
+}
+
+// false: the slot has no tile
+__device__ __forceinline__ bool tile_of(const PagedParams& P, const TileGrid& G, int slot, int tm, TileOf& t) {
+    int tiles;
+    if (!G.spread) {
+        const int i = slot / P.batch;
+        if (!chunk_of(P, G, slot - i * P.batch, t, tm, tiles) || i >= tiles) return false;
+        t.tile = tiles - 1 - i;
+        t.step = G.per_seq;
+        t.one = tiles <= G.per_seq;
+    } else {
+        const int lane = threadIdx.x & (kWave - 1);
+        int left = slot, found = -1, at = 0;
+        for (int base = 0; base < P.batch && found < 0; base += kWave) {
+            int mine = 0;
+            if (base + lane < P.batch) chunk_of(P, G, base + lane, t, tm, mine);
+            int incl = mine;
+#pragma unroll
+            for (int off = 1; off < kWave; off <<= 1) {
+                const int o = __shfl_up(incl, off);
+                if (lane >= off) incl += o;
+            }
+            const unsigned long long m = __ballot(incl > left);
+            if (m) {
+                const int src = __ffsll((long long)m) - 1;
+                found = base + src;
+                at = left - __shfl(incl - mine, src);
+            } else {
+                left -= __shfl(incl, kWave - 1);
+            }
+        }
+        found = scalar(found);
+        if (found < 0) return false;
+        chunk_of(P, G, found, t, tm, tiles);
+        t.tile = tiles - 1 - scalar(at);
+        t.step = 1 << 30;   // (as many slots as there can be tiles)
+        t.one = true;
+    }
+    // (the same for every lane, which the compiler is told: branches on them are scalar)
+    t.b = scalar(t.b);
+    t.begin = scalar(t.begin);
+    t.nq = scalar(t.nq);
+    t.tile = scalar(t.tile);
+    t.step = scalar(t.step);
+    t.n = min(max(load_uniform(P.kv_len, t.b), 0), P.max_pages << P.page_shift);
+    t.first = t.n - t.nq;
+    return true;
+}
+
+// The key tiles of kt pairs that rows at positions lo .. hi see something of: na tiles from the first on, then those from b0 to b1.
+struct KeyTiles {
+    int na, b0, total;
+    __device__ __forceinline__ int at(int i) const { return i < na ? i : i - na + b0; }
+};
+__device__ __forceinline__ KeyTiles key_tiles(const PagedParams& P, int lo, int hi, int kt) {
+    KeyTiles k;
+    const int end = hi + 1;                                         // pairs up to here
+    const int from = P.window == 0x7fffffff ? 0 : max(0, lo - P.window + 1);
+    k.na = (min(P.sink, max(end, 0)) + kt - 1) / kt;
+    k.b0 = from / kt;
+    if (k.b0 <= k.na) k.na = k.b0 = 0;
+    const int b1 = (max(end, 0) + kt - 1) / kt;
+    k.total = k.na + max(b1 - k.b0, 0);
+    return k;
+}
 
 // ---- host side ---------------------------------------------------------------------------------------------------
 inline fk_status check_paged(const fk_paged_desc* d) {
@@ -54,6 +166,14 @@ inline fk_status check_chunks(const fk_paged_desc* d, int32_t n_tokens, int32_t 
     if (n_tokens < 0 || max_chunk <= 0 || max_len <= 0 || (int64_t)max_len > (int64_t)d->max_pages * d->page_size) return FK_ERR_INVALID_ARG;
     if ((int64_t)n_tokens * d->n_q_heads >= (1 << 28)) return FK_ERR_UNSUPPORTED;
     return FK_OK;
+}
+
+// Places for the tiles of tm rows of a call, without knowing the chunks
+inline TileGrid tile_grid(const fk_paged_desc* d, int32_t n_tokens, int32_t max_chunk, int tm) {
+    const long long g = d->n_q_heads / d->n_kv_heads, most = (long long)n_tokens * g / tm + d->batch;
+    const long long chunk = max_chunk < n_tokens ? max_chunk : n_tokens > 0 ? n_tokens : 1, per_seq = (chunk * g + tm - 1) / tm;
+    if (per_seq * d->batch <= 2 * most) return {false, (int)(per_seq * d->batch), (int)per_seq, 1, 0x7fffffff};
+    return {true, (int)most, 1, 1, 0x7fffffff};
 }
 
 inline PagedParams paged_params(const fk_paged_desc* d, const int32_t* table, const int32_t* kv_len, const int32_t* q_start, int32_t n_tokens) {

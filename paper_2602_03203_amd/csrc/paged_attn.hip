@@ -1,6 +1,6 @@
 // fk_paged_attn and fk_paged_weights: attention of chunks over the pages of a prompt, and the weights that its pairs received.
 // One workgroup per (token, KV head), a thread per key: the plain form.
-#include "paged.h"
+#include "thin.h"
 #include <climits>
 #include <cmath>
 
@@ -9,74 +9,6 @@ namespace fk {
 template <typename T> __device__ __forceinline__ float load1(const T* p);
 template <> __device__ __forceinline__ float load1<float>(const float* p) { return *p; }
 template <> __device__ __forceinline__ float load1<bf16_t>(const bf16_t* p) { return bf16_lo(*p); }
-
-template <typename T>
-__global__ __launch_bounds__(256) void paged_attn_plain_kernel(const PagedParams P, T* out, float2* stats, int D) {
-    const int t = blockIdx.x, h = blockIdx.y, tid = threadIdx.x;
-    const int b = sequence_of(P, t);
-    if (b < 0) return;
-    const int begin = chunk_begin(P, b), p = pairs_of(P, b) - (chunk_end(P, b, begin) - t);
-    __shared__ float s_q[8][128], s_p[8][256], s_red[256], s_o[256][8];
-    const T *q = reinterpret_cast<const T*>(P.q), *K = reinterpret_cast<const T*>(P.K), *V = reinterpret_cast<const T*>(P.V);
-    for (int i = tid; i < P.g * D; i += 256) s_q[i / D][i % D] = load1(q + ((size_t)t * P.n_kv + h) * P.g * D + i);
-    __syncthreads();
-    float m[8], l[8], o[8];
-    for (int k = 0; k < 8; ++k) {
-        m[k] = -INFINITY;
-        l[k] = o[k] = 0.f;
-    }
-    const int d = tid % D, part = tid / D, parts = 256 / D;
-    for (int base = 0; base <= p; base += 256) {
-        const int j = base + tid;
-        const int page = j <= p ? P.table[(size_t)b * P.max_pages + (j >> P.page_shift)] : -1;
-        const bool seen = sees(P, p, j) && page_ok(P, page);
-        const T* kr = K + ((((size_t)(seen ? page : 0) * P.n_kv + h) << P.page_shift) + (j & ((1 << P.page_shift) - 1))) * D;
-        for (int k = 0; k < P.g; ++k) {
-            float s = 0.f;
-            if (seen)
-                for (int e = 0; e < D; ++e) s = fmaf(s_q[k][e], load1(kr + e), s);
-            s = seen ? s * P.scale_log2e * (P.negate ? -1.f : 1.f) : -INFINITY;
-            s_red[tid] = s;
-            __syncthreads();
-            for (int w = 128; w; w /= 2) {
-                if (tid < w) s_red[tid] = fmaxf(s_red[tid], s_red[tid + w]);
-                __syncthreads();
-            }
-            const float mn = fmaxf(m[k], s_red[0]), ref = mn == -INFINITY ? 0.f : mn, c = exp2f(m[k] - ref);
-            __syncthreads();
-            m[k] = mn;
-            l[k] *= c;
-            o[k] *= c;
-            s_p[k][tid] = seen ? exp2f(s - ref) : -1.f;   // -1: not seen
-        }
-        __syncthreads();
-        for (int x = part; x < 256 && base + x <= p; x += parts) {
-            if (s_p[0][x] == -1.f) continue;
-            const int jj = base + x, pg = P.table[(size_t)b * P.max_pages + (jj >> P.page_shift)];
-            const float v = load1(V + ((((size_t)pg * P.n_kv + h) << P.page_shift) + (jj & ((1 << P.page_shift) - 1))) * D + d);
-            for (int k = 0; k < P.g; ++k) {
-                o[k] = fmaf(s_p[k][x], v, o[k]);
-                l[k] += s_p[k][x];
-            }
-        }
-        __syncthreads();
-    }
-    for (int k = 0; k < P.g; ++k) s_o[tid][k] = o[k];
-    for (int k = 0; k < P.g; ++k) s_p[k][tid] = l[k];
-    __syncthreads();
-    if (part == 0) {
-        for (int k = 0; k < P.g; ++k) {
-            float a = 0.f, s = 0.f;
-            for (int x = 0; x < parts; ++x) {
-                a += s_o[x * D + d][k];
-                s += s_p[k][x * D + d];
-            }
-            const size_t row = ((size_t)t * P.n_kv + h) * P.g + k;
-            store_out(out + row * D + d, m[k] == -INFINITY ? 0.f : a / s);
-            if (stats && d == 0) stats[row] = make_float2(m[k], s);
-        }
-    }
-}
 
 template <typename T>
 __global__ __launch_bounds__(256) void paged_weights_plain_kernel(const PagedParams P, const float2* stats, float* acc, int D) {
@@ -129,7 +61,7 @@ static PagedParams view_params(const fk_paged_desc* desc, const void* q, const v
 
 extern "C" size_t fk_paged_attn_workspace(const fk_paged_desc* desc, int32_t n_tokens, int32_t max_chunk, int32_t max_len) {
     if (check_paged(desc) != FK_OK || check_chunks(desc, n_tokens, max_chunk, max_len) != FK_OK) return 0;
-    return 16;
+    return 16 + thin_paged_workspace(desc, tile_grid(desc, n_tokens, max_chunk, 16), max_len);
 }
 
 extern "C" fk_status fk_paged_attn(const fk_paged_desc* desc, const void* q, const void* K, const void* V, const int32_t* page_table,
@@ -143,14 +75,17 @@ extern "C" fk_status fk_paged_attn(const fk_paged_desc* desc, const void* q, con
     if (n_tokens == 0) return FK_OK;
     PagedParams P = view_params(desc, q, K, page_table, kv_len, q_start, n_tokens, window, n_sink, softmax_scale);
     P.V = V;
-    const dim3 grid(n_tokens, desc->n_kv_heads);
-    if (desc->dtype == FK_F32) hipLaunchKernelGGL(paged_attn_plain_kernel<float>, grid, dim3(256), 0, (hipStream_t)stream, P, (float*)out, (float2*)stats, desc->head_dim);
-    else hipLaunchKernelGGL(paged_attn_plain_kernel<bf16_t>, grid, dim3(256), 0, (hipStream_t)stream, P, (bf16_t*)out, (float2*)stats, desc->head_dim);
-    return launch_status();
+    ThinParams T = {};
+    T.view = P;
+    T.out = out;
+    T.stats = reinterpret_cast<float2*>(stats);
+    T.grid = tile_grid(desc, n_tokens, max_chunk, 16);
+    return thin_paged(desc, T, max_len, workspace, (hipStream_t)stream);
 }
 
 extern "C" size_t fk_paged_weights_workspace(const fk_paged_desc* desc, int32_t n_tokens, int32_t max_chunk, int32_t max_len) {
-    return fk_paged_attn_workspace(desc, n_tokens, max_chunk, max_len);
+    if (check_paged(desc) != FK_OK || check_chunks(desc, n_tokens, max_chunk, max_len) != FK_OK) return 0;
+    return 16;
 }
 
 extern "C" fk_status fk_paged_weights(const fk_paged_desc* desc, const void* q, const void* K, const int32_t* page_table, const int32_t* kv_len,
