@@ -1,0 +1,246 @@
+// fk_paged_weights: acc_j += sum over the chunk's queries that see pair j, over the group's heads, of 2^(s - M) / L.
+//
+// A wavefront owns KG * 16 keys, whose K stays in registers as matrix operands; the chunk's query rows (tokens x heads) pass by in
+// tiles of 64 through LDS, with their M and 1 / L, shared by the four wavefronts.  A product of 16 keys x 16 rows leaves a lane with four keys of
+// ONE row, so M and 1 / L are one register each and a pair's weight is added by one fma; the 16 lanes of a key are summed once, at the end.
+// The order of all sums is fixed.  The products are those of the attention kernels, step by step the same ones, so that logits are the same
+// bits: beyond 2^24, where a logit's rounding is more than an exponent may be off, M still belongs to them.
+//
+// Bound by matrix and vector instructions together: per 16 x 16 logits D / 32 products and, per lane, four times an fma, an exponential and an fma.
+// Few keys and many queries: the queries are split over workgroups too, partial sums meet in a second launch.
+#include "weights.h"
+#include "window.h"
+
+namespace fk {
+
+typedef __attribute__((ext_vector_type(8))) __bf16 wbf16x8_t;
+typedef __attribute__((ext_vector_type(4))) float wf32x4_t;
+typedef __attribute__((ext_vector_type(4))) uint32_t wu32x4_t;
+union W128 {
+    wu32x4_t u;
+    float f[4];
+    wbf16x8_t v;
+};
+
+template <typename T, int D> struct WeightsCfg {
+    static constexpr bool BF = sizeof(T) == 2;
+    static constexpr int CH = D * (int)sizeof(T) / 16, KS = CH / 4;
+    static constexpr int KG = BF || D == 64 ? 4 : 2;      // groups of 16 keys per wavefront
+    static constexpr int KEYS = 4 * KG * 16;              // of a workgroup
+    static constexpr int QT = BF ? 64 : 32;               // query rows of a tile
+    static constexpr int QRS = CH * 16 + 16;              // byte stride of a row in LDS
+    static constexpr int LD = QT * CH / 256;              // 16-byte loads of a tile per thread
+};
+
+// |logits| from which products and maxima are subtracted as rounded numbers, not inside an fma
+static constexpr float kHugeLogit = 16777216.f;
+
+template <typename T, int D>
+__global__ __launch_bounds__(256, 2) void weights_kernel(const WeightsParams P) {
+    using C = WeightsCfg<T, D>;
+    constexpr bool BF = C::BF;
+    constexpr int CH = C::CH, KS = C::KS, KG = C::KG, QT = C::QT, QRS = C::QRS, LD = C::LD;
+    const PagedParams& W = P.view;
+    const int tid = threadIdx.x, lane = tid & (kWave - 1), n16 = lane & 15, quad = lane >> 4, wave = scalar(tid / kWave);
+    const int place = scalar(blockIdx.x / W.n_kv), h = (int)blockIdx.x - place * W.n_kv, b = scalar(place / P.blocks), split = blockIdx.y;
+    const int g = W.g;
+    __shared__ __attribute__((aligned(16))) unsigned char s_q[2][QT * QRS];
+    __shared__ float s_m[2][QT], s_il[2][QT];
+
+    const int begin = scalar(chunk_begin(W, b)), nq = scalar(chunk_end(W, b, begin)) - begin, n = scalar(pairs_of(W, b)), first = n - nq;
+    if (nq == 0) return;
+    auto token_of = [&](int row) { return g == 1 ? row : (int)__umulhi((uint32_t)row, P.g_magic); };
+    const float scale = W.scale_log2e;
+    for (int k0 = (place - b * P.blocks) * C::KEYS; k0 < n; k0 += P.blocks * C::KEYS) {
+        const int k1 = min(k0 + C::KEYS, n);
+        // tokens that see any of these keys: from position k0 on, and under a window up to the last key's reach
+        int t0 = max(k0 - first, 0), t1 = nq;
+        if (W.window != 0x7fffffff && k0 >= W.sink) t1 = min((long long)nq, max(0ll, (long long)k1 - 1 + W.window - first));
+        const int row_lo = t0 * g, row_hi = max(t1, t0) * g;
+        const int tiles = (row_hi - row_lo + QT - 1) / QT, per = scalar((tiles + P.splits - 1) / P.splits);
+        const int i0 = min(split * per, tiles), i1 = min(i0 + per, tiles);
+
+        const int kw = k0 + wave * (KG * 16);   // the wavefront's keys
+        W128 k[KG][KS];
+        bool there[KG];
+        const int32_t* tab = scalar_ptr(W.table + (size_t)b * W.max_pages);
+#pragma unroll
+        for (int j = 0; j < KG; ++j) {
+            const int key = kw + j * 16;
+            const int page = key < n ? load_uniform(tab, min(key >> W.page_shift, W.max_pages - 1)) : -1;
+            there[j] = page_ok(W, page);
+            const wu32x4_t* run = reinterpret_cast<const wu32x4_t*>(W.K) +
+                                  ((((size_t)(there[j] ? page : 0) * W.n_kv + h) << W.page_shift) + (key & ((1 << W.page_shift) - 1)) + n16) * CH;
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks) {
+                k[j][ks].u = run[ks * 4 + quad];
+                if (W.negate) k[j][ks].u ^= BF ? 0x80008000u : 0x80000000u;
+            }
+        }
+        wf32x4_t a[KG];
+#pragma unroll
+        for (int j = 0; j < KG; ++j) a[j] = (wf32x4_t){0.f, 0.f, 0.f, 0.f};
+
+        W128 qr[LD];
+        float2 st;
+        auto fetch = [&](int i) {
+            const int base = row_lo + i * QT;
+#pragma unroll
+            for (int u = 0; u < LD; ++u) {
+                const int x = tid + u * 256, row = min(base + x / CH, row_hi - 1), tok = token_of(row);
+                qr[u].u = reinterpret_cast<const wu32x4_t*>(W.q)[(((size_t)(begin + tok) * W.n_kv + h) * g + (row - tok * g)) * CH + x % CH];
+            }
+            const int row = base + tid % QT, rc = min(row, row_hi - 1), tok = token_of(rc);
+            st = P.stats[((size_t)(begin + tok) * W.n_kv + h) * g + (rc - tok * g)];
+            if (row >= row_hi || st.y == 0.f) st = make_float2(0.f, INFINITY);   // no query, or one that sees nothing: weight 0
+        };
+        auto stage = [&](int buf) {
+#pragma unroll
+            for (int u = 0; u < LD; ++u) {
+                const int x = tid + u * 256;
+                *reinterpret_cast<wu32x4_t*>(s_q[buf] + x / CH * QRS + x % CH * 16) = qr[u].u;
+            }
+            if (tid < QT) {
+                s_m[buf][tid] = st.x;
+                s_il[buf][tid] = 1.0f / st.y;
+            }
+        };
+        if (i0 < i1) {
+            fetch(i0);
+            stage(0);
+        }
+        __syncthreads();
+        for (int i = i0, buf = 0; i < i1; ++i, buf ^= 1) {
+            if (i + 1 < i1) fetch(i + 1);
+            const int base = row_lo + i * QT;
+#pragma unroll
+            for (int qt = 0; qt < QT / 16; ++qt) {
+                const int r0 = base + qt * 16;
+                if (r0 >= row_hi) break;
+                W128 q[KS];
+#pragma unroll
+                for (int ks = 0; ks < KS; ++ks) q[ks].u = *reinterpret_cast<const wu32x4_t*>(s_q[buf] + (qt * 16 + n16) * QRS + (ks * 4 + quad) * 16);
+                const float m = s_m[buf][qt * 16 + n16], il = s_il[buf][qt * 16 + n16];
+                const int lo = first + scalar(token_of(r0)), hi = first + scalar(token_of(min(r0 + 15, row_hi - 1)));   // positions
+                wf32x4_t c[KG];
+#pragma unroll
+                for (int j = 0; j < KG; ++j) {
+                    c[j] = (wf32x4_t){0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                    for (int ks = 0; ks < KS; ++ks) {
+                        if constexpr (BF) {
+                            c[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k[j][ks].v, q[ks].v, c[j], 0, 0, 0);
+                        } else {
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) c[j] = __builtin_amdgcn_mfma_f32_16x16x4f32(k[j][ks].f[e], q[ks].f[e], c[j], 0, 0, 0);
+                        }
+                    }
+                }
+                if (__any(fabsf(m) >= kHugeLogit)) {
+#pragma unroll
+                    for (int j = 0; j < KG; ++j)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) c[j][e] = attn_logit(c[j][e], scale) - m;
+                } else {
+#pragma unroll
+                    for (int j = 0; j < KG; ++j)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) c[j][e] = fmaf(c[j][e], scale, -m);
+                }
+                const bool whole = kw + KG * 16 <= lo + 1 && r0 + 16 <= row_hi && (W.window == 0x7fffffff || kw > hi - W.window || kw + KG * 16 <= W.sink);
+                if (!whole) {
+                    const int row = r0 + n16, p = row < row_hi ? first + token_of(row) : -1;
+                    const int from = W.window == 0x7fffffff ? -1 : p - W.window;
+#pragma unroll
+                    for (int j = 0; j < KG; ++j)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            const int key = kw + j * 16 + quad * 4 + e;
+                            const bool seen = (key <= p) & ((key > from) | (key < W.sink));
+                            c[j][e] = seen ? c[j][e] : -INFINITY;
+                        }
+                }
+#pragma unroll
+                for (int j = 0; j < KG; ++j)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) a[j][e] = fmaf(__builtin_amdgcn_exp2f(c[j][e]), il, a[j][e]);
+            }
+            if (i + 1 < i1) stage(buf ^ 1);
+            __syncthreads();
+        }
+        // the 16 rows of a key, then one lane a key
+        const size_t row = (size_t)b * W.n_kv + h;
+#pragma unroll
+        for (int j = 0; j < KG; ++j) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const float s = group_sum<16>(a[j][e]);
+                const int key = kw + j * 16 + quad * 4 + e;
+                if (n16 != e || key >= n) continue;
+                const float w = there[j] ? s : 0.f;
+                if (P.splits > 1) {
+                    if (key < P.part_len) P.part[((size_t)split * W.batch * W.n_kv + row) * P.part_len + key] = w;
+                } else {
+                    float* x = P.acc + row * ((size_t)W.max_pages << W.page_shift) + key;
+                    *x = (key >= first ? 0.f : *x) + w;
+                }
+            }
+        }
+    }
+}
+
+// partial sums of the splits, in their order
+__global__ __launch_bounds__(256) void weights_sum_kernel(const WeightsParams P) {
+    const PagedParams& W = P.view;
+    const int row = blockIdx.y, b = row / W.n_kv, key = blockIdx.x * 256 + threadIdx.x;
+    const int begin = chunk_begin(W, b), nq = chunk_end(W, b, begin) - begin, n = pairs_of(W, b);
+    if (nq == 0 || key >= n) return;
+    float s = 0.f;
+    for (int i = 0; i < P.splits; ++i) s += P.part[((size_t)i * W.batch * W.n_kv + row) * P.part_len + key];
+    float* x = P.acc + (size_t)row * ((size_t)W.max_pages << W.page_shift) + key;
+    *x = (key >= n - nq ? 0.f : *x) + s;
+}
+
+// ---- host side ---------------------------------------------------------------------------------------------------
+// Queries are split where the keys alone leave CUs without a workgroup, into no less than four tiles.  Partial sums are kept up to the table's
+// length, so that a length hint below a sequence's length loses nothing.
+static int weights_splits(const fk_paged_desc* d, int n_tokens, int max_chunk, int max_len, int keys, int qt) {
+    const long long blocks = (long long)d->batch * d->n_kv_heads * ((max_len + keys - 1) / keys);
+    const long long rows = (long long)(max_chunk < n_tokens ? max_chunk : n_tokens) * (d->n_q_heads / d->n_kv_heads);
+    long long s = 512 / blocks;
+    if (s > rows / (4 * qt)) s = rows / (4 * qt);
+    if (s > 16) s = 16;
+    return s < 1 || (long long)d->batch * d->n_kv_heads > 65535 ? 1 : (int)s;
+}
+
+template <typename T, int D> static int weights_splits_of(const fk_paged_desc* d, int n_tokens, int max_chunk, int max_len) {
+    return weights_splits(d, n_tokens, max_chunk, max_len, WeightsCfg<T, D>::KEYS, WeightsCfg<T, D>::QT);
+}
+static int weights_splits_for(const fk_paged_desc* d, int n_tokens, int max_chunk, int max_len) {
+    if (d->dtype == FK_F32) return d->head_dim == 64 ? weights_splits_of<float, 64>(d, n_tokens, max_chunk, max_len) : weights_splits_of<float, 128>(d, n_tokens, max_chunk, max_len);
+    return d->head_dim == 64 ? weights_splits_of<bf16_t, 64>(d, n_tokens, max_chunk, max_len) : weights_splits_of<bf16_t, 128>(d, n_tokens, max_chunk, max_len);
+}
+
+size_t weights_workspace(const fk_paged_desc* d, int n_tokens, int max_chunk, int max_len) {
+    const int s = weights_splits_for(d, n_tokens, max_chunk, max_len);
+    return s > 1 ? (size_t)s * d->batch * d->n_kv_heads * d->max_pages * d->page_size * sizeof(float) : 0;
+}
+
+template <typename T, int D>
+static fk_status weights_run(const fk_paged_desc* d, WeightsParams& P, int max_len, hipStream_t st) {
+    P.blocks = (max_len + WeightsCfg<T, D>::KEYS - 1) / WeightsCfg<T, D>::KEYS;
+    hipLaunchKernelGGL((weights_kernel<T, D>), dim3((unsigned)(d->batch * d->n_kv_heads * (long long)P.blocks), P.splits), dim3(256), 0, st, P);
+    if (P.splits > 1) hipLaunchKernelGGL(weights_sum_kernel, dim3((P.part_len + 255) / 256, d->batch * d->n_kv_heads), dim3(256), 0, st, P);
+    return launch_status();
+}
+
+fk_status weights_launch(const fk_paged_desc* d, WeightsParams P, int max_chunk, int max_len, void* ws, hipStream_t st) {
+    P.splits = weights_splits_for(d, P.view.n_tokens, max_chunk, max_len);
+    P.part = static_cast<float*>(ws);
+    P.part_len = d->max_pages * d->page_size;
+    P.g_magic = (uint32_t)(((1ull << 32) + P.view.g - 1) / P.view.g);   // row * g_magic >> 32 = row / g for rows below 2^28 and g from 2 on
+    if (d->dtype == FK_F32) return d->head_dim == 64 ? weights_run<float, 64>(d, P, max_len, st) : weights_run<float, 128>(d, P, max_len, st);
+    return d->head_dim == 64 ? weights_run<bf16_t, 64>(d, P, max_len, st) : weights_run<bf16_t, 128>(d, P, max_len, st);
+}
+
+}  // namespace fk
