@@ -1,5 +1,6 @@
 // fk_decode_step_acc: the decode step that adds its attention weights to those that the retained pairs have accumulated (thin.hip).
-#include "thin.h"
+#include "attn_paged.h"
+#include <cfloat>
 #include <climits>
 #include <cmath>
 
@@ -19,7 +20,7 @@ extern "C" fk_status fk_decode_step_acc(const fk_cache_desc* desc, const void* q
     if (!aligned16(q) || !aligned16(K) || !aligned16(V) || !aligned16(out) || !aligned16(k_new) || !aligned16(v_new) || !aligned16(acc)) return FK_ERR_INVALID_ARG;
     if (max_len <= 0 || max_len > desc->capacity) return FK_ERR_INVALID_ARG;
     if (!workspace || workspace_bytes < fk_decode_step_acc_workspace(desc) || !aligned16(workspace)) return FK_ERR_WORKSPACE;
-    ThinParams P = {};
+    AttnPagedParams P = {};
     P.view.q = q;
     P.view.K = K;
     P.view.V = V;
@@ -28,7 +29,7 @@ extern "C" fk_status fk_decode_step_acc(const fk_cache_desc* desc, const void* q
     P.view.g = desc->n_q_heads / desc->n_kv_heads;
     P.view.window = INT_MAX;
     P.view.negate = std::signbit(softmax_scale);
-    P.view.scale_log2e = std::fabs(softmax_scale) * 1.4426950408889634f;
+    P.view.scale_log2e = std::fmax(std::fabs(softmax_scale) * 1.4426950408889634f, FLT_MIN);   // (0: all logits equal)
     P.out = out;
     P.cap = desc->capacity;
     P.pos = pos;

@@ -1,7 +1,8 @@
-// The entry points of attention over the pages of a prompt and of the weights that its pairs received: fk_paged_attn (thin.hip), fk_paged_weights
-// (weights.hip).
-#include "thin.h"
+// The entry points of attention over the pages of a prompt and of the weights that its pairs received: fk_paged_attn (thin.hip, prompt.hip),
+// fk_paged_weights (weights.hip).
+#include "attn_paged.h"
 #include "weights.h"
+#include <cfloat>
 #include <climits>
 #include <cmath>
 
@@ -22,16 +23,43 @@ static PagedParams view_params(const fk_paged_desc* desc, const void* q, const v
     PagedParams P = paged_params(desc, table, kv_len, q_start, n_tokens);
     P.q = q;
     P.K = K;
-    P.window = window == 0 ? INT_MAX : window;
+    P.window = window == 0 || window >= (1 << 24) ? INT_MAX : window;   // (longer than any sequence: none)
     P.sink = n_sink;
     P.negate = std::signbit(softmax_scale);
-    P.scale_log2e = std::fabs(softmax_scale) * 1.4426950408889634f;
+    // (0: as near to it as keeps what is not seen at -inf; all logits are equal)
+    P.scale_log2e = std::fmax(std::fabs(softmax_scale) * 1.4426950408889634f, FLT_MIN);
     return P;
+}
+
+// Which kernel takes a chunk goes by its query rows: up to kThinRows the one that reads every pair once for 16 of them, beyond it the one with
+// tiles of 128.  A call that may hold both kinds is two launches, each of which leaves the other's chunks alone.
+static constexpr int kThinRows = 16;
+struct AttnPlanPaged {
+    bool thin, prompt;
+    TileGrid thin_grid, prompt_grid;
+};
+static AttnPlanPaged plan_paged(const fk_paged_desc* d, int32_t n_tokens, int32_t max_chunk) {
+    const int g = d->n_q_heads / d->n_kv_heads;
+    AttnPlanPaged p = {};
+    const bool all_longest = (long long)d->batch * max_chunk <= n_tokens;   // as many tokens as chunks of the bound's length have
+    p.prompt = (long long)max_chunk * g > kThinRows && (long long)n_tokens * g > kThinRows;
+    p.thin = !p.prompt || !all_longest;
+    if (p.thin) {   // (also all chunks there are, should they be longer than max_chunk says)
+        p.thin_grid = tile_grid(d, n_tokens, p.prompt ? (kThinRows + g - 1) / g : max_chunk, 16);
+        if (p.prompt) p.thin_grid.most = kThinRows;
+    }
+    if (p.prompt) {
+        p.prompt_grid = tile_grid(d, n_tokens, max_chunk, kPromptRows);
+        if (p.thin) p.prompt_grid.least = kThinRows + 1;
+    }
+    return p;
 }
 
 extern "C" size_t fk_paged_attn_workspace(const fk_paged_desc* desc, int32_t n_tokens, int32_t max_chunk, int32_t max_len) {
     if (check_paged(desc) != FK_OK || check_chunks(desc, n_tokens, max_chunk, max_len) != FK_OK) return 0;
-    return 16 + thin_paged_workspace(desc, tile_grid(desc, n_tokens, max_chunk, 16), max_len);
+    const AttnPlanPaged p = plan_paged(desc, n_tokens, max_chunk);
+    const size_t a = p.thin ? thin_paged_workspace(desc, p.thin_grid, max_len) : 0, b = p.prompt ? prompt_workspace(desc, p.prompt_grid, max_len) : 0;
+    return 16 + (a > b ? a : b);   // (one launch after the other)
 }
 
 extern "C" fk_status fk_paged_attn(const fk_paged_desc* desc, const void* q, const void* K, const void* V, const int32_t* page_table,
@@ -45,11 +73,17 @@ extern "C" fk_status fk_paged_attn(const fk_paged_desc* desc, const void* q, con
     if (n_tokens == 0) return FK_OK;
     PagedParams P = view_params(desc, q, K, page_table, kv_len, q_start, n_tokens, window, n_sink, softmax_scale);
     P.V = V;
-    ThinParams T = {};
+    AttnPagedParams T = {};
     T.view = P;
     T.out = out;
     T.stats = reinterpret_cast<float2*>(stats);
-    T.grid = tile_grid(desc, n_tokens, max_chunk, 16);
+    const AttnPlanPaged p = plan_paged(desc, n_tokens, max_chunk);
+    if (p.prompt) {
+        T.grid = p.prompt_grid;
+        const fk_status r = prompt_paged(desc, T, max_len, workspace, (hipStream_t)stream);
+        if (r != FK_OK || !p.thin) return r;
+    }
+    T.grid = p.thin_grid;
     return thin_paged(desc, T, max_len, workspace, (hipStream_t)stream);
 }
 

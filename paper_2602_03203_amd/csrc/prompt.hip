@@ -1,0 +1,409 @@
+// Attention of prompt chunks over the pages of a prompt: tiles of 128 query rows (tokens x heads of a group) against tiles of 64 pairs (fp32: 32).
+//
+// A wavefront owns 32 rows: their q, online softmax and outputs stay in its registers.  The pairs pass by in tiles, each read once for
+// the four wavefronts: global loads a tile ahead, LDS in two buffers, one barrier a tile.  Products and operand layouts are those of thin.hip
+// (logits K.Q^T with the keys in an order that makes a lane's probabilities an operand of V^T.P^T as they are; the same 16x16 products in
+// the same order, so that logits are the same bits everywhere); an operand read from LDS serves two products, one for each 16 rows.
+//   K in LDS: 16-byte chunks of a row swizzled so that the 16 rows of an operand lie in different banks (swizzle_k)
+//   V in LDS, bf16: rows as in memory; the operand is 8 keys of one channel per lane, which the transposing LDS read delivers, 4 keys at a time
+//   (ds_read_tr16_b64: lane l of 16 gets element l % 4 of what lanes l / 4, + 4, + 8, + 12 address); swizzled for those reads (swizzle_v)
+//   fp32: four channels a lane, each a product of its own
+// References follow a row's maximum only where it has grown by more than 2^8 (probabilities up to 256, sums in fp32: nothing is lost), so that
+// outputs are hardly ever rescaled.
+#include "attn_paged.h"
+#include <climits>
+
+namespace fk {
+
+template <typename T, int D> struct PromptCfg {
+    static constexpr bool BF = sizeof(T) == 2;
+    static constexpr int CH = D * (int)sizeof(T) / 16, KS = CH / 4, ET = D / 16;
+    static constexpr int KT = BF ? 64 : 32;       // pairs of a tile
+    static constexpr int NT = BF ? 2 : 1;         // 16-key products of a block (as many keys as a product of P.V takes)
+    static constexpr int BLK = 16 * NT, NB = KT / BLK, GI = KT / 16;
+    static constexpr int CT = 2;                  // 16-row tiles of a wavefront
+    static constexpr int TM = kPromptRows;
+    static constexpr int LD = KT * CH / 256, RPU = 256 / CH;   // loads of a tile per thread and tensor; rows that one load of the workgroup covers
+    static constexpr int TILE_BYTES = KT * CH * 16;
+    static constexpr size_t LDS_BYTES = 4 * (size_t)TILE_BYTES;   // K, V, two buffers
+};
+static constexpr float kPromptHuge = 16777216.f;   // |logits| from which they are rounded before a maximum is subtracted
+
+// 16-byte chunk of a row -> its place
+template <bool BF, int CH> __device__ __forceinline__ int swizzle_k(int row) {
+    if constexpr (!BF) return row & 15;
+    else if constexpr (CH == 16) return (row & 3) | ((row >> 3) & 3) << 2;
+    else return ((row >> 1) & 1) | ((row >> 3) & 3) << 1;
+}
+template <bool BF, int CH> __device__ __forceinline__ int swizzle_v(int row) {
+    if constexpr (!BF) return 0;
+    else if constexpr (CH == 16) return (row & 3) << 1 | ((row >> 3) & 1) << 3;
+    else return ((row >> 1) & 1) << 1 | ((row >> 3) & 1) << 2;
+}
+
+typedef short ps16x4_t __attribute__((ext_vector_type(4)));
+__device__ __forceinline__ tu32x2_t read_transposed(const unsigned char* p) {
+    typedef __attribute__((address_space(3))) ps16x4_t lds_t;
+    return __builtin_bit_cast(tu32x2_t, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_t*)p));
+}
+
+template <typename T, int D>
+__global__ __launch_bounds__(256, 2) void prompt_kernel(const AttnPagedParams P) {
+    using C = PromptCfg<T, D>;
+    constexpr bool BF = C::BF;
+    constexpr int CH = C::CH, KS = C::KS, ET = C::ET, KT = C::KT, NT = C::NT, BLK = C::BLK, NB = C::NB, GI = C::GI, CT = C::CT, TM = C::TM, LD = C::LD, RPU = C::RPU;
+    const PagedParams& W = P.view;
+    const int tid = threadIdx.x, lane = tid & (kWave - 1), n16 = lane & 15, quad = lane >> 4, wave = scalar(tid / kWave);
+    const int n_kv = W.n_kv, slot = scalar(blockIdx.x / n_kv), h = (int)blockIdx.x - slot * n_kv, split = blockIdx.y, g = W.g;
+    extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
+    __shared__ int s_bad;
+    TileOf t;
+    if (!tile_of(W, P.grid, slot, TM, t)) return;
+    const int32_t* tab = scalar_ptr(W.table + (size_t)t.b * W.max_pages);
+    const float scale = W.scale_log2e;
+    const bool windowed = W.window != 0x7fffffff;
+
+    // LDS places of this lane's operands, and of what this thread stages (rows RPU apart have the same swizzle: RPU >= 8, or bits that swizzles skip)
+    int k_at[KS];
+    {
+        const int row = BF ? n16 / 4 * 8 + n16 % 4 : n16;   // of MFMA row n16 in the first product of a block
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) k_at[ks] = row * CH * 16 + ((ks * 4 + quad) ^ swizzle_k<BF, CH>(row)) * 16;
+    }
+    const int v_row = BF ? quad * 8 + n16 / 4 : quad * 4;
+    auto v_at = [&](int e) {   // bf16: the lane's share of channel tile e
+        return v_row * CH * 16 + ((2 * e + n16 % 4 / 2) ^ swizzle_v<BF, CH>(v_row)) * 16 + n16 % 2 * 8;
+    };
+    const int st_row = tid / CH, st_ch = tid % CH;
+
+    for (; t.tile >= 0; t.tile -= t.step) {
+        const int r0 = t.tile * TM, rows = min(TM, t.nq * g - r0);
+        const int tile_lo = scalar(t.first + r0 / g), tile_hi = scalar(t.first + (r0 + rows - 1) / g);
+        const KeyTiles kt = key_tiles(W, tile_lo, tile_hi, KT);
+        const int splits = scalar(splits_of(kt.total, t.one ? P.splits : 1, P.split_tiles));
+        if (split >= splits) continue;
+        const int per = scalar((kt.total + splits - 1) / splits), t_begin = min(split * per, kt.total), t_end = min(t_begin + per, kt.total);
+
+        // the wavefront's rows
+        const int w0 = r0 + wave * 32, w_rows = min(32, rows - wave * 32);   // <= 0: none
+        const int w_first = scalar(t.first + w0 / g), w_last = scalar(t.first + (w0 + max(w_rows, 1) - 1) / g);
+        int pos[CT];
+        T128 q[CT][KS];
+#pragma unroll
+        for (int ct = 0; ct < CT; ++ct) {
+            const int r = w0 + ct * 16 + n16, rc = min(r, r0 + rows - 1), tok = rc / g;
+            pos[ct] = r < r0 + rows ? t.first + tok : INT_MIN;   // (negative ones see nothing)
+            const size_t q_row = ((size_t)(t.begin + tok) * n_kv + h) * g + (rc - tok * g);
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks) {
+                q[ct][ks].u = reinterpret_cast<const tu32x4_t*>(W.q)[q_row * CH + ks * 4 + quad];
+                if (W.negate) q[ct][ks].u ^= BF ? 0x80008000u : 0x80000000u;
+            }
+        }
+
+        // A row gives the pairs that it does not see weight 0, which must not meet an infinity or a NaN that another row sees: where there is any, the
+        // run starts over with half of its tokens.
+        for (int lo = tile_lo, hi = tile_hi;;) {
+            if (tid == 0) s_bad = 0;
+            __syncthreads();
+            const int w_lo = max(w_first, lo), w_hi = w_rows > 0 ? min(w_last, hi) : -1;
+            int p[CT], p_from[CT], p_sink[CT];
+            bool mine[CT];   // this run's rows
+            float m_ref[CT], m_top[CT], l_run[CT];
+            tf32x4_t o[ET][CT];
+#pragma unroll
+            for (int ct = 0; ct < CT; ++ct) {
+                mine[ct] = pos[ct] >= lo && pos[ct] <= hi;
+                p[ct] = mine[ct] ? pos[ct] : -1;
+                p_from[ct] = p[ct] < 0 || !windowed ? -1 : p[ct] - W.window;
+                p_sink[ct] = min(W.sink, p[ct] + 1);
+                m_ref[ct] = m_top[ct] = -INFINITY;
+                l_run[ct] = 0.f;
+#pragma unroll
+                for (int e = 0; e < ET; ++e) o[e][ct] = (tf32x4_t){0.f, 0.f, 0.f, 0.f};
+            }
+            T128 kr[LD], vr[LD];
+            int page[GI], page_next[GI];
+            auto pages_of = [&](int i, int (&pg)[GI]) {
+                const int base = kt.at(i) * KT;
+#pragma unroll
+                for (int r = 0; r < GI; ++r) pg[r] = load_uniform(tab, min((base + r * 16) >> W.page_shift, W.max_pages - 1));
+            };
+            // load u of this wavefront lies in run .. of 16 pairs
+            auto page_of = [&](const int (&pg)[GI], int u) {
+                if constexpr (RPU == 32) return wave >= 2 ? pg[2 * u + 1] : pg[2 * u];
+                else return pg[u * RPU / 16];
+            };
+            auto fetch = [&](int base, const int (&pg)[GI]) {
+#pragma unroll
+                for (int u = 0; u < LD; ++u) {
+                    const int pgu = page_of(pg, u), in_tile = RPU == 32 ? u * 32 + (wave >= 2 ? 16 : 0) : u * RPU / 16 * 16;
+                    const size_t run = ((((size_t)(page_ok(W, pgu) ? pgu : 0) * n_kv + h) << W.page_shift) + ((base + in_tile) & ((1 << W.page_shift) - 1))) * CH;
+                    const int lane_at = (st_row + u * RPU) % 16 * CH + st_ch;
+                    kr[u].u = reinterpret_cast<const tu32x4_t*>(W.K)[run + lane_at];
+                    vr[u].u = reinterpret_cast<const tu32x4_t*>(W.V)[run + lane_at];
+                }
+            };
+            auto all_there = [&](const int (&pg)[GI]) {
+                bool ok = true;
+#pragma unroll
+                for (int r = 0; r < GI; ++r) ok = ok && page_ok(W, pg[r]);
+                return ok;
+            };
+            auto stage = [&](int buf, int base, const int (&pg)[GI]) {
+                unsigned char *sk = smem + buf * C::TILE_BYTES, *sv = smem + (2 + buf) * C::TILE_BYTES;
+                const bool whole = base + KT <= lo + 1 && (!windowed || base > hi - W.window || base + KT <= W.sink) && all_there(pg);
+                if (!whole) {   // values of weight 0 must not meet the products as infinities or NaN
+                    const int any_from = windowed ? lo - W.window : -1, all_from = windowed ? hi - W.window : -1;
+                    bool bad = false;
+#pragma unroll
+                    for (int u = 0; u < LD; ++u) {
+                        const int key = base + st_row + u * RPU;
+                        const bool someone = page_ok(W, page_of(pg, u)) & (key <= hi) & ((key > any_from) | (key < W.sink));
+                        const bool everyone = (key <= lo) & ((key > all_from) | (key < W.sink));   // of those that someone sees
+                        const uint32_t keep = someone ? ~0u : 0u;
+#pragma unroll
+                        for (int w = 0; w < 4; ++w) {
+                            vr[u].w[w] &= keep;
+                            bad |= !everyone & word_not_finite<T>(vr[u].w[w]);
+                        }
+                    }
+                    if (bad && hi > lo) s_bad = 1;
+                }
+#pragma unroll
+                for (int u = 0; u < LD; ++u) {
+                    const int row = st_row + u * RPU;
+                    *reinterpret_cast<tu32x4_t*>(sk + row * CH * 16 + (st_ch ^ swizzle_k<BF, CH>(row)) * 16) = kr[u].u;
+                    *reinterpret_cast<tu32x4_t*>(sv + row * CH * 16 + (st_ch ^ swizzle_v<BF, CH>(row)) * 16) = vr[u].u;
+                }
+            };
+            auto compute = [&](int buf, int base, const int (&pg)[GI]) {
+                if (base > w_hi) return;   // nothing that this wavefront sees
+                if (windowed && base + KT - 1 <= w_lo - W.window && base >= W.sink) return;
+                const unsigned char *sk = smem + buf * C::TILE_BYTES, *sv = smem + (2 + buf) * C::TILE_BYTES;
+                tf32x4_t c[GI][CT];
+#pragma unroll
+                for (int gi = 0; gi < GI; ++gi) {
+#pragma unroll
+                    for (int ct = 0; ct < CT; ++ct) c[gi][ct] = (tf32x4_t){0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                    for (int ks = 0; ks < KS; ++ks) {
+                        T128 k;
+                        k.u = *reinterpret_cast<const tu32x4_t*>(sk + k_at[ks] + (gi / NT * BLK + gi % NT * 4) * CH * 16);
+#pragma unroll
+                        for (int ct = 0; ct < CT; ++ct) {
+                            if constexpr (BF) {
+                                c[gi][ct] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k.v, q[ct][ks].v, c[gi][ct], 0, 0, 0);
+                            } else {
+#pragma unroll
+                                for (int e = 0; e < 4; ++e) c[gi][ct] = __builtin_amdgcn_mfma_f32_16x16x4f32(k.f[e], q[ct][ks].f[e], c[gi][ct], 0, 0, 0);
+                            }
+                        }
+                    }
+                }
+                const bool whole = base + KT <= w_lo + 1 && (!windowed || base > w_hi - W.window || base + KT <= W.sink) && all_there(pg);
+                if (!whole) {
+#pragma unroll
+                    for (int gi = 0; gi < GI; ++gi) {
+                        const int b = gi / NT;
+                        const bool there = BF ? page_ok(W, quad >= 2 ? pg[2 * b + (BF ? 1 : 0)] : pg[BF ? 2 * b : b]) : page_ok(W, pg[b]);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            const int key = base + b * BLK + quad * (NT * 4) + gi % NT * 4 + e;
+#pragma unroll
+                            for (int ct = 0; ct < CT; ++ct) {
+                                const bool seen = there & (key <= p[ct]) & ((key > p_from[ct]) | (key < p_sink[ct]));
+                                c[gi][ct][e] = seen ? c[gi][ct][e] : -INFINITY;
+                            }
+                        }
+                    }
+                }
+                bool need = false, huge = false;
+                float m_new[CT];
+#pragma unroll
+                for (int ct = 0; ct < CT; ++ct) {
+                    float mx = -INFINITY;
+#pragma unroll
+                    for (int gi = 0; gi < GI; ++gi)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) mx = fmaxf(mx, c[gi][ct][e]);
+                    mx = attn_logit(quad_max(mx), scale);
+                    m_top[ct] = fmaxf(m_top[ct], mx);
+                    const bool grown = mx > m_ref[ct] + 8.f;
+                    m_new[ct] = grown ? mx : m_ref[ct];
+                    need |= grown;
+                    huge |= fabsf(m_new[ct]) >= kPromptHuge;   // (nothing seen: -inf as well, with nothing to lose)
+                }
+                if (__any(need)) {
+#pragma unroll
+                    for (int ct = 0; ct < CT; ++ct) {
+                        const float corr = __builtin_amdgcn_exp2f(m_ref[ct] - ref_of(m_new[ct]));
+                        m_ref[ct] = m_new[ct];
+                        l_run[ct] *= corr;
+#pragma unroll
+                        for (int e = 0; e < ET; ++e)
+#pragma unroll
+                            for (int k = 0; k < 4; ++k) o[e][ct][k] *= corr;
+                    }
+                }
+                if (__any(huge)) {
+#pragma unroll
+                    for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+                        for (int gi = 0; gi < GI; ++gi)
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) c[gi][ct][e] = attn_logit(c[gi][ct][e], scale) - ref_of(m_ref[ct]);
+                } else {
+#pragma unroll
+                    for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+                        for (int gi = 0; gi < GI; ++gi)
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) c[gi][ct][e] = fmaf(c[gi][ct][e], scale, -m_ref[ct]);
+                }
+#pragma unroll
+                for (int ct = 0; ct < CT; ++ct) {
+                    float sum = 0.f;
+#pragma unroll
+                    for (int gi = 0; gi < GI; ++gi)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            c[gi][ct][e] = __builtin_amdgcn_exp2f(c[gi][ct][e]);
+                            sum += c[gi][ct][e];
+                        }
+                    l_run[ct] += sum;
+                }
+#pragma unroll
+                for (int b = 0; b < NB; ++b) {
+                    if constexpr (BF) {
+                        T128 pr[CT];   // rounded: each weight by half a step of bf16 at most, sums of them in fp32
+#pragma unroll
+                        for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+                            for (int w = 0; w < 4; ++w) pr[ct].w[w] = pack_bf16(c[2 * b + w / 2][ct][w % 2 * 2], c[2 * b + w / 2][ct][w % 2 * 2 + 1]);
+#pragma unroll
+                        for (int e = 0; e < ET; ++e) {
+                            T128 v;
+                            const unsigned char* at = sv + v_at(e) + b * BLK * CH * 16;
+                            const tu32x2_t v0 = read_transposed(at), v1 = read_transposed(at + 4 * CH * 16);
+                            v.u = tu32x4_t{v0.x, v0.y, v1.x, v1.y};
+#pragma unroll
+                            for (int ct = 0; ct < CT; ++ct) o[e][ct] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v.v, pr[ct].v, o[e][ct], 0, 0, 0);
+                        }
+                    } else {
+#pragma unroll
+                        for (int u = 0; u < 4; ++u)
+#pragma unroll
+                            for (int cc = 0; cc < D / 64; ++cc) {
+                                T128 v;
+                                v.u = *reinterpret_cast<const tu32x4_t*>(sv + (b * BLK + v_row + u) * CH * 16 + (cc * 16 + n16) * 16);
+#pragma unroll
+                                for (int e = 0; e < 4; ++e)
+#pragma unroll
+                                    for (int ct = 0; ct < CT; ++ct) o[cc * 4 + e][ct] = __builtin_amdgcn_mfma_f32_16x16x4f32(v.f[e], c[b][ct][u], o[cc * 4 + e][ct], 0, 0, 0);
+                            }
+                    }
+                }
+            };
+
+            if (t_begin < t_end) {
+                pages_of(t_begin, page);
+                const int base = kt.at(t_begin) * KT;
+                fetch(base, page);
+                stage(0, base, page);
+                pages_of(min(t_begin + 1, t_end - 1), page_next);
+            }
+            __syncthreads();
+            for (int i = t_begin, buf = 0; i < t_end; ++i, buf ^= 1) {
+                const int base = kt.at(i) * KT, next = kt.at(min(i + 1, t_end - 1)) * KT;
+                const bool more = i + 1 < t_end;
+                if (more) fetch(next, page_next);
+                compute(buf, base, page);
+                if (more) stage(buf ^ 1, next, page_next);
+#pragma unroll
+                for (int r = 0; r < GI; ++r) page[r] = page_next[r];
+                pages_of(min(i + 2, t_end - 1), page_next);
+                __syncthreads();
+            }
+            if (scalar(s_bad)) {   // (the same for every thread)
+                hi = lo + (hi - lo) / 2;
+                __syncthreads();
+                continue;
+            }
+
+            // ---- results: every wavefront has its rows' own -------------------------------------------------------------
+#pragma unroll
+            for (int ct = 0; ct < CT; ++ct) {
+                const float l = quad_sum(l_run[ct]), f = __builtin_amdgcn_exp2f(m_ref[ct] - ref_of(m_top[ct]));
+                if (!mine[ct]) continue;
+                const int r = w0 + ct * 16 + n16, tok = r / g;
+                const size_t row = ((size_t)(t.begin + tok) * n_kv + h) * g + (r - tok * g);
+                const bool none = m_top[ct] == -INFINITY;
+                const size_t rec = (((size_t)slot * n_kv + h) * P.splits + split) * TM + (r - r0);
+                const float mul = splits > 1 ? f : none ? 0.f : 1.0f / l;
+#pragma unroll
+                for (int e = 0; e < ET; e += BF ? 1 : 4) {
+                    if constexpr (BF) {   // channels e * 16 + quad * 4 ..
+                        const tf32x4_t a = o[e][ct] * mul;
+                        const int d = e * 16 + quad * 4;
+                        if (splits > 1) *reinterpret_cast<float4*>(P.rec + rec * D + d) = make_float4(a[0], a[1], a[2], a[3]);
+                        else *reinterpret_cast<tu32x2_t*>(reinterpret_cast<bf16_t*>(P.out) + row * D + d) = tu32x2_t{pack_bf16(a[0], a[1]), pack_bf16(a[2], a[3])};
+                    } else {
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) {   // e / 4 * 64 + (quad * 4 + k) * 4 ..
+                            const float4 a = make_float4(o[e][ct][k] * mul, o[e + 1][ct][k] * mul, o[e + 2][ct][k] * mul, o[e + 3][ct][k] * mul);
+                            const int d = e / 4 * 64 + (quad * 4 + k) * 4;
+                            if (splits > 1) *reinterpret_cast<float4*>(P.rec + rec * D + d) = a;
+                            else *reinterpret_cast<float4*>(reinterpret_cast<float*>(P.out) + row * D + d) = a;
+                        }
+                    }
+                }
+                if (quad == 0) {
+                    const float2 ml = make_float2(m_top[ct], none ? 0.f : l * f);
+                    if (splits > 1) P.rec_ml[rec] = ml;
+                    else if (P.stats) P.stats[row] = ml;
+                }
+            }
+            if (hi == tile_hi) break;
+            lo = hi + 1;
+            hi = tile_hi;
+        }
+        __syncthreads();   // the LDS is the next tile's
+    }
+}
+
+// ---- host side ---------------------------------------------------------------------------------------------------
+// Splits of the pairs where the tiles alone leave CUs without a workgroup, 512 pairs and more each
+static int prompt_splits(const fk_paged_desc* d, const TileGrid& G, int max_len, int kt, int& least) {
+    least = 512 / kt;
+    long long s = 512 / ((long long)G.places * d->n_kv_heads);
+    if (s > max_len / 512) s = max_len / 512;
+    if (s > 16) s = 16;
+    return s < 1 ? 1 : (int)s;
+}
+size_t prompt_workspace(const fk_paged_desc* d, const TileGrid& G, int max_len) {
+    int least;
+    return record_bytes((long long)G.places * d->n_kv_heads, prompt_splits(d, G, max_len, d->dtype == FK_BF16 ? 64 : 32, least), kPromptRows, d->head_dim);
+}
+
+template <typename T, int D>
+static fk_status prompt_launch(const fk_paged_desc* d, AttnPagedParams& P, int max_len, void* ws, hipStream_t st) {
+    using C = PromptCfg<T, D>;
+    const long long items = (long long)P.grid.places * d->n_kv_heads;
+    P.splits = prompt_splits(d, P.grid, max_len, C::KT, P.split_tiles);
+    P.rec_ml = reinterpret_cast<float2*>(ws);
+    P.rec = reinterpret_cast<float*>(static_cast<char*>(ws) + up256((size_t)items * P.splits * kPromptRows * sizeof(float2)));
+    auto kern = prompt_kernel<T, D>;
+    static bool lds_ok[kMaxDevices] = {};
+    if (!allow_dynamic_lds((const void*)kern, C::LDS_BYTES, lds_ok)) return FK_ERR_LAUNCH;
+    hipLaunchKernelGGL(kern, dim3((unsigned)items, P.splits), dim3(256), C::LDS_BYTES, st, P);
+    if (P.splits > 1) hipLaunchKernelGGL((merge_kernel<T, D, kPromptRows, C::KT, false>), dim3((unsigned)items, kPromptRows / 16), dim3(256), 0, st, P);
+    return launch_status();
+}
+
+fk_status prompt_paged(const fk_paged_desc* d, AttnPagedParams P, int max_len, void* ws, hipStream_t st) {
+    if (d->dtype == FK_F32) return d->head_dim == 64 ? prompt_launch<float, 64>(d, P, max_len, ws, st) : prompt_launch<float, 128>(d, P, max_len, ws, st);
+    return d->head_dim == 64 ? prompt_launch<bf16_t, 64>(d, P, max_len, ws, st) : prompt_launch<bf16_t, 128>(d, P, max_len, ws, st);
+}
+
+}  // namespace fk

@@ -10,22 +10,10 @@
 // K of the next tile is sent off when this one's logits are formed, V when its outputs are: the registers that held them are free, and loads are
 // in flight all the time.  Bound by the memory system.
 // Several splits: records in the workspace, a second launch merges them (and adds the weights).
-#include "thin.h"
-#include "window.h"
+#include "attn_paged.h"
 #include <type_traits>
 
 namespace fk {
-
-typedef __attribute__((ext_vector_type(8))) __bf16 tbf16x8_t;
-typedef __attribute__((ext_vector_type(4))) float tf32x4_t;
-typedef __attribute__((ext_vector_type(4))) uint32_t tu32x4_t;
-typedef __attribute__((ext_vector_type(2))) uint32_t tu32x2_t;
-union T128 {
-    tu32x4_t u;
-    uint32_t w[4];
-    float f[4];
-    tbf16x8_t v;
-};
 
 template <typename T, int D> struct ThinCfg {
     static constexpr bool BF = sizeof(T) == 2;
@@ -39,27 +27,6 @@ template <typename T, int D> struct ThinCfg {
     static constexpr int PART = D + 4;                   // float stride of a row of a partial output in LDS
 };
 
-__device__ __forceinline__ float quad_max(float v) {   // over the four lanes of a row (lane % 16)
-    auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-    v = fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
-    auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-    return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
-}
-__device__ __forceinline__ float quad_sum(float v) {
-    auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-    v = __uint_as_float(a[0]) + __uint_as_float(a[1]);
-    auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-    return __uint_as_float(b[0]) + __uint_as_float(b[1]);
-}
-
-// 0 where nothing has been seen: what an exponent is taken against
-__device__ __forceinline__ float ref_of(float m) { return m == -INFINITY ? 0.f : m; }
-
-template <typename T> __device__ __forceinline__ bool word_not_finite(uint32_t w) {
-    if constexpr (sizeof(T) == 2) return ((w & 0x7f80u) == 0x7f80u) | ((w & 0x7f800000u) == 0x7f800000u);   // (no branch)
-    else return (w & 0x7f800000u) == 0x7f800000u;
-}
-
 // channel of element i of a lane's output registers o[e]: MFMA row quad * 4 + i of channel tile e
 template <typename T, int D> __device__ __forceinline__ int channel_of(int row, int e) {
     if constexpr (sizeof(T) == 2) return row * (D / 16) + e;
@@ -67,7 +34,7 @@ template <typename T, int D> __device__ __forceinline__ int channel_of(int row, 
 }
 
 template <typename T, int D, bool ROWS, int WAVES, bool NT_LOADS>
-__global__ __launch_bounds__(WAVES * kWave, WAVES == 8 ? 2 : 3) void thin_kernel(const ThinParams P) {
+__global__ __launch_bounds__(WAVES * kWave, WAVES == 8 ? 2 : 3) void thin_kernel(const AttnPagedParams P) {
     using C = ThinCfg<T, D>;
     constexpr bool BF = C::BF;
     constexpr int CH = C::CH, KT = C::KT, NT = C::NT, KS = C::KS, VL = C::VL, ET = C::ET, PART = C::PART;
@@ -97,7 +64,7 @@ __global__ __launch_bounds__(WAVES * kWave, WAVES == 8 ? 2 : 3) void thin_kernel
         const int r0 = t.tile * 16, rows = min(16, t.nq * g - r0);
         const int tile_lo = scalar(t.first + r0 / g), tile_hi = scalar(t.first + (r0 + rows - 1) / g);   // positions of the first and the last row
         const KeyTiles kt = key_tiles(W, tile_lo, tile_hi, KT);
-        const int splits = scalar(thin_splits(kt.total, t.one ? P.splits : 1, P.split_tiles));
+        const int splits = scalar(splits_of(kt.total, t.one ? P.splits : 1, P.split_tiles));
         if (split >= splits) continue;
         const int per = scalar((kt.total + splits - 1) / splits), t_begin = min(split * per, kt.total), t_end = min(t_begin + per, kt.total);
 
@@ -193,7 +160,7 @@ __global__ __launch_bounds__(WAVES * kWave, WAVES == 8 ? 2 : 3) void thin_kernel
         auto v_key = [&](int x) { return BF ? quad * 8 + x : quad * 4 + x / (D / 64); };   // key of V load x in the tile
 
         // The rows of all tokens at once.  A row gives the pairs that it does not see weight 0, which must not meet an infinity or a NaN that another
-        // row sees: where there is any, the tile starts over, token by token.
+        // row sees: where there is any, the run starts over with half of its tokens.
         for (int lo = tile_lo, hi = tile_hi;;) {
         if (!ROWS && tid == 0) s_bad = 0;
         if constexpr (!ROWS) __syncthreads();
@@ -289,16 +256,17 @@ __global__ __launch_bounds__(WAVES * kWave, WAVES == 8 ? 2 : 3) void thin_kernel
             if (!whole) {   // values of weight 0 must not meet the products as infinities or NaN
                 bool bad = false;
                 const bool v_ok = BF && quad >= 2 ? page_ok(W, pb) : page_ok(W, pa);
-                const int any_from = W.window == 0x7fffffff ? -1 : lo - W.window;
+                const int any_from = W.window == 0x7fffffff ? -1 : lo - W.window, all_from = W.window == 0x7fffffff ? -1 : hi - W.window;
 #pragma unroll
                 for (int x = 0; x < VL; ++x) {
                     const int key = base + v_key(x);
                     const bool someone = (ROWS || v_ok) && key <= hi && (key > any_from || key < W.sink);
+                    const bool everyone = (key <= lo) & ((key > all_from) | (key < W.sink));   // of those that someone sees
                     const uint32_t keep = someone ? ~0u : 0u;   // (no branch: the registers of both ways would be kept)
 #pragma unroll
                     for (int w = 0; w < VW; ++w) {
                         vr[x].w[w] &= keep;
-                        if constexpr (!ROWS) bad |= word_not_finite<T>(vr[x].w[w]);
+                        if constexpr (!ROWS) bad |= !everyone & word_not_finite<T>(vr[x].w[w]);
                     }
                 }
                 if (!ROWS && bad && hi > lo) s_bad = 1;
@@ -345,7 +313,7 @@ __global__ __launch_bounds__(WAVES * kWave, WAVES == 8 ? 2 : 3) void thin_kernel
         __syncthreads();
         if constexpr (!ROWS) {
             if (scalar(s_bad)) {   // (the same for every thread)
-                hi = lo;
+                hi = lo + (hi - lo) / 2;
                 __syncthreads();
                 continue;
             }
@@ -418,124 +386,39 @@ __global__ __launch_bounds__(WAVES * kWave, WAVES == 8 ? 2 : 3) void thin_kernel
         }
         __syncthreads();   // the LDS is the next run's
         if (hi == tile_hi) break;
-        lo = ++hi;
+        lo = hi + 1;
+        hi = tile_hi;
         }
-    }
-}
-
-// ---------------------------------------------------------------------------------------------------------
-// The second launch, where tiles may have been split: out = sum_s o_s 2^(m_s - M) / sum_s l_s 2^(m_s - M).
-// ROWS: also the weights of the row's pairs, a stretch of them per workgroup, and its length.
-// ---------------------------------------------------------------------------------------------------------
-template <typename T, int D, bool ROWS>
-__global__ __launch_bounds__(256) void thin_merge_kernel(const ThinParams P) {
-    constexpr int KT = ThinCfg<T, D>::KT;
-    const PagedParams& W = P.view;
-    const int tid = threadIdx.x, n_kv = ROWS ? 1 : W.n_kv, slot = ROWS ? (int)blockIdx.x : scalar(blockIdx.x / n_kv), h = ROWS ? 0 : (int)blockIdx.x - slot * n_kv, g = W.g;
-    __shared__ float s_w[16][64], s_M[16], s_L[16];
-    TileOf t;
-    int fresh = -1;
-    if constexpr (ROWS) {
-        const int2 info = P.info[slot];
-        fresh = info.y;
-        if (blockIdx.y == 0 && tid == 0 && fresh >= 0) P.len[slot] = info.x;
-        t = {slot, slot, 1, info.x, info.x - 1, 0, 1, true};
-    } else {
-        if (!tile_of(W, P.grid, slot, 16, t)) return;
-    }
-    for (; t.tile >= 0; t.tile -= t.step) {
-        const int r0 = t.tile * 16, rows = min(16, t.nq * g - r0);
-        const int lo = t.first + r0 / g, hi = t.first + (r0 + rows - 1) / g;
-        const int splits = thin_splits(key_tiles(W, lo, hi, KT).total, t.one ? P.splits : 1, P.split_tiles);
-        if (splits == 1) continue;
-        const size_t rec = ((size_t)slot * n_kv + h) * P.splits * 16;
-        if (tid < rows) {
-            float M = -INFINITY, L = 0.f;
-            for (int s = 0; s < splits; ++s) M = fmaxf(M, P.rec_ml[rec + s * 16 + tid].x);
-            const float ref = ref_of(M);
-            for (int s = 0; s < splits; ++s) {
-                const float2 ml = P.rec_ml[rec + s * 16 + tid];
-                const float f = __builtin_amdgcn_exp2f(ml.x - ref);
-                s_w[tid][s] = f;
-                L = fmaf(ml.y, f, L);
-            }
-            s_M[tid] = M;
-            s_L[tid] = L;
-        }
-        __syncthreads();
-        if (!ROWS || blockIdx.y == 0) {
-            for (int x = tid; x < rows * (D / 4); x += 256) {
-                const int r = x / (D / 4), d = x % (D / 4) * 4;
-                float a[4] = {0.f, 0.f, 0.f, 0.f};
-                for (int s = 0; s < splits; ++s) {
-                    const float4 v = *reinterpret_cast<const float4*>(P.rec + (rec + s * 16 + r) * D + d);
-                    const float f = s_w[r][s];
-                    a[0] = fmaf(v.x, f, a[0]);
-                    a[1] = fmaf(v.y, f, a[1]);
-                    a[2] = fmaf(v.z, f, a[2]);
-                    a[3] = fmaf(v.w, f, a[3]);
-                }
-                const float L = s_L[r];
-                const size_t row = ((size_t)(t.begin + (r0 + r) / g) * n_kv + h) * g + (r0 + r) % g;
-                if (L == 0.f) a[0] = a[1] = a[2] = a[3] = 0.f;
-                const float inv = L == 0.f ? 1.f : L;
-                if constexpr (sizeof(T) == 2) {
-                    const tu32x2_t y = {pack_bf16(a[0] / inv, a[1] / inv), pack_bf16(a[2] / inv, a[3] / inv)};
-                    *reinterpret_cast<tu32x2_t*>(reinterpret_cast<bf16_t*>(P.out) + row * D + d) = y;
-                } else {
-                    *reinterpret_cast<float4*>(reinterpret_cast<float*>(P.out) + row * D + d) = make_float4(a[0] / inv, a[1] / inv, a[2] / inv, a[3] / inv);
-                }
-                if (P.stats && d == 0) P.stats[row] = make_float2(s_M[r], L);
-            }
-        }
-        if constexpr (ROWS) {
-            float* acc = P.acc + (size_t)slot * P.cap;
-            for (int key = blockIdx.y * 256 + tid; key < t.n; key += gridDim.y * 256) {
-                float w = 0.f;
-                for (int k = 0; k < g; ++k) w += __builtin_amdgcn_exp2f(P.logit[((size_t)slot * g + k) * P.cap + key] - ref_of(s_M[k])) / s_L[k];
-                acc[key] = (key == fresh ? 0.f : acc[key]) + w;
-            }
-            return;
-        }
-        __syncthreads();
     }
 }
 
 // ---- host side ---------------------------------------------------------------------------------------------------
-static constexpr int kThinSplits = 64;   // (s_w above)
-
 // Workgroups that share the tiles' pairs: enough to fill the chip, each with enough pairs to be worth a record
 static int thin_split_count(long long items, long long pairs, int kt, int waves, int& least) {
     least = 2 * waves;   // two rounds of the wavefronts
     long long s = 512 / items;
     const long long most = pairs / ((long long)least * kt);
     if (s > most) s = most;
-    if (s > kThinSplits) s = kThinSplits;
+    if (s > kMostSplits) s = kMostSplits;
     return s < 1 ? 1 : (int)s;
-}
-
-static size_t up256(size_t n) { return (n + 255) / 256 * 256; }
-
-static size_t thin_record_bytes(long long items, int splits, int D) {
-    return splits > 1 ? up256((size_t)items * splits * 16 * sizeof(float2)) + (size_t)items * splits * 16 * D * sizeof(float) : 0;
 }
 
 size_t thin_paged_workspace(const fk_paged_desc* d, const TileGrid& G, int max_len) {
     const long long items = (long long)G.places * d->n_kv_heads;
     int least;
-    return thin_record_bytes(items, thin_split_count(items, max_len, d->dtype == FK_BF16 ? 32 : 16, 4, least), d->head_dim);
+    return record_bytes(items, thin_split_count(items, max_len, d->dtype == FK_BF16 ? 32 : 16, 4, least), 16, d->head_dim);
 }
 
 template <typename T, int D>
-static fk_status thin_paged_launch(const fk_paged_desc* d, ThinParams& P, bool cold, hipStream_t st) {
+static fk_status thin_paged_launch(const fk_paged_desc* d, AttnPagedParams& P, bool cold, hipStream_t st) {
     const dim3 grid(P.grid.places * d->n_kv_heads, P.splits);
     if (cold) hipLaunchKernelGGL((thin_kernel<T, D, false, 4, true>), grid, dim3(256), 0, st, P);
     else hipLaunchKernelGGL((thin_kernel<T, D, false, 4, false>), grid, dim3(256), 0, st, P);
-    if (P.splits > 1) hipLaunchKernelGGL((thin_merge_kernel<T, D, false>), dim3(grid.x), dim3(256), 0, st, P);
+    if (P.splits > 1) hipLaunchKernelGGL((merge_kernel<T, D, 16, ThinCfg<T, D>::KT, false>), dim3(grid.x), dim3(256), 0, st, P);
     return launch_status();
 }
 
-fk_status thin_paged(const fk_paged_desc* d, ThinParams P, int max_len, void* ws, hipStream_t st) {
+fk_status thin_paged(const fk_paged_desc* d, AttnPagedParams P, int max_len, void* ws, hipStream_t st) {
     const long long items = (long long)P.grid.places * d->n_kv_heads;
     P.splits = thin_split_count(items, max_len, d->dtype == FK_BF16 ? 32 : 16, 4, P.split_tiles);
     P.rec_ml = reinterpret_cast<float2*>(ws);
@@ -554,19 +437,19 @@ static size_t rows_logit_bytes(const fk_cache_desc* d) { return up256((size_t)d-
 size_t thin_rows_workspace(const fk_cache_desc* d) {
     const size_t rows = (size_t)d->batch * d->n_kv_heads;
     int least;
-    return up256(rows * sizeof(int2)) + rows_logit_bytes(d) + thin_record_bytes(rows, rows_splits(d, d->capacity, 4, least), d->head_dim);
+    return up256(rows * sizeof(int2)) + rows_logit_bytes(d) + record_bytes(rows, rows_splits(d, d->capacity, 4, least), 16, d->head_dim);
 }
 
 template <typename T, int D, int WAVES>
-static fk_status thin_rows_launch(ThinParams& P, int max_len, bool cold, hipStream_t st) {
+static fk_status thin_rows_launch(AttnPagedParams& P, int max_len, bool cold, hipStream_t st) {
     const dim3 grid(P.view.batch, P.splits);
     if (cold) hipLaunchKernelGGL((thin_kernel<T, D, true, WAVES, true>), grid, dim3(WAVES * kWave), 0, st, P);
     else hipLaunchKernelGGL((thin_kernel<T, D, true, WAVES, false>), grid, dim3(WAVES * kWave), 0, st, P);
-    if (P.splits > 1) hipLaunchKernelGGL((thin_merge_kernel<T, D, true>), dim3(grid.x, (max_len + 1023) / 1024), dim3(256), 0, st, P);
+    if (P.splits > 1) hipLaunchKernelGGL((merge_kernel<T, D, 16, ThinCfg<T, D>::KT, true>), dim3(grid.x, (max_len + 1023) / 1024), dim3(256), 0, st, P);
     return launch_status();
 }
 
-fk_status thin_rows(const fk_cache_desc* d, ThinParams P, int max_len, void* ws, hipStream_t st) {
+fk_status thin_rows(const fk_cache_desc* d, AttnPagedParams P, int max_len, void* ws, hipStream_t st) {
     const size_t rows = (size_t)d->batch * d->n_kv_heads;
     P.splits = rows_splits(d, max_len, 4, P.split_tiles);
     char* at = static_cast<char*>(ws);
