@@ -56,7 +56,8 @@ struct AttnPagedParams {
     const void *k_new, *v_new;
     int batch_of_pos;          // KV heads: row r belongs to sequence r / batch_of_pos
     float* acc;                // [rows][cap]
-    float* logit;              // [rows][g][cap] scratch
+    float* logit;              // [rows][g][logit_stride] scratch
+    int logit_stride;          // cap, rounded up to whole 16-byte groups
     int2* info;                // [rows] (pairs, the new pair's slot or -1): for the second launch
 };
 
@@ -67,81 +68,127 @@ __host__ __device__ inline int splits_of(int total, int splits, int least) {
 }
 
 // ---------------------------------------------------------------------------------------------------------
-// The second launch, where tiles may have been split: out = sum_s o_s 2^(m_s - M) / sum_s l_s 2^(m_s - M).
-// ROWS: also the weights of the row's pairs, a stretch of them per workgroup, and its length.
+// The second launch, where tiles may have been split: out = sum_s o_s 2^(m_s - M) / sum_s l_s 2^(m_s - M), eight records' loads in flight.
 // ---------------------------------------------------------------------------------------------------------
-template <typename T, int D, int TM, int KT, bool ROWS>
+template <int D> struct Merged {
+    float M, L, a[4];
+};
+template <int D>
+__device__ __forceinline__ Merged<D> merge_records(const AttnPagedParams& P, size_t rec /* the row in the first split's record */, int tm, int splits, int d) {
+    Merged<D> o = {-INFINITY, 0.f, {0.f, 0.f, 0.f, 0.f}};
+    for (int s0 = 0; s0 < splits; s0 += 8) {
+        float2 ml[8];
+        float4 v[8];
+#pragma unroll
+        for (int u = 0; u < 8; ++u) {
+            const size_t r = rec + (size_t)min(s0 + u, splits - 1) * tm;
+            ml[u] = P.rec_ml[r];
+            v[u] = *reinterpret_cast<const float4*>(P.rec + r * D + d);
+        }
+        float m = o.M;
+#pragma unroll
+        for (int u = 0; u < 8; ++u) m = fmaxf(m, ml[u].x);   // (the copies past the end change nothing)
+        const float ref = ref_of(m), c0 = __builtin_amdgcn_exp2f(o.M - ref);
+        o.M = m;
+        o.L *= c0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) o.a[i] *= c0;
+#pragma unroll
+        for (int u = 0; u < 8; ++u) {
+            if (s0 + u >= splits) break;
+            const float f = __builtin_amdgcn_exp2f(ml[u].x - ref);
+            o.L = fmaf(ml[u].y, f, o.L);
+            o.a[0] = fmaf(v[u].x, f, o.a[0]);
+            o.a[1] = fmaf(v[u].y, f, o.a[1]);
+            o.a[2] = fmaf(v[u].z, f, o.a[2]);
+            o.a[3] = fmaf(v[u].w, f, o.a[3]);
+        }
+    }
+    return o;
+}
+
+// four channels of a row from the sum of its weighted values and of its weights; 0 where nothing has been seen
+template <typename T, int D>
+__device__ __forceinline__ void store_row(const AttnPagedParams& P, size_t row, int d, const float (&a)[4], float M, float L) {
+    const float inv = L == 0.f ? 0.f : 1.0f / L;
+    if constexpr (sizeof(T) == 2) {
+        const tu32x2_t y = {pack_bf16(a[0] * inv, a[1] * inv), pack_bf16(a[2] * inv, a[3] * inv)};
+        *reinterpret_cast<tu32x2_t*>(reinterpret_cast<bf16_t*>(P.out) + row * D + d) = y;
+    } else {
+        *reinterpret_cast<float4*>(reinterpret_cast<float*>(P.out) + row * D + d) = make_float4(a[0] * inv, a[1] * inv, a[2] * inv, a[3] * inv);
+    }
+    if (P.stats && d == 0) P.stats[row] = make_float2(M, L);
+}
+
+template <typename T, int D, int TM, int KT>
 __global__ __launch_bounds__(256) void merge_kernel(const AttnPagedParams P) {
     const PagedParams& W = P.view;
-    const int tid = threadIdx.x, n_kv = ROWS ? 1 : W.n_kv, slot = ROWS ? (int)blockIdx.x : scalar(blockIdx.x / n_kv), h = ROWS ? 0 : (int)blockIdx.x - slot * n_kv, g = W.g;
-    const int sub = ROWS ? 0 : (int)blockIdx.y * 16;   // the workgroup's 16 rows of the tile
-    __shared__ float s_w[16][kMostSplits], s_M[16], s_L[16];
+    const int tid = threadIdx.x, n_kv = W.n_kv, slot = scalar(blockIdx.x / n_kv), h = (int)blockIdx.x - slot * n_kv, g = W.g;
+    const int sub = blockIdx.y * 16;   // the workgroup's 16 rows of the tile
     TileOf t;
-    int fresh = -1;
-    if constexpr (ROWS) {
-        const int2 info = P.info[slot];
-        fresh = info.y;
-        if (blockIdx.y == 0 && tid == 0 && fresh >= 0) P.len[slot] = info.x;
-        t = {slot, slot, 1, info.x, info.x - 1, 0, 1, true};
-    } else {
-        if (!tile_of(W, P.grid, slot, TM, t)) return;
+    if (!tile_of(W, P.grid, slot, TM, t) || !t.one) return;   // (places that take several tiles do not split them)
+    const int tile_rows = min(TM, t.nq * g - t.tile * TM), rows = min(16, tile_rows - sub), r0 = t.tile * TM + sub;
+    const int lo = t.first + t.tile * TM / g, hi = t.first + (t.tile * TM + tile_rows - 1) / g;
+    const int splits = splits_of(key_tiles(W, lo, hi, KT).total, P.splits, P.split_tiles);
+    if (rows <= 0 || splits == 1) return;
+    const size_t rec = ((size_t)slot * n_kv + h) * P.splits * TM + sub;
+    for (int x = tid; x < rows * (D / 4); x += 256) {
+        const int r = x / (D / 4), d = x % (D / 4) * 4;
+        const Merged<D> o = merge_records<D>(P, rec + r, TM, splits, d);
+        store_row<T, D>(P, ((size_t)(t.begin + (r0 + r) / g) * n_kv + h) * g + (r0 + r) % g, d, o.a, o.M, o.L);
     }
-    for (; t.tile >= 0; t.tile -= t.step) {
-        const int tile_rows = min(TM, t.nq * g - t.tile * TM), rows = min(16, tile_rows - sub), r0 = t.tile * TM + sub;
-        if (rows <= 0) continue;
-        const int lo = t.first + t.tile * TM / g, hi = t.first + (t.tile * TM + tile_rows - 1) / g;
-        const int splits = splits_of(key_tiles(W, lo, hi, KT).total, t.one ? P.splits : 1, P.split_tiles);
-        if (splits == 1) continue;
-        const size_t rec = ((size_t)slot * n_kv + h) * P.splits * TM + sub;
-        if (tid < rows) {
-            float M = -INFINITY, L = 0.f;
-            for (int s = 0; s < splits; ++s) M = fmaxf(M, P.rec_ml[rec + s * TM + tid].x);
-            const float ref = ref_of(M);
-            for (int s = 0; s < splits; ++s) {
-                const float2 ml = P.rec_ml[rec + s * TM + tid];
-                const float f = __builtin_amdgcn_exp2f(ml.x - ref);
-                s_w[tid][s] = f;
-                L = fmaf(ml.y, f, L);
-            }
-            s_M[tid] = M;
-            s_L[tid] = L;
+}
+
+// Rows of a budgeted cache: the last workgroup of a row merges its outputs and sets its length, the others add its pairs' weights, a pair per thread,
+// whose logits are on their way while the splits' maxima and sums are put together.
+template <typename T, int D, int KT>
+__global__ __launch_bounds__(256) void merge_rows_kernel(const AttnPagedParams P) {
+    const int tid = threadIdx.x, slot = blockIdx.x, g = P.view.g;
+    __shared__ float2 s_ml[kMostSplits][8];
+    __shared__ float s_M[8], s_inv[8];
+    const int n = load_uniform(&P.info[slot].x, 0), fresh = load_uniform(&P.info[slot].y, 0);
+    const int splits = splits_of(key_tiles(P.view, n - 1, n - 1, KT).total, P.splits, P.split_tiles);
+    const size_t rec = (size_t)slot * P.splits * 16;
+    if (blockIdx.y == gridDim.y - 1) {
+        if (tid == 0 && fresh >= 0) P.len[slot] = n;
+        if (splits > 1 && tid < g * (D / 4)) {
+            const int r = tid / (D / 4), d = tid % (D / 4) * 4;
+            const Merged<D> o = merge_records<D>(P, rec + r, 16, splits, d);
+            store_row<T, D>(P, (size_t)slot * g + r, d, o.a, o.M, o.L);
         }
-        __syncthreads();
-        if (!ROWS || blockIdx.y == 0) {
-            for (int x = tid; x < rows * (D / 4); x += 256) {
-                const int r = x / (D / 4), d = x % (D / 4) * 4;
-                float a[4] = {0.f, 0.f, 0.f, 0.f};
-                for (int s = 0; s < splits; ++s) {
-                    const float4 v = *reinterpret_cast<const float4*>(P.rec + (rec + s * TM + r) * D + d);
-                    const float f = s_w[r][s];
-                    a[0] = fmaf(v.x, f, a[0]);
-                    a[1] = fmaf(v.y, f, a[1]);
-                    a[2] = fmaf(v.z, f, a[2]);
-                    a[3] = fmaf(v.w, f, a[3]);
-                }
-                const float L = s_L[r];
-                const size_t row = ((size_t)(t.begin + (r0 + r) / g) * n_kv + h) * g + (r0 + r) % g;
-                if (L == 0.f) a[0] = a[1] = a[2] = a[3] = 0.f;
-                const float inv = L == 0.f ? 1.f : L;
-                if constexpr (sizeof(T) == 2) {
-                    const tu32x2_t y = {pack_bf16(a[0] / inv, a[1] / inv), pack_bf16(a[2] / inv, a[3] / inv)};
-                    *reinterpret_cast<tu32x2_t*>(reinterpret_cast<bf16_t*>(P.out) + row * D + d) = y;
-                } else {
-                    *reinterpret_cast<float4*>(reinterpret_cast<float*>(P.out) + row * D + d) = make_float4(a[0] / inv, a[1] / inv, a[2] / inv, a[3] / inv);
-                }
-                if (P.stats && d == 0) P.stats[row] = make_float2(s_M[r], L);
-            }
-        }
-        if constexpr (ROWS) {
-            float* acc = P.acc + (size_t)slot * P.cap;
-            for (int key = blockIdx.y * 256 + tid; key < t.n; key += gridDim.y * 256) {
-                float w = 0.f;
-                for (int k = 0; k < g; ++k) w += __builtin_amdgcn_exp2f(P.logit[((size_t)slot * g + k) * P.cap + key] - ref_of(s_M[k])) / s_L[k];
-                acc[key] = (key == fresh ? 0.f : acc[key]) + w;
-            }
-            return;
-        }
-        __syncthreads();
+        return;
+    }
+    if (splits == 1) return;   // all done
+    float* acc = P.acc + (size_t)slot * P.cap;
+    const float* lg = P.logit + (size_t)slot * g * P.logit_stride;
+    int key = blockIdx.y * 256 + tid;
+    float x[8], before = 0.f;
+    auto fetch = [&]() {
+        const int kc = min(key, n - 1);
+        before = acc[kc];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) x[k] = lg[(size_t)min(k, g - 1) * P.logit_stride + kc];
+    };
+    fetch();
+    for (int i = tid; i < splits * 8; i += 256) s_ml[i / 8][i % 8] = P.rec_ml[rec + i / 8 * 16 + i % 8];
+    __syncthreads();
+    if (tid < g) {
+        float M = -INFINITY, L = 0.f;
+        for (int s = 0; s < splits; ++s) M = fmaxf(M, s_ml[s][tid].x);
+        M = ref_of(M);
+        for (int s = 0; s < splits; ++s) L = fmaf(s_ml[s][tid].y, __builtin_amdgcn_exp2f(s_ml[s][tid].x - M), L);
+        s_M[tid] = M;
+        s_inv[tid] = 1.0f / L;
+    }
+    __syncthreads();
+    while (key < n) {
+        float w = 0.f;
+#pragma unroll
+        for (int k = 0; k < 8; ++k)
+            if (k < g) w = fmaf(__builtin_amdgcn_exp2f(x[k] - s_M[k]), s_inv[k], w);
+        acc[key] = (key == fresh ? 0.f : before) + w;
+        key += (gridDim.y - 1) * 256;
+        if (key < n) fetch();
     }
 }
 

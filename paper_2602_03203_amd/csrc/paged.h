@@ -41,15 +41,20 @@ __device__ __forceinline__ int pairs_of(const PagedParams& P, int b) { return mi
 
 __device__ __forceinline__ bool page_ok(const PagedParams& P, int page) { return (unsigned)page < (unsigned)P.n_pages; }
 
-// The sequence that token t belongs to, -1 for none (q_start ascending: the last one that starts at or before t)
-__device__ __forceinline__ int sequence_of(const PagedParams& P, int t) {
-    int lo = 0, hi = P.batch;
-    while (lo < hi) {
-        const int mid = (lo + hi) / 2;
-        if (P.q_start[mid + 1] > t) hi = mid;
-        else lo = mid + 1;
+// The sequence that token t belongs to, -1 for none (q_start ascending: the first one that ends behind t), and its end.  `from`: the first token that
+// any lane of the wavefront asks for; the ends are looked at 64 at a time, then a lane walks on from there.
+__device__ __forceinline__ int sequence_of(const PagedParams& P, int t, int from) {
+    const int lane = threadIdx.x & (kWave - 1);
+    int b = P.batch;
+    for (int base = 0; base < P.batch; base += kWave) {
+        const unsigned long long m = __ballot(base + lane < P.batch && P.q_start[min(base + lane, P.batch - 1) + 1] > from);
+        if (m) {
+            b = base + __ffsll((long long)m) - 1;
+            break;
+        }
     }
-    return lo < P.batch && P.q_start[lo] <= t ? lo : -1;
+    while (b < P.batch && P.q_start[b + 1] <= t) ++b;
+    return b < P.batch && P.q_start[b] <= t ? b : -1;
 }
 
 __device__ __forceinline__ bool sees(const PagedParams& P, int p, int j) { return j <= p && (j > p - P.window || j < P.sink); }
@@ -85,8 +90,14 @@ __device__ __forceinline__ bool chunk_of(const PagedParams& P, const TileGrid& G
 __device__ __forceinline__ bool tile_of(const PagedParams& P, const TileGrid& G, int slot, int tm, TileOf& t) {
     int tiles;
     if (!G.spread) {
-        const int i = slot / P.batch;
-        if (!chunk_of(P, G, slot - i * P.batch, t, tm, tiles) || i >= tiles) return false;
+        const int i = scalar(slot / P.batch);
+        t.b = slot - i * P.batch;
+        t.begin = min(max(load_uniform(P.q_start, t.b), 0), P.n_tokens);
+        t.nq = min(max(load_uniform(P.q_start, t.b + 1), t.begin), P.n_tokens) - t.begin;
+        t.n = min(max(load_uniform(P.kv_len, t.b), 0), P.max_pages << P.page_shift);
+        const int rows = t.nq * P.g;
+        tiles = rows >= G.least && rows <= G.most ? (rows + tm - 1) / tm : 0;
+        if (i >= tiles) return false;
         t.tile = tiles - 1 - i;
         t.step = G.per_seq;
         t.one = tiles <= G.per_seq;
@@ -115,6 +126,7 @@ __device__ __forceinline__ bool tile_of(const PagedParams& P, const TileGrid& G,
         if (found < 0) return false;
         chunk_of(P, G, found, t, tm, tiles);
         t.tile = tiles - 1 - scalar(at);
+        t.n = pairs_of(P, found);
         t.step = 1 << 30;   // (as many slots as there can be tiles)
         t.one = true;
     }
@@ -122,9 +134,9 @@ __device__ __forceinline__ bool tile_of(const PagedParams& P, const TileGrid& G,
     t.b = scalar(t.b);
     t.begin = scalar(t.begin);
     t.nq = scalar(t.nq);
+    t.n = scalar(t.n);
     t.tile = scalar(t.tile);
     t.step = scalar(t.step);
-    t.n = min(max(load_uniform(P.kv_len, t.b), 0), P.max_pages << P.page_shift);
     t.first = t.n - t.nq;
     return true;
 }

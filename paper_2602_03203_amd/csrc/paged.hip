@@ -15,9 +15,8 @@ __global__ __launch_bounds__(256) void paged_append_kernel(const PagedParams P, 
     const size_t pair = i >> chunk_shift;
     const int c = (int)(i & ((1u << chunk_shift) - 1));
     const int t = (int)(pair / P.n_kv), h = (int)(pair % P.n_kv);
-    if (t >= P.n_tokens) return;
-    const int b = sequence_of(P, t);
-    if (b < 0) return;
+    const int b = sequence_of(P, min(t, P.n_tokens - 1), min(__builtin_amdgcn_readfirstlane(t), P.n_tokens - 1));   // (all lanes take part)
+    if (t >= P.n_tokens || b < 0) return;
     const int begin = chunk_begin(P, b), p = pairs_of(P, b) - (chunk_end(P, b, begin) - t);
     if (p < 0) return;
     const int page = P.table[(size_t)b * P.max_pages + (p >> P.page_shift)];

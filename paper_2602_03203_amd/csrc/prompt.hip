@@ -397,7 +397,7 @@ static fk_status prompt_launch(const fk_paged_desc* d, AttnPagedParams& P, int m
     static bool lds_ok[kMaxDevices] = {};
     if (!allow_dynamic_lds((const void*)kern, C::LDS_BYTES, lds_ok)) return FK_ERR_LAUNCH;
     hipLaunchKernelGGL(kern, dim3((unsigned)items, P.splits), dim3(256), C::LDS_BYTES, st, P);
-    if (P.splits > 1) hipLaunchKernelGGL((merge_kernel<T, D, kPromptRows, C::KT, false>), dim3((unsigned)items, kPromptRows / 16), dim3(256), 0, st, P);
+    if (P.splits > 1) hipLaunchKernelGGL((merge_kernel<T, D, kPromptRows, C::KT>), dim3((unsigned)items, kPromptRows / 16), dim3(256), 0, st, P);
     return launch_status();
 }
 

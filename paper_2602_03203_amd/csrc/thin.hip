@@ -25,6 +25,12 @@ template <typename T, int D> struct ThinCfg {
     static constexpr int VL = BF ? 8 : 4 * D / 64;       // V loads per lane and tile (bf16 D = 64: 8 bytes each)
     static constexpr int ET = D / 16;                    // channel tiles of the output
     static constexpr int PART = D + 4;                   // float stride of a row of a partial output in LDS
+    // dynamic LDS: partial outputs [WAVES][R][PART] (R rows: 16, for rows of a cache 8, the heads of a group) | maxima, sums, merge weights
+    // [WAVES][16] each | merged maxima and sums [16] each | rows of a cache, sixteen wavefronts: logits [8][LGN]
+    static constexpr int LGN = 1024;
+    static constexpr size_t lds(bool rows, int waves) {
+        return sizeof(float) * ((size_t)waves * (rows ? 8 : 16) * PART + 3 * waves * 16 + 32 + (rows && waves == 16 ? 8 * LGN : 0));
+    }
 };
 
 // channel of element i of a lane's output registers o[e]: MFMA row quad * 4 + i of channel tile e
@@ -34,7 +40,7 @@ template <typename T, int D> __device__ __forceinline__ int channel_of(int row, 
 }
 
 template <typename T, int D, bool ROWS, int WAVES, bool NT_LOADS>
-__global__ __launch_bounds__(WAVES * kWave, WAVES == 8 ? 2 : 3) void thin_kernel(const AttnPagedParams P) {
+__global__ __launch_bounds__(WAVES * kWave, WAVES == 4 ? 3 : WAVES / 4) void thin_kernel(const AttnPagedParams P) {
     using C = ThinCfg<T, D>;
     constexpr bool BF = C::BF;
     constexpr int CH = C::CH, KT = C::KT, NT = C::NT, KS = C::KS, VL = C::VL, ET = C::ET, PART = C::PART;
@@ -44,8 +50,12 @@ __global__ __launch_bounds__(WAVES * kWave, WAVES == 8 ? 2 : 3) void thin_kernel
     const int n_kv = ROWS ? 1 : W.n_kv, slot = ROWS ? (int)blockIdx.x : scalar(blockIdx.x / n_kv), h = ROWS ? 0 : (int)blockIdx.x - slot * n_kv, split = blockIdx.y;
     const int g = W.g;
 
-    __shared__ __attribute__((aligned(16))) float s_o[WAVES][16][PART];
-    __shared__ float s_m[WAVES][16], s_l[WAVES][16], s_w[WAVES][16], s_M[16], s_L[16];
+    constexpr int R = ROWS ? 8 : 16;
+    extern __shared__ __attribute__((aligned(16))) float smem_thin[];
+    float (*s_o)[R][PART] = reinterpret_cast<float (*)[R][PART]>(smem_thin);
+    float (*s_m)[16] = reinterpret_cast<float (*)[16]>(smem_thin + WAVES * R * PART), (*s_l)[16] = s_m + WAVES, (*s_w)[16] = s_l + WAVES;
+    float *s_M = s_w[WAVES], *s_L = s_M + 16, *s_lg = s_L + 16;
+    constexpr int LGN = ROWS && WAVES == 16 ? C::LGN : 0;   // rows of up to so many pairs keep their logits in LDS
     __shared__ int s_bad;   // a value that not every row of a run sees is infinite or NaN
 
     TileOf t;
@@ -71,6 +81,8 @@ __global__ __launch_bounds__(WAVES * kWave, WAVES == 8 ? 2 : 3) void thin_kernel
         // this lane's row
         const int my_token = (r0 + min(n16, rows - 1)) / g, my_head = (r0 + min(n16, rows - 1)) % g;
         const size_t q_row = ((size_t)(t.begin + my_token) * n_kv + h) * g + my_head;
+        const bool lg_local = LGN > 0 && splits == 1 && t.n <= LGN;
+        const float acc_first = ROWS && splits == 1 && tid < t.n ? P.acc[(size_t)slot * P.cap + tid] : 0.f;   // (on its way over the whole loop)
         T128 q[KS];
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks) {
@@ -217,7 +229,7 @@ __global__ __launch_bounds__(WAVES * kWave, WAVES == 8 ? 2 : 3) void thin_kernel
             }
             if constexpr (ROWS) {   // kept: with the final maximum and sum they become weights
                 if (n16 < g) {
-                    float* lg = P.logit + ((size_t)slot * g + n16) * P.cap + base + quad * (NT * 4);
+                    float* lg = lg_local ? s_lg + n16 * LGN + base + quad * (NT * 4) : P.logit + ((size_t)slot * g + n16) * P.logit_stride + base + quad * (NT * 4);
                     if (base + KT <= t.n) {
 #pragma unroll
                         for (int j = 0; j < NT * 4; j += 4) *reinterpret_cast<float4*>(lg + j) = make_float4(s[j], s[j + 1], s[j + 2], s[j + 3]);
@@ -305,6 +317,7 @@ __global__ __launch_bounds__(WAVES * kWave, WAVES == 8 ? 2 : 3) void thin_kernel
             s_m[wave][n16] = m_run;
             s_l[wave][n16] = l_run;
         }
+        if (!ROWS || n16 < R)
 #pragma unroll
         for (int k = 0; k < 4; ++k)
 #pragma unroll
@@ -352,17 +365,7 @@ __global__ __launch_bounds__(WAVES * kWave, WAVES == 8 ? 2 : 3) void thin_kernel
                 if (d == 0) P.rec_ml[rec + r] = make_float2(s_M[r], s_L[r]);
                 continue;
             }
-            const float L = s_L[r];
-            const size_t row = ((size_t)(t.begin + (r0 + r) / g) * n_kv + h) * g + (r0 + r) % g;
-            if (L == 0.f) a[0] = a[1] = a[2] = a[3] = 0.f;   // nothing seen
-            const float inv = L == 0.f ? 1.f : L;
-            if constexpr (BF) {
-                const tu32x2_t y = {pack_bf16(a[0] / inv, a[1] / inv), pack_bf16(a[2] / inv, a[3] / inv)};
-                *reinterpret_cast<tu32x2_t*>(reinterpret_cast<bf16_t*>(P.out) + row * D + d) = y;
-            } else {
-                *reinterpret_cast<float4*>(reinterpret_cast<float*>(P.out) + row * D + d) = make_float4(a[0] / inv, a[1] / inv, a[2] / inv, a[3] / inv);
-            }
-            if (P.stats && d == 0) P.stats[row] = make_float2(s_M[r], L);
+            store_row<T, D>(P, ((size_t)(t.begin + (r0 + r) / g) * n_kv + h) * g + (r0 + r) % g, d, a, s_M[r], s_L[r]);
         }
         if constexpr (ROWS) {
             // the new pair joins the cache (its slot is read by nobody in this launch)
@@ -376,10 +379,19 @@ __global__ __launch_bounds__(WAVES * kWave, WAVES == 8 ? 2 : 3) void thin_kernel
             if (splits > 1) return;
             // one workgroup a row: the weights, from the logits that this workgroup has written (the barriers above make them visible)
             float* acc = P.acc + (size_t)slot * P.cap;
+            const float* lg = lg_local ? s_lg : P.logit + (size_t)slot * g * P.logit_stride;
+            const int stride = lg_local ? LGN : P.logit_stride;
+            float inv[8];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) inv[k] = k < g ? 1.0f / s_L[k] : 0.f;
             for (int key = tid; key < t.n; key += WAVES * kWave) {
-                float w = 0.f;
-                for (int k = 0; k < g; ++k) w += __builtin_amdgcn_exp2f(P.logit[((size_t)slot * g + k) * P.cap + key] - ref_of(s_M[k])) / s_L[k];
-                acc[key] = (key == fresh ? 0.f : acc[key]) + w;
+                float x[8], w = 0.f;
+#pragma unroll
+                for (int k = 0; k < 8; ++k) x[k] = lg[(size_t)min(k, g - 1) * stride + key];
+#pragma unroll
+                for (int k = 0; k < 8; ++k)
+                    if (k < g) w = fmaf(__builtin_amdgcn_exp2f(x[k] - ref_of(s_M[k])), inv[k], w);
+                acc[key] = (key == fresh ? 0.f : key == tid ? acc_first : acc[key]) + w;
             }
             if (tid == 0 && fresh >= 0 && P.splits == 1) P.len[slot] = t.n;
             return;
@@ -409,12 +421,22 @@ size_t thin_paged_workspace(const fk_paged_desc* d, const TileGrid& G, int max_l
     return record_bytes(items, thin_split_count(items, max_len, d->dtype == FK_BF16 ? 32 : 16, 4, least), 16, d->head_dim);
 }
 
+template <typename T, int D, bool ROWS, int WAVES, bool NT_LOADS>
+static fk_status thin_start(const AttnPagedParams& P, dim3 grid, hipStream_t st) {
+    auto kern = thin_kernel<T, D, ROWS, WAVES, NT_LOADS>;
+    constexpr size_t lds = ThinCfg<T, D>::lds(ROWS, WAVES);
+    static bool lds_ok[kMaxDevices] = {};
+    if (lds > 48 * 1024 && !allow_dynamic_lds((const void*)kern, lds, lds_ok)) return FK_ERR_LAUNCH;
+    hipLaunchKernelGGL(kern, grid, dim3(WAVES * kWave), lds, st, P);
+    return launch_status();
+}
+
 template <typename T, int D>
 static fk_status thin_paged_launch(const fk_paged_desc* d, AttnPagedParams& P, bool cold, hipStream_t st) {
     const dim3 grid(P.grid.places * d->n_kv_heads, P.splits);
-    if (cold) hipLaunchKernelGGL((thin_kernel<T, D, false, 4, true>), grid, dim3(256), 0, st, P);
-    else hipLaunchKernelGGL((thin_kernel<T, D, false, 4, false>), grid, dim3(256), 0, st, P);
-    if (P.splits > 1) hipLaunchKernelGGL((merge_kernel<T, D, 16, ThinCfg<T, D>::KT, false>), dim3(grid.x), dim3(256), 0, st, P);
+    const fk_status s = cold ? thin_start<T, D, false, 4, true>(P, grid, st) : thin_start<T, D, false, 4, false>(P, grid, st);
+    if (s != FK_OK) return s;
+    if (P.splits > 1) hipLaunchKernelGGL((merge_kernel<T, D, 16, ThinCfg<T, D>::KT>), dim3(grid.x), dim3(256), 0, st, P);
     return launch_status();
 }
 
@@ -428,40 +450,56 @@ fk_status thin_paged(const fk_paged_desc* d, AttnPagedParams P, int max_len, voi
     return d->head_dim == 64 ? thin_paged_launch<bf16_t, 64>(d, P, cold, st) : thin_paged_launch<bf16_t, 128>(d, P, cold, st);
 }
 
-// workspace of the accumulating step: info [rows] | logits [rows][g][cap] | records
-static int rows_splits(const fk_cache_desc* d, int max_len, int waves, int& least) {
-    return thin_split_count((long long)d->batch * d->n_kv_heads, max_len, d->dtype == FK_BF16 ? 32 : 16, waves, least);
+// workspace of the accumulating step: info [rows] | logits [rows][g][cap rounded up] | records
+struct RowsPlan {
+    int waves, splits, least;
+};
+static RowsPlan rows_plan(const fk_cache_desc* d, int max_len) {
+    RowsPlan p = {4, 1, 0};
+    p.splits = thin_split_count((long long)d->batch * d->n_kv_heads, max_len, d->dtype == FK_BF16 ? 32 : 16, 4, p.least);
+    return p;
 }
-static size_t rows_logit_bytes(const fk_cache_desc* d) { return up256((size_t)d->batch * d->n_q_heads * d->capacity * sizeof(float)); }
+static int logit_stride(const fk_cache_desc* d) { return (d->capacity + 3) / 4 * 4; }
+static size_t rows_logit_bytes(const fk_cache_desc* d) { return up256((size_t)d->batch * d->n_q_heads * logit_stride(d) * sizeof(float)); }
 
 size_t thin_rows_workspace(const fk_cache_desc* d) {
     const size_t rows = (size_t)d->batch * d->n_kv_heads;
-    int least;
-    return up256(rows * sizeof(int2)) + rows_logit_bytes(d) + record_bytes(rows, rows_splits(d, d->capacity, 4, least), 16, d->head_dim);
+    int least;   // (records for the most splits of any length)
+    const int splits = thin_split_count(rows, d->capacity, d->dtype == FK_BF16 ? 32 : 16, 4, least);
+    return up256(rows * sizeof(int2)) + rows_logit_bytes(d) + record_bytes(rows, splits, 16, d->head_dim);
 }
 
-template <typename T, int D, int WAVES>
-static fk_status thin_rows_launch(AttnPagedParams& P, int max_len, bool cold, hipStream_t st) {
+template <typename T, int D>
+static fk_status thin_rows_launch(AttnPagedParams& P, const RowsPlan& p, int max_len, bool cold, hipStream_t st) {
     const dim3 grid(P.view.batch, P.splits);
-    if (cold) hipLaunchKernelGGL((thin_kernel<T, D, true, WAVES, true>), grid, dim3(WAVES * kWave), 0, st, P);
-    else hipLaunchKernelGGL((thin_kernel<T, D, true, WAVES, false>), grid, dim3(WAVES * kWave), 0, st, P);
-    if (P.splits > 1) hipLaunchKernelGGL((merge_kernel<T, D, 16, ThinCfg<T, D>::KT, true>), dim3(grid.x, (max_len + 1023) / 1024), dim3(256), 0, st, P);
+    fk_status s;
+    if (p.waves == 4) s = cold ? thin_start<T, D, true, 4, true>(P, grid, st) : thin_start<T, D, true, 4, false>(P, grid, st);
+    else if (p.waves == 8 || D == 128) s = cold ? thin_start<T, D, true, 8, true>(P, grid, st) : thin_start<T, D, true, 8, false>(P, grid, st);
+    else s = thin_start<T, 64, true, 16, false>(P, grid, st);
+    if (s != FK_OK) return s;
+    if (P.splits > 1) {
+        const int parts = max_len < 4096 * 256 ? (max_len + 255) / 256 : 4096;
+        hipLaunchKernelGGL((merge_rows_kernel<T, D, ThinCfg<T, D>::KT>), dim3(grid.x, parts + 1), dim3(256), 0, st, P);
+    }
     return launch_status();
 }
 
 fk_status thin_rows(const fk_cache_desc* d, AttnPagedParams P, int max_len, void* ws, hipStream_t st) {
     const size_t rows = (size_t)d->batch * d->n_kv_heads;
-    P.splits = rows_splits(d, max_len, 4, P.split_tiles);
+    const RowsPlan p = rows_plan(d, max_len);
+    P.splits = p.splits;
+    P.split_tiles = p.least;
     char* at = static_cast<char*>(ws);
     P.info = reinterpret_cast<int2*>(at);
     at += up256(rows * sizeof(int2));
     P.logit = reinterpret_cast<float*>(at);
+    P.logit_stride = logit_stride(d);
     at += rows_logit_bytes(d);
     P.rec_ml = reinterpret_cast<float2*>(at);
     P.rec = reinterpret_cast<float*>(at + up256(rows * P.splits * 16 * sizeof(float2)));
     const bool cold = (d->flags & FK_CACHE_COLD) || rows * max_len * d->head_dim * (d->dtype == FK_F32 ? 8 : 4) >= ((size_t)352 << 20);
-    if (d->dtype == FK_F32) return d->head_dim == 64 ? thin_rows_launch<float, 64, 4>(P, max_len, cold, st) : thin_rows_launch<float, 128, 4>(P, max_len, cold, st);
-    return d->head_dim == 64 ? thin_rows_launch<bf16_t, 64, 4>(P, max_len, cold, st) : thin_rows_launch<bf16_t, 128, 4>(P, max_len, cold, st);
+    if (d->dtype == FK_F32) return d->head_dim == 64 ? thin_rows_launch<float, 64>(P, p, max_len, cold, st) : thin_rows_launch<float, 128>(P, p, max_len, cold, st);
+    return d->head_dim == 64 ? thin_rows_launch<bf16_t, 64>(P, p, max_len, cold, st) : thin_rows_launch<bf16_t, 128>(P, p, max_len, cold, st);
 }
 
 }  // namespace fk
