@@ -46,7 +46,7 @@ struct AttnPagedParams {
     float2* stats;             // [tokens][heads] or null
     TileGrid grid;
     int splits;                // of a tile's pairs, at most
-    int split_tiles;           // key tiles of a split, at least
+    int split_shift;           // key tiles of a split, at least 2^split_shift
     float* rec;                // [slot][head][split][16][D], with more than one split
     float2* rec_ml;            // [slot][head][split][16]
     // rows of a budgeted cache
@@ -57,13 +57,14 @@ struct AttnPagedParams {
     int batch_of_pos;          // KV heads: row r belongs to sequence r / batch_of_pos
     float* acc;                // [rows][cap]
     float* logit;              // [rows][g][logit_stride] scratch
+    bool logits_lds;           // unsplit rows keep them in LDS
     int logit_stride;          // cap, rounded up to whole 16-byte groups
     int2* info;                // [rows] (pairs, the new pair's slot or -1): for the second launch
 };
 
-// Splits of a tile of `total` key tiles: as many as leave `least` to each
-__host__ __device__ inline int splits_of(int total, int splits, int least) {
-    const int s = total / least;
+// Splits of a tile of `total` key tiles: as many as leave 2^shift to each
+__host__ __device__ inline int splits_of(int total, int splits, int shift) {
+    const int s = total >> shift;
     return s < 1 ? 1 : s < splits ? s : splits;
 }
 
@@ -123,19 +124,20 @@ __device__ __forceinline__ void store_row(const AttnPagedParams& P, size_t row, 
 template <typename T, int D, int TM, int KT>
 __global__ __launch_bounds__(256) void merge_kernel(const AttnPagedParams P) {
     const PagedParams& W = P.view;
-    const int tid = threadIdx.x, n_kv = W.n_kv, slot = scalar(blockIdx.x / n_kv), h = (int)blockIdx.x - slot * n_kv, g = W.g;
+    const int tid = threadIdx.x, n_kv = W.n_kv, slot = scalar(divide(blockIdx.x, n_kv, W.kv_magic)), h = (int)blockIdx.x - slot * n_kv, g = W.g;
     const int sub = blockIdx.y * 16;   // the workgroup's 16 rows of the tile
     TileOf t;
     if (!tile_of(W, P.grid, slot, TM, t) || !t.one) return;   // (places that take several tiles do not split them)
     const int tile_rows = min(TM, t.nq * g - t.tile * TM), rows = min(16, tile_rows - sub), r0 = t.tile * TM + sub;
-    const int lo = t.first + t.tile * TM / g, hi = t.first + (t.tile * TM + tile_rows - 1) / g;
-    const int splits = splits_of(key_tiles(W, lo, hi, KT).total, P.splits, P.split_tiles);
+    const int lo = t.first + divide(t.tile * TM, g, W.g_magic), hi = t.first + divide(t.tile * TM + tile_rows - 1, g, W.g_magic);
+    const int splits = splits_of(key_tiles(W, lo, hi, KT).total, P.splits, P.split_shift);
     if (rows <= 0 || splits == 1) return;
     const size_t rec = ((size_t)slot * n_kv + h) * P.splits * TM + sub;
     for (int x = tid; x < rows * (D / 4); x += 256) {
         const int r = x / (D / 4), d = x % (D / 4) * 4;
         const Merged<D> o = merge_records<D>(P, rec + r, TM, splits, d);
-        store_row<T, D>(P, ((size_t)(t.begin + (r0 + r) / g) * n_kv + h) * g + (r0 + r) % g, d, o.a, o.M, o.L);
+        const int tok = divide(r0 + r, g, W.g_magic);
+        store_row<T, D>(P, ((size_t)(t.begin + tok) * n_kv + h) * g + (r0 + r - tok * g), d, o.a, o.M, o.L);
     }
 }
 
@@ -147,7 +149,7 @@ __global__ __launch_bounds__(256) void merge_rows_kernel(const AttnPagedParams P
     __shared__ float2 s_ml[kMostSplits][8];
     __shared__ float s_M[8], s_inv[8];
     const int n = load_uniform(&P.info[slot].x, 0), fresh = load_uniform(&P.info[slot].y, 0);
-    const int splits = splits_of(key_tiles(P.view, n - 1, n - 1, KT).total, P.splits, P.split_tiles);
+    const int splits = splits_of(key_tiles(P.view, n - 1, n - 1, KT).total, P.splits, P.split_shift);
     const size_t rec = (size_t)slot * P.splits * 16;
     if (blockIdx.y == gridDim.y - 1) {
         if (tid == 0 && fresh >= 0) P.len[slot] = n;

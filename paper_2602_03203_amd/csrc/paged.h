@@ -12,7 +12,23 @@ struct PagedParams {
     int window, sink;      // window: INT_MAX without one
     float scale_log2e;     // >= 0: queries are negated as they are read where softmax_scale is negative (exact)
     bool negate;
+    uint32_t g_magic, kv_magic, batch_magic;   // for divisions by g, n_kv, batch (magic_of)
 };
+
+// x / n for 0 <= x < 2^31 by a multiplication: magic = floor(2^32 / n) (n = 1: 2^32 - 1) is short by less than one unit of the quotient
+inline uint32_t magic_of(int n) { return n == 1 ? 0xffffffffu : (uint32_t)((1ull << 32) / n); }
+__device__ __forceinline__ int divide(int x, int n, uint32_t magic) {
+    int q = (int)__umulhi((uint32_t)x, magic);
+    if (x - q * n >= n) ++q;
+    return q;
+}
+// small quotients (x < 2^24) of numbers that only the device knows
+__device__ __forceinline__ int divide(int x, int n) {
+    int q = (int)((float)x * __builtin_amdgcn_rcpf((float)n));
+    if (x - q * n >= n) ++q;
+    if (x - q * n < 0) --q;
+    return q;
+}
 
 // A value that is the same for every lane, in a scalar register.  (Opaque first: the builtin is dropped where the compiler knows as much; it then
 // keeps what integer divisions gave, and all that follows from it, in vector registers: page numbers by vector loads, branches by exec masks, 60
@@ -90,13 +106,13 @@ __device__ __forceinline__ bool chunk_of(const PagedParams& P, const TileGrid& G
 __device__ __forceinline__ bool tile_of(const PagedParams& P, const TileGrid& G, int slot, int tm, TileOf& t) {
     int tiles;
     if (!G.spread) {
-        const int i = scalar(slot / P.batch);
+        const int i = scalar(divide(slot, P.batch, P.batch_magic));
         t.b = slot - i * P.batch;
         t.begin = min(max(load_uniform(P.q_start, t.b), 0), P.n_tokens);
         t.nq = min(max(load_uniform(P.q_start, t.b + 1), t.begin), P.n_tokens) - t.begin;
         t.n = min(max(load_uniform(P.kv_len, t.b), 0), P.max_pages << P.page_shift);
         const int rows = t.nq * P.g;
-        tiles = rows >= G.least && rows <= G.most ? (rows + tm - 1) / tm : 0;
+        tiles = rows >= G.least && rows <= G.most ? (uint32_t)(rows + tm - 1) / (uint32_t)tm : 0;
         if (i >= tiles) return false;
         t.tile = tiles - 1 - i;
         t.step = G.per_seq;
@@ -150,10 +166,10 @@ __device__ __forceinline__ KeyTiles key_tiles(const PagedParams& P, int lo, int 
     KeyTiles k;
     const int end = hi + 1;                                         // pairs up to here
     const int from = P.window == 0x7fffffff ? 0 : max(0, lo - P.window + 1);
-    k.na = (min(P.sink, max(end, 0)) + kt - 1) / kt;
-    k.b0 = from / kt;
+    k.na = (uint32_t)(min(P.sink, max(end, 0)) + kt - 1) / (uint32_t)kt;
+    k.b0 = (uint32_t)from / (uint32_t)kt;
     if (k.b0 <= k.na) k.na = k.b0 = 0;
-    const int b1 = (max(end, 0) + kt - 1) / kt;
+    const int b1 = (uint32_t)(max(end, 0) + kt - 1) / (uint32_t)kt;
     k.total = k.na + max(b1 - k.b0, 0);
     return k;
 }
@@ -200,6 +216,9 @@ inline PagedParams paged_params(const fk_paged_desc* d, const int32_t* table, co
     P.n_pages = d->n_pages;
     P.max_pages = d->max_pages;
     P.n_tokens = n_tokens;
+    P.g_magic = magic_of(P.g);
+    P.kv_magic = magic_of(P.n_kv);
+    P.batch_magic = magic_of(P.batch);
     return P;
 }
 

@@ -54,7 +54,7 @@ __global__ __launch_bounds__(256, 2) void prompt_kernel(const AttnPagedParams P)
     constexpr int CH = C::CH, KS = C::KS, ET = C::ET, KT = C::KT, NT = C::NT, BLK = C::BLK, NB = C::NB, GI = C::GI, CT = C::CT, TM = C::TM, LD = C::LD, RPU = C::RPU;
     const PagedParams& W = P.view;
     const int tid = threadIdx.x, lane = tid & (kWave - 1), n16 = lane & 15, quad = lane >> 4, wave = scalar(tid / kWave);
-    const int n_kv = W.n_kv, slot = scalar(blockIdx.x / n_kv), h = (int)blockIdx.x - slot * n_kv, split = blockIdx.y, g = W.g;
+    const int n_kv = W.n_kv, slot = scalar(divide(blockIdx.x, n_kv, W.kv_magic)), h = (int)blockIdx.x - slot * n_kv, split = blockIdx.y, g = W.g;
     extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
     __shared__ int s_bad;
     TileOf t;
@@ -78,20 +78,21 @@ __global__ __launch_bounds__(256, 2) void prompt_kernel(const AttnPagedParams P)
 
     for (; t.tile >= 0; t.tile -= t.step) {
         const int r0 = t.tile * TM, rows = min(TM, t.nq * g - r0);
-        const int tile_lo = scalar(t.first + r0 / g), tile_hi = scalar(t.first + (r0 + rows - 1) / g);
+        auto token_of = [&](int r) { return divide(r, g, W.g_magic); };
+        const int tile_lo = scalar(t.first + token_of(r0)), tile_hi = scalar(t.first + token_of(r0 + rows - 1));
         const KeyTiles kt = key_tiles(W, tile_lo, tile_hi, KT);
-        const int splits = scalar(splits_of(kt.total, t.one ? P.splits : 1, P.split_tiles));
+        const int splits = scalar(splits_of(kt.total, t.one ? P.splits : 1, P.split_shift));
         if (split >= splits) continue;
-        const int per = scalar((kt.total + splits - 1) / splits), t_begin = min(split * per, kt.total), t_end = min(t_begin + per, kt.total);
+        const int per = splits == 1 ? kt.total : scalar(divide(kt.total + splits - 1, splits)), t_begin = min(split * per, kt.total), t_end = min(t_begin + per, kt.total);
 
         // the wavefront's rows
         const int w0 = r0 + wave * 32, w_rows = min(32, rows - wave * 32);   // <= 0: none
-        const int w_first = scalar(t.first + w0 / g), w_last = scalar(t.first + (w0 + max(w_rows, 1) - 1) / g);
+        const int w_first = scalar(t.first + token_of(w0)), w_last = scalar(t.first + token_of(w0 + max(w_rows, 1) - 1));
         int pos[CT];
         T128 q[CT][KS];
 #pragma unroll
         for (int ct = 0; ct < CT; ++ct) {
-            const int r = w0 + ct * 16 + n16, rc = min(r, r0 + rows - 1), tok = rc / g;
+            const int r = w0 + ct * 16 + n16, rc = min(r, r0 + rows - 1), tok = token_of(rc);
             pos[ct] = r < r0 + rows ? t.first + tok : INT_MIN;   // (negative ones see nothing)
             const size_t q_row = ((size_t)(t.begin + tok) * n_kv + h) * g + (rc - tok * g);
 #pragma unroll
@@ -336,7 +337,7 @@ __global__ __launch_bounds__(256, 2) void prompt_kernel(const AttnPagedParams P)
             for (int ct = 0; ct < CT; ++ct) {
                 const float l = quad_sum(l_run[ct]), f = __builtin_amdgcn_exp2f(m_ref[ct] - ref_of(m_top[ct]));
                 if (!mine[ct]) continue;
-                const int r = w0 + ct * 16 + n16, tok = r / g;
+                const int r = w0 + ct * 16 + n16, tok = token_of(r);
                 const size_t row = ((size_t)(t.begin + tok) * n_kv + h) * g + (r - tok * g);
                 const bool none = m_top[ct] == -INFINITY;
                 const size_t rec = (((size_t)slot * n_kv + h) * P.splits + split) * TM + (r - r0);
@@ -374,23 +375,23 @@ __global__ __launch_bounds__(256, 2) void prompt_kernel(const AttnPagedParams P)
 
 // ---- host side ---------------------------------------------------------------------------------------------------
 // Splits of the pairs where the tiles alone leave CUs without a workgroup, 512 pairs and more each
-static int prompt_splits(const fk_paged_desc* d, const TileGrid& G, int max_len, int kt, int& least) {
-    least = 512 / kt;
+static int prompt_splits(const fk_paged_desc* d, const TileGrid& G, int max_len, int kt, int& shift) {
+    shift = kt == 64 ? 3 : 4;
     long long s = 512 / ((long long)G.places * d->n_kv_heads);
     if (s > max_len / 512) s = max_len / 512;
     if (s > 16) s = 16;
     return s < 1 ? 1 : (int)s;
 }
 size_t prompt_workspace(const fk_paged_desc* d, const TileGrid& G, int max_len) {
-    int least;
-    return record_bytes((long long)G.places * d->n_kv_heads, prompt_splits(d, G, max_len, d->dtype == FK_BF16 ? 64 : 32, least), kPromptRows, d->head_dim);
+    int shift;
+    return record_bytes((long long)G.places * d->n_kv_heads, prompt_splits(d, G, max_len, d->dtype == FK_BF16 ? 64 : 32, shift), kPromptRows, d->head_dim);
 }
 
 template <typename T, int D>
 static fk_status prompt_launch(const fk_paged_desc* d, AttnPagedParams& P, int max_len, void* ws, hipStream_t st) {
     using C = PromptCfg<T, D>;
     const long long items = (long long)P.grid.places * d->n_kv_heads;
-    P.splits = prompt_splits(d, P.grid, max_len, C::KT, P.split_tiles);
+    P.splits = prompt_splits(d, P.grid, max_len, C::KT, P.split_shift);
     P.rec_ml = reinterpret_cast<float2*>(ws);
     P.rec = reinterpret_cast<float*>(static_cast<char*>(ws) + up256((size_t)items * P.splits * kPromptRows * sizeof(float2)));
     auto kern = prompt_kernel<T, D>;

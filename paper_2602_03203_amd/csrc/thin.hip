@@ -26,10 +26,10 @@ template <typename T, int D> struct ThinCfg {
     static constexpr int ET = D / 16;                    // channel tiles of the output
     static constexpr int PART = D + 4;                   // float stride of a row of a partial output in LDS
     // dynamic LDS: partial outputs [WAVES][R][PART] (R rows: 16, for rows of a cache 8, the heads of a group) | maxima, sums, merge weights
-    // [WAVES][16] each | merged maxima and sums [16] each | rows of a cache, sixteen wavefronts: logits [8][LGN]
+    // [WAVES][16] each | merged maxima and sums [16] each | rows of a cache: logits [8][LGN]
     static constexpr int LGN = 1024;
-    static constexpr size_t lds(bool rows, int waves) {
-        return sizeof(float) * ((size_t)waves * (rows ? 8 : 16) * PART + 3 * waves * 16 + 32 + (rows && waves == 16 ? 8 * LGN : 0));
+    static constexpr size_t lds(bool rows, int waves, bool logits) {
+        return sizeof(float) * ((size_t)waves * (rows ? 8 : 16) * PART + 3 * waves * 16 + 32 + (logits ? 8 * LGN : 0));
     }
 };
 
@@ -47,7 +47,7 @@ __global__ __launch_bounds__(WAVES * kWave, WAVES == 4 ? 3 : WAVES / 4) void thi
     const PagedParams& W = P.view;
     const int tid = threadIdx.x, lane = tid & (kWave - 1), n16 = lane & 15, quad = lane >> 4;
     const int wave = scalar(tid / kWave);
-    const int n_kv = ROWS ? 1 : W.n_kv, slot = ROWS ? (int)blockIdx.x : scalar(blockIdx.x / n_kv), h = ROWS ? 0 : (int)blockIdx.x - slot * n_kv, split = blockIdx.y;
+    const int n_kv = ROWS ? 1 : W.n_kv, slot = ROWS ? (int)blockIdx.x : scalar(divide(blockIdx.x, n_kv, W.kv_magic)), h = ROWS ? 0 : (int)blockIdx.x - slot * n_kv, split = blockIdx.y;
     const int g = W.g;
 
     constexpr int R = ROWS ? 8 : 16;
@@ -55,7 +55,7 @@ __global__ __launch_bounds__(WAVES * kWave, WAVES == 4 ? 3 : WAVES / 4) void thi
     float (*s_o)[R][PART] = reinterpret_cast<float (*)[R][PART]>(smem_thin);
     float (*s_m)[16] = reinterpret_cast<float (*)[16]>(smem_thin + WAVES * R * PART), (*s_l)[16] = s_m + WAVES, (*s_w)[16] = s_l + WAVES;
     float *s_M = s_w[WAVES], *s_L = s_M + 16, *s_lg = s_L + 16;
-    constexpr int LGN = ROWS && WAVES == 16 ? C::LGN : 0;   // rows of up to so many pairs keep their logits in LDS
+    constexpr int LGN = ROWS ? C::LGN : 0;   // rows of up to so many pairs keep their logits in LDS
     __shared__ int s_bad;   // a value that not every row of a run sees is infinite or NaN
 
     TileOf t;
@@ -72,16 +72,17 @@ __global__ __launch_bounds__(WAVES * kWave, WAVES == 4 ? 3 : WAVES / 4) void thi
     const tu32x4_t* Vp = reinterpret_cast<const tu32x4_t*>(W.V);
     for (; t.tile >= 0; t.tile -= t.step) {
         const int r0 = t.tile * 16, rows = min(16, t.nq * g - r0);
-        const int tile_lo = scalar(t.first + r0 / g), tile_hi = scalar(t.first + (r0 + rows - 1) / g);   // positions of the first and the last row
+        auto token_of = [&](int r) { return ROWS ? 0 : divide(r, g, W.g_magic); };
+        const int tile_lo = ROWS ? t.first : scalar(t.first + token_of(r0)), tile_hi = ROWS ? t.first : scalar(t.first + token_of(r0 + rows - 1));   // positions
         const KeyTiles kt = key_tiles(W, tile_lo, tile_hi, KT);
-        const int splits = scalar(splits_of(kt.total, t.one ? P.splits : 1, P.split_tiles));
+        const int splits = scalar(splits_of(kt.total, t.one ? P.splits : 1, P.split_shift));
         if (split >= splits) continue;
-        const int per = scalar((kt.total + splits - 1) / splits), t_begin = min(split * per, kt.total), t_end = min(t_begin + per, kt.total);
+        const int per = splits == 1 ? kt.total : scalar(divide(kt.total + splits - 1, splits)), t_begin = min(split * per, kt.total), t_end = min(t_begin + per, kt.total);
 
         // this lane's row
-        const int my_token = (r0 + min(n16, rows - 1)) / g, my_head = (r0 + min(n16, rows - 1)) % g;
+        const int my_row = r0 + min(n16, rows - 1), my_token = token_of(my_row), my_head = my_row - my_token * g;
         const size_t q_row = ((size_t)(t.begin + my_token) * n_kv + h) * g + my_head;
-        const bool lg_local = LGN > 0 && splits == 1 && t.n <= LGN;
+        const bool lg_local = LGN > 0 && P.logits_lds && t.n <= LGN;
         const float acc_first = ROWS && splits == 1 && tid < t.n ? P.acc[(size_t)slot * P.cap + tid] : 0.f;   // (on its way over the whole loop)
         T128 q[KS];
 #pragma unroll
@@ -228,8 +229,7 @@ __global__ __launch_bounds__(WAVES * kWave, WAVES == 4 ? 3 : WAVES / 4) void thi
                 }
             }
             if constexpr (ROWS) {   // kept: with the final maximum and sum they become weights
-                if (n16 < g) {
-                    float* lg = lg_local ? s_lg + n16 * LGN + base + quad * (NT * 4) : P.logit + ((size_t)slot * g + n16) * P.logit_stride + base + quad * (NT * 4);
+                auto keep = [&](float* lg) {
                     if (base + KT <= t.n) {
 #pragma unroll
                         for (int j = 0; j < NT * 4; j += 4) *reinterpret_cast<float4*>(lg + j) = make_float4(s[j], s[j + 1], s[j + 2], s[j + 3]);
@@ -238,6 +238,10 @@ __global__ __launch_bounds__(WAVES * kWave, WAVES == 4 ? 3 : WAVES / 4) void thi
                         for (int j = 0; j < NT * 4; ++j)
                             if (key_at(j) < t.n) lg[j] = s[j];
                     }
+                };
+                if (n16 < g) {
+                    if (lg_local) keep(s_lg + n16 * LGN + base + quad * (NT * 4));
+                    else keep(P.logit + ((size_t)slot * g + n16) * P.logit_stride + base + quad * (NT * 4));
                 }
             }
             float mx = s[0];
@@ -349,7 +353,8 @@ __global__ __launch_bounds__(WAVES * kWave, WAVES == 4 ? 3 : WAVES / 4) void thi
         const size_t rec = (((size_t)slot * n_kv + h) * P.splits + split) * 16;
         for (int x = tid; x < rows * (D / 4); x += WAVES * kWave) {
             const int r = x / (D / 4), d = x % (D / 4) * 4;
-            if (!ROWS && (t.first + (r0 + r) / g < lo || t.first + (r0 + r) / g > hi)) continue;
+            const int tok = token_of(r0 + r);
+            if (!ROWS && (t.first + tok < lo || t.first + tok > hi)) continue;
             float a[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int w = 0; w < WAVES; ++w) {
@@ -365,7 +370,7 @@ __global__ __launch_bounds__(WAVES * kWave, WAVES == 4 ? 3 : WAVES / 4) void thi
                 if (d == 0) P.rec_ml[rec + r] = make_float2(s_M[r], s_L[r]);
                 continue;
             }
-            store_row<T, D>(P, ((size_t)(t.begin + (r0 + r) / g) * n_kv + h) * g + (r0 + r) % g, d, a, s_M[r], s_L[r]);
+            store_row<T, D>(P, ((size_t)(t.begin + tok) * n_kv + h) * g + (r0 + r - tok * g), d, a, s_M[r], s_L[r]);
         }
         if constexpr (ROWS) {
             // the new pair joins the cache (its slot is read by nobody in this launch)
@@ -379,20 +384,22 @@ __global__ __launch_bounds__(WAVES * kWave, WAVES == 4 ? 3 : WAVES / 4) void thi
             if (splits > 1) return;
             // one workgroup a row: the weights, from the logits that this workgroup has written (the barriers above make them visible)
             float* acc = P.acc + (size_t)slot * P.cap;
-            const float* lg = lg_local ? s_lg : P.logit + (size_t)slot * g * P.logit_stride;
-            const int stride = lg_local ? LGN : P.logit_stride;
             float inv[8];
 #pragma unroll
             for (int k = 0; k < 8; ++k) inv[k] = k < g ? 1.0f / s_L[k] : 0.f;
-            for (int key = tid; key < t.n; key += WAVES * kWave) {
-                float x[8], w = 0.f;
+            auto add = [&](const float* lg, int stride) {
+                for (int key = tid; key < t.n; key += WAVES * kWave) {
+                    float x[8], w = 0.f;
 #pragma unroll
-                for (int k = 0; k < 8; ++k) x[k] = lg[(size_t)min(k, g - 1) * stride + key];
+                    for (int k = 0; k < 8; ++k) x[k] = lg[(size_t)min(k, g - 1) * stride + key];
 #pragma unroll
-                for (int k = 0; k < 8; ++k)
-                    if (k < g) w = fmaf(__builtin_amdgcn_exp2f(x[k] - ref_of(s_M[k])), inv[k], w);
-                acc[key] = (key == fresh ? 0.f : key == tid ? acc_first : acc[key]) + w;
-            }
+                    for (int k = 0; k < 8; ++k)
+                        if (k < g) w = fmaf(__builtin_amdgcn_exp2f(x[k] - ref_of(s_M[k])), inv[k], w);
+                    acc[key] = (key == fresh ? 0.f : key == tid ? acc_first : acc[key]) + w;
+                }
+            };
+            if (lg_local) add(s_lg, LGN);
+            else add(P.logit + (size_t)slot * g * P.logit_stride, P.logit_stride);
             if (tid == 0 && fresh >= 0 && P.splits == 1) P.len[slot] = t.n;
             return;
         }
@@ -406,10 +413,10 @@ __global__ __launch_bounds__(WAVES * kWave, WAVES == 4 ? 3 : WAVES / 4) void thi
 
 // ---- host side ---------------------------------------------------------------------------------------------------
 // Workgroups that share the tiles' pairs: enough to fill the chip, each with enough pairs to be worth a record
-static int thin_split_count(long long items, long long pairs, int kt, int waves, int& least) {
-    least = 2 * waves;   // two rounds of the wavefronts
+static int thin_split_count(long long items, long long pairs, int kt, int& shift) {
+    shift = 3;   // two rounds of the wavefronts
     long long s = 512 / items;
-    const long long most = pairs / ((long long)least * kt);
+    const long long most = pairs / ((long long)kt << shift);
     if (s > most) s = most;
     if (s > kMostSplits) s = kMostSplits;
     return s < 1 ? 1 : (int)s;
@@ -417,16 +424,17 @@ static int thin_split_count(long long items, long long pairs, int kt, int waves,
 
 size_t thin_paged_workspace(const fk_paged_desc* d, const TileGrid& G, int max_len) {
     const long long items = (long long)G.places * d->n_kv_heads;
-    int least;
-    return record_bytes(items, thin_split_count(items, max_len, d->dtype == FK_BF16 ? 32 : 16, 4, least), 16, d->head_dim);
+    int shift;
+    return record_bytes(items, thin_split_count(items, max_len, d->dtype == FK_BF16 ? 32 : 16, shift), 16, d->head_dim);
 }
 
 template <typename T, int D, bool ROWS, int WAVES, bool NT_LOADS>
 static fk_status thin_start(const AttnPagedParams& P, dim3 grid, hipStream_t st) {
     auto kern = thin_kernel<T, D, ROWS, WAVES, NT_LOADS>;
-    constexpr size_t lds = ThinCfg<T, D>::lds(ROWS, WAVES);
+    constexpr size_t most = ThinCfg<T, D>::lds(ROWS, WAVES, ROWS);
+    const size_t lds = ThinCfg<T, D>::lds(ROWS, WAVES, P.logits_lds);
     static bool lds_ok[kMaxDevices] = {};
-    if (lds > 48 * 1024 && !allow_dynamic_lds((const void*)kern, lds, lds_ok)) return FK_ERR_LAUNCH;
+    if (most > 48 * 1024 && !allow_dynamic_lds((const void*)kern, most, lds_ok)) return FK_ERR_LAUNCH;
     hipLaunchKernelGGL(kern, grid, dim3(WAVES * kWave), lds, st, P);
     return launch_status();
 }
@@ -442,7 +450,7 @@ static fk_status thin_paged_launch(const fk_paged_desc* d, AttnPagedParams& P, b
 
 fk_status thin_paged(const fk_paged_desc* d, AttnPagedParams P, int max_len, void* ws, hipStream_t st) {
     const long long items = (long long)P.grid.places * d->n_kv_heads;
-    P.splits = thin_split_count(items, max_len, d->dtype == FK_BF16 ? 32 : 16, 4, P.split_tiles);
+    P.splits = thin_split_count(items, max_len, d->dtype == FK_BF16 ? 32 : 16, P.split_shift);
     P.rec_ml = reinterpret_cast<float2*>(ws);
     P.rec = reinterpret_cast<float*>(static_cast<char*>(ws) + up256((size_t)items * P.splits * 16 * sizeof(float2)));
     const bool cold = (size_t)d->batch * d->n_kv_heads * max_len * d->head_dim * (d->dtype == FK_F32 ? 8 : 4) >= ((size_t)352 << 20);
@@ -452,11 +460,31 @@ fk_status thin_paged(const fk_paged_desc* d, AttnPagedParams P, int max_len, voi
 
 // workspace of the accumulating step: info [rows] | logits [rows][g][cap rounded up] | records
 struct RowsPlan {
-    int waves, splits, least;
+    int waves, splits, shift;
 };
+// Short rows, and as many rows as CUs, take a workgroup of eight wavefronts each, which adds the weights itself; others are split over 256 workgroups of
+// four, each with a tile for every wavefront or more, and the second launch, 3 us, adds them.  us a step, a row to a workgroup and split:
+//   bf16 D = 128, g = 4   8 rows of 300 8.0 and 8.9, of 1000 14.6 and 8.3; 32 of 500 9.9 and 8.3; 128 of 300 8.2 and 9.3, of 1000 16.9 and 16.8, of 2112
+//                         31 and 27; 256 of 600 16.4 and 21; D = 64  8 of 300 6.8 and 8.0, 32 of 500 7.4 and 7.3, 128 of 1000 11.4 and 11.4, of 2112 21 and 18
+//   fp32 D = 64           2 of 144 6.4 and 7.5, 8 of 300 8.2 and 7.9, 128 of 300 8.7 and 9.2, of 1000 20 and 17.5;  D = 128  2 of 144 9.0 and 9.2, 8 of 300
+//                         12.8 and 9.8, 128 of 300 14.1 and 14.3, of 1000 33 and 27
+// Splits: 8 rows of 4000 pairs, bf16, 8: 11.2, 16: 10.0, 32: 11.6; 32 of 2000 4: 13.4, 8: 11.8, 16: 14.1.  From 512 rows on, and fp32 with D = 128, four
+// wavefronts a row: 512 rows of 1000 44.0, eight 44.4 (fp32 88 and 92).
 static RowsPlan rows_plan(const fk_cache_desc* d, int max_len) {
-    RowsPlan p = {4, 1, 0};
-    p.splits = thin_split_count((long long)d->batch * d->n_kv_heads, max_len, d->dtype == FK_BF16 ? 32 : 16, 4, p.least);
+    const int rows = d->batch * d->n_kv_heads;
+    const bool bf16 = d->dtype == FK_BF16;
+    RowsPlan p = {8, 1, 2};
+    const int alone = bf16 ? (rows < 128 ? 384 : 1024) : d->head_dim == 64 ? (rows < 128 ? 224 : 512) : rows < 128 ? 160 : 256;
+    if (rows >= 256) {
+        if (rows >= 512 || (!bf16 && d->head_dim == 128)) p.waves = 4;
+        return p;
+    }
+    if (max_len <= alone) return p;
+    p.waves = 4;
+    p.splits = max_len / ((bf16 ? 32 : 16) << p.shift);
+    if (p.splits > 256 / rows) p.splits = 256 / rows;
+    if (p.splits > kMostSplits) p.splits = kMostSplits;
+    if (p.splits < 1) p.splits = 1;
     return p;
 }
 static int logit_stride(const fk_cache_desc* d) { return (d->capacity + 3) / 4 * 4; }
@@ -464,9 +492,7 @@ static size_t rows_logit_bytes(const fk_cache_desc* d) { return up256((size_t)d-
 
 size_t thin_rows_workspace(const fk_cache_desc* d) {
     const size_t rows = (size_t)d->batch * d->n_kv_heads;
-    int least;   // (records for the most splits of any length)
-    const int splits = thin_split_count(rows, d->capacity, d->dtype == FK_BF16 ? 32 : 16, 4, least);
-    return up256(rows * sizeof(int2)) + rows_logit_bytes(d) + record_bytes(rows, splits, 16, d->head_dim);
+    return up256(rows * sizeof(int2)) + rows_logit_bytes(d) + record_bytes(rows, rows_plan(d, d->capacity).splits, 16, d->head_dim);   // (longer rows have no fewer splits)
 }
 
 template <typename T, int D>
@@ -474,8 +500,7 @@ static fk_status thin_rows_launch(AttnPagedParams& P, const RowsPlan& p, int max
     const dim3 grid(P.view.batch, P.splits);
     fk_status s;
     if (p.waves == 4) s = cold ? thin_start<T, D, true, 4, true>(P, grid, st) : thin_start<T, D, true, 4, false>(P, grid, st);
-    else if (p.waves == 8 || D == 128) s = cold ? thin_start<T, D, true, 8, true>(P, grid, st) : thin_start<T, D, true, 8, false>(P, grid, st);
-    else s = thin_start<T, 64, true, 16, false>(P, grid, st);
+    else s = cold ? thin_start<T, D, true, 8, true>(P, grid, st) : thin_start<T, D, true, 8, false>(P, grid, st);
     if (s != FK_OK) return s;
     if (P.splits > 1) {
         const int parts = max_len < 4096 * 256 ? (max_len + 255) / 256 : 4096;
@@ -488,7 +513,8 @@ fk_status thin_rows(const fk_cache_desc* d, AttnPagedParams P, int max_len, void
     const size_t rows = (size_t)d->batch * d->n_kv_heads;
     const RowsPlan p = rows_plan(d, max_len);
     P.splits = p.splits;
-    P.split_tiles = p.least;
+    P.split_shift = p.shift;
+    P.logits_lds = p.splits == 1 && max_len <= ThinCfg<float, 64>::LGN;
     char* at = static_cast<char*>(ws);
     P.info = reinterpret_cast<int2*>(at);
     at += up256(rows * sizeof(int2));

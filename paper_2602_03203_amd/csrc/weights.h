@@ -11,7 +11,7 @@ struct WeightsParams {
     float* part;           // [splits][batch * n_kv][part_len], with more than one split of the queries
     int splits, part_len;
     int blocks;            // key blocks of a sequence in the launch
-    uint32_t g_magic;      // row / g
+    uint32_t blocks_magic;
 };
 
 size_t weights_workspace(const fk_paged_desc* d, int n_tokens, int max_chunk, int max_len);

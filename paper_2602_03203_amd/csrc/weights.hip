@@ -22,10 +22,10 @@ union W128 {
     wbf16x8_t v;
 };
 
-template <typename T, int D> struct WeightsCfg {
+template <typename T, int D, bool FEW> struct WeightsCfg {   // FEW: few keys, 16 to a wavefront
     static constexpr bool BF = sizeof(T) == 2;
     static constexpr int CH = D * (int)sizeof(T) / 16, KS = CH / 4;
-    static constexpr int KG = BF || D == 64 ? 4 : 2;      // groups of 16 keys per wavefront
+    static constexpr int KG = FEW ? 1 : BF || D == 64 ? 4 : 2;      // groups of 16 keys per wavefront
     static constexpr int KEYS = 4 * KG * 16;              // of a workgroup
     static constexpr int QT = BF ? 64 : 32;               // query rows of a tile
     static constexpr int QRS = CH * 16 + 16;              // byte stride of a row in LDS
@@ -35,21 +35,21 @@ template <typename T, int D> struct WeightsCfg {
 // |logits| from which products and maxima are subtracted as rounded numbers, not inside an fma
 static constexpr float kHugeLogit = 16777216.f;
 
-template <typename T, int D>
+template <typename T, int D, bool FEW>
 __global__ __launch_bounds__(256, 2) void weights_kernel(const WeightsParams P) {
-    using C = WeightsCfg<T, D>;
+    using C = WeightsCfg<T, D, FEW>;
     constexpr bool BF = C::BF;
     constexpr int CH = C::CH, KS = C::KS, KG = C::KG, QT = C::QT, QRS = C::QRS, LD = C::LD;
     const PagedParams& W = P.view;
     const int tid = threadIdx.x, lane = tid & (kWave - 1), n16 = lane & 15, quad = lane >> 4, wave = scalar(tid / kWave);
-    const int place = scalar(blockIdx.x / W.n_kv), h = (int)blockIdx.x - place * W.n_kv, b = scalar(place / P.blocks), split = blockIdx.y;
+    const int place = scalar(divide(blockIdx.x, W.n_kv, W.kv_magic)), h = (int)blockIdx.x - place * W.n_kv, b = scalar(divide(place, P.blocks, P.blocks_magic)), split = blockIdx.y;
     const int g = W.g;
     __shared__ __attribute__((aligned(16))) unsigned char s_q[2][QT * QRS];
     __shared__ float s_m[2][QT], s_il[2][QT];
 
     const int begin = scalar(chunk_begin(W, b)), nq = scalar(chunk_end(W, b, begin)) - begin, n = scalar(pairs_of(W, b)), first = n - nq;
     if (nq == 0) return;
-    auto token_of = [&](int row) { return g == 1 ? row : (int)__umulhi((uint32_t)row, P.g_magic); };
+    auto token_of = [&](int row) { return divide(row, g, W.g_magic); };
     const float scale = W.scale_log2e;
     for (int k0 = (place - b * P.blocks) * C::KEYS; k0 < n; k0 += P.blocks * C::KEYS) {
         const int k1 = min(k0 + C::KEYS, n);
@@ -202,45 +202,54 @@ __global__ __launch_bounds__(256) void weights_sum_kernel(const WeightsParams P)
 }
 
 // ---- host side ---------------------------------------------------------------------------------------------------
-// Queries are split where the keys alone leave CUs without a workgroup, into no less than four tiles.  Partial sums are kept up to the table's
-// length, so that a length hint below a sequence's length loses nothing.
-static int weights_splits(const fk_paged_desc* d, int n_tokens, int max_chunk, int max_len, int keys, int qt) {
-    const long long blocks = (long long)d->batch * d->n_kv_heads * ((max_len + keys - 1) / keys);
-    const long long rows = (long long)(max_chunk < n_tokens ? max_chunk : n_tokens) * (d->n_q_heads / d->n_kv_heads);
-    long long s = 512 / blocks;
-    if (s > rows / (4 * qt)) s = rows / (4 * qt);
+// Few keys leave CUs without a workgroup: then a wavefront takes 16 of them instead of 64, and beyond that the queries are split, into no less than two
+// tiles each.  Partial sums are kept up to the table's length, so that a length hint below a sequence's length loses nothing.
+struct WeightsPlan {
+    bool few;
+    int keys, splits;
+};
+template <typename T, int D> static WeightsPlan weights_plan_of(const fk_paged_desc* d, int n_tokens, int max_chunk, int max_len) {
+    const long long rows = (long long)d->batch * d->n_kv_heads;
+    auto blocks = [&](int keys) { return rows * ((max_len + keys - 1) / keys); };
+    WeightsPlan p;
+    p.few = blocks(WeightsCfg<T, D, false>::KEYS) < 128;
+    p.keys = p.few ? WeightsCfg<T, D, true>::KEYS : WeightsCfg<T, D, false>::KEYS;
+    const long long queries = (long long)(max_chunk < n_tokens ? max_chunk : n_tokens) * (d->n_q_heads / d->n_kv_heads);
+    long long s = 512 / blocks(p.keys);
+    const long long most = queries / (2 * WeightsCfg<T, D, false>::QT);
+    if (s > most) s = most;
     if (s > 16) s = 16;
-    return s < 1 || (long long)d->batch * d->n_kv_heads > 65535 ? 1 : (int)s;
+    p.splits = s < 1 || rows > 65535 ? 1 : (int)s;
+    return p;
 }
-
-template <typename T, int D> static int weights_splits_of(const fk_paged_desc* d, int n_tokens, int max_chunk, int max_len) {
-    return weights_splits(d, n_tokens, max_chunk, max_len, WeightsCfg<T, D>::KEYS, WeightsCfg<T, D>::QT);
-}
-static int weights_splits_for(const fk_paged_desc* d, int n_tokens, int max_chunk, int max_len) {
-    if (d->dtype == FK_F32) return d->head_dim == 64 ? weights_splits_of<float, 64>(d, n_tokens, max_chunk, max_len) : weights_splits_of<float, 128>(d, n_tokens, max_chunk, max_len);
-    return d->head_dim == 64 ? weights_splits_of<bf16_t, 64>(d, n_tokens, max_chunk, max_len) : weights_splits_of<bf16_t, 128>(d, n_tokens, max_chunk, max_len);
+static WeightsPlan weights_plan(const fk_paged_desc* d, int n_tokens, int max_chunk, int max_len) {
+    if (d->dtype == FK_F32) return d->head_dim == 64 ? weights_plan_of<float, 64>(d, n_tokens, max_chunk, max_len) : weights_plan_of<float, 128>(d, n_tokens, max_chunk, max_len);
+    return d->head_dim == 64 ? weights_plan_of<bf16_t, 64>(d, n_tokens, max_chunk, max_len) : weights_plan_of<bf16_t, 128>(d, n_tokens, max_chunk, max_len);
 }
 
 size_t weights_workspace(const fk_paged_desc* d, int n_tokens, int max_chunk, int max_len) {
-    const int s = weights_splits_for(d, n_tokens, max_chunk, max_len);
+    const int s = weights_plan(d, n_tokens, max_chunk, max_len).splits;
     return s > 1 ? (size_t)s * d->batch * d->n_kv_heads * d->max_pages * d->page_size * sizeof(float) : 0;
 }
 
 template <typename T, int D>
-static fk_status weights_run(const fk_paged_desc* d, WeightsParams& P, int max_len, hipStream_t st) {
-    P.blocks = (max_len + WeightsCfg<T, D>::KEYS - 1) / WeightsCfg<T, D>::KEYS;
-    hipLaunchKernelGGL((weights_kernel<T, D>), dim3((unsigned)(d->batch * d->n_kv_heads * (long long)P.blocks), P.splits), dim3(256), 0, st, P);
+static fk_status weights_run(const fk_paged_desc* d, WeightsParams& P, const WeightsPlan& p, int max_len, hipStream_t st) {
+    P.splits = p.splits;
+    P.blocks = (max_len + p.keys - 1) / p.keys;
+    P.blocks_magic = magic_of(P.blocks);
+    const dim3 grid((unsigned)(d->batch * d->n_kv_heads * (long long)P.blocks), P.splits);
+    if (p.few) hipLaunchKernelGGL((weights_kernel<T, D, true>), grid, dim3(256), 0, st, P);
+    else hipLaunchKernelGGL((weights_kernel<T, D, false>), grid, dim3(256), 0, st, P);
     if (P.splits > 1) hipLaunchKernelGGL(weights_sum_kernel, dim3((P.part_len + 255) / 256, d->batch * d->n_kv_heads), dim3(256), 0, st, P);
     return launch_status();
 }
 
 fk_status weights_launch(const fk_paged_desc* d, WeightsParams P, int max_chunk, int max_len, void* ws, hipStream_t st) {
-    P.splits = weights_splits_for(d, P.view.n_tokens, max_chunk, max_len);
+    const WeightsPlan p = weights_plan(d, P.view.n_tokens, max_chunk, max_len);
     P.part = static_cast<float*>(ws);
     P.part_len = d->max_pages * d->page_size;
-    P.g_magic = (uint32_t)(((1ull << 32) + P.view.g - 1) / P.view.g);   // row * g_magic >> 32 = row / g for rows below 2^28 and g from 2 on
-    if (d->dtype == FK_F32) return d->head_dim == 64 ? weights_run<float, 64>(d, P, max_len, st) : weights_run<float, 128>(d, P, max_len, st);
-    return d->head_dim == 64 ? weights_run<bf16_t, 64>(d, P, max_len, st) : weights_run<bf16_t, 128>(d, P, max_len, st);
+    if (d->dtype == FK_F32) return d->head_dim == 64 ? weights_run<float, 64>(d, P, p, max_len, st) : weights_run<float, 128>(d, P, p, max_len, st);
+    return d->head_dim == 64 ? weights_run<bf16_t, 64>(d, P, p, max_len, st) : weights_run<bf16_t, 128>(d, P, p, max_len, st);
 }
 
 }  // namespace fk
