@@ -412,20 +412,34 @@ __global__ __launch_bounds__(WAVES * kWave, WAVES == 4 ? 3 : WAVES / 4) void thi
 }
 
 // ---- host side ---------------------------------------------------------------------------------------------------
-// Workgroups that share the tiles' pairs: enough to fill the chip, each with enough pairs to be worth a record
-static int thin_split_count(long long items, long long pairs, int kt, int& shift) {
-    shift = 3;   // two rounds of the wavefronts
-    long long s = 512 / items;
-    const long long most = pairs / ((long long)kt << shift);
-    if (s > most) s = most;
-    if (s > kMostSplits) s = kMostSplits;
-    return s < 1 ? 1 : (int)s;
+// Splits of a tile's pairs, by the tiles of the launch and by the pairs that one may see.  us, splits at most and pairs of one at least:
+//   few tiles    8 of 32768 pairs 4 splits 78, 8 45, 16 31, 32 35;  32 of 4000 4 18.8, 8 18.3, 16 20.9;  8 of 1000 unsplit 14.5, 3 10.5;  64 of 3000
+//                (D = 64) unsplit 21.8, 2 17.1, 4 16.0, 8 16.9: up to 256 workgroups, up to sixteen splits
+//   128 and more, which fill the memory system by themselves, unsplit where they are short (128 of 2048 24.7, 2 27.1).  Long ones differ in length as a rule,
+//                and only the device knows: splits of 1024 pairs and more even them out (512 of 1024 to 32768 pairs unsplit 947, so 840; 128 of 1024 to
+//                8192 118 and 69) and cost equal ones little (512 of 4096 163 and 170, 128 of 8192 in two 86, so 89)
+struct ThinPlan {
+    int splits, shift;
+};
+static ThinPlan thin_plan(const fk_paged_desc* d, const TileGrid& G, long long pairs) {
+    const long long items = (long long)G.places * d->n_kv_heads;
+    const int kt_shift = d->dtype == FK_BF16 ? 5 : 4;
+    ThinPlan p = {1, items < 128 ? 8 - kt_shift : 10 - kt_shift};
+    long long s = 1;
+    if (items < 128) s = 256 / items;
+    else if (pairs >= 6144) s = 16;
+    if (s > 16) s = 16;
+    if (s > pairs >> (p.shift + kt_shift)) s = pairs >> (p.shift + kt_shift);
+    if (s > 1) p.splits = (int)s;
+    return p;
+}
+// the pairs that a query of the call may see
+static long long most_pairs(const PagedParams& P, int max_len) {
+    return P.window == 0x7fffffff || (long long)P.window + P.sink > max_len ? max_len : (long long)P.window + P.sink;
 }
 
 size_t thin_paged_workspace(const fk_paged_desc* d, const TileGrid& G, int max_len) {
-    const long long items = (long long)G.places * d->n_kv_heads;
-    int shift;
-    return record_bytes(items, thin_split_count(items, max_len, d->dtype == FK_BF16 ? 32 : 16, shift), 16, d->head_dim);
+    return record_bytes((long long)G.places * d->n_kv_heads, thin_plan(d, G, max_len).splits, 16, d->head_dim);   // (a window sees no more)
 }
 
 template <typename T, int D, bool ROWS, int WAVES, bool NT_LOADS>
@@ -450,7 +464,9 @@ static fk_status thin_paged_launch(const fk_paged_desc* d, AttnPagedParams& P, b
 
 fk_status thin_paged(const fk_paged_desc* d, AttnPagedParams P, int max_len, void* ws, hipStream_t st) {
     const long long items = (long long)P.grid.places * d->n_kv_heads;
-    P.splits = thin_split_count(items, max_len, d->dtype == FK_BF16 ? 32 : 16, P.split_shift);
+    const ThinPlan p = thin_plan(d, P.grid, most_pairs(P.view, max_len));
+    P.splits = p.splits;
+    P.split_shift = p.shift;
     P.rec_ml = reinterpret_cast<float2*>(ws);
     P.rec = reinterpret_cast<float*>(static_cast<char*>(ws) + up256((size_t)items * P.splits * 16 * sizeof(float2)));
     const bool cold = (size_t)d->batch * d->n_kv_heads * max_len * d->head_dim * (d->dtype == FK_F32 ? 8 : 4) >= ((size_t)352 << 20);
