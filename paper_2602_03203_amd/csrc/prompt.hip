@@ -1,13 +1,15 @@
 // Attention of prompt chunks over the pages of a prompt: tiles of 128 query rows (tokens x heads of a group) against tiles of 64 pairs (fp32: 32).
 //
 // A wavefront owns 32 rows: their q, online softmax and outputs stay in its registers.  The pairs pass by in tiles, each read once for
-// the four wavefronts: global loads a tile ahead, LDS in two buffers, one barrier a tile.  Products and operand layouts are those of thin.hip
-// (logits K.Q^T with the keys in an order that makes a lane's probabilities an operand of V^T.P^T as they are; the same 16x16 products in
-// the same order, so that logits are the same bits everywhere); an operand read from LDS serves two products, one for each 16 rows.
-//   K in LDS: 16-byte chunks of a row swizzled so that the 16 rows of an operand lie in different banks (swizzle_k)
-//   V in LDS, bf16: rows as in memory; the operand is 8 keys of one channel per lane, which the transposing LDS read delivers, 4 keys at a time
-//   (ds_read_tr16_b64: lane l of 16 gets element l % 4 of what lanes l / 4, + 4, + 8, + 12 address); swizzled for those reads (swizzle_v)
-//   fp32: four channels a lane, each a product of its own
+// the four wavefronts, straight into LDS (two buffers each for K and V, one barrier a tile).  While the vector units turn one tile's logits into
+// probabilities, the matrix units form the next one's: with a tile's steps one after the other a wavefront alone on its SIMD took 2.2 us a tile,
+// of which the products are 0.4.  Products and operand layouts are those of thin.hip (logits K.Q^T with the keys in an order that makes a
+// lane's probabilities an operand of V^T.P^T as they are; the same 16x16 products in the same order, so that logits are the same bits
+// everywhere); an operand read from LDS serves two products, one for each 16 rows.
+//   in LDS a row's 16-byte chunks change places (swizzle_k, swizzle_v), so that the 16 rows of an operand lie in different banks; a load writes LDS in
+//   the order of its lanes, so each lane fetches the chunk that belongs in its place
+//   V, bf16: the operand is 8 keys of one channel per lane, which the transposing LDS read delivers, 4 keys at a time (ds_read_tr16_b64: lane l of
+//   16 gets element l % 4 of what lanes l / 4, + 4, + 8, + 12 address); fp32: four channels a lane, each a product of its own
 // References follow a row's maximum only where it has grown by more than 2^8 (probabilities up to 256, sums in fp32: nothing is lost), so that
 // outputs are hardly ever rescaled.
 #include "attn_paged.h"
@@ -39,6 +41,11 @@ template <bool BF, int CH> __device__ __forceinline__ int swizzle_v(int row) {
     if constexpr (!BF) return 0;
     else if constexpr (CH == 16) return (row & 3) << 1 | ((row >> 3) & 1) << 3;
     else return ((row >> 1) & 1) << 1 | ((row >> 3) & 1) << 2;
+}
+
+// 16 bytes per lane from global memory to LDS, at `to` + lane * 16
+__device__ __forceinline__ void load_to_lds(const void* from, unsigned char* to) {
+    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)from, (__attribute__((address_space(3))) void*)to, 16, 0, 0);
 }
 
 typedef short ps16x4_t __attribute__((ext_vector_type(4)));
@@ -123,66 +130,64 @@ __global__ __launch_bounds__(256, 2) void prompt_kernel(const AttnPagedParams P)
 #pragma unroll
                 for (int e = 0; e < ET; ++e) o[e][ct] = (tf32x4_t){0.f, 0.f, 0.f, 0.f};
             }
-            T128 kr[LD], vr[LD];
-            int page[GI], page_next[GI];
-            auto pages_of = [&](int i, int (&pg)[GI]) {
-                const int base = kt.at(i) * KT;
+            auto base_of = [&](int i) { return kt.at(i) * KT; };
+            struct Pages {
+                int page[GI];
+            };
+            auto pages_of = [&](int i) {   // (past the end: the last tile's)
+                Pages pg;
+                const int base = base_of(min(i, t_end - 1));
 #pragma unroll
-                for (int r = 0; r < GI; ++r) pg[r] = load_uniform(tab, min((base + r * 16) >> W.page_shift, W.max_pages - 1));
+                for (int r = 0; r < GI; ++r) pg.page[r] = load_uniform(tab, min((base + r * 16) >> W.page_shift, W.max_pages - 1));
+                return pg;
             };
-            // load u of this wavefront lies in run .. of 16 pairs
-            auto page_of = [&](const int (&pg)[GI], int u) {
-                if constexpr (RPU == 32) return wave >= 2 ? pg[2 * u + 1] : pg[2 * u];
-                else return pg[u * RPU / 16];
-            };
-            auto fetch = [&](int base, const int (&pg)[GI]) {
-#pragma unroll
-                for (int u = 0; u < LD; ++u) {
-                    const int pgu = page_of(pg, u), in_tile = RPU == 32 ? u * 32 + (wave >= 2 ? 16 : 0) : u * RPU / 16 * 16;
-                    const size_t run = ((((size_t)(page_ok(W, pgu) ? pgu : 0) * n_kv + h) << W.page_shift) + ((base + in_tile) & ((1 << W.page_shift) - 1))) * CH;
-                    const int lane_at = (st_row + u * RPU) % 16 * CH + st_ch;
-                    kr[u].u = reinterpret_cast<const tu32x4_t*>(W.K)[run + lane_at];
-                    vr[u].u = reinterpret_cast<const tu32x4_t*>(W.V)[run + lane_at];
-                }
-            };
-            auto all_there = [&](const int (&pg)[GI]) {
+            auto all_there = [&](const Pages& pg) {
                 bool ok = true;
 #pragma unroll
-                for (int r = 0; r < GI; ++r) ok = ok && page_ok(W, pg[r]);
+                for (int r = 0; r < GI; ++r) ok = ok && page_ok(W, pg.page[r]);
                 return ok;
             };
-            auto stage = [&](int buf, int base, const int (&pg)[GI]) {
-                unsigned char *sk = smem + buf * C::TILE_BYTES, *sv = smem + (2 + buf) * C::TILE_BYTES;
-                const bool whole = base + KT <= lo + 1 && (!windowed || base > hi - W.window || base + KT <= W.sink) && all_there(pg);
-                if (!whole) {   // values of weight 0 must not meet the products as infinities or NaN
-                    const int any_from = windowed ? lo - W.window : -1, all_from = windowed ? hi - W.window : -1;
-                    bool bad = false;
-#pragma unroll
-                    for (int u = 0; u < LD; ++u) {
-                        const int key = base + st_row + u * RPU;
-                        const bool someone = page_ok(W, page_of(pg, u)) & (key <= hi) & ((key > any_from) | (key < W.sink));
-                        const bool everyone = (key <= lo) & ((key > all_from) | (key < W.sink));   // of those that someone sees
-                        const uint32_t keep = someone ? ~0u : 0u;
-#pragma unroll
-                        for (int w = 0; w < 4; ++w) {
-                            vr[u].w[w] &= keep;
-                            bad |= !everyone & word_not_finite<T>(vr[u].w[w]);
-                        }
-                    }
-                    if (bad && hi > lo) s_bad = 1;
-                }
+            // load u of this wavefront lies in one run of 16 pairs
+            auto page_of = [&](const Pages& pg, int u) {
+                if constexpr (RPU == 32) return wave >= 2 ? pg.page[2 * u + 1] : pg.page[2 * u];
+                else return pg.page[u * RPU / 16];
+            };
+            auto send = [&](const void* X, bool is_k, int buf, int base, const Pages& pg) {
 #pragma unroll
                 for (int u = 0; u < LD; ++u) {
-                    const int row = st_row + u * RPU;
-                    *reinterpret_cast<tu32x4_t*>(sk + row * CH * 16 + (st_ch ^ swizzle_k<BF, CH>(row)) * 16) = kr[u].u;
-                    *reinterpret_cast<tu32x4_t*>(sv + row * CH * 16 + (st_ch ^ swizzle_v<BF, CH>(row)) * 16) = vr[u].u;
+                    const int pgu = page_of(pg, u), in_tile = RPU == 32 ? u * 32 + (wave >= 2 ? 16 : 0) : u * RPU / 16 * 16, row = st_row + u * RPU;
+                    const size_t run = ((((size_t)(page_ok(W, pgu) ? pgu : 0) * n_kv + h) << W.page_shift) + ((base + in_tile) & ((1 << W.page_shift) - 1))) * (CH * 16);
+                    const int ch = st_ch ^ (is_k ? swizzle_k<BF, CH>(row) : swizzle_v<BF, CH>(row));
+                    load_to_lds(static_cast<const unsigned char*>(X) + run + (uint32_t)((row % 16 * CH + ch) * 16),
+                                smem + (is_k ? 0 : 2 * C::TILE_BYTES) + buf * C::TILE_BYTES + (u * 256 + wave * 64) * 16);
                 }
             };
-            auto compute = [&](int buf, int base, const int (&pg)[GI]) {
-                if (base > w_hi) return;   // nothing that this wavefront sees
-                if (windowed && base + KT - 1 <= w_lo - W.window && base >= W.sink) return;
-                const unsigned char *sk = smem + buf * C::TILE_BYTES, *sv = smem + (2 + buf) * C::TILE_BYTES;
-                tf32x4_t c[GI][CT];
+            auto whole_for = [&](int base, int from, int to, const Pages& pg) {   // every row at positions from .. to sees all of the tile
+                return base + KT <= from + 1 && (!windowed || base > to - W.window || base + KT <= W.sink) && all_there(pg);
+            };
+            // V of a tile that not every row sees: values of weight 0 must not meet the products as infinities or NaN
+            auto clear_hidden = [&](int buf, int base, const Pages& pg) {
+                const int any_from = windowed ? lo - W.window : -1, all_from = windowed ? hi - W.window : -1;
+                bool bad = false;
+#pragma unroll
+                for (int u = 0; u < LD; ++u) {
+                    const int key = base + st_row + u * RPU;
+                    const bool someone = page_ok(W, page_of(pg, u)) & (key <= hi) & ((key > any_from) | (key < W.sink));
+                    const bool everyone = (key <= lo) & ((key > all_from) | (key < W.sink));   // of those that someone sees
+                    tu32x4_t* at = reinterpret_cast<tu32x4_t*>(smem + (2 + buf) * C::TILE_BYTES + (u * 256 + tid) * 16);
+                    if (!someone) *at = tu32x4_t{0, 0, 0, 0};
+                    else if (!everyone) {
+                        const tu32x4_t x = *at;
+#pragma unroll
+                        for (int w = 0; w < 4; ++w) bad |= word_not_finite<T>(x[w]);
+                    }
+                }
+                if (bad && hi > lo) s_bad = 1;
+            };
+            typedef tf32x4_t Logits[GI][CT];
+            // logits of a tile, raw, and the largest of a lane's of every row
+            auto products = [&](int buf, Logits& c) {
+                const unsigned char* sk = smem + buf * C::TILE_BYTES;
 #pragma unroll
                 for (int gi = 0; gi < GI; ++gi) {
 #pragma unroll
@@ -202,12 +207,23 @@ __global__ __launch_bounds__(256, 2) void prompt_kernel(const AttnPagedParams P)
                         }
                     }
                 }
-                const bool whole = base + KT <= w_lo + 1 && (!windowed || base > w_hi - W.window || base + KT <= W.sink) && all_there(pg);
-                if (!whole) {
+            };
+            auto largest = [&](const Logits& c, float (&mx)[CT]) {
+#pragma unroll
+                for (int ct = 0; ct < CT; ++ct) {
+                    mx[ct] = c[0][ct][0];
+#pragma unroll
+                    for (int x = 1; x < GI * 4; ++x) mx[ct] = fmaxf(mx[ct], c[x / 4][ct][x % 4]);
+                }
+            };
+            // One tile: its logits c (largest mx) become weights and meet V; the next one's (next, mx_next) are formed beside them.
+            auto step = [&](int i, const Pages& pg, Logits& c, float (&mx)[CT], Logits& next, float (&mx_next)[CT]) {
+                const int base = base_of(i), buf = i - t_begin & 1;
+                if (!whole_for(base, w_lo, w_hi, pg)) {
 #pragma unroll
                     for (int gi = 0; gi < GI; ++gi) {
                         const int b = gi / NT;
-                        const bool there = BF ? page_ok(W, quad >= 2 ? pg[2 * b + (BF ? 1 : 0)] : pg[BF ? 2 * b : b]) : page_ok(W, pg[b]);
+                        const bool there = BF ? page_ok(W, quad >= 2 ? pg.page[2 * b + (BF ? 1 : 0)] : pg.page[BF ? 2 * b : b]) : page_ok(W, pg.page[b]);
 #pragma unroll
                         for (int e = 0; e < 4; ++e) {
                             const int key = base + b * BLK + quad * (NT * 4) + gi % NT * 4 + e;
@@ -218,20 +234,16 @@ __global__ __launch_bounds__(256, 2) void prompt_kernel(const AttnPagedParams P)
                             }
                         }
                     }
+                    largest(c, mx);
                 }
                 bool need = false, huge = false;
                 float m_new[CT];
 #pragma unroll
                 for (int ct = 0; ct < CT; ++ct) {
-                    float mx = -INFINITY;
-#pragma unroll
-                    for (int gi = 0; gi < GI; ++gi)
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) mx = fmaxf(mx, c[gi][ct][e]);
-                    mx = attn_logit(quad_max(mx), scale);
-                    m_top[ct] = fmaxf(m_top[ct], mx);
-                    const bool grown = mx > m_ref[ct] + 8.f;
-                    m_new[ct] = grown ? mx : m_ref[ct];
+                    const float m = attn_logit(quad_max(mx[ct]), scale);
+                    m_top[ct] = fmaxf(m_top[ct], m);
+                    const bool grown = m > m_ref[ct] + 8.f;
+                    m_new[ct] = grown ? m : m_ref[ct];
                     need |= grown;
                     huge |= fabsf(m_new[ct]) >= kPromptHuge;   // (nothing seen: -inf as well, with nothing to lose)
                 }
@@ -247,33 +259,30 @@ __global__ __launch_bounds__(256, 2) void prompt_kernel(const AttnPagedParams P)
                             for (int k = 0; k < 4; ++k) o[e][ct][k] *= corr;
                     }
                 }
-                if (__any(huge)) {
+                if (__any(huge)) {   // rounded before the maximum is subtracted; below, the difference is all that is left to multiply by 1
 #pragma unroll
                     for (int ct = 0; ct < CT; ++ct)
 #pragma unroll
-                        for (int gi = 0; gi < GI; ++gi)
-#pragma unroll
-                            for (int e = 0; e < 4; ++e) c[gi][ct][e] = attn_logit(c[gi][ct][e], scale) - ref_of(m_ref[ct]);
+                        for (int x = 0; x < GI * 4; ++x) c[x / 4][ct][x % 4] = attn_logit(c[x / 4][ct][x % 4], scale) - ref_of(m_ref[ct]);
                 } else {
 #pragma unroll
                     for (int ct = 0; ct < CT; ++ct)
 #pragma unroll
-                        for (int gi = 0; gi < GI; ++gi)
-#pragma unroll
-                            for (int e = 0; e < 4; ++e) c[gi][ct][e] = fmaf(c[gi][ct][e], scale, -m_ref[ct]);
+                        for (int x = 0; x < GI * 4; ++x) c[x / 4][ct][x % 4] = fmaf(c[x / 4][ct][x % 4], scale, -m_ref[ct]);
                 }
+                products(buf ^ 1, next);   // (behind the last tile: of what lies there, for nobody)
 #pragma unroll
                 for (int ct = 0; ct < CT; ++ct) {
                     float sum = 0.f;
 #pragma unroll
-                    for (int gi = 0; gi < GI; ++gi)
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            c[gi][ct][e] = __builtin_amdgcn_exp2f(c[gi][ct][e]);
-                            sum += c[gi][ct][e];
-                        }
+                    for (int x = 0; x < GI * 4; ++x) {
+                        const float w = __builtin_amdgcn_exp2f(c[x / 4][ct][x % 4]);
+                        c[x / 4][ct][x % 4] = w;
+                        sum += w;
+                    }
                     l_run[ct] += sum;
                 }
+                const unsigned char* sv = smem + (2 + buf) * C::TILE_BYTES;
 #pragma unroll
                 for (int b = 0; b < NB; ++b) {
                     if constexpr (BF) {
@@ -305,26 +314,44 @@ __global__ __launch_bounds__(256, 2) void prompt_kernel(const AttnPagedParams P)
                             }
                     }
                 }
+                largest(next, mx_next);
             };
 
+            // K of tile i lies in buffer (i - t_begin) % 2 from two tiles ahead on, V from one tile ahead on.
+            Logits ca, cb;
+            float mxa[CT], mxb[CT];
             if (t_begin < t_end) {
-                pages_of(t_begin, page);
-                const int base = kt.at(t_begin) * KT;
-                fetch(base, page);
-                stage(0, base, page);
-                pages_of(min(t_begin + 1, t_end - 1), page_next);
-            }
-            __syncthreads();
-            for (int i = t_begin, buf = 0; i < t_end; ++i, buf ^= 1) {
-                const int base = kt.at(i) * KT, next = kt.at(min(i + 1, t_end - 1)) * KT;
-                const bool more = i + 1 < t_end;
-                if (more) fetch(next, page_next);
-                compute(buf, base, page);
-                if (more) stage(buf ^ 1, next, page_next);
-#pragma unroll
-                for (int r = 0; r < GI; ++r) page[r] = page_next[r];
-                pages_of(min(i + 2, t_end - 1), page_next);
+                Pages pg = pages_of(t_begin), pg1 = pages_of(t_begin + 1), pg2 = pages_of(t_begin + 2);
+                send(W.K, true, 0, base_of(t_begin), pg);
+                send(W.V, false, 0, base_of(t_begin), pg);
+                if (t_begin + 1 < t_end) send(W.K, true, 1, base_of(t_begin + 1), pg1);
                 __syncthreads();
+                if (w_rows > 0) {
+                    products(0, ca);
+                    largest(ca, mxa);
+                }
+                __syncthreads();
+                auto turn = [&](int i, Logits& c, float (&mx)[CT], Logits& next, float (&mx_next)[CT]) {
+                    const int base = base_of(i), buf = i - t_begin & 1;
+                    if (!whole_for(base, lo, hi, pg)) {
+                        clear_hidden(buf, base, pg);
+                        __syncthreads();
+                    }
+                    if (i + 2 < t_end) send(W.K, true, buf, base_of(i + 2), pg2);
+                    if (i + 1 < t_end) send(W.V, false, buf ^ 1, base_of(i + 1), pg1);
+                    const Pages pg3 = pages_of(i + 3);
+                    if (w_rows > 0) step(i, pg, c, mx, next, mx_next);
+                    pg = pg1;
+                    pg1 = pg2;
+                    pg2 = pg3;
+                    __syncthreads();
+                };
+                for (int i = t_begin;;) {
+                    turn(i, ca, mxa, cb, mxb);
+                    if (++i == t_end) break;
+                    turn(i, cb, mxb, ca, mxa);
+                    if (++i == t_end) break;
+                }
             }
             if (scalar(s_bad)) {   // (the same for every thread)
                 hi = lo + (hi - lo) / 2;
