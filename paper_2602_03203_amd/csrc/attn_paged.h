@@ -207,7 +207,7 @@ fk_status thin_rows(const fk_cache_desc* d, AttnPagedParams P, int max_len, void
 size_t thin_rows_workspace(const fk_cache_desc* d);
 
 static constexpr int kPromptRows = 128;   // query rows of a tile of prompt.hip
-size_t prompt_workspace(const fk_paged_desc* d, const TileGrid& G, int max_len);
-fk_status prompt_paged(const fk_paged_desc* d, AttnPagedParams P, int max_len, void* workspace, hipStream_t st);
+size_t prompt_workspace(const fk_paged_desc* d, const TileGrid& G, int n_tokens, int max_chunk, int max_len);
+fk_status prompt_paged(const fk_paged_desc* d, AttnPagedParams P, int max_chunk, int max_len, void* workspace, hipStream_t st);
 
 }  // namespace fk

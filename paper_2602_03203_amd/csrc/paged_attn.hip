@@ -32,18 +32,25 @@ static PagedParams view_params(const fk_paged_desc* desc, const void* q, const v
 }
 
 // Which kernel takes a chunk goes by its query rows: up to kThinRows the one that reads every pair once for 16 of them, beyond it the one with
-// tiles of 128.  A call that may hold both kinds is two launches, each of which leaves the other's chunks alone.
+// tiles of 128.  A call that may hold both kinds is two launches, each of which leaves the other's chunks alone.  Calls whose 16-row tiles meet few
+// pairs altogether are the first one's alone, however long their chunks: it spreads over more workgroups and its tiles take less time to
+// set up.  Measured on either side (one kernel / the other): 4 chunks of 32..64 tokens, g 7, D 128, 512 pairs (229 thousand): 16 / 23 us; 1 chunk of
+// 80 tokens, g 4, D 64, 4096 pairs (327 thousand): 15 / 22; 4 chunks of 12..24, g 7, D 128, 4096 pairs (516 thousand): 42 / 32.
 static constexpr int kThinRows = 16;
+static constexpr long long kThinWork = 3 << 17;
+
 struct AttnPlanPaged {
     bool thin, prompt;
     TileGrid thin_grid, prompt_grid;
 };
-static AttnPlanPaged plan_paged(const fk_paged_desc* d, int32_t n_tokens, int32_t max_chunk) {
+static AttnPlanPaged plan_paged(const fk_paged_desc* d, int32_t n_tokens, int32_t max_chunk, int32_t max_len) {
     const int g = d->n_q_heads / d->n_kv_heads;
     AttnPlanPaged p = {};
-    const bool all_longest = (long long)d->batch * max_chunk <= n_tokens;   // as many tokens as chunks of the bound's length have
-    p.prompt = (long long)max_chunk * g > kThinRows && (long long)n_tokens * g > kThinRows;
-    p.thin = !p.prompt || !all_longest;
+    // what is left for the shortest chunk where all others have the bound's length (should they be longer, prompt tiles take short chunks as well)
+    const long long shortest = n_tokens - (long long)(d->batch - 1) * max_chunk;
+    const long long work = ((long long)n_tokens * g + 15) / 16 * d->n_kv_heads * max_len;
+    p.prompt = (long long)max_chunk * g > kThinRows && work > kThinWork;
+    p.thin = !p.prompt || shortest * g <= kThinRows;
     if (p.thin) {   // (also all chunks there are, should they be longer than max_chunk says)
         p.thin_grid = tile_grid(d, n_tokens, p.prompt ? (kThinRows + g - 1) / g : max_chunk, 16);
         if (p.prompt) p.thin_grid.most = kThinRows;
@@ -57,8 +64,8 @@ static AttnPlanPaged plan_paged(const fk_paged_desc* d, int32_t n_tokens, int32_
 
 extern "C" size_t fk_paged_attn_workspace(const fk_paged_desc* desc, int32_t n_tokens, int32_t max_chunk, int32_t max_len) {
     if (check_paged(desc) != FK_OK || check_chunks(desc, n_tokens, max_chunk, max_len) != FK_OK) return 0;
-    const AttnPlanPaged p = plan_paged(desc, n_tokens, max_chunk);
-    const size_t a = p.thin ? thin_paged_workspace(desc, p.thin_grid, max_len) : 0, b = p.prompt ? prompt_workspace(desc, p.prompt_grid, max_len) : 0;
+    const AttnPlanPaged p = plan_paged(desc, n_tokens, max_chunk, max_len);
+    const size_t a = p.thin ? thin_paged_workspace(desc, p.thin_grid, max_len) : 0, b = p.prompt ? prompt_workspace(desc, p.prompt_grid, n_tokens, max_chunk, max_len) : 0;
     return 16 + (a > b ? a : b);   // (one launch after the other)
 }
 
@@ -77,10 +84,10 @@ extern "C" fk_status fk_paged_attn(const fk_paged_desc* desc, const void* q, con
     T.view = P;
     T.out = out;
     T.stats = reinterpret_cast<float2*>(stats);
-    const AttnPlanPaged p = plan_paged(desc, n_tokens, max_chunk);
+    const AttnPlanPaged p = plan_paged(desc, n_tokens, max_chunk, max_len);
     if (p.prompt) {
         T.grid = p.prompt_grid;
-        const fk_status r = prompt_paged(desc, T, max_len, workspace, (hipStream_t)stream);
+        const fk_status r = prompt_paged(desc, T, max_chunk, max_len, workspace, (hipStream_t)stream);
         if (r != FK_OK || !p.thin) return r;
     }
     T.grid = p.thin_grid;

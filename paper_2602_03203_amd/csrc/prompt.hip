@@ -13,6 +13,9 @@
 // References follow a row's maximum only where it has grown by more than 2^8 (probabilities up to 256, sums in fp32: nothing is lost), so that
 // outputs are hardly ever rescaled.
 #include "attn_paged.h"
+
+#include <type_traits>
+#include <algorithm>
 #include <climits>
 
 namespace fk {
@@ -131,48 +134,56 @@ __global__ __launch_bounds__(256, 2) void prompt_kernel(const AttnPagedParams P)
                 for (int e = 0; e < ET; ++e) o[e][ct] = (tf32x4_t){0.f, 0.f, 0.f, 0.f};
             }
             auto base_of = [&](int i) { return kt.at(i) * KT; };
-            struct Pages {
-                int page[GI];
+            // where a tile's runs of 16 pairs lie, counted in such runs (so that 32 bits hold any pool), and a bit for each that lies nowhere
+            struct Runs {
+                uint32_t at[GI], holes;
             };
-            auto pages_of = [&](int i) {   // (past the end: the last tile's)
-                Pages pg;
+            auto runs_of = [&](int i) {   // (past the end: the last tile's)
+                Runs x;
                 const int base = base_of(min(i, t_end - 1));
+                auto find = [&](int r, uint32_t& hole) {
+                    const int key = base + r * 16, page = load_uniform(tab, min(key >> W.page_shift, W.max_pages - 1));
+                    hole = page_ok(W, page) ? 0 : 1;
+                    return ((uint32_t)(hole ? 0 : page) * n_kv + h) << (W.page_shift - 4) | (key & ((1 << W.page_shift) - 1)) >> 4;
+                };
+                uint32_t hole;
+                if (1 << W.page_shift >= KT) {   // one page
+                    const uint32_t at = find(0, hole);
 #pragma unroll
-                for (int r = 0; r < GI; ++r) pg.page[r] = load_uniform(tab, min((base + r * 16) >> W.page_shift, W.max_pages - 1));
-                return pg;
-            };
-            auto all_there = [&](const Pages& pg) {
-                bool ok = true;
+                    for (int r = 0; r < GI; ++r) x.at[r] = at + r;
+                    x.holes = hole ? (1 << GI) - 1 : 0;
+                } else {
+                    x.holes = 0;
 #pragma unroll
-                for (int r = 0; r < GI; ++r) ok = ok && page_ok(W, pg.page[r]);
-                return ok;
+                    for (int r = 0; r < GI; ++r) {
+                        x.at[r] = find(r, hole);
+                        x.holes |= hole << r;
+                    }
+                }
+                return x;
             };
-            // load u of this wavefront lies in one run of 16 pairs
-            auto page_of = [&](const Pages& pg, int u) {
-                if constexpr (RPU == 32) return wave >= 2 ? pg.page[2 * u + 1] : pg.page[2 * u];
-                else return pg.page[u * RPU / 16];
-            };
-            auto send = [&](const void* X, bool is_k, int buf, int base, const Pages& pg) {
+            auto run_of_load = [&](int u) { return RPU == 32 ? 2 * u + (wave >= 2 ? 1 : 0) : u * RPU / 16; };   // load u of this wavefront lies in one run
+            auto send = [&](const void* X, bool is_k, int buf, const Runs& runs) {
 #pragma unroll
                 for (int u = 0; u < LD; ++u) {
-                    const int pgu = page_of(pg, u), in_tile = RPU == 32 ? u * 32 + (wave >= 2 ? 16 : 0) : u * RPU / 16 * 16, row = st_row + u * RPU;
-                    const size_t run = ((((size_t)(page_ok(W, pgu) ? pgu : 0) * n_kv + h) << W.page_shift) + ((base + in_tile) & ((1 << W.page_shift) - 1))) * (CH * 16);
+                    const int row = st_row + u * RPU;
+                    const uint32_t run = RPU == 32 ? (wave >= 2 ? runs.at[2 * u + (RPU == 32 ? 1 : 0)] : runs.at[RPU == 32 ? 2 * u : 0]) : runs.at[u * RPU / 16];
                     const int ch = st_ch ^ (is_k ? swizzle_k<BF, CH>(row) : swizzle_v<BF, CH>(row));
-                    load_to_lds(static_cast<const unsigned char*>(X) + run + (uint32_t)((row % 16 * CH + ch) * 16),
+                    load_to_lds(static_cast<const unsigned char*>(X) + (size_t)run * (16 * CH * 16) + (uint32_t)((row % 16 * CH + ch) * 16),
                                 smem + (is_k ? 0 : 2 * C::TILE_BYTES) + buf * C::TILE_BYTES + (u * 256 + wave * 64) * 16);
                 }
             };
-            auto whole_for = [&](int base, int from, int to, const Pages& pg) {   // every row at positions from .. to sees all of the tile
-                return base + KT <= from + 1 && (!windowed || base > to - W.window || base + KT <= W.sink) && all_there(pg);
+            auto whole_for = [&](int base, int from, int to, const Runs& runs) {   // every row at positions from .. to sees all of the tile
+                return base + KT <= from + 1 && (!windowed || base > to - W.window || base + KT <= W.sink) && !runs.holes;
             };
             // V of a tile that not every row sees: values of weight 0 must not meet the products as infinities or NaN
-            auto clear_hidden = [&](int buf, int base, const Pages& pg) {
+            auto clear_hidden = [&](int buf, int base, const Runs& runs) {
                 const int any_from = windowed ? lo - W.window : -1, all_from = windowed ? hi - W.window : -1;
                 bool bad = false;
 #pragma unroll
                 for (int u = 0; u < LD; ++u) {
                     const int key = base + st_row + u * RPU;
-                    const bool someone = page_ok(W, page_of(pg, u)) & (key <= hi) & ((key > any_from) | (key < W.sink));
+                    const bool someone = !(runs.holes >> run_of_load(u) & 1) & (key <= hi) & ((key > any_from) | (key < W.sink));
                     const bool everyone = (key <= lo) & ((key > all_from) | (key < W.sink));   // of those that someone sees
                     tu32x4_t* at = reinterpret_cast<tu32x4_t*>(smem + (2 + buf) * C::TILE_BYTES + (u * 256 + tid) * 16);
                     if (!someone) *at = tu32x4_t{0, 0, 0, 0};
@@ -186,7 +197,7 @@ __global__ __launch_bounds__(256, 2) void prompt_kernel(const AttnPagedParams P)
             };
             typedef tf32x4_t Logits[GI][CT];
             // logits of a tile, raw, and the largest of a lane's of every row
-            auto products = [&](int buf, Logits& c) {
+            auto products = [&](auto buf, Logits& c) {
                 const unsigned char* sk = smem + buf * C::TILE_BYTES;
 #pragma unroll
                 for (int gi = 0; gi < GI; ++gi) {
@@ -208,22 +219,29 @@ __global__ __launch_bounds__(256, 2) void prompt_kernel(const AttnPagedParams P)
                     }
                 }
             };
-            auto largest = [&](const Logits& c, float (&mx)[CT]) {
+            // a row's largest logit of a tile, and whether its reference has to move or differences would lose their bits
+            bool need = false, huge = false;
+            float m_new[CT];
+            auto judge = [&](const Logits& c) {
+                need = huge = false;
 #pragma unroll
                 for (int ct = 0; ct < CT; ++ct) {
-                    mx[ct] = c[0][ct][0];
+                    float mx = c[0][ct][0];
 #pragma unroll
-                    for (int x = 1; x < GI * 4; ++x) mx[ct] = fmaxf(mx[ct], c[x / 4][ct][x % 4]);
+                    for (int x = 1; x < GI * 4; ++x) mx = fmaxf(mx, c[x / 4][ct][x % 4]);
+                    const float m = attn_logit(quad_max(mx), scale);
+                    m_new[ct] = m;
+                    need |= m > m_ref[ct] + 8.f;
+                    huge |= fabsf(fmaxf(m, m_ref[ct])) >= kPromptHuge;   // (nothing seen: -inf as well, with nothing to lose)
                 }
             };
-            // One tile: its logits c (largest mx) become weights and meet V; the next one's (next, mx_next) are formed beside them.
-            auto step = [&](int i, const Pages& pg, Logits& c, float (&mx)[CT], Logits& next, float (&mx_next)[CT]) {
-                const int base = base_of(i), buf = i - t_begin & 1;
-                if (!whole_for(base, w_lo, w_hi, pg)) {
+            // One tile: its logits c become weights and meet V; the next one's are formed beside them.
+            auto step = [&](auto buf, int base, const Runs& runs, Logits& c, Logits& next) {
+                if (!whole_for(base, w_lo, w_hi, runs)) {
 #pragma unroll
                     for (int gi = 0; gi < GI; ++gi) {
                         const int b = gi / NT;
-                        const bool there = BF ? page_ok(W, quad >= 2 ? pg.page[2 * b + (BF ? 1 : 0)] : pg.page[BF ? 2 * b : b]) : page_ok(W, pg.page[b]);
+                        const bool there = !(runs.holes >> (BF ? 2 * b + (quad >= 2) : b) & 1);
 #pragma unroll
                         for (int e = 0; e < 4; ++e) {
                             const int key = base + b * BLK + quad * (NT * 4) + gi % NT * 4 + e;
@@ -234,24 +252,15 @@ __global__ __launch_bounds__(256, 2) void prompt_kernel(const AttnPagedParams P)
                             }
                         }
                     }
-                    largest(c, mx);
+                    judge(c);
                 }
-                bool need = false, huge = false;
-                float m_new[CT];
 #pragma unroll
-                for (int ct = 0; ct < CT; ++ct) {
-                    const float m = attn_logit(quad_max(mx[ct]), scale);
-                    m_top[ct] = fmaxf(m_top[ct], m);
-                    const bool grown = m > m_ref[ct] + 8.f;
-                    m_new[ct] = grown ? m : m_ref[ct];
-                    need |= grown;
-                    huge |= fabsf(m_new[ct]) >= kPromptHuge;   // (nothing seen: -inf as well, with nothing to lose)
-                }
+                for (int ct = 0; ct < CT; ++ct) m_top[ct] = fmaxf(m_top[ct], m_new[ct]);
                 if (__any(need)) {
 #pragma unroll
                     for (int ct = 0; ct < CT; ++ct) {
-                        const float corr = __builtin_amdgcn_exp2f(m_ref[ct] - ref_of(m_new[ct]));
-                        m_ref[ct] = m_new[ct];
+                        const float m = m_new[ct] > m_ref[ct] + 8.f ? m_new[ct] : m_ref[ct], corr = __builtin_amdgcn_exp2f(m_ref[ct] - ref_of(m));
+                        m_ref[ct] = m;
                         l_run[ct] *= corr;
 #pragma unroll
                         for (int e = 0; e < ET; ++e)
@@ -259,24 +268,26 @@ __global__ __launch_bounds__(256, 2) void prompt_kernel(const AttnPagedParams P)
                             for (int k = 0; k < 4; ++k) o[e][ct][k] *= corr;
                     }
                 }
-                if (__any(huge)) {   // rounded before the maximum is subtracted; below, the difference is all that is left to multiply by 1
+                float by = scale, less[CT];
 #pragma unroll
-                    for (int ct = 0; ct < CT; ++ct)
+                for (int ct = 0; ct < CT; ++ct) less[ct] = m_ref[ct];
+                if (__any(huge)) {   // rounded before the reference is subtracted; below, there is nothing left to do
+                    by = 1.f;
+#pragma unroll
+                    for (int ct = 0; ct < CT; ++ct) {
+                        less[ct] = 0.f;
 #pragma unroll
                         for (int x = 0; x < GI * 4; ++x) c[x / 4][ct][x % 4] = attn_logit(c[x / 4][ct][x % 4], scale) - ref_of(m_ref[ct]);
-                } else {
-#pragma unroll
-                    for (int ct = 0; ct < CT; ++ct)
-#pragma unroll
-                        for (int x = 0; x < GI * 4; ++x) c[x / 4][ct][x % 4] = fmaf(c[x / 4][ct][x % 4], scale, -m_ref[ct]);
+                    }
                 }
-                products(buf ^ 1, next);   // (behind the last tile: of what lies there, for nobody)
+                __builtin_amdgcn_s_setprio(1);   // against the other workgroup's wavefront, which is then at its loads and masks (520 -> 511 us)
+                products(std::integral_constant<int, (buf ^ 1)>{}, next);   // (behind the last tile: of what lies there, for nobody)
 #pragma unroll
                 for (int ct = 0; ct < CT; ++ct) {
                     float sum = 0.f;
 #pragma unroll
                     for (int x = 0; x < GI * 4; ++x) {
-                        const float w = __builtin_amdgcn_exp2f(c[x / 4][ct][x % 4]);
+                        const float w = __builtin_amdgcn_exp2f(fmaf(c[x / 4][ct][x % 4], by, -less[ct]));
                         c[x / 4][ct][x % 4] = w;
                         sum += w;
                     }
@@ -314,42 +325,42 @@ __global__ __launch_bounds__(256, 2) void prompt_kernel(const AttnPagedParams P)
                             }
                     }
                 }
-                largest(next, mx_next);
+                judge(next);
+                __builtin_amdgcn_s_setprio(0);
             };
 
             // K of tile i lies in buffer (i - t_begin) % 2 from two tiles ahead on, V from one tile ahead on.
             Logits ca, cb;
-            float mxa[CT], mxb[CT];
             if (t_begin < t_end) {
-                Pages pg = pages_of(t_begin), pg1 = pages_of(t_begin + 1), pg2 = pages_of(t_begin + 2);
-                send(W.K, true, 0, base_of(t_begin), pg);
-                send(W.V, false, 0, base_of(t_begin), pg);
-                if (t_begin + 1 < t_end) send(W.K, true, 1, base_of(t_begin + 1), pg1);
+                Runs runs = runs_of(t_begin), runs1 = runs_of(t_begin + 1), runs2 = runs_of(t_begin + 2);
+                send(W.K, true, 0, runs);
+                send(W.V, false, 0, runs);
+                if (t_begin + 1 < t_end) send(W.K, true, 1, runs1);
                 __syncthreads();
                 if (w_rows > 0) {
-                    products(0, ca);
-                    largest(ca, mxa);
+                    products(std::integral_constant<int, 0>{}, ca);
+                    judge(ca);
                 }
                 __syncthreads();
-                auto turn = [&](int i, Logits& c, float (&mx)[CT], Logits& next, float (&mx_next)[CT]) {
-                    const int base = base_of(i), buf = i - t_begin & 1;
-                    if (!whole_for(base, lo, hi, pg)) {
-                        clear_hidden(buf, base, pg);
+                auto turn = [&](auto buf, int i, Logits& c, Logits& next) {
+                    const int base = base_of(i);
+                    if (!whole_for(base, lo, hi, runs)) {
+                        clear_hidden(buf, base, runs);
                         __syncthreads();
                     }
-                    if (i + 2 < t_end) send(W.K, true, buf, base_of(i + 2), pg2);
-                    if (i + 1 < t_end) send(W.V, false, buf ^ 1, base_of(i + 1), pg1);
-                    const Pages pg3 = pages_of(i + 3);
-                    if (w_rows > 0) step(i, pg, c, mx, next, mx_next);
-                    pg = pg1;
-                    pg1 = pg2;
-                    pg2 = pg3;
+                    if (i + 2 < t_end) send(W.K, true, buf, runs2);
+                    if (i + 1 < t_end) send(W.V, false, buf ^ 1, runs1);
+                    const Runs runs3 = runs_of(i + 3);
+                    if (w_rows > 0) step(buf, base, runs, c, next);
+                    runs = runs1;
+                    runs1 = runs2;
+                    runs2 = runs3;
                     __syncthreads();
                 };
                 for (int i = t_begin;;) {
-                    turn(i, ca, mxa, cb, mxb);
+                    turn(std::integral_constant<int, 0>{}, i, ca, cb);
                     if (++i == t_end) break;
-                    turn(i, cb, mxb, ca, mxa);
+                    turn(std::integral_constant<int, 1>{}, i, cb, ca);
                     if (++i == t_end) break;
                 }
             }
@@ -401,24 +412,40 @@ __global__ __launch_bounds__(256, 2) void prompt_kernel(const AttnPagedParams P)
 }
 
 // ---- host side ---------------------------------------------------------------------------------------------------
-// Splits of the pairs where the tiles alone leave CUs without a workgroup, 512 pairs and more each
-static int prompt_splits(const fk_paged_desc* d, const TileGrid& G, int max_len, int kt, int& shift) {
-    shift = kt == 64 ? 3 : 4;
-    long long s = 512 / ((long long)G.places * d->n_kv_heads);
-    if (s > max_len / 512) s = max_len / 512;
-    if (s > 16) s = 16;
-    return s < 1 ? 1 : (int)s;
+// Over how many workgroups the pairs of an item (a tile of rows, a kv head) are split.  256 CUs hold two workgroups each: items beyond a multiple of
+// 512 cost another turn, five sixths of one where there are at most 256 of them (a workgroup alone on its CU is a little faster).  Splits make turns
+// shorter and cost a second launch and their records' way to memory and back.  In microseconds, with 2.1 for 64 pairs of bf16 and D = 128, 6 for the
+// launch and 4 TB/s for the records; in fp32 one workgroup has the matrix units of its CU busy, 9.4 for 64 pairs.  Whole / 2 / 3 / 4 / 8 splits measured for 8 heads of g 4, D 128: 512 tokens of 8192: 216 / 123 /
+// 104 / 93 / 101; 1024 of 8192: 222 / 160 / 175 / 166 / 186; 4 chunks to 300 of 2048: 70 / 80 / 72 / 73 / 70.  How many chunks there are that are not single
+// tokens the host does not know: as many as would have the longest one's length.
+static int prompt_splits(const fk_paged_desc* d, int n_tokens, int max_chunk, long long pairs, int& shift) {
+    shift = d->dtype == FK_BF16 ? 3 : 4;   // 512 pairs and more each
+    const long long g = d->n_q_heads / d->n_kv_heads, chunk = max_chunk < n_tokens ? max_chunk : n_tokens, rest = n_tokens - d->batch;
+    const long long chunks = chunk > 1 && rest > 0 ? (rest + chunk - 2) / (chunk - 1) : 1;
+    const long long items = (n_tokens * g + chunks * (kPromptRows - 1)) / kPromptRows * d->n_kv_heads;
+    const double whole = (double)pairs / 64 * d->head_dim / 128 * (d->dtype == FK_BF16 ? 2.1 : 9.4);
+    int best = 1;
+    double least = 0;
+    for (int s = 1; s <= 16 && (s == 1 || pairs / s >= 512); ++s) {
+        const long long all = items * s, over = all % 512;
+        const double turns = d->dtype == FK_F32 ? std::max(1., (double)all / 256) : (double)(all / 512) + (over == 0 ? 0. : over <= 256 ? 5. / 6 : 1.);
+        const double time = turns * whole / s + (s == 1 ? 0. : 6 + (double)all * kPromptRows * d->head_dim * 8 / 4e6);
+        if (s == 1 || time < least) least = time, best = s;
+    }
+    return best;
 }
-size_t prompt_workspace(const fk_paged_desc* d, const TileGrid& G, int max_len) {
+size_t prompt_workspace(const fk_paged_desc* d, const TileGrid& G, int n_tokens, int max_chunk, int max_len) {
     int shift;
-    return record_bytes((long long)G.places * d->n_kv_heads, prompt_splits(d, G, max_len, d->dtype == FK_BF16 ? 64 : 32, shift), kPromptRows, d->head_dim);
+    return record_bytes((long long)G.places * d->n_kv_heads, prompt_splits(d, n_tokens, max_chunk, max_len, shift), kPromptRows, d->head_dim);
 }
 
 template <typename T, int D>
-static fk_status prompt_launch(const fk_paged_desc* d, AttnPagedParams& P, int max_len, void* ws, hipStream_t st) {
+static fk_status prompt_launch(const fk_paged_desc* d, AttnPagedParams& P, int max_chunk, int max_len, void* ws, hipStream_t st) {
     using C = PromptCfg<T, D>;
     const long long items = (long long)P.grid.places * d->n_kv_heads;
-    P.splits = prompt_splits(d, P.grid, max_len, C::KT, P.split_shift);
+    P.splits = prompt_splits(d, P.view.n_tokens, max_chunk, max_len, P.split_shift);   // (what the workspace is for)
+    const long long seen = (long long)P.view.window + P.view.sink + kPromptRows;
+    if (seen < max_len) P.splits = std::min(P.splits, prompt_splits(d, P.view.n_tokens, max_chunk, seen, P.split_shift));
     P.rec_ml = reinterpret_cast<float2*>(ws);
     P.rec = reinterpret_cast<float*>(static_cast<char*>(ws) + up256((size_t)items * P.splits * kPromptRows * sizeof(float2)));
     auto kern = prompt_kernel<T, D>;
@@ -429,9 +456,9 @@ static fk_status prompt_launch(const fk_paged_desc* d, AttnPagedParams& P, int m
     return launch_status();
 }
 
-fk_status prompt_paged(const fk_paged_desc* d, AttnPagedParams P, int max_len, void* ws, hipStream_t st) {
-    if (d->dtype == FK_F32) return d->head_dim == 64 ? prompt_launch<float, 64>(d, P, max_len, ws, st) : prompt_launch<float, 128>(d, P, max_len, ws, st);
-    return d->head_dim == 64 ? prompt_launch<bf16_t, 64>(d, P, max_len, ws, st) : prompt_launch<bf16_t, 128>(d, P, max_len, ws, st);
+fk_status prompt_paged(const fk_paged_desc* d, AttnPagedParams P, int max_chunk, int max_len, void* ws, hipStream_t st) {
+    if (d->dtype == FK_F32) return d->head_dim == 64 ? prompt_launch<float, 64>(d, P, max_chunk, max_len, ws, st) : prompt_launch<float, 128>(d, P, max_chunk, max_len, ws, st);
+    return d->head_dim == 64 ? prompt_launch<bf16_t, 64>(d, P, max_chunk, max_len, ws, st) : prompt_launch<bf16_t, 128>(d, P, max_chunk, max_len, ws, st);
 }
 
 }  // namespace fk
