@@ -75,6 +75,12 @@ __device__ __forceinline__ int sequence_of(const PagedParams& P, int t, int from
 
 __device__ __forceinline__ bool sees(const PagedParams& P, int p, int j) { return j <= p && (j > p - P.window || j < P.sink); }
 
+// 16 bytes per lane from global memory to LDS, at `to` + lane * 16.  A barrier alone does not wait for them: arrived() before it.
+__device__ __forceinline__ void load_to_lds(const void* from, unsigned char* to) {
+    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)from, (__attribute__((address_space(3))) void*)to, 16, 0, 0);
+}
+__device__ __forceinline__ void arrived() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }   // this wavefront's
+
 // ---- tiles of query rows --------------------------------------------------------------------------------------------
 // The queries of a (chunk, KV head) are rows: row r is head r % g of token r / g.  A tile is TM of them.  `slot` counts the places of a launch:
 // either place i of sequence b is slot i * batch + b (spread == false; a sequence has `per_seq` places, whose workgroups take every

@@ -46,11 +46,6 @@ template <bool BF, int CH> __device__ __forceinline__ int swizzle_v(int row) {
     else return ((row >> 1) & 1) << 1 | ((row >> 3) & 1) << 2;
 }
 
-// 16 bytes per lane from global memory to LDS, at `to` + lane * 16
-__device__ __forceinline__ void load_to_lds(const void* from, unsigned char* to) {
-    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)from, (__attribute__((address_space(3))) void*)to, 16, 0, 0);
-}
-
 typedef short ps16x4_t __attribute__((ext_vector_type(4)));
 __device__ __forceinline__ tu32x2_t read_transposed(const unsigned char* p) {
     typedef __attribute__((address_space(3))) ps16x4_t lds_t;
@@ -336,6 +331,7 @@ __global__ __launch_bounds__(256, 2) void prompt_kernel(const AttnPagedParams P)
                 send(W.K, true, 0, runs);
                 send(W.V, false, 0, runs);
                 if (t_begin + 1 < t_end) send(W.K, true, 1, runs1);
+                arrived();
                 __syncthreads();
                 if (w_rows > 0) {
                     products(std::integral_constant<int, 0>{}, ca);
@@ -355,6 +351,7 @@ __global__ __launch_bounds__(256, 2) void prompt_kernel(const AttnPagedParams P)
                     runs = runs1;
                     runs1 = runs2;
                     runs2 = runs3;
+                    arrived();
                     __syncthreads();
                 };
                 for (int i = t_begin;;) {

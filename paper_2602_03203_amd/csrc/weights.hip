@@ -28,7 +28,7 @@ template <typename T, int D, bool FEW> struct WeightsCfg {   // FEW: few keys, 1
     static constexpr int KG = FEW ? 1 : BF || D == 64 ? 4 : 2;      // groups of 16 keys per wavefront
     static constexpr int KEYS = 4 * KG * 16;              // of a workgroup
     static constexpr int QT = BF ? 64 : 32;               // query rows of a tile
-    static constexpr int QRS = CH * 16 + 16;              // byte stride of a row in LDS
+    static constexpr int NQ = QT / 16, TILE_BYTES = QT * CH * 16;
     static constexpr int LD = QT * CH / 256;              // 16-byte loads of a tile per thread
 };
 
@@ -39,12 +39,12 @@ template <typename T, int D, bool FEW>
 __global__ __launch_bounds__(256, 2) void weights_kernel(const WeightsParams P) {
     using C = WeightsCfg<T, D, FEW>;
     constexpr bool BF = C::BF;
-    constexpr int CH = C::CH, KS = C::KS, KG = C::KG, QT = C::QT, QRS = C::QRS, LD = C::LD;
+    constexpr int CH = C::CH, KS = C::KS, KG = C::KG, QT = C::QT, NQ = C::NQ, LD = C::LD;
     const PagedParams& W = P.view;
     const int tid = threadIdx.x, lane = tid & (kWave - 1), n16 = lane & 15, quad = lane >> 4, wave = scalar(tid / kWave);
     const int place = scalar(divide(blockIdx.x, W.n_kv, W.kv_magic)), h = (int)blockIdx.x - place * W.n_kv, b = scalar(divide(place, P.blocks, P.blocks_magic)), split = blockIdx.y;
     const int g = W.g;
-    __shared__ __attribute__((aligned(16))) unsigned char s_q[2][QT * QRS];
+    extern __shared__ __attribute__((aligned(16))) unsigned char s_q[];   // two tiles
     __shared__ float s_m[2][QT], s_il[2][QT];
 
     const int begin = scalar(chunk_begin(W, b)), nq = scalar(chunk_end(W, b, begin)) - begin, n = scalar(pairs_of(W, b)), first = n - nq;
@@ -81,75 +81,78 @@ __global__ __launch_bounds__(256, 2) void weights_kernel(const WeightsParams P) 
 #pragma unroll
         for (int j = 0; j < KG; ++j) a[j] = (wf32x4_t){0.f, 0.f, 0.f, 0.f};
 
-        W128 qr[LD];
+        // Queries go straight into LDS, two tiles ahead.  There the 16-byte chunks of a row change places, so that 16 rows' operands lie in different
+        // banks; a load writes in the order of its lanes, so each lane fetches the chunk that belongs in its place.
+        constexpr int kSwap = (CH < 16 ? CH : 16) - 1;
+        const uint32_t q_first = ((uint32_t)begin * W.n_kv + h) * g, q_token = (uint32_t)(W.n_kv - 1) * g;   // query row r of token t: q_first + r + t * q_token, below 2^28
         float2 st;
-        auto fetch = [&](int i) {
+        int st_row;
+        auto send = [&](int i, int buf) {
             const int base = row_lo + i * QT;
 #pragma unroll
             for (int u = 0; u < LD; ++u) {
-                const int x = tid + u * 256, row = min(base + x / CH, row_hi - 1), tok = token_of(row);
-                qr[u].u = reinterpret_cast<const wu32x4_t*>(W.q)[(((size_t)(begin + tok) * W.n_kv + h) * g + (row - tok * g)) * CH + x % CH];
+                const int x = tid + u * 256, in_tile = x / CH, row = min(base + in_tile, row_hi - 1);
+                load_to_lds(reinterpret_cast<const wu32x4_t*>(W.q) + (size_t)(q_first + row + token_of(row) * q_token) * CH + (x % CH ^ (in_tile & kSwap)),
+                            s_q + buf * C::TILE_BYTES + (u * 256 + wave * 64) * 16);
             }
-            const int row = base + tid % QT, rc = min(row, row_hi - 1), tok = token_of(rc);
-            st = P.stats[((size_t)(begin + tok) * W.n_kv + h) * g + (rc - tok * g)];
-            if (row >= row_hi || st.y == 0.f) st = make_float2(0.f, INFINITY);   // no query, or one that sees nothing: weight 0
+            st_row = base + tid % QT;
+            const int row = min(st_row, row_hi - 1);
+            st = P.stats[q_first + row + token_of(row) * q_token];
         };
         auto stage = [&](int buf) {
-#pragma unroll
-            for (int u = 0; u < LD; ++u) {
-                const int x = tid + u * 256;
-                *reinterpret_cast<wu32x4_t*>(s_q[buf] + x / CH * QRS + x % CH * 16) = qr[u].u;
-            }
             if (tid < QT) {
-                s_m[buf][tid] = st.x;
-                s_il[buf][tid] = 1.0f / st.y;
+                const bool none = st_row >= row_hi || st.y == 0.f;   // no query, or one that sees nothing: weight 0
+                s_m[buf][tid] = none ? 0.f : st.x;
+                s_il[buf][tid] = none ? 0.f : 1.0f / st.y;
             }
         };
-        if (i0 < i1) {
-            fetch(i0);
-            stage(0);
-        }
-        __syncthreads();
-        for (int i = i0, buf = 0; i < i1; ++i, buf ^= 1) {
-            if (i + 1 < i1) fetch(i + 1);
-            const int base = row_lo + i * QT;
+        int q_at[KS];
 #pragma unroll
-            for (int qt = 0; qt < QT / 16; ++qt) {
-                const int r0 = base + qt * 16;
-                if (r0 >= row_hi) break;
-                W128 q[KS];
+        for (int ks = 0; ks < KS; ++ks) q_at[ks] = (n16 * CH + ((ks * 4 + quad) ^ (n16 & kSwap))) * 16;
+        float m = 0.f, il = 0.f;   // of the rows whose logits are next
+        auto products = [&](int buf, int qt, wf32x4_t (&c)[KG], float& m, float& il) {
+            W128 q[KS];
 #pragma unroll
-                for (int ks = 0; ks < KS; ++ks) q[ks].u = *reinterpret_cast<const wu32x4_t*>(s_q[buf] + (qt * 16 + n16) * QRS + (ks * 4 + quad) * 16);
-                const float m = s_m[buf][qt * 16 + n16], il = s_il[buf][qt * 16 + n16];
-                const int lo = first + scalar(token_of(r0)), hi = first + scalar(token_of(min(r0 + 15, row_hi - 1)));   // positions
-                wf32x4_t c[KG];
+            for (int ks = 0; ks < KS; ++ks) q[ks].u = *reinterpret_cast<const wu32x4_t*>(s_q + buf * C::TILE_BYTES + qt * 16 * CH * 16 + q_at[ks]);
+            m = s_m[buf][qt * 16 + n16];
+            il = s_il[buf][qt * 16 + n16];
 #pragma unroll
-                for (int j = 0; j < KG; ++j) {
-                    c[j] = (wf32x4_t){0.f, 0.f, 0.f, 0.f};
+            for (int j = 0; j < KG; ++j) {
+                c[j] = (wf32x4_t){0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                    for (int ks = 0; ks < KS; ++ks) {
-                        if constexpr (BF) {
-                            c[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k[j][ks].v, q[ks].v, c[j], 0, 0, 0);
-                        } else {
+                for (int ks = 0; ks < KS; ++ks) {
+                    if constexpr (BF) {
+                        c[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k[j][ks].v, q[ks].v, c[j], 0, 0, 0);
+                    } else {
 #pragma unroll
-                            for (int e = 0; e < 4; ++e) c[j] = __builtin_amdgcn_mfma_f32_16x16x4f32(k[j][ks].f[e], q[ks].f[e], c[j], 0, 0, 0);
-                        }
+                        for (int e = 0; e < 4; ++e) c[j] = __builtin_amdgcn_mfma_f32_16x16x4f32(k[j][ks].f[e], q[ks].f[e], c[j], 0, 0, 0);
                     }
                 }
-                if (__any(fabsf(m) >= kHugeLogit)) {
+            }
+        };
+        wf32x4_t c[2][KG];
+        if (i0 < i1) {
+            send(i0, 0);
+            stage(0);
+            if (i0 + 1 < i1) send(i0 + 1, 1);
+        }
+        arrived();
+        __syncthreads();
+        if (i0 < i1) products(0, 0, c[0], m, il);
+        for (int i = i0, buf = 0; i < i1; ++i, buf ^= 1) {
+            const int base = row_lo + i * QT, lo = first + scalar(token_of(base)), hi = first + scalar(token_of(min(base + QT, row_hi) - 1));   // positions
+            const bool whole = kw + KG * 16 <= lo + 1 && base + QT <= row_hi && (W.window == 0x7fffffff || kw > hi - W.window || kw + KG * 16 <= W.sink);
 #pragma unroll
-                    for (int j = 0; j < KG; ++j)
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) c[j][e] = attn_logit(c[j][e], scale) - m;
-                } else {
-#pragma unroll
-                    for (int j = 0; j < KG; ++j)
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) c[j][e] = fmaf(c[j][e], scale, -m);
+            for (int qt = 0; qt < NQ; ++qt) {
+                if (qt == NQ - 1) {   // what the tile's rows are read for is done
+                    stage(buf ^ 1);
+                    arrived();
+                    __syncthreads();
+                    if (i + 2 < i1) send(i + 2, buf);
                 }
-                const bool whole = kw + KG * 16 <= lo + 1 && r0 + 16 <= row_hi && (W.window == 0x7fffffff || kw > hi - W.window || kw + KG * 16 <= W.sink);
+                wf32x4_t (&now)[KG] = c[qt & 1];
                 if (!whole) {
-                    const int row = r0 + n16, p = row < row_hi ? first + token_of(row) : -1;
+                    const int row = base + qt * 16 + n16, p = row < row_hi ? first + token_of(row) : -1;
                     const int from = W.window == 0x7fffffff ? -1 : p - W.window;
 #pragma unroll
                     for (int j = 0; j < KG; ++j)
@@ -157,17 +160,32 @@ __global__ __launch_bounds__(256, 2) void weights_kernel(const WeightsParams P) 
                         for (int e = 0; e < 4; ++e) {
                             const int key = kw + j * 16 + quad * 4 + e;
                             const bool seen = (key <= p) & ((key > from) | (key < W.sink));
-                            c[j][e] = seen ? c[j][e] : -INFINITY;
+                            now[j][e] = seen ? now[j][e] : -INFINITY;
                         }
                 }
+                float by = scale, less = m;
+                if (__any(fabsf(m) >= kHugeLogit)) {   // rounded before the maximum is subtracted; below, there is nothing left to do
+                    by = 1.f;
+                    less = 0.f;
+#pragma unroll
+                    for (int j = 0; j < KG; ++j)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) now[j][e] = attn_logit(now[j][e], scale) - m;
+                }
+                // beside these rows' weights, the next ones' logits (behind the last tile: of what lies there, for nobody)
+                float m_next, il_next;
+                products(qt == NQ - 1 ? buf ^ 1 : buf, (qt + 1) % NQ, c[(qt + 1) & 1], m_next, il_next);
 #pragma unroll
                 for (int j = 0; j < KG; ++j)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) a[j][e] = fmaf(__builtin_amdgcn_exp2f(c[j][e]), il, a[j][e]);
+                    for (int e = 0; e < 4; ++e) a[j][e] = fmaf(__builtin_amdgcn_exp2f(fmaf(now[j][e], by, -less)), il, a[j][e]);
+#pragma unroll
+                for (int j = 0; j < KG; ++j) asm volatile("" : "+v"(a[j]));   // here, not behind the tile's last branch
+                m = m_next;
+                il = il_next;
             }
-            if (i + 1 < i1) stage(buf ^ 1);
-            __syncthreads();
         }
+        __syncthreads();   // the LDS is the next keys'
         // the 16 rows of a key, then one lane a key
         const size_t row = (size_t)b * W.n_kv + h;
 #pragma unroll
@@ -238,8 +256,8 @@ static fk_status weights_run(const fk_paged_desc* d, WeightsParams& P, const Wei
     P.blocks = (max_len + p.keys - 1) / p.keys;
     P.blocks_magic = magic_of(P.blocks);
     const dim3 grid((unsigned)(d->batch * d->n_kv_heads * (long long)P.blocks), P.splits);
-    if (p.few) hipLaunchKernelGGL((weights_kernel<T, D, true>), grid, dim3(256), 0, st, P);
-    else hipLaunchKernelGGL((weights_kernel<T, D, false>), grid, dim3(256), 0, st, P);
+    if (p.few) hipLaunchKernelGGL((weights_kernel<T, D, true>), grid, dim3(256), (2 * WeightsCfg<T, D, true>::TILE_BYTES), st, P);
+    else hipLaunchKernelGGL((weights_kernel<T, D, false>), grid, dim3(256), (2 * WeightsCfg<T, D, false>::TILE_BYTES), st, P);
     if (P.splits > 1) hipLaunchKernelGGL(weights_sum_kernel, dim3((P.part_len + 255) / 256, d->batch * d->n_kv_heads), dim3(256), 0, st, P);
     return launch_status();
 }
