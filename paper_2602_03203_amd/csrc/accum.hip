@@ -1,4 +1,4 @@
-// fk_decode_step_acc: the decode step that adds its attention weights to those that the retained pairs have accumulated (thin.hip).
+// fk_decode_step_acc: the decode step that adds its attention weights to those that the retained pairs have accumulated (thin.h).
 #include "attn_paged.h"
 #include <cfloat>
 #include <climits>

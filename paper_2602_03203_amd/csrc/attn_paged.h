@@ -1,5 +1,5 @@
-// Attention over pages and rows: what its kernels share - few query rows over many pairs (thin.hip: single tokens and short chunks over a paged cache,
-// the decode step that accumulates its weights over the rows of a budgeted cache) and many query rows (prompt.hip) - and the merge of split tiles.
+// Attention over pages and rows: what its kernels share - few query rows over many pairs (thin.h: single tokens and short chunks over a paged cache,
+// the decode step that accumulates its weights over the rows of a budgeted cache) and many query rows (prompt.h) - and the merge of split tiles.
 #pragma once
 #include "paged.h"
 #include "window.h"
@@ -122,10 +122,9 @@ __device__ __forceinline__ void store_row(const AttnPagedParams& P, size_t row, 
 }
 
 template <typename T, int D, int TM, int KT>
-__global__ __launch_bounds__(256) void merge_kernel(const AttnPagedParams P) {
+__device__ __forceinline__ void merge_tile(const AttnPagedParams& P, int item, int part) {   // part: 16 of a tile's rows
     const PagedParams& W = P.view;
-    const int tid = threadIdx.x, n_kv = W.n_kv, slot = scalar(divide(blockIdx.x, n_kv, W.kv_magic)), h = (int)blockIdx.x - slot * n_kv, g = W.g;
-    const int sub = blockIdx.y * 16;   // the workgroup's 16 rows of the tile
+    const int tid = threadIdx.x, n_kv = W.n_kv, slot = scalar(divide(item, n_kv, W.kv_magic)), h = item - slot * n_kv, g = W.g, sub = part * 16;
     TileOf t;
     if (!tile_of(W, P.grid, slot, TM, t) || !t.one) return;   // (places that take several tiles do not split them)
     const int tile_rows = min(TM, t.nq * g - t.tile * TM), rows = min(16, tile_rows - sub), r0 = t.tile * TM + sub;
@@ -202,12 +201,14 @@ inline size_t record_bytes(long long items, int splits, int tm, int D) {
 }
 
 size_t thin_paged_workspace(const fk_paged_desc* d, const TileGrid& G, int max_len);
+void thin_prepare(const fk_paged_desc* d, AttnPagedParams& P, int max_len, void* workspace, bool& cold);   // splits and records
 fk_status thin_paged(const fk_paged_desc* d, AttnPagedParams P, int max_len, void* workspace, hipStream_t st);
 fk_status thin_rows(const fk_cache_desc* d, AttnPagedParams P, int max_len, void* workspace, hipStream_t st);
 size_t thin_rows_workspace(const fk_cache_desc* d);
 
-static constexpr int kPromptRows = 128;   // query rows of a tile of prompt.hip
+static constexpr int kPromptRows = 128;   // query rows of a tile of prompt.h
 size_t prompt_workspace(const fk_paged_desc* d, const TileGrid& G, int n_tokens, int max_chunk, int max_len);
-fk_status prompt_paged(const fk_paged_desc* d, AttnPagedParams P, int max_chunk, int max_len, void* workspace, hipStream_t st);
+// thin: the call's chunks of few rows, prepared, or null
+fk_status prompt_paged(const fk_paged_desc* d, AttnPagedParams P, const AttnPagedParams* thin, bool cold, int max_chunk, int max_len, void* workspace, hipStream_t st);
 
 }  // namespace fk

@@ -1,4 +1,4 @@
-// The entry points of attention over the pages of a prompt and of the weights that its pairs received: fk_paged_attn (thin.hip, prompt.hip),
+// The entry points of attention over the pages of a prompt and of the weights that its pairs received: fk_paged_attn (thin.h, prompt.h),
 // fk_paged_weights (weights.hip).
 #include "attn_paged.h"
 #include "weights.h"
@@ -32,7 +32,7 @@ static PagedParams view_params(const fk_paged_desc* desc, const void* q, const v
 }
 
 // Which kernel takes a chunk goes by its query rows: up to kThinRows the one that reads every pair once for 16 of them, beyond it the one with
-// tiles of 128.  A call that may hold both kinds is two launches, each of which leaves the other's chunks alone.  Calls whose 16-row tiles meet few
+// tiles of 128.  A call that may hold both kinds is one launch of both kernels' tiles.  Calls whose 16-row tiles meet few
 // pairs altogether are the first one's alone, however long their chunks: it spreads over more workgroups and its tiles take less time to
 // set up.  Measured on either side (one kernel / the other): 4 chunks of 32..64 tokens, g 7, D 128, 512 pairs (229 thousand): 16 / 23 us; 1 chunk of
 // 80 tokens, g 4, D 64, 4096 pairs (327 thousand): 15 / 22; 4 chunks of 12..24, g 7, D 128, 4096 pairs (516 thousand): 42 / 32.
@@ -66,7 +66,7 @@ extern "C" size_t fk_paged_attn_workspace(const fk_paged_desc* desc, int32_t n_t
     if (check_paged(desc) != FK_OK || check_chunks(desc, n_tokens, max_chunk, max_len) != FK_OK) return 0;
     const AttnPlanPaged p = plan_paged(desc, n_tokens, max_chunk, max_len);
     const size_t a = p.thin ? thin_paged_workspace(desc, p.thin_grid, max_len) : 0, b = p.prompt ? prompt_workspace(desc, p.prompt_grid, n_tokens, max_chunk, max_len) : 0;
-    return 16 + (a > b ? a : b);   // (one launch after the other)
+    return 16 + up256(a) + b;
 }
 
 extern "C" fk_status fk_paged_attn(const fk_paged_desc* desc, const void* q, const void* K, const void* V, const int32_t* page_table,
@@ -85,13 +85,20 @@ extern "C" fk_status fk_paged_attn(const fk_paged_desc* desc, const void* q, con
     T.out = out;
     T.stats = reinterpret_cast<float2*>(stats);
     const AttnPlanPaged p = plan_paged(desc, n_tokens, max_chunk, max_len);
-    if (p.prompt) {
-        T.grid = p.prompt_grid;
-        const fk_status r = prompt_paged(desc, T, max_chunk, max_len, workspace, (hipStream_t)stream);
-        if (r != FK_OK || !p.thin) return r;
+    if (!p.prompt) {
+        T.grid = p.thin_grid;
+        return thin_paged(desc, T, max_len, workspace, (hipStream_t)stream);
     }
-    T.grid = p.thin_grid;
-    return thin_paged(desc, T, max_len, workspace, (hipStream_t)stream);
+    AttnPagedParams F = T;
+    bool cold = false;
+    char* ws = static_cast<char*>(workspace);
+    if (p.thin) {
+        F.grid = p.thin_grid;
+        thin_prepare(desc, F, max_len, ws, cold);
+        ws += up256(thin_paged_workspace(desc, p.thin_grid, max_len));
+    }
+    T.grid = p.prompt_grid;
+    return prompt_paged(desc, T, p.thin ? &F : nullptr, cold, max_chunk, max_len, ws, (hipStream_t)stream);
 }
 
 extern "C" size_t fk_paged_weights_workspace(const fk_paged_desc* desc, int32_t n_tokens, int32_t max_chunk, int32_t max_len) {
