@@ -13,13 +13,13 @@ UB = 2.0 ** -8       # half a step of bf16, relative
 class Case:
     """chunks: [(kv_len, chunk), ...] one per sequence.  Host tensors, bf16 values exact in float64."""
 
-    def __init__(self, dtype, D, g, hkv, page, chunks, window=0, n_sink=0, scale=None, seed=0, before=0, behind=0, spare=2, key_scale=1.0):
+    def __init__(self, dtype, D, g, hkv, page, chunks, window=0, n_sink=0, scale=None, seed=0, before=0, behind=0, spare=2, key_scale=1.0, room=0):
         gen = torch.Generator().manual_seed(seed)
         self.dtype, self.D, self.g, self.H, self.page, self.chunks = dtype, D, g, hkv, page, chunks
         self.window, self.n_sink, self.scale = window, n_sink, D ** -0.5 if scale is None else scale
         self.dt = torch.float32 if dtype == "f32" else torch.bfloat16
         used = [-(-max(n, 1) // page) for n, _ in chunks]
-        self.max_pages, self.n_pages = max(used) + 1, sum(used) + spare
+        self.max_pages, self.n_pages = max(used) + 1 + room, sum(used) + spare   # room: for sequences this much longer, which max_len then covers
         self.table = torch.full((len(chunks), self.max_pages), -1, dtype=torch.int32)
         order = torch.randperm(self.n_pages, generator=gen)
         at = 0
@@ -36,7 +36,7 @@ class Case:
         self.k_new = torch.randn((self.n_tokens, hkv, D), generator=gen).mul_(key_scale).to(self.dt)
         self.v_new = torch.randn((self.n_tokens, hkv, D), generator=gen).to(self.dt)
         self.acc = torch.rand((len(chunks), hkv, self.max_pages * page), generator=gen)
-        self.max_chunk, self.max_len = max(1, max(c for _, c in chunks)), max(1, max(n for n, _ in chunks))
+        self.max_chunk, self.max_len = max(1, max(c for _, c in chunks)), max(1, max(n for n, _ in chunks)) if room == 0 else self.max_pages * page
 
     def appended(self):
         """The pools after the append, position by position."""
