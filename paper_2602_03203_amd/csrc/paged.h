@@ -73,8 +73,6 @@ __device__ __forceinline__ int sequence_of(const PagedParams& P, int t, int from
     return b < P.batch && P.q_start[b] <= t ? b : -1;
 }
 
-__device__ __forceinline__ bool sees(const PagedParams& P, int p, int j) { return j <= p && (j > p - P.window || j < P.sink); }
-
 // 16 bytes per lane from global memory to LDS, at `to` + lane * 16.  A barrier alone does not wait for them: arrived() before it.
 __device__ __forceinline__ void load_to_lds(const void* from, unsigned char* to) {
     __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)from, (__attribute__((address_space(3))) void*)to, 16, 0, 0);

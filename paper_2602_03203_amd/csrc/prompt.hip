@@ -44,7 +44,7 @@ __global__ __launch_bounds__(256) void mixed_merge_kernel(const MixedParams P) {
 // launch and 4 TB/s for the records; in fp32 one workgroup has the matrix units of its CU busy, 9.4 for 64 pairs.  Whole / 2 / 3 / 4 / 8 splits measured for 8 heads of g 4, D 128: 512 tokens of 8192: 216 / 123 /
 // 104 / 93 / 101; 1024 of 8192: 222 / 160 / 175 / 166 / 186; 4 chunks to 300 of 2048: 70 / 80 / 72 / 73 / 70.  How many chunks there are that are not single
 // tokens the host does not know: as many as would have the longest one's length.
-static int prompt_splits(const fk_paged_desc* d, int n_tokens, int max_chunk, long long pairs, int& shift) {
+static int prompt_splits(const fk_paged_desc* d, const TileGrid& G, int n_tokens, int max_chunk, long long pairs, int& shift) {
     shift = d->dtype == FK_BF16 ? 3 : 4;   // 512 pairs and more each
     const long long g = d->n_q_heads / d->n_kv_heads, chunk = max_chunk < n_tokens ? max_chunk : n_tokens, rest = n_tokens - d->batch;
     const long long chunks = chunk > 1 && rest > 0 ? (rest + chunk - 2) / (chunk - 1) : 1;
@@ -52,7 +52,7 @@ static int prompt_splits(const fk_paged_desc* d, int n_tokens, int max_chunk, lo
     const double whole = (double)pairs / 64 * d->head_dim / 128 * (d->dtype == FK_BF16 ? 2.1 : 9.4);
     int best = 1;
     double least = 0;
-    for (int s = 1; s <= 16 && (s == 1 || pairs / s >= 512); ++s) {
+    for (int s = 1; s <= 16 && (s == 1 || (pairs / s >= 512 && (long long)G.places * d->n_kv_heads * s <= 4096 /* a quarter of a GiB of records */)); ++s) {
         const long long all = items * s, over = all % 512;
         const double turns = d->dtype == FK_F32 ? std::max(1., (double)all / 256) : (double)(all / 512) + (over == 0 ? 0. : over <= 256 ? 5. / 6 : 1.);
         const double time = turns * whole / s + (s == 1 ? 0. : 6 + (double)all * kPromptRows * d->head_dim * 8 / 4e6);
@@ -62,7 +62,7 @@ static int prompt_splits(const fk_paged_desc* d, int n_tokens, int max_chunk, lo
 }
 size_t prompt_workspace(const fk_paged_desc* d, const TileGrid& G, int n_tokens, int max_chunk, int max_len) {
     int shift;
-    return record_bytes((long long)G.places * d->n_kv_heads, prompt_splits(d, n_tokens, max_chunk, max_len, shift), kPromptRows, d->head_dim);
+    return record_bytes((long long)G.places * d->n_kv_heads, prompt_splits(d, G, n_tokens, max_chunk, max_len, shift), kPromptRows, d->head_dim);
 }
 
 template <typename T, int D, bool NT_LOADS> static fk_status mixed_launch(const MixedParams& P, hipStream_t st) {
@@ -81,9 +81,9 @@ template <typename T, int D>
 static fk_status prompt_launch(const fk_paged_desc* d, AttnPagedParams& P, const AttnPagedParams* thin, bool cold, int max_chunk, int max_len, void* ws, hipStream_t st) {
     using C = PromptCfg<T, D>;
     const long long items = (long long)P.grid.places * d->n_kv_heads;
-    P.splits = prompt_splits(d, P.view.n_tokens, max_chunk, max_len, P.split_shift);   // (what the workspace is for)
+    P.splits = prompt_splits(d, P.grid, P.view.n_tokens, max_chunk, max_len, P.split_shift);   // (what the workspace is for)
     const long long seen = (long long)P.view.window + P.view.sink + kPromptRows;
-    if (seen < max_len) P.splits = std::min(P.splits, prompt_splits(d, P.view.n_tokens, max_chunk, seen, P.split_shift));
+    if (seen < max_len) P.splits = std::min(P.splits, prompt_splits(d, P.grid, P.view.n_tokens, max_chunk, seen, P.split_shift));
     P.rec_ml = reinterpret_cast<float2*>(ws);
     P.rec = reinterpret_cast<float*>(static_cast<char*>(ws) + up256((size_t)items * P.splits * kPromptRows * sizeof(float2)));
     if (thin) {

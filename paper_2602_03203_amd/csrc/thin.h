@@ -22,7 +22,6 @@ template <typename T, int D> struct ThinCfg {
     static constexpr int KT = BF ? 32 : 16;
     static constexpr int NT = KT / 16;                   // 16-key products of a tile
     static constexpr int KS = CH / 4;                    // chunks of a key per lane
-    static constexpr int KL = NT * KS;                   // K loads per lane and tile
     static constexpr int VL = BF ? 8 : 4 * D / 64;       // V loads per lane and tile (bf16 D = 64: 8 bytes each)
     static constexpr int ET = D / 16;                    // channel tiles of the output
     static constexpr int PART = D + 4;                   // float stride of a row of a partial output in LDS

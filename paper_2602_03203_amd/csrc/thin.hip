@@ -29,7 +29,7 @@ static ThinPlan thin_plan(const fk_paged_desc* d, const TileGrid& G, long long p
     if (items < 128) s = 256 / items;
     else if (pairs >= 6144) s = 16;
     if (s > 16) s = 16;
-    if (s > (1 << 22) / items) s = (1 << 22) / items;   // (what a launch holds)
+    if (s > (1 << 16) / items) s = (1 << 16) / items;   // (half a GiB of records; so many items even out by themselves)
     if (s > pairs >> (p.shift + kt_shift)) s = pairs >> (p.shift + kt_shift);
     if (s > 1) p.splits = (int)s;
     return p;
