@@ -45,10 +45,11 @@ struct AttnPagedParams {
     void* out;
     float2* stats;             // [tokens][heads] or null
     TileGrid grid;
+    int whole;                 // items (slot, head) before this one are not split
     int splits;                // of a tile's pairs, at most
     int split_shift;           // key tiles of a split, at least 2^split_shift
-    float* rec;                // [slot][head][split][16][D], with more than one split
-    float2* rec_ml;            // [slot][head][split][16]
+    float* rec;                // [item - whole][split][rows of a tile][D], with more than one split
+    float2* rec_ml;            // [item - whole][split][rows of a tile]
     // rows of a budgeted cache
     int cap;
     int32_t *pos, *len;
@@ -131,7 +132,7 @@ __device__ __forceinline__ void merge_tile(const AttnPagedParams& P, int item, i
     const int lo = t.first + divide(t.tile * TM, g, W.g_magic), hi = t.first + divide(t.tile * TM + tile_rows - 1, g, W.g_magic);
     const int splits = splits_of(key_tiles(W, lo, hi, KT).total, P.splits, P.split_shift);
     if (rows <= 0 || splits == 1) return;
-    const size_t rec = ((size_t)slot * n_kv + h) * P.splits * TM + sub;
+    const size_t rec = (size_t)(item - P.whole) * P.splits * TM + sub;
     for (int x = tid; x < rows * (D / 4); x += 256) {
         const int r = x / (D / 4), d = x % (D / 4) * 4;
         const Merged<D> o = merge_records<D>(P, rec + r, TM, splits, d);

@@ -87,7 +87,7 @@ __device__ __forceinline__ void prompt_tile(const AttnPagedParams& P, int item, 
         auto token_of = [&](int r) { return divide(r, g, W.g_magic); };
         const int tile_lo = scalar(t.first + token_of(r0)), tile_hi = scalar(t.first + token_of(r0 + rows - 1));
         const KeyTiles kt = key_tiles(W, tile_lo, tile_hi, KT);
-        const int splits = scalar(splits_of(kt.total, t.one ? P.splits : 1, P.split_shift));
+        const int splits = scalar(splits_of(kt.total, t.one && item >= P.whole ? P.splits : 1, P.split_shift));
         if (split >= splits) continue;
         const int per = splits == 1 ? kt.total : scalar(divide(kt.total + splits - 1, splits)), t_begin = min(split * per, kt.total), t_end = min(t_begin + per, kt.total);
 
@@ -376,7 +376,7 @@ __device__ __forceinline__ void prompt_tile(const AttnPagedParams& P, int item, 
                 const int r = w0 + ct * 16 + n16, tok = token_of(r);
                 const size_t row = ((size_t)(t.begin + tok) * n_kv + h) * g + (r - tok * g);
                 const bool none = m_top[ct] == -INFINITY;
-                const size_t rec = (((size_t)slot * n_kv + h) * P.splits + split) * TM + (r - r0);
+                const size_t rec = ((size_t)(item - P.whole) * P.splits + split) * TM + (r - r0);
                 const float mul = splits > 1 ? f : none ? 0.f : 1.0f / l;
 #pragma unroll
                 for (int e = 0; e < ET; e += BF ? 1 : 4) {
