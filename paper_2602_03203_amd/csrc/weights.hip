@@ -11,6 +11,8 @@
 #include "weights.h"
 #include "window.h"
 
+#include <algorithm>
+
 namespace fk {
 
 typedef __attribute__((ext_vector_type(8))) __bf16 wbf16x8_t;
@@ -220,8 +222,14 @@ __global__ __launch_bounds__(256) void weights_sum_kernel(const WeightsParams P)
 }
 
 // ---- host side ---------------------------------------------------------------------------------------------------
-// Few keys leave CUs without a workgroup: then a wavefront takes 16 of them instead of 64, and beyond that the queries are split, into no less than two
-// tiles each.  Partial sums are kept up to the table's length, so that a length hint below a sequence's length loses nothing.
+// Splits of the queries, whose partial sums a second launch puts together: so many that 2048 workgroups (fp32, where one has the matrix units of its CU
+// busy, 512) even out what the chunk's own keys and the last turn leave idle, each with 8 tiles of queries and more.  Where that is below 512 workgroups -
+// few keys, or few queries - a wavefront takes 16 keys instead of 64, each tile then costs less, and 1024 workgroups with two tiles and more are enough.
+// us, by splits; 8 heads of g 4, D 128:  2048 tokens of 16384 1: 312, 2: 293, 4: 293, 8: 306;  of 20000 459, 361, 362, 377;  1024 of 9000 149, 125, 107, 109;  4096 of
+// 4096 416, 223, 156, 134, 16: 136;  512 of 32768 180, 180, 197;  128 of 8192 30, 26, 32, with 16 keys a wavefront 24, 27, 33;  2048 of 2048 220, 124,
+// 76, 55, with 16 keys 148, 85, 65;  two of 150 to 300 of to 4000, 2 heads, D 64: 37, 27, 19, 16, with 16 keys 20, 16, 13;  fp32, 4 heads: 1000 of 4000, D 64: 332, 175,
+// 100, 88, 16: 98, with 16 keys 141, 107, 96;  64 of 10000 33, 33, 34, with 16 keys 25, 25, 28.
+// Partial sums are kept up to the table's length, so that a length hint below a sequence's length loses nothing.
 struct WeightsPlan {
     bool few;
     int keys, splits;
@@ -229,15 +237,16 @@ struct WeightsPlan {
 template <typename T, int D> static WeightsPlan weights_plan_of(const fk_paged_desc* d, int n_tokens, int max_chunk, int max_len) {
     const long long rows = (long long)d->batch * d->n_kv_heads;
     auto blocks = [&](int keys) { return rows * ((max_len + keys - 1) / keys); };
-    WeightsPlan p;
-    p.few = blocks(WeightsCfg<T, D, false>::KEYS) < 128;
-    p.keys = p.few ? WeightsCfg<T, D, true>::KEYS : WeightsCfg<T, D, false>::KEYS;
     const long long queries = (long long)(max_chunk < n_tokens ? max_chunk : n_tokens) * (d->n_q_heads / d->n_kv_heads);
-    long long s = 512 / blocks(p.keys);
-    const long long most = queries / (2 * WeightsCfg<T, D, false>::QT);
-    if (s > most) s = most;
-    if (s > 16) s = 16;
-    p.splits = s < 1 || rows > 65535 ? 1 : (int)s;
+    const long long tiles = (queries + WeightsCfg<T, D, false>::QT - 1) / WeightsCfg<T, D, false>::QT;
+    const long long space = (1ll << 26) / (rows * d->max_pages * d->page_size);   // a quarter of a GiB of partial sums
+    const int most = WeightsCfg<T, D, false>::BF ? 2048 : 512;
+    auto splits = [&](int keys, int workgroups, int least) {
+        const long long s = std::min({workgroups / blocks(keys), tiles / least, space, 16ll});
+        return s < 1 || rows > 65535 ? 1 : (int)s;
+    };
+    WeightsPlan p = {false, WeightsCfg<T, D, false>::KEYS, splits(WeightsCfg<T, D, false>::KEYS, most, 8)};
+    if (blocks(p.keys) * p.splits < 512) p = {true, WeightsCfg<T, D, true>::KEYS, splits(WeightsCfg<T, D, true>::KEYS, 1024, 2)};
     return p;
 }
 static WeightsPlan weights_plan(const fk_paged_desc* d, int n_tokens, int max_chunk, int max_len) {
