@@ -1,12 +1,15 @@
 // fk_paged_weights: acc_j += sum over the chunk's queries that see pair j, over the group's heads, of 2^(s - M) / L.
 //
 // A wavefront owns KG * 16 keys, whose K stays in registers as matrix operands; the chunk's query rows (tokens x heads) pass by in
-// tiles of 64 through LDS, with their M and 1 / L, shared by the four wavefronts.  A product of 16 keys x 16 rows leaves a lane with four keys of
-// ONE row, so M and 1 / L are one register each and a pair's weight is added by one fma; the 16 lanes of a key are summed once, at the end.
-// The order of all sums is fixed.  The products are those of the attention kernels, step by step the same ones, so that logits are the same
-// bits: beyond 2^24, where a logit's rounding is more than an exponent may be off, M still belongs to them.
+// tiles of 64, straight into LDS two tiles ahead, with their M and 1 / L, shared by the four wavefronts.  A product of 16 keys x 16 rows leaves a
+// lane with four keys of ONE row, so M and 1 / L are one register each and a pair's weight is added by one fma; the 16 lanes of a key are
+// summed once, at the end.  The order of all sums is fixed.  The products are those of the attention kernels, step by step the same ones, so that
+// logits are the same bits: beyond 2^24, where a logit's rounding is more than an exponent may be off, M still belongs to them.
 //
-// Bound by matrix and vector instructions together: per 16 x 16 logits D / 32 products and, per lane, four times an fma, an exponential and an fma.
+// Bound by matrix and vector instructions together: per 16 x 16 logits D / 32 products and, per lane, four times an fma, an exponential and an fma.  16
+// products and the vector work that goes with them, registers alone, two wavefronts to a SIMD, take 272 and 214 ns by themselves and 404 together; the
+// kernel is at 1.4 times that (2048 tokens of 16384 pairs, 8 heads of g 4, D 128: 286 us, 910 TFLOP/s).  Three wavefronts to a SIMD do as well as two
+// whose next logits are formed beside their exponentials (286 and 290), with half of the code.
 // Few keys and many queries: the queries are split over workgroups too, partial sums meet in a second launch.
 #include "weights.h"
 #include "window.h"
@@ -38,7 +41,7 @@ template <typename T, int D, bool FEW> struct WeightsCfg {   // FEW: few keys, 1
 static constexpr float kHugeLogit = 16777216.f;
 
 template <typename T, int D, bool FEW>
-__global__ __launch_bounds__(256, 2) void weights_kernel(const WeightsParams P) {
+__global__ __launch_bounds__(256, 3) void weights_kernel(const WeightsParams P) {
     using C = WeightsCfg<T, D, FEW>;
     constexpr bool BF = C::BF;
     constexpr int CH = C::CH, KS = C::KS, KG = C::KG, QT = C::QT, NQ = C::NQ, LD = C::LD;
@@ -87,19 +90,41 @@ __global__ __launch_bounds__(256, 2) void weights_kernel(const WeightsParams P) 
         // banks; a load writes in the order of its lanes, so each lane fetches the chunk that belongs in its place.
         constexpr int kSwap = (CH < 16 ? CH : 16) - 1;
         const uint32_t q_first = ((uint32_t)begin * W.n_kv + h) * g, q_token = (uint32_t)(W.n_kv - 1) * g;   // query row r of token t: q_first + r + t * q_token, below 2^28
+        // where the rows that this thread fetches lie: a tile further they are QT rows and QT / g tokens on, or one token more (no division a tile)
+        struct Place {
+            uint32_t at;   // query row q_first + r + t * q_token
+            int head;      // of its token's g
+        };
+        auto place_of = [&](int in_tile) {
+            const int row = row_lo + i0 * QT + in_tile, tok = token_of(row);
+            return Place{q_first + row + tok * q_token, row - tok * g};
+        };
+        const uint32_t last = q_first + row_hi - 1 + token_of(max(row_hi - 1, 0)) * q_token;   // (rows behind it: its copies)
+        const int step_token = scalar(token_of(QT)), step_head = QT - step_token * g;
+        const uint32_t step = QT + step_token * q_token;
+        auto advance = [&](Place& x) {
+            x.at += step;
+            x.head += step_head;
+            const bool over = x.head >= g;
+            x.at += over ? q_token : 0;
+            x.head -= over ? g : 0;
+        };
+        Place at_q[LD], at_st;
+#pragma unroll
+        for (int u = 0; u < LD; ++u) at_q[u] = place_of((tid + u * 256) / CH);
+        at_st = place_of(tid % QT);
         float2 st;
-        int st_row;
-        auto send = [&](int i, int buf) {
-            const int base = row_lo + i * QT;
+        int st_row = row_lo + i0 * QT + tid % QT - QT;
+        auto send = [&](int buf) {   // the next tile
 #pragma unroll
             for (int u = 0; u < LD; ++u) {
-                const int x = tid + u * 256, in_tile = x / CH, row = min(base + in_tile, row_hi - 1);
-                load_to_lds(reinterpret_cast<const wu32x4_t*>(W.q) + (size_t)(q_first + row + token_of(row) * q_token) * CH + (x % CH ^ (in_tile & kSwap)),
-                            s_q + buf * C::TILE_BYTES + (u * 256 + wave * 64) * 16);
+                const int x = tid + u * 256;
+                load_to_lds(reinterpret_cast<const wu32x4_t*>(W.q) + (size_t)min(at_q[u].at, last) * CH + (x % CH ^ (x / CH & kSwap)), s_q + buf * C::TILE_BYTES + (u * 256 + wave * 64) * 16);
+                advance(at_q[u]);
             }
-            st_row = base + tid % QT;
-            const int row = min(st_row, row_hi - 1);
-            st = P.stats[q_first + row + token_of(row) * q_token];
+            if (wave * kWave < QT) st = P.stats[min(at_st.at, last)];
+            st_row += QT;
+            advance(at_st);
         };
         auto stage = [&](int buf) {
             if (tid < QT) {
@@ -111,48 +136,36 @@ __global__ __launch_bounds__(256, 2) void weights_kernel(const WeightsParams P) 
         int q_at[KS];
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks) q_at[ks] = (n16 * CH + ((ks * 4 + quad) ^ (n16 & kSwap))) * 16;
-        float m = 0.f, il = 0.f;   // of the rows whose logits are next
-        auto products = [&](int buf, int qt, wf32x4_t (&c)[KG], float& m, float& il) {
-            W128 q[KS];
-#pragma unroll
-            for (int ks = 0; ks < KS; ++ks) q[ks].u = *reinterpret_cast<const wu32x4_t*>(s_q + buf * C::TILE_BYTES + qt * 16 * CH * 16 + q_at[ks]);
-            m = s_m[buf][qt * 16 + n16];
-            il = s_il[buf][qt * 16 + n16];
-#pragma unroll
-            for (int j = 0; j < KG; ++j) {
-                c[j] = (wf32x4_t){0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                for (int ks = 0; ks < KS; ++ks) {
-                    if constexpr (BF) {
-                        c[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k[j][ks].v, q[ks].v, c[j], 0, 0, 0);
-                    } else {
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) c[j] = __builtin_amdgcn_mfma_f32_16x16x4f32(k[j][ks].f[e], q[ks].f[e], c[j], 0, 0, 0);
-                    }
-                }
-            }
-        };
-        wf32x4_t c[2][KG];
         if (i0 < i1) {
-            send(i0, 0);
+            send(0);
             stage(0);
-            if (i0 + 1 < i1) send(i0 + 1, 1);
+            if (i0 + 1 < i1) send(1);
         }
         arrived();
         __syncthreads();
-        if (i0 < i1) products(0, 0, c[0], m, il);
         for (int i = i0, buf = 0; i < i1; ++i, buf ^= 1) {
             const int base = row_lo + i * QT, lo = first + scalar(token_of(base)), hi = first + scalar(token_of(min(base + QT, row_hi) - 1));   // positions
             const bool whole = kw + KG * 16 <= lo + 1 && base + QT <= row_hi && (W.window == 0x7fffffff || kw > hi - W.window || kw + KG * 16 <= W.sink);
 #pragma unroll
             for (int qt = 0; qt < NQ; ++qt) {
-                if (qt == NQ - 1) {   // what the tile's rows are read for is done
-                    stage(buf ^ 1);
-                    arrived();
-                    __syncthreads();
-                    if (i + 2 < i1) send(i + 2, buf);
+                W128 q[KS];
+#pragma unroll
+                for (int ks = 0; ks < KS; ++ks) q[ks].u = *reinterpret_cast<const wu32x4_t*>(s_q + buf * C::TILE_BYTES + qt * 16 * CH * 16 + q_at[ks]);
+                const float m = s_m[buf][qt * 16 + n16], il = s_il[buf][qt * 16 + n16];
+                wf32x4_t c[KG];   // (side by side: a product waits for the one before it in its sum)
+#pragma unroll
+                for (int j = 0; j < KG; ++j) c[j] = (wf32x4_t){0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int ks = 0; ks < KS; ++ks) {
+#pragma unroll
+                    for (int e = 0; e < (BF ? 1 : 4); ++e) {
+#pragma unroll
+                        for (int j = 0; j < KG; ++j) {
+                            if constexpr (BF) c[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k[j][ks].v, q[ks].v, c[j], 0, 0, 0);
+                            else c[j] = __builtin_amdgcn_mfma_f32_16x16x4f32(k[j][ks].f[e], q[ks].f[e], c[j], 0, 0, 0);
+                        }
+                    }
                 }
-                wf32x4_t (&now)[KG] = c[qt & 1];
                 if (!whole) {
                     const int row = base + qt * 16 + n16, p = row < row_hi ? first + token_of(row) : -1;
                     const int from = W.window == 0x7fffffff ? -1 : p - W.window;
@@ -162,7 +175,7 @@ __global__ __launch_bounds__(256, 2) void weights_kernel(const WeightsParams P) 
                         for (int e = 0; e < 4; ++e) {
                             const int key = kw + j * 16 + quad * 4 + e;
                             const bool seen = (key <= p) & ((key > from) | (key < W.sink));
-                            now[j][e] = seen ? now[j][e] : -INFINITY;
+                            c[j][e] = seen ? c[j][e] : -INFINITY;
                         }
                 }
                 float by = scale, less = m;
@@ -172,20 +185,19 @@ __global__ __launch_bounds__(256, 2) void weights_kernel(const WeightsParams P) 
 #pragma unroll
                     for (int j = 0; j < KG; ++j)
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) now[j][e] = attn_logit(now[j][e], scale) - m;
+                        for (int e = 0; e < 4; ++e) c[j][e] = attn_logit(c[j][e], scale) - m;
                 }
-                // beside these rows' weights, the next ones' logits (behind the last tile: of what lies there, for nobody)
-                float m_next, il_next;
-                products(qt == NQ - 1 ? buf ^ 1 : buf, (qt + 1) % NQ, c[(qt + 1) & 1], m_next, il_next);
 #pragma unroll
                 for (int j = 0; j < KG; ++j)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) a[j][e] = fmaf(__builtin_amdgcn_exp2f(fmaf(now[j][e], by, -less)), il, a[j][e]);
+                    for (int e = 0; e < 4; ++e) a[j][e] = fmaf(__builtin_amdgcn_exp2f(fmaf(c[j][e], by, -less)), il, a[j][e]);
 #pragma unroll
                 for (int j = 0; j < KG; ++j) asm volatile("" : "+v"(a[j]));   // here, not behind the tile's last branch
-                m = m_next;
-                il = il_next;
             }
+            stage(buf ^ 1);
+            arrived();
+            __syncthreads();
+            if (i + 2 < i1) send(buf);
         }
         __syncthreads();   // the LDS is the next keys'
         // the 16 rows of a key, then one lane a key
