@@ -236,7 +236,7 @@ __global__ __launch_bounds__(256) void weights_sum_kernel(const WeightsParams P)
 // ---- host side ---------------------------------------------------------------------------------------------------
 // Splits of the queries, whose partial sums a second launch puts together: so many that 2048 workgroups (fp32, where one has the matrix units of its CU
 // busy, 512) even out what the chunk's own keys and the last turn leave idle, each with 8 tiles of queries and more.  Where that is below 512 workgroups -
-// few keys, or few queries - a wavefront takes 16 keys instead of 64, each tile then costs less, and 1024 workgroups with two tiles and more are enough.
+// few keys, or few queries - a wavefront takes 16 keys instead of 64, each tile then costs less, and 1024 workgroups with four tiles and more are enough.
 // us, by splits; 8 heads of g 4, D 128:  2048 tokens of 16384 1: 312, 2: 293, 4: 293, 8: 306;  of 20000 459, 361, 362, 377;  1024 of 9000 149, 125, 107, 109;  4096 of
 // 4096 416, 223, 156, 134, 16: 136;  512 of 32768 180, 180, 197;  128 of 8192 30, 26, 32, with 16 keys a wavefront 24, 27, 33;  2048 of 2048 220, 124,
 // 76, 55, with 16 keys 148, 85, 65;  two of 150 to 300 of to 4000, 2 heads, D 64: 37, 27, 19, 16, with 16 keys 20, 16, 13;  fp32, 4 heads: 1000 of 4000, D 64: 332, 175,
@@ -258,7 +258,7 @@ template <typename T, int D> static WeightsPlan weights_plan_of(const fk_paged_d
         return s < 1 || rows > 65535 ? 1 : (int)s;
     };
     WeightsPlan p = {false, WeightsCfg<T, D, false>::KEYS, splits(WeightsCfg<T, D, false>::KEYS, most, 8)};
-    if (blocks(p.keys) * p.splits < 512) p = {true, WeightsCfg<T, D, true>::KEYS, splits(WeightsCfg<T, D, true>::KEYS, 1024, 2)};
+    if (blocks(p.keys) * p.splits < 512) p = {true, WeightsCfg<T, D, true>::KEYS, splits(WeightsCfg<T, D, true>::KEYS, 1024, 4)};
     return p;
 }
 static WeightsPlan weights_plan(const fk_paged_desc* d, int n_tokens, int max_chunk, int max_len) {
