@@ -1,6 +1,5 @@
 // fk_decode_step_acc: the decode step that adds its attention weights to those that the retained pairs have accumulated (thin.h).
 #include "attn_paged.h"
-#include <cfloat>
 #include <climits>
 #include <cmath>
 
@@ -29,7 +28,7 @@ extern "C" fk_status fk_decode_step_acc(const fk_cache_desc* desc, const void* q
     P.view.g = desc->n_q_heads / desc->n_kv_heads;
     P.view.window = INT_MAX;
     P.view.negate = std::signbit(softmax_scale);
-    P.view.scale_log2e = std::fmax(std::fabs(softmax_scale) * 1.4426950408889634f, FLT_MIN);   // (0: all logits equal)
+    P.view.scale_log2e = base2_scale(softmax_scale);
     P.out = out;
     P.cap = desc->capacity;
     P.pos = pos;

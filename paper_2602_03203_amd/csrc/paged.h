@@ -2,6 +2,9 @@
 #pragma once
 #include "fk_common.h"
 
+#include <cfloat>
+#include <cmath>
+
 namespace fk {
 
 struct PagedParams {
@@ -179,6 +182,12 @@ __device__ __forceinline__ KeyTiles key_tiles(const PagedParams& P, int lo, int 
 }
 
 // ---- host side ---------------------------------------------------------------------------------------------------
+// |softmax_scale| for exponents of 2; 0: as near to it as keeps what is not seen at -inf, all logits are equal; NaN stays NaN
+inline float base2_scale(float softmax_scale) {
+    const float s = std::fabs(softmax_scale) * 1.4426950408889634f;
+    return s < FLT_MIN ? FLT_MIN : s;
+}
+
 inline fk_status check_paged(const fk_paged_desc* d) {
     if (!d) return FK_ERR_INVALID_ARG;
     if (d->batch <= 0 || d->n_q_heads <= 0 || d->n_kv_heads <= 0 || d->head_dim <= 0 || d->page_size <= 0 || d->n_pages <= 0 || d->max_pages <= 0)

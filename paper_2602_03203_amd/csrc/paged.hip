@@ -95,7 +95,7 @@ extern "C" fk_status fk_paged_append(const fk_paged_desc* desc, void* K, void* V
     fk_status s = check_paged(desc);
     if (s == FK_OK) s = check_chunks(desc, n_tokens, 1, 1);
     if (s != FK_OK) return s;
-    if (!K || !V || !page_table || !kv_len || !q_start || !k_new || !v_new) return FK_ERR_INVALID_ARG;
+    if (!K || !V || !page_table || !kv_len || !q_start || ((!k_new || !v_new) && n_tokens > 0)) return FK_ERR_INVALID_ARG;
     if (!aligned16(K) || !aligned16(V) || !aligned16(k_new) || !aligned16(v_new)) return FK_ERR_INVALID_ARG;
     if (n_tokens == 0) return FK_OK;
     const PagedParams P = paged_params(desc, page_table, kv_len, q_start, n_tokens);

@@ -2,7 +2,6 @@
 // fk_paged_weights (weights.hip).
 #include "attn_paged.h"
 #include "weights.h"
-#include <cfloat>
 #include <climits>
 #include <cmath>
 
@@ -13,7 +12,7 @@ static fk_status check_view(const fk_paged_desc* desc, const void* q, const void
     fk_status s = check_paged(desc);
     if (s == FK_OK) s = check_chunks(desc, n_tokens, max_chunk, max_len);
     if (s != FK_OK) return s;
-    if (!q || !K || !table || !kv_len || !q_start || window < 0 || n_sink < 0) return FK_ERR_INVALID_ARG;
+    if ((!q && n_tokens > 0) || !K || !table || !kv_len || !q_start || window < 0 || n_sink < 0) return FK_ERR_INVALID_ARG;   // (no token: an empty q)
     if (!aligned16(q) || !aligned16(K) || (reinterpret_cast<uintptr_t>(stats) & 7)) return FK_ERR_INVALID_ARG;
     return FK_OK;
 }
@@ -26,8 +25,7 @@ static PagedParams view_params(const fk_paged_desc* desc, const void* q, const v
     P.window = window == 0 || window >= (1 << 24) ? INT_MAX : window;   // (longer than any sequence: none)
     P.sink = n_sink;
     P.negate = std::signbit(softmax_scale);
-    // (0: as near to it as keeps what is not seen at -inf; all logits are equal)
-    P.scale_log2e = std::fmax(std::fabs(softmax_scale) * 1.4426950408889634f, FLT_MIN);
+    P.scale_log2e = base2_scale(softmax_scale);
     return P;
 }
 
@@ -75,7 +73,7 @@ extern "C" fk_status fk_paged_attn(const fk_paged_desc* desc, const void* q, con
                                    size_t workspace_bytes, void* stream) {
     const fk_status s = check_view(desc, q, K, page_table, kv_len, q_start, n_tokens, max_chunk, max_len, window, n_sink, stats);
     if (s != FK_OK) return s;
-    if (!V || !out || !aligned16(V) || !aligned16(out)) return FK_ERR_INVALID_ARG;
+    if (!V || (!out && n_tokens > 0) || !aligned16(V) || !aligned16(out)) return FK_ERR_INVALID_ARG;
     if (!workspace || workspace_bytes < fk_paged_attn_workspace(desc, n_tokens, max_chunk, max_len) || !aligned16(workspace)) return FK_ERR_WORKSPACE;
     if (n_tokens == 0) return FK_OK;
     PagedParams P = view_params(desc, q, K, page_table, kv_len, q_start, n_tokens, window, n_sink, softmax_scale);
@@ -112,7 +110,7 @@ extern "C" fk_status fk_paged_weights(const fk_paged_desc* desc, const void* q, 
                                       size_t workspace_bytes, void* stream) {
     const fk_status s = check_view(desc, q, K, page_table, kv_len, q_start, n_tokens, max_chunk, max_len, window, n_sink, stats);
     if (s != FK_OK) return s;
-    if (!stats || !acc) return FK_ERR_INVALID_ARG;
+    if ((!stats && n_tokens > 0) || !acc) return FK_ERR_INVALID_ARG;
     if (!workspace || workspace_bytes < fk_paged_weights_workspace(desc, n_tokens, max_chunk, max_len) || !aligned16(workspace)) return FK_ERR_WORKSPACE;
     if (n_tokens == 0) return FK_OK;
     WeightsParams P = {};

@@ -124,3 +124,11 @@ def test_accumulated_weights_refuse(fklib):
     for budget in (0, 513):
         assert L.fk_compact_acc(ctypes.byref(d), *good, budget, 0) == fklib.FK_ERR_INVALID_ARG
     assert L.fk_compact_acc(ctypes.byref(R(2, 8, 2, 96, 512, 1)), *good, 256, 0) == fklib.FK_ERR_UNSUPPORTED
+
+
+def test_no_tokens_and_no_buffers(fklib):
+    """A call without tokens, whose token buffers are empty, has nothing to do."""
+    L = fklib.lib()
+    d, rows = fklib.fk_paged_desc(2, 8, 2, 128, 16, 100, 40, fklib.FK_BF16), fklib.fk_cache_desc(2, 8, 2, 128, 512, fklib.FK_BF16)
+    got = calls(L, d, rows, n=0, bytes=1 << 40, q=0, out=0, stats=0, k_new=0, v_new=0)
+    assert set(got.values()) == {fklib.FK_OK}

@@ -1,5 +1,9 @@
 """The kernel for chunks of many query rows, alone and beside single tokens, against the oracle.  Calls of little work are the other kernel's, by their
 length bound: these have tables, and a bound, for sequences much longer than theirs."""
+import copy
+import subprocess
+import sys
+
 import numpy as np
 import pytest
 import torch
@@ -180,3 +184,76 @@ def test_captured_on_one_workspace():
 def test_many_sequences():
     """More sequences than one wavefront looks at in a step, a few with chunks."""
     _go(_case("bf16", 64, 4, 1, 16, [(20 + b % 50, 1 if b % 9 else 17) for b in range(150)], seed=30))
+
+
+@pytest.mark.parametrize("long", [True, False])
+def test_replayed_with_other_sequences(long):
+    """A captured call follows what the device arrays hold at its replay: other lengths, other chunks, the same buffers."""
+    make = _case if long else Case
+    c = make("bf16", 128, 4, 2, 64, [(900, 1), (1300, 64), (700, 5)], seed=50)
+    s = c.dev()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        c.run(s)
+    side.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        c.run(s)
+    for chunks in ([(850, 64), (1290, 1), (640, 5)], [(900, 0), (33, 33), (700, 37)], [(900, 1), (1300, 64), (700, 5)], [(1, 1), (1, 1), (70, 68)]):
+        c2 = copy.copy(c)
+        c2.chunks = chunks
+        c2.kv_len = torch.tensor([n for n, _ in chunks], dtype=torch.int32)
+        c2.q_start = torch.tensor(np.concatenate([[0], np.cumsum([m for _, m in chunks])]), dtype=torch.int32)
+        for k in ("K", "V", "kv_len", "q_start", "acc"):
+            s[k].copy_(getattr(c2, k))
+        s["out"].fill_(7.0)
+        s["stats"].fill_(7.0)
+        torch.cuda.synchronize()
+        g.replay()
+        torch.cuda.synchronize()
+        ref, tol = c2.reference()
+        c2.check(s, ref, tol, what=str(chunks))
+
+
+@pytest.mark.parametrize("dtype, D", TYPES)
+def test_lengths_beyond_the_table(dtype, D):
+    """kv_len is taken as what the table has entries for; a negative one as 0."""
+    c = Case(dtype, D, 4, 2, 16, [(40, 3), (70, 30), (20, 2)], seed=51)
+    room = c.max_pages * 16
+    c.kv_len = torch.tensor([room + 12345, 1 << 30, -5], dtype=torch.int32)
+    c.chunks = [(room, 3), (room, 30), (0, 2)]
+    _go(c, weights=True)
+
+
+def test_first_call_of_a_process_is_captured():
+    """Nothing but the capture has called the library: both kinds of tiles, weights and the step that accumulates."""
+    code = """
+import sys
+sys.path[:0] = [%r, %r]
+import torch
+import paper_2602_03203_amd as fk
+from test_gpu_paged_prompt import _case
+c = _case("f32", 128, 4, 2, 64, [(900, 1), (1300, 64)], seed=52)
+s = c.dev()
+torch.cuda.synchronize()
+g = torch.cuda.CUDAGraph()
+with torch.cuda.graph(g):
+    c.run(s)
+g.replay()
+torch.cuda.synchronize()
+ref, tol = c.reference()
+c.check(s, ref, tol)
+print("as it should be")
+""" % (str(__file__).rsplit("/", 2)[0], str(__file__).rsplit("/", 1)[0])
+    r = subprocess.run([sys.executable, "-c", code], capture_output=True, text=True, timeout=100)
+    assert r.returncode == 0 and "as it should be" in r.stdout, r.stdout[-500:] + r.stderr[-2000:]
+
+
+def test_scale_that_is_no_number():
+    c = _case("bf16", 64, 4, 1, 16, [(30, 1), (60, 20)], seed=53)
+    c.scale = float("nan")
+    s = c.dev()
+    c.run(s, weights=False)
+    torch.cuda.synchronize()
+    assert torch.isnan(s["out"]).all()
