@@ -129,8 +129,10 @@ __global__ __launch_bounds__(256, 3) void weights_kernel(const WeightsParams P) 
         auto stage = [&](int buf) {
             if (tid < QT) {
                 const bool none = st_row >= row_hi || st.y == 0.f;   // no query, or one that sees nothing: weight 0
-                s_m[buf][tid] = none ? 0.f : st.x;
-                s_il[buf][tid] = none ? 0.f : 1.0f / st.y;
+                const float il = 1.0f / st.y;
+                const bool lost = !(il < INFINITY);   // a sum that is no number: by way of M, pairs that the query does not see keep theirs
+                s_m[buf][tid] = none ? 0.f : lost ? NAN : st.x;
+                s_il[buf][tid] = none ? 0.f : lost ? 1.f : il;
             }
         };
         int q_at[KS];
@@ -166,6 +168,15 @@ __global__ __launch_bounds__(256, 3) void weights_kernel(const WeightsParams P) 
                         }
                     }
                 }
+                float by = scale, less = m;
+                if (__any(fabsf(m) >= kHugeLogit)) {   // rounded before the maximum is subtracted; below, there is nothing left to do
+                    by = 1.f;
+                    less = 0.f;
+#pragma unroll
+                    for (int j = 0; j < KG; ++j)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) c[j][e] = attn_logit(c[j][e], scale) - m;
+                }
                 if (!whole) {
                     const int row = base + qt * 16 + n16, p = row < row_hi ? first + token_of(row) : -1;
                     const int from = W.window == 0x7fffffff ? -1 : p - W.window;
@@ -175,17 +186,10 @@ __global__ __launch_bounds__(256, 3) void weights_kernel(const WeightsParams P) 
                         for (int e = 0; e < 4; ++e) {
                             const int key = kw + j * 16 + quad * 4 + e;
                             const bool seen = (key <= p) & ((key > from) | (key < W.sink));
-                            c[j][e] = seen ? c[j][e] : -INFINITY;
+                            c[j][e] = seen ? fmaf(c[j][e], by, -less) : -INFINITY;
                         }
-                }
-                float by = scale, less = m;
-                if (__any(fabsf(m) >= kHugeLogit)) {   // rounded before the maximum is subtracted; below, there is nothing left to do
                     by = 1.f;
                     less = 0.f;
-#pragma unroll
-                    for (int j = 0; j < KG; ++j)
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) c[j][e] = attn_logit(c[j][e], scale) - m;
                 }
 #pragma unroll
                 for (int j = 0; j < KG; ++j)

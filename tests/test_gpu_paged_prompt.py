@@ -257,3 +257,24 @@ def test_scale_that_is_no_number():
     c.run(s, weights=False)
     torch.cuda.synchronize()
     assert torch.isnan(s["out"]).all()
+
+
+@pytest.mark.parametrize("dtype, D", TYPES)
+@pytest.mark.parametrize("long", [True, False])
+@pytest.mark.parametrize("bad", [float("nan"), float("inf")])
+def test_weights_of_queries_without_numbers(dtype, D, long, bad):
+    """A query that is not finite gives the pairs that it sees no number, and all others theirs."""
+    make = _case if long else Case
+    c = make(dtype, D, 4, 1, 16, [(90, 40), (200, 150), (33, 1)], 20, 2, seed=54)
+    c.q[13, 2, 5] = bad
+    c.q[60, 0] = bad
+    c.k_new[100, 0, 3] = bad     # a key, seen by the queries behind it that reach it
+    s = c.dev()
+    c.run(s)
+    torch.cuda.synchronize()
+    ref, tol = c.reference()
+    assert np.isnan(ref["acc"]).any() and np.isfinite(ref["acc"][:, :, :300]).sum() > 100
+    got = s["acc"].double().cpu().numpy()
+    assert (np.isnan(got) == np.isnan(ref["acc"])).all()
+    ok = np.isfinite(ref["acc"])
+    assert (np.abs(got - ref["acc"])[ok] <= np.where(np.isfinite(tol["acc"]), tol["acc"], 1e-5)[ok]).all()
