@@ -141,23 +141,37 @@ __device__ __forceinline__ void merge_tile(const AttnPagedParams& P, int item, i
     }
 }
 
-// Rows of a budgeted cache: the last workgroup of a row merges its outputs and sets its length, the others add its pairs' weights, a pair per thread,
-// whose logits are on their way while the splits' maxima and sums are put together.
+// Rows of a budgeted cache: the last workgroup of a row merges its outputs - threads beyond a row's channels take a share of its splits - and sets its
+// length, the others add its pairs' weights, a pair per thread, whose logits are on their way while the splits' maxima and sums are put together, 32 lanes
+// a head.
 template <typename T, int D, int KT>
 __global__ __launch_bounds__(256) void merge_rows_kernel(const AttnPagedParams P) {
     const int tid = threadIdx.x, slot = blockIdx.x, g = P.view.g;
-    __shared__ float2 s_ml[kMostSplits][8];
     __shared__ float s_M[8], s_inv[8];
     const int n = load_uniform(&P.info[slot].x, 0), fresh = load_uniform(&P.info[slot].y, 0);
     const int splits = splits_of(key_tiles(P.view, n - 1, n - 1, KT).total, P.splits, P.split_shift);
     const size_t rec = (size_t)slot * P.splits * 16;
     if (blockIdx.y == gridDim.y - 1) {
+        __shared__ Merged<D> s_part[256];
         if (tid == 0 && fresh >= 0) P.len[slot] = n;
-        if (splits > 1 && tid < g * (D / 4)) {
-            const int r = tid / (D / 4), d = tid % (D / 4) * 4;
-            const Merged<D> o = merge_records<D>(P, rec + r, 16, splits, d);
-            store_row<T, D>(P, (size_t)slot * g + r, d, o.a, o.M, o.L);
+        if (splits == 1) return;
+        const int units = g * (D / 4), shares = 256 / units, share = tid / units, unit = tid - share * units;
+        const int per = (splits + shares - 1) / shares, s0 = min(share * per, splits), count = min(per, splits - s0);
+        const int r = unit / (D / 4), d = unit % (D / 4) * 4;
+        Merged<D> o = {-INFINITY, 0.f, {0.f, 0.f, 0.f, 0.f}};
+        if (share < shares && count > 0) o = merge_records<D>(P, rec + (size_t)s0 * 16 + r, 16, count, d);
+        if (share > 0) s_part[tid] = o;
+        __syncthreads();
+        if (share > 0) return;
+        for (int i = 1; i < shares; ++i) {
+            const Merged<D> x = s_part[tid + i * units];
+            const float m = fmaxf(o.M, x.M), ref = ref_of(m), fo = __builtin_amdgcn_exp2f(o.M - ref), fx = __builtin_amdgcn_exp2f(x.M - ref);
+            o.M = m;
+            o.L = o.L * fo + x.L * fx;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) o.a[k] = o.a[k] * fo + x.a[k] * fx;
         }
+        store_row<T, D>(P, (size_t)slot * g + r, d, o.a, o.M, o.L);
         return;
     }
     if (splits == 1) return;   // all done
@@ -172,15 +186,27 @@ __global__ __launch_bounds__(256) void merge_rows_kernel(const AttnPagedParams P
         for (int k = 0; k < 8; ++k) x[k] = lg[(size_t)min(k, g - 1) * P.logit_stride + kc];
     };
     fetch();
-    for (int i = tid; i < splits * 8; i += 256) s_ml[i / 8][i % 8] = P.rec_ml[rec + i / 8 * 16 + i % 8];
-    __syncthreads();
-    if (tid < g) {
+    {
+        const int head = tid / 32, s = tid % 32;
+        float2 ml[kMostSplits / 32];
         float M = -INFINITY, L = 0.f;
-        for (int s = 0; s < splits; ++s) M = fmaxf(M, s_ml[s][tid].x);
+#pragma unroll
+        for (int u = 0; u < kMostSplits / 32; ++u) {
+            ml[u] = P.rec_ml[rec + (size_t)min(s + u * 32, splits - 1) * 16 + head];
+            M = fmaxf(M, ml[u].x);
+        }
+#pragma unroll
+        for (int off = 16; off > 0; off >>= 1) M = fmaxf(M, __shfl_xor(M, off));
         M = ref_of(M);
-        for (int s = 0; s < splits; ++s) L = fmaf(s_ml[s][tid].y, __builtin_amdgcn_exp2f(s_ml[s][tid].x - M), L);
-        s_M[tid] = M;
-        s_inv[tid] = 1.0f / L;
+#pragma unroll
+        for (int u = 0; u < kMostSplits / 32; ++u)
+            if (s + u * 32 < splits) L = fmaf(ml[u].y, __builtin_amdgcn_exp2f(ml[u].x - M), L);
+#pragma unroll
+        for (int off = 16; off > 0; off >>= 1) L += __shfl_xor(L, off);
+        if (s == 0 && head < g) {
+            s_M[head] = M;
+            s_inv[head] = 1.0f / L;
+        }
     }
     __syncthreads();
     while (key < n) {

@@ -90,6 +90,8 @@ struct RowsPlan {
 //                         31 and 27; 256 of 600 16.4 and 21; D = 64  8 of 300 6.8 and 8.0, 32 of 500 7.4 and 7.3, 128 of 1000 11.4 and 11.4, of 2112 21 and 18
 //   fp32 D = 64           2 of 144 6.4 and 7.5, 8 of 300 8.2 and 7.9, 128 of 300 8.7 and 9.2, of 1000 20 and 17.5;  D = 128  2 of 144 9.0 and 9.2, 8 of 300
 //                         12.8 and 9.8, 128 of 300 14.1 and 14.3, of 1000 33 and 27
+// Between 128 rows and 256: 152 of 2000 (bf16 D = 128 / 64, fp32 64 / 128) eight wavefronts 32, 21.5, 37, 75, in three splits 30, 20.3, 31, 63; 200 of 2000 37,
+// 23.5, 38, 85 and 40, 26, 42, 88; fp32 D = 64 152 of 1000 20.1 and 20.0.
 // Splits: 8 rows of 4000 pairs, bf16, 8: 11.2, 16: 10.0, 32: 11.6; 32 of 2000 4: 13.4, 8: 11.8, 16: 14.1.  From 512 rows on, and fp32 with D = 128, four
 // wavefronts a row: 512 rows of 1000 44.0, eight 44.4 (fp32 88 and 92).
 static RowsPlan rows_plan(const fk_cache_desc* d, int max_len) {
@@ -101,10 +103,11 @@ static RowsPlan rows_plan(const fk_cache_desc* d, int max_len) {
         if (rows >= 512 || (!bf16 && d->head_dim == 128)) p.waves = 4;
         return p;
     }
-    if (max_len <= alone) return p;
+    if (max_len <= alone || (rows > 128 && (rows > 160 || max_len <= 1024))) return p;
     p.waves = 4;
     p.splits = max_len / ((bf16 ? 32 : 16) << p.shift);
-    if (p.splits > 256 / rows) p.splits = 256 / rows;
+    const int most = rows > 128 ? 3 : 256 / rows;
+    if (p.splits > most) p.splits = most;
     if (p.splits > kMostSplits) p.splits = kMostSplits;
     if (p.splits < 1) p.splits = 1;
     return p;
