@@ -58,7 +58,7 @@ struct AttnPagedParams {
     int batch_of_pos;          // KV heads: row r belongs to sequence r / batch_of_pos
     float* acc;                // [rows][cap]
     float* logit;              // [rows][g][logit_stride] scratch
-    bool logits_lds;           // unsplit rows keep them in LDS
+    int logits_lds;            // unsplit rows of up to so many pairs (whole tiles) keep them in LDS
     int logit_stride;          // cap, rounded up to whole 16-byte groups
     int2* info;                // [rows] (pairs, the new pair's slot or -1): for the second launch
 };

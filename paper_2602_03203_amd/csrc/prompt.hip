@@ -90,7 +90,7 @@ size_t prompt_workspace(const fk_paged_desc* d, const TileGrid& G, int n_tokens,
 
 template <typename T, int D, bool NT_LOADS> static fk_status mixed_launch(const MixedParams& P, hipStream_t st) {
     auto kern = mixed_kernel<T, D, NT_LOADS>;
-    constexpr size_t lds = std::max(PromptCfg<T, D>::LDS_BYTES, ThinCfg<T, D>::lds(false, 4, false));
+    constexpr size_t lds = std::max(PromptCfg<T, D>::LDS_BYTES, ThinCfg<T, D>::lds(false, 4, 0));
     static bool lds_ok[kMaxDevices] = {};
     if (!allow_dynamic_lds((const void*)kern, lds, lds_ok)) return FK_ERR_LAUNCH;
     const int thin = P.thin.grid.places * P.thin.view.n_kv;

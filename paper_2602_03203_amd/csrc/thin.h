@@ -26,10 +26,10 @@ template <typename T, int D> struct ThinCfg {
     static constexpr int ET = D / 16;                    // channel tiles of the output
     static constexpr int PART = D + 4;                   // float stride of a row of a partial output in LDS
     // dynamic LDS: partial outputs [WAVES][R][PART] (R rows: 16, for rows of a cache 8, the heads of a group) | maxima, sums, merge weights
-    // [WAVES][16] each | merged maxima and sums [16] each | rows of a cache: logits [8][LGN]
-    static constexpr int LGN = 1024;
-    static constexpr size_t lds(bool rows, int waves, bool logits) {
-        return sizeof(float) * ((size_t)waves * (rows ? 8 : 16) * PART + 3 * waves * 16 + 32 + (logits ? 8 * LGN : 0));
+    // [WAVES][16] each | merged maxima and sums [16] each | rows of a cache: logits [g][pairs]
+    static constexpr int LOGITS = 9344;   // so many logits of a row fit LDS beside another workgroup's (200 rows of 2000, g 4: 34 us, through the workspace 37)
+    static constexpr size_t lds(bool rows, int waves, int logits) {
+        return sizeof(float) * ((size_t)waves * (rows ? 8 : 16) * PART + 3 * waves * 16 + 32 + logits);
     }
 };
 
@@ -55,7 +55,6 @@ __device__ __forceinline__ void thin_tile(const AttnPagedParams& P, int item, in
     float (*s_o)[R][PART] = reinterpret_cast<float (*)[R][PART]>(smem_thin);
     float (*s_m)[16] = reinterpret_cast<float (*)[16]>(smem_thin + WAVES * R * PART), (*s_l)[16] = s_m + WAVES, (*s_w)[16] = s_l + WAVES;
     float *s_M = s_w[WAVES], *s_L = s_M + 16, *s_lg = s_L + 16;
-    constexpr int LGN = ROWS ? C::LGN : 0;   // rows of up to so many pairs keep their logits in LDS
     __shared__ int s_bad;   // a value that not every row of a run sees is infinite or NaN
 
     TileOf t;
@@ -82,7 +81,7 @@ __device__ __forceinline__ void thin_tile(const AttnPagedParams& P, int item, in
         // this lane's row
         const int my_row = r0 + min(n16, rows - 1), my_token = token_of(my_row), my_head = my_row - my_token * g;
         const size_t q_row = ((size_t)(t.begin + my_token) * n_kv + h) * g + my_head;
-        const bool lg_local = LGN > 0 && P.logits_lds && t.n <= LGN;
+        const bool lg_local = ROWS && t.n <= P.logits_lds;
         const float acc_first = ROWS && splits == 1 && tid < t.n ? P.acc[(size_t)slot * P.cap + tid] : 0.f;   // (on its way over the whole loop)
         T128 q[KS];
 #pragma unroll
@@ -240,7 +239,7 @@ __device__ __forceinline__ void thin_tile(const AttnPagedParams& P, int item, in
                     }
                 };
                 if (n16 < g) {
-                    if (lg_local) keep(s_lg + n16 * LGN + base + quad * (NT * 4));
+                    if (lg_local) keep(s_lg + n16 * P.logits_lds + base + quad * (NT * 4));
                     else keep(P.logit + ((size_t)slot * g + n16) * P.logit_stride + base + quad * (NT * 4));
                 }
             }
@@ -398,7 +397,7 @@ __device__ __forceinline__ void thin_tile(const AttnPagedParams& P, int item, in
                     acc[key] = (key == fresh ? 0.f : key == tid ? acc_first : acc[key]) + w;
                 }
             };
-            if (lg_local) add(s_lg, LGN);
+            if (lg_local) add(s_lg, P.logits_lds);
             else add(P.logit + (size_t)slot * g * P.logit_stride, P.logit_stride);
             if (tid == 0 && fresh >= 0 && P.splits == 1) P.len[slot] = t.n;
             return;

@@ -46,8 +46,8 @@ size_t thin_paged_workspace(const fk_paged_desc* d, const TileGrid& G, int max_l
 template <typename T, int D, bool ROWS, int WAVES, bool NT_LOADS>
 static fk_status thin_start(const AttnPagedParams& P, dim3 grid, hipStream_t st) {
     auto kern = thin_kernel<T, D, ROWS, WAVES, NT_LOADS>;
-    constexpr size_t most = ThinCfg<T, D>::lds(ROWS, WAVES, ROWS);
-    const size_t lds = ThinCfg<T, D>::lds(ROWS, WAVES, P.logits_lds);
+    constexpr size_t most = ThinCfg<T, D>::lds(ROWS, WAVES, ROWS ? ThinCfg<T, D>::LOGITS : 0);
+    const size_t lds = ThinCfg<T, D>::lds(ROWS, WAVES, P.logits_lds * P.view.g);
     static bool lds_ok[kMaxDevices] = {};
     if (most > 48 * 1024 && !allow_dynamic_lds((const void*)kern, most, lds_ok)) return FK_ERR_LAUNCH;
     hipLaunchKernelGGL(kern, grid, dim3(WAVES * kWave), lds, st, P);
@@ -87,13 +87,13 @@ struct RowsPlan {
 // Short rows, and as many rows as CUs, take a workgroup of eight wavefronts each, which adds the weights itself; others are split over 256 workgroups of
 // four, each with a tile for every wavefront or more, and the second launch, 3 us, adds them.  us a step, a row to a workgroup and split:
 //   bf16 D = 128, g = 4   8 rows of 300 8.0 and 8.9, of 1000 14.6 and 8.3; 32 of 500 9.9 and 8.3; 128 of 300 8.2 and 9.3, of 1000 16.9 and 16.8, of 2112
-//                         31 and 27; 256 of 600 16.4 and 21; D = 64  8 of 300 6.8 and 8.0, 32 of 500 7.4 and 7.3, 128 of 1000 11.4 and 11.4, of 2112 21 and 18
-//   fp32 D = 64           2 of 144 6.4 and 7.5, 8 of 300 8.2 and 7.9, 128 of 300 8.7 and 9.2, of 1000 20 and 17.5;  D = 128  2 of 144 9.0 and 9.2, 8 of 300
-//                         12.8 and 9.8, 128 of 300 14.1 and 14.3, of 1000 33 and 27
-// Between 128 rows and 256: 152 of 2000 (bf16 D = 128 / 64, fp32 64 / 128) eight wavefronts 32, 21.5, 37, 75, in three splits 30, 20.3, 31, 63; 200 of 2000 37,
-// 23.5, 38, 85 and 40, 26, 42, 88; fp32 D = 64 152 of 1000 20.1 and 20.0.
+//                         28 and 28; 256 of 600 16.4 and 21; D = 64  8 of 300 6.8 and 8.0, 32 of 500 7.4 and 7.3, 128 of 1000 11.4 and 11.4, of 2112 20 and 18
+//   fp32 D = 64           2 of 144 6.4 and 7.5, 8 of 300 8.2 and 7.9, 128 of 300 8.7 and 9.2, of 1000 20 and 18;  D = 128  2 of 144 9.0 and 9.2, 8 of 300
+//                         12.8 and 9.8, 128 of 300 14.1 and 14.3, of 1000 34 and 27
+// Between 128 rows and 256, us of eight wavefronts and of three splits: 152 of 2112 bf16 D = 128 29.6 and 30.7, D = 64 19.9 and 19.9, fp32 D = 64 36 and 31, 128 70
+// and 70; of 1000 fp32 D = 64 20.2 and 20.0, 128 34 and 31; 200 of 2112 bf16 36 and 41, 22 and 26, fp32 37 and 44, 82 and 92.
 // Splits: 8 rows of 4000 pairs, bf16, 8: 11.2, 16: 10.0, 32: 11.6; 32 of 2000 4: 13.4, 8: 11.8, 16: 14.1.  From 512 rows on, and fp32 with D = 128, four
-// wavefronts a row: 512 rows of 1000 44.0, eight 44.4 (fp32 88 and 92).
+// wavefronts a row: 512 rows of 1000 43.5, eight 44.4 (fp32 87 and 92).
 static RowsPlan rows_plan(const fk_cache_desc* d, int max_len) {
     const int rows = d->batch * d->n_kv_heads;
     const bool bf16 = d->dtype == FK_BF16;
@@ -103,7 +103,7 @@ static RowsPlan rows_plan(const fk_cache_desc* d, int max_len) {
         if (rows >= 512 || (!bf16 && d->head_dim == 128)) p.waves = 4;
         return p;
     }
-    if (max_len <= alone || (rows > 128 && (rows > 160 || max_len <= 1024))) return p;
+    if (max_len <= alone || (rows > 128 && (bf16 || rows > 160 || max_len <= 1024))) return p;
     p.waves = 4;
     p.splits = max_len / ((bf16 ? 32 : 16) << p.shift);
     const int most = rows > 128 ? 3 : 256 / rows;
@@ -139,7 +139,8 @@ fk_status thin_rows(const fk_cache_desc* d, AttnPagedParams P, int max_len, void
     const RowsPlan p = rows_plan(d, max_len);
     P.splits = p.splits;
     P.split_shift = p.shift;
-    P.logits_lds = p.splits == 1 && max_len <= ThinCfg<float, 64>::LGN;
+    const int whole = (max_len + 31) / 32 * 32;
+    P.logits_lds = p.splits == 1 && (long long)whole * P.view.g <= ThinCfg<float, 64>::LOGITS ? whole : 0;
     char* at = static_cast<char*>(ws);
     P.info = reinterpret_cast<int2*>(at);
     at += up256(rows * sizeof(int2));

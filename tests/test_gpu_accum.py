@@ -98,6 +98,24 @@ def test_longer_rows(dtype, D, g, hkv, lens):
     c.check(s)
 
 
+@pytest.mark.parametrize("dtype, D, g, n", [("bf16", 64, 4, 2334), ("bf16", 64, 4, 2400), ("bf16", 128, 8, 1150), ("bf16", 64, 7, 1330), ("f32", 64, 4, 1100), ("f32", 128, 5, 1860)])
+def test_many_rows_around_what_lds_holds(dtype, D, g, n):
+    """As many rows as take a workgroup each, with logits that do and do not fit LDS, and that grow beyond it from one step to the next."""
+    c = Rows(dtype, D, g, 8, [n, n - 1, 1, 33, n, 1025, 500] * 3, n + 3, 3, seed=11)
+    s = c.dev()
+    c.run(s)
+    c.check(s)
+
+
+@pytest.mark.parametrize("g", [1, 4])
+def test_many_splits(g):
+    """One row over more splits than a wavefront has half lanes."""
+    c = Rows("bf16", 64, g, 1, [9000], 9010, 2, seed=12)
+    s = c.dev()
+    c.run(s)
+    c.check(s)
+
+
 def test_hint_below_the_row_length():
     for dtype, D in (("bf16", 128), ("f32", 64)):
         c = Rows(dtype, D, 4, 2, [900, 33], 1024, 2, seed=4)
