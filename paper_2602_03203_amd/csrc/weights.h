@@ -10,7 +10,7 @@ struct WeightsParams {
     float* acc;            // [batch][n_kv][max_pages * page_size]
     float* part;           // [splits][batch * n_kv][part_len], with more than one split of the queries
     int splits, part_len;
-    int blocks;            // key blocks of a sequence in the launch
+    int keys, blocks;      // keys of a block, blocks of a sequence in the launch
     uint32_t blocks_magic;
 };
 

@@ -64,6 +64,7 @@ __global__ __launch_bounds__(256, 3) void weights_kernel(const WeightsParams P) 
         const int row_lo = t0 * g, row_hi = max(t1, t0) * g;
         const int tiles = (row_hi - row_lo + QT - 1) / QT, per = scalar((tiles + P.splits - 1) / P.splits);
         const int i0 = min(split * per, tiles), i1 = min(i0 + per, tiles);
+        if (tiles == 0 && k1 <= first) continue;   // older keys, outside of all windows: their sums stay as they are
 
         const int kw = k0 + wave * (KG * 16);   // the wavefront's keys
         W128 k[KG][KS];
@@ -72,7 +73,7 @@ __global__ __launch_bounds__(256, 3) void weights_kernel(const WeightsParams P) 
 #pragma unroll
         for (int j = 0; j < KG; ++j) {
             const int key = kw + j * 16;
-            const int page = key < n ? load_uniform(tab, min(key >> W.page_shift, W.max_pages - 1)) : -1;
+            const int page = key < n && i0 < i1 ? load_uniform(tab, min(key >> W.page_shift, W.max_pages - 1)) : -1;
             there[j] = page_ok(W, page);
             const wu32x4_t* run = reinterpret_cast<const wu32x4_t*>(W.K) +
                                   ((((size_t)(there[j] ? page : 0) * W.n_kv + h) << W.page_shift) + (key & ((1 << W.page_shift) - 1)) + n16) * CH;
@@ -229,12 +230,16 @@ __global__ __launch_bounds__(256, 3) void weights_kernel(const WeightsParams P) 
 __global__ __launch_bounds__(256) void weights_sum_kernel(const WeightsParams P) {
     const PagedParams& W = P.view;
     const int row = blockIdx.y, b = row / W.n_kv, key = blockIdx.x * 256 + threadIdx.x;
-    const int begin = chunk_begin(W, b), nq = chunk_end(W, b, begin) - begin, n = pairs_of(W, b);
+    const int begin = chunk_begin(W, b), nq = chunk_end(W, b, begin) - begin, n = pairs_of(W, b), first = n - nq;
     if (nq == 0 || key >= n) return;
+    if (W.window != 0x7fffffff) {   // key blocks that no query sees have no partial sums
+        const int k0 = key / P.keys * P.keys, k1 = min(k0 + P.keys, n);
+        if (k0 >= W.sink && k1 <= first && k1 - 1 + W.window <= first) return;
+    }
     float s = 0.f;
     for (int i = 0; i < P.splits; ++i) s += P.part[((size_t)i * W.batch * W.n_kv + row) * P.part_len + key];
     float* x = P.acc + (size_t)row * ((size_t)W.max_pages << W.page_shift) + key;
-    *x = (key >= n - nq ? 0.f : *x) + s;
+    *x = (key >= first ? 0.f : *x) + s;
 }
 
 // ---- host side ---------------------------------------------------------------------------------------------------
@@ -245,14 +250,16 @@ __global__ __launch_bounds__(256) void weights_sum_kernel(const WeightsParams P)
 // 4096 416, 223, 156, 134, 16: 136;  512 of 32768 180, 180, 197;  128 of 8192 30, 26, 32, with 16 keys a wavefront 24, 27, 33;  2048 of 2048 220, 124,
 // 76, 55, with 16 keys 148, 85, 65;  two of 150 to 300 of to 4000, 2 heads, D 64: 37, 27, 19, 16, with 16 keys 20, 16, 13;  fp32, 4 heads: 1000 of 4000, D 64: 332, 175,
 // 100, 88, 16: 98, with 16 keys 141, 107, 96;  64 of 10000 33, 33, 34, with 16 keys 25, 25, 28.
-// Partial sums are kept up to the table's length, so that a length hint below a sequence's length loses nothing.
+// Partial sums are kept up to the table's length, so that a length hint below a sequence's length loses nothing.  Under a window the pairs that count are
+// those that the chunk sees (4 chunks to 1000 of 12000, 4 heads of g 7, window 4096: 150, by the whole length 186; 4 to 72 of 6000, fp32, window 24: 18 and 25).  The
+// workspace, which knows no window, holds four splits where they are 64 MiB at most.
 struct WeightsPlan {
     bool few;
     int keys, splits;
 };
-template <typename T, int D> static WeightsPlan weights_plan_of(const fk_paged_desc* d, int n_tokens, int max_chunk, int max_len) {
+template <typename T, int D> static WeightsPlan weights_plan_of(const fk_paged_desc* d, int n_tokens, int max_chunk, long long pairs) {
     const long long rows = (long long)d->batch * d->n_kv_heads;
-    auto blocks = [&](int keys) { return rows * ((max_len + keys - 1) / keys); };
+    auto blocks = [&](int keys) { return rows * ((pairs + keys - 1) / keys); };
     const long long queries = (long long)(max_chunk < n_tokens ? max_chunk : n_tokens) * (d->n_q_heads / d->n_kv_heads);
     const long long tiles = (queries + WeightsCfg<T, D, false>::QT - 1) / WeightsCfg<T, D, false>::QT;
     const long long space = (1ll << 26) / (rows * d->max_pages * d->page_size);   // a quarter of a GiB of partial sums
@@ -265,20 +272,27 @@ template <typename T, int D> static WeightsPlan weights_plan_of(const fk_paged_d
     if (blocks(p.keys) * p.splits < 512) p = {true, WeightsCfg<T, D, true>::KEYS, splits(WeightsCfg<T, D, true>::KEYS, 1024, 4)};
     return p;
 }
-static WeightsPlan weights_plan(const fk_paged_desc* d, int n_tokens, int max_chunk, int max_len) {
-    if (d->dtype == FK_F32) return d->head_dim == 64 ? weights_plan_of<float, 64>(d, n_tokens, max_chunk, max_len) : weights_plan_of<float, 128>(d, n_tokens, max_chunk, max_len);
-    return d->head_dim == 64 ? weights_plan_of<bf16_t, 64>(d, n_tokens, max_chunk, max_len) : weights_plan_of<bf16_t, 128>(d, n_tokens, max_chunk, max_len);
+static WeightsPlan weights_plan(const fk_paged_desc* d, int n_tokens, int max_chunk, long long pairs) {
+    if (d->dtype == FK_F32) return d->head_dim == 64 ? weights_plan_of<float, 64>(d, n_tokens, max_chunk, pairs) : weights_plan_of<float, 128>(d, n_tokens, max_chunk, pairs);
+    return d->head_dim == 64 ? weights_plan_of<bf16_t, 64>(d, n_tokens, max_chunk, pairs) : weights_plan_of<bf16_t, 128>(d, n_tokens, max_chunk, pairs);
 }
 
-size_t weights_workspace(const fk_paged_desc* d, int n_tokens, int max_chunk, int max_len) {
+static size_t part_bytes(const fk_paged_desc* d) { return (size_t)d->batch * d->n_kv_heads * d->max_pages * d->page_size * sizeof(float); }
+// splits that the workspace holds
+static int weights_space(const fk_paged_desc* d, int n_tokens, int max_chunk, int max_len) {
     const int s = weights_plan(d, n_tokens, max_chunk, max_len).splits;
-    return s > 1 ? (size_t)s * d->batch * d->n_kv_heads * d->max_pages * d->page_size * sizeof(float) : 0;
+    return s < 4 && 4 * part_bytes(d) <= ((size_t)64 << 20) ? 4 : s;
+}
+size_t weights_workspace(const fk_paged_desc* d, int n_tokens, int max_chunk, int max_len) {
+    const int s = weights_space(d, n_tokens, max_chunk, max_len);
+    return s > 1 ? s * part_bytes(d) : 0;
 }
 
 template <typename T, int D>
 static fk_status weights_run(const fk_paged_desc* d, WeightsParams& P, const WeightsPlan& p, int max_len, hipStream_t st) {
     P.splits = p.splits;
-    P.blocks = (max_len + p.keys - 1) / p.keys;
+    P.keys = p.keys;
+    P.blocks = (int)std::min((max_len + p.keys - 1ll) / p.keys, std::max(1ll, (1ll << 23) / ((long long)d->batch * d->n_kv_heads)));   // (a workgroup goes on behind them)
     P.blocks_magic = magic_of(P.blocks);
     const dim3 grid((unsigned)(d->batch * d->n_kv_heads * (long long)P.blocks), P.splits);
     if (p.few) hipLaunchKernelGGL((weights_kernel<T, D, true>), grid, dim3(256), (2 * WeightsCfg<T, D, true>::TILE_BYTES), st, P);
@@ -288,7 +302,9 @@ static fk_status weights_run(const fk_paged_desc* d, WeightsParams& P, const Wei
 }
 
 fk_status weights_launch(const fk_paged_desc* d, WeightsParams P, int max_chunk, int max_len, void* ws, hipStream_t st) {
-    const WeightsPlan p = weights_plan(d, P.view.n_tokens, max_chunk, max_len);
+    const long long seen = (long long)P.view.window + P.view.sink + max_chunk;
+    WeightsPlan p = weights_plan(d, P.view.n_tokens, max_chunk, std::min<long long>(max_len, seen));
+    p.splits = std::min(p.splits, weights_space(d, P.view.n_tokens, max_chunk, max_len));
     P.part = static_cast<float*>(ws);
     P.part_len = d->max_pages * d->page_size;
     if (d->dtype == FK_F32) return d->head_dim == 64 ? weights_run<float, 64>(d, P, p, max_len, st) : weights_run<float, 128>(d, P, p, max_len, st);
