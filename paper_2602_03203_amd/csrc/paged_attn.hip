@@ -33,9 +33,11 @@ static PagedParams view_params(const fk_paged_desc* desc, const void* q, const v
 // tiles of 128.  A call that may hold both kinds is one launch of both kernels' tiles.  Calls whose 16-row tiles meet few
 // pairs altogether are the first one's alone, however long their chunks: it spreads over more workgroups and its tiles take less time to
 // set up.  Measured on either side (one kernel / the other): 4 chunks of 32..64 tokens, g 7, D 128, 512 pairs (229 thousand): 16 / 23 us; 1 chunk of
-// 80 tokens, g 4, D 64, 4096 pairs (327 thousand): 15 / 22; 4 chunks of 12..24, g 7, D 128, 4096 pairs (516 thousand): 42 / 32.
+// 80 tokens, g 4, D 64, 4096 pairs (327 thousand): 15 / 22; 4 chunks of 12..24, g 7, D 128, 4096 pairs (516 thousand): 42 / 32.  In fp32, where
+// a tile's products take longer than its loads: 1 chunk of 896, g 8, D 64, 896 pairs (401 thousand) 20 / 49; 2 of 30..60, 8 heads of g 4, D 128, 4096 pairs
+// (737 thousand) 80 / 95; 1 of 64 of 8192 (1.05 million) 113 / 105.
 static constexpr int kThinRows = 16;
-static constexpr long long kThinWork = 3 << 17;
+static constexpr long long kThinWork = 3 << 17, kThinWorkF32 = 1 << 20;
 
 struct AttnPlanPaged {
     bool thin, prompt;
@@ -47,7 +49,7 @@ static AttnPlanPaged plan_paged(const fk_paged_desc* d, int32_t n_tokens, int32_
     // what is left for the shortest chunk where all others have the bound's length (should they be longer, prompt tiles take short chunks as well)
     const long long shortest = n_tokens - (long long)(d->batch - 1) * max_chunk;
     const long long work = ((long long)n_tokens * g + 15) / 16 * d->n_kv_heads * max_len;
-    p.prompt = (long long)max_chunk * g > kThinRows && work > kThinWork;
+    p.prompt = (long long)max_chunk * g > kThinRows && work > (d->dtype == FK_F32 ? kThinWorkF32 : kThinWork);
     p.thin = !p.prompt || shortest * g <= kThinRows;
     if (p.thin) {   // (also all chunks there are, should they be longer than max_chunk says)
         p.thin_grid = tile_grid(d, n_tokens, p.prompt ? (kThinRows + g - 1) / g : max_chunk, 16);

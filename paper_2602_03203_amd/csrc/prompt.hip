@@ -58,7 +58,7 @@ __global__ __launch_bounds__(256) void mixed_merge_kernel(const MixedParams P) {
 // microseconds, with 2.1 for 64 pairs of bf16 and D = 128, 6 for the launch and 4 TB/s for the records; in fp32 one workgroup has the matrix units of its CU
 // busy, 9.4 for 64 pairs, half of one more has a CU to share, and all items are split alike.  Whole / 2 / 3 / 4 / 8 splits measured for 8 heads of g 4, D 128: 512 tokens of 8192 pairs: 216 / 123 / 104 / 93 / 101; 1024 of
 // 8192: 222 / 160 / 175 / 166 / 186; 4 chunks to 300 of 2048: 70 / 80 / 72 / 73 / 70.  A split has 512 pairs and more, or 256 where no
-// sequence is longer than 2048: 2 chunks to 908 of 908, 2 heads 35 whole, 29 in two; 4 to 100 of 1000 37 and 33; but a batch of 300 to 4096 pairs (mixed_kernel)
+// sequence is longer than 2048: 2 chunks to 908 of 908, 2 heads 35 whole, 29 in two, fp32 896 of 896, one head of g 8, D 64 80 and 49; 4 to 100 of 1000 37 and 33; but a batch of 300 to 4096 pairs (mixed_kernel)
 // 35 by splits of 512, 37 of 256.  The rest of the last turn alone split, against nothing and everything
 // split: 2400 tokens of 16384 606, 822 and 662; two chunks to 1200 of 8192 298, 425 and 340.  How many chunks there are that are not single tokens the host
 // does not know: as many as would have the longest one's length.
@@ -74,8 +74,8 @@ static PromptPlan prompt_plan(const fk_paged_desc* d, const TileGrid& G, int n_t
     whole -= whole % d->n_kv_heads;
     whole = std::min(whole, places);
     const long long left = items - whole;
-    const int fewest = bf16 && pairs <= 2048 ? 256 : 512;   // pairs of a split
-    PromptPlan p = {(int)whole, 1, bf16 ? (fewest == 256 ? 2 : 3) : 4};
+    const int fewest = pairs <= 2048 ? 256 : 512;   // pairs of a split
+    PromptPlan p = {(int)whole, 1, (fewest == 256 ? 2 : 3) + (bf16 ? 0 : 1)};
     const double one = (double)pairs / 64 * d->head_dim / 128 * (bf16 ? 2.1 : 9.4);
     double least = 0;
     for (int s = 1; s <= 16 && (s == 1 || (pairs / s >= fewest && (places - whole) * s <= 4096 /* a quarter of a GiB of records */)); ++s) {

@@ -17,7 +17,7 @@ TYPES = [("bf16", 128), ("bf16", 64), ("f32", 64), ("f32", 128)]
 
 def _case(dtype, D, g, hkv, page, chunks, *args, **kw):
     tokens = sum(c for _, c in chunks)
-    room = (1 << 19) // (max(1, tokens * g // 16) * hkv) // page + 1
+    room = (1 << 21) // (max(1, tokens * g // 16) * hkv) // page + 1
     return Case(dtype, D, g, hkv, page, chunks, *args, room=room, **kw)
 
 
@@ -49,6 +49,13 @@ def test_beside_single_tokens(dtype, D, page):
 def test_splits(dtype, D, g, chunks):
     """Pairs enough for several splits, of both kinds."""
     _go(_case(dtype, D, g, 1, 64, chunks, seed=40 + g))
+
+
+@pytest.mark.parametrize("dtype, D", TYPES)
+@pytest.mark.parametrize("window", [0, 300])
+def test_splits_of_short_sequences(dtype, D, window):
+    """Work enough for this kernel by the bounds that the sequences have: splits of few pairs."""
+    _go(Case(dtype, D, 4, 8, 64, [(1100, 500), (900, 30), (1, 1), (1000, 7)], window, 2, seed=45))
 
 
 @pytest.mark.parametrize("dtype, D", TYPES)
