@@ -52,7 +52,7 @@ static AttnPlanPaged plan_paged(const fk_paged_desc* d, int32_t n_tokens, int32_
     p.prompt = (long long)max_chunk * g > kThinRows && work > (d->dtype == FK_F32 ? kThinWorkF32 : kThinWork);
     p.thin = !p.prompt || shortest * g <= kThinRows;
     if (p.thin) {   // (also all chunks there are, should they be longer than max_chunk says)
-        p.thin_grid = tile_grid(d, n_tokens, p.prompt ? (kThinRows + g - 1) / g : max_chunk, 16);
+        p.thin_grid = tile_grid(d, n_tokens, p.prompt ? kThinRows / g : max_chunk, 16);
         if (p.prompt) p.thin_grid.most = kThinRows;
     }
     if (p.prompt) {

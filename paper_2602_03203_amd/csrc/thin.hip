@@ -1,6 +1,8 @@
 // fk_paged_attn: its launch for chunks of few query rows, and fk_decode_step_acc
 #include "thin.h"
 
+#include <algorithm>
+
 namespace fk {
 
 template <typename T, int D, bool ROWS, int WAVES, bool NT_LOADS>
@@ -17,17 +19,19 @@ __global__ __launch_bounds__(256) void thin_merge_kernel(const AttnPagedParams P
 //                (D = 64) unsplit 21.8, 2 17.1, 4 16.0, 8 16.9: up to 256 workgroups, up to sixteen splits
 //   128 and more, which fill the memory system by themselves, unsplit where they are short (128 of 2048 24.7, 2 27.1).  Long ones differ in length as a rule,
 //                and only the device knows: splits of 1024 pairs and more even them out (512 of 1024 to 32768 pairs unsplit 947, so 840; 128 of 1024 to
-//                8192 118 and 69) and cost equal ones little (512 of 4096 163 and 170, 128 of 8192 in two 86, so 89)
+//                8192 118 and 69) and cost equal ones little (512 of 4096 163 and 170, 128 of 8192 in two 86, so 89).  Chunks of several tiles beside
+//                single tokens leave places empty: splits of 512 pairs (19 sequences, 3 with 8 to 15 tokens, g 2, 2315 to 3761 pairs: unsplit 69, so 53)
 struct ThinPlan {
     int splits, shift;
 };
 static ThinPlan thin_plan(const fk_paged_desc* d, const TileGrid& G, long long pairs) {
     const long long items = (long long)G.places * d->n_kv_heads;
     const int kt_shift = d->dtype == FK_BF16 ? 5 : 4;
-    ThinPlan p = {1, items < 128 ? 8 - kt_shift : 10 - kt_shift};
+    const bool uneven = G.spread || G.per_seq > 1;
+    ThinPlan p = {1, (items < 128 ? 8 : pairs >= 6144 ? 10 : 9) - kt_shift};
     long long s = 1;
     if (items < 128) s = 256 / items;
-    else if (pairs >= 6144) s = 16;
+    else if (pairs >= 6144 || uneven) s = 16;
     if (s > 16) s = 16;
     if (s > (1 << 16) / items) s = (1 << 16) / items;   // (half a GiB of records; so many items even out by themselves)
     if (s > pairs >> (p.shift + kt_shift)) s = pairs >> (p.shift + kt_shift);
@@ -40,7 +44,7 @@ static long long most_pairs(const PagedParams& P, int max_len) {
 }
 
 size_t thin_paged_workspace(const fk_paged_desc* d, const TileGrid& G, int max_len) {
-    return record_bytes((long long)G.places * d->n_kv_heads, thin_plan(d, G, max_len).splits, 16, d->head_dim);   // (a window sees no more)
+    return record_bytes((long long)G.places * d->n_kv_heads, thin_plan(d, G, max_len).splits, 16, d->head_dim);
 }
 
 template <typename T, int D, bool ROWS, int WAVES, bool NT_LOADS>
@@ -66,7 +70,7 @@ static fk_status thin_paged_launch(const fk_paged_desc* d, AttnPagedParams& P, b
 void thin_prepare(const fk_paged_desc* d, AttnPagedParams& P, int max_len, void* ws, bool& cold) {
     const long long items = (long long)P.grid.places * d->n_kv_heads;
     const ThinPlan p = thin_plan(d, P.grid, most_pairs(P.view, max_len));
-    P.splits = p.splits;
+    P.splits = std::min(p.splits, thin_plan(d, P.grid, max_len).splits);   // (what the workspace is for)
     P.split_shift = p.shift;
     P.rec_ml = reinterpret_cast<float2*>(ws);
     P.rec = reinterpret_cast<float*>(static_cast<char*>(ws) + up256((size_t)items * P.splits * 16 * sizeof(float2)));

@@ -8,7 +8,7 @@
 //
 // Bound by matrix and vector instructions together: per 16 x 16 logits D / 32 products and, per lane, four times an fma, an exponential and an fma.  16
 // products and the vector work that goes with them, registers alone, two wavefronts to a SIMD, take 272 and 214 ns by themselves and 404 together; the
-// kernel is at 1.4 times that (2048 tokens of 16384 pairs, 8 heads of g 4, D 128: 286 us, 910 TFLOP/s).  Three wavefronts to a SIMD do as well as two
+// kernel is at 1.4 times that (2048 tokens of 16384 pairs, 8 heads of g 4, D 128: 278 us, 940 TFLOP/s).  Three wavefronts to a SIMD do as well as two
 // whose next logits are formed beside their exponentials (286 and 290), with half of the code.
 // Few keys and many queries: the queries are split over workgroups too, partial sums meet in a second launch.
 #include "weights.h"
@@ -149,6 +149,8 @@ __global__ __launch_bounds__(256, 3) void weights_kernel(const WeightsParams P) 
         for (int i = i0, buf = 0; i < i1; ++i, buf ^= 1) {
             const int base = row_lo + i * QT, lo = first + scalar(token_of(base)), hi = first + scalar(token_of(min(base + QT, row_hi) - 1));   // positions
             const bool whole = kw + KG * 16 <= lo + 1 && base + QT <= row_hi && (W.window == 0x7fffffff || kw > hi - W.window || kw + KG * 16 <= W.sink);
+            const bool none = kw > hi || (W.window != 0x7fffffff && kw >= W.sink && kw + KG * 16 - 1 <= lo - W.window);   // of these keys any of these rows
+            if (!none) {
 #pragma unroll
             for (int qt = 0; qt < NQ; ++qt) {
                 W128 q[KS];
@@ -199,6 +201,7 @@ __global__ __launch_bounds__(256, 3) void weights_kernel(const WeightsParams P) 
 #pragma unroll
                 for (int j = 0; j < KG; ++j) asm volatile("" : "+v"(a[j]));   // here, not behind the tile's last branch
             }
+            }
             stage(buf ^ 1);
             arrived();
             __syncthreads();
@@ -236,8 +239,16 @@ __global__ __launch_bounds__(256) void weights_sum_kernel(const WeightsParams P)
         const int k0 = key / P.keys * P.keys, k1 = min(k0 + P.keys, n);
         if (k0 >= W.sink && k1 <= first && k1 - 1 + W.window <= first) return;
     }
+    const size_t stride = (size_t)W.batch * W.n_kv * P.part_len;
+    const float* part = P.part + (size_t)row * P.part_len + key;
     float s = 0.f;
-    for (int i = 0; i < P.splits; ++i) s += P.part[((size_t)i * W.batch * W.n_kv + row) * P.part_len + key];
+    for (int i = 0; i < P.splits; i += 8) {   // (eight loads in flight)
+        float y[8];
+#pragma unroll
+        for (int u = 0; u < 8; ++u) y[u] = part[min(i + u, P.splits - 1) * stride];
+#pragma unroll
+        for (int u = 0; u < 8; ++u) s += i + u < P.splits ? y[u] : 0.f;
+    }
     float* x = P.acc + (size_t)row * ((size_t)W.max_pages << W.page_shift) + key;
     *x = (key >= first ? 0.f : *x) + s;
 }

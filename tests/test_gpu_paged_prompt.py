@@ -285,3 +285,22 @@ def test_weights_of_queries_without_numbers(dtype, D, long, bad):
     assert (np.isnan(got) == np.isnan(ref["acc"])).all()
     ok = np.isfinite(ref["acc"])
     assert (np.abs(got - ref["acc"])[ok] <= np.where(np.isfinite(tol["acc"]), tol["acc"], 1e-5)[ok]).all()
+
+
+@pytest.mark.parametrize("dtype, D, page", [("bf16", 64, 16), ("f32", 64, 64)])
+def test_workspace_under_a_window(dtype, D, page):
+    """Windows change how work is split, the workspace does not know them: nothing behind it is written."""
+    for chunks, window in (([(700 + 31 * b, 1 + b % 5) for b in range(70)], 6000), ([(900, 4)] * 3, 500), ([(1300, 70), (1100, 1)], 700)):
+        c = Case(dtype, D, 8, 2, page, chunks, window, 2, seed=56, room=6400 // page)
+        s = c.dev()
+        behind = 1 << 16
+        for k in ("ws", "wws"):
+            n = s[k].numel()
+            s[k + "_all"] = torch.full((n + behind,), 77, dtype=torch.uint8, device="cuda")
+            s[k] = s[k + "_all"][:n]
+        c.run(s)
+        torch.cuda.synchronize()
+        for k in ("ws", "wws"):
+            assert (s[k + "_all"][s[k].numel():] == 77).all(), (k, len(chunks))
+        ref, tol = c.reference()
+        c.check(s, ref, tol)
