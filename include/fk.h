@@ -435,8 +435,8 @@ size_t fk_decode_step_acc_workspace(const fk_cache_desc *desc);
 
 /*
  * fk_decode_step that also adds the step's attention weights (softmax over the retained set including the new pair, fp32 weights from the
- * unrounded exponentials), summed over the group's query heads, to acc; the slot of the new pair starts from zero.  Other arguments and
- * results as fk_decode_step.  Calls sharing a workspace must not overlap in time.
+ * unrounded exponentials and their sum), summed over the group's query heads, to acc; the slot of the new pair starts from zero.  Other arguments
+ * and results as fk_decode_step (the outputs' own weights and normaliser too: fk_decode_attn).  Calls sharing a workspace must not overlap in time.
  */
 fk_status fk_decode_step_acc(const fk_cache_desc *desc, const void *q, void *K, void *V, int32_t *pos, int32_t *len,
                              const void *k_new, const void *v_new, const int32_t *pos_new, int32_t max_len,

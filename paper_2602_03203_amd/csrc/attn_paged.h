@@ -49,7 +49,7 @@ struct AttnPagedParams {
     int splits;                // of a tile's pairs, at most
     int split_shift;           // key tiles of a split, at least 2^split_shift
     float* rec;                // [item - whole][split][rows of a tile][D], with more than one split
-    float2* rec_ml;            // [item - whole][split][rows of a tile]
+    float2* rec_ml;            // [item - whole][split][rows of a tile]; rows of a cache: eight heads, then the same with the outputs' normaliser
     // rows of a budgeted cache
     int cap;
     int32_t *pos, *len;
@@ -76,7 +76,8 @@ template <int D> struct Merged {
     float M, L, a[4];
 };
 template <int D>
-__device__ __forceinline__ Merged<D> merge_records(const AttnPagedParams& P, size_t rec /* the row in the first split's record */, int tm, int splits, int d) {
+__device__ __forceinline__ Merged<D> merge_records(const AttnPagedParams& P, size_t rec /* the row in the first split's record */, int tm, int splits, int d,
+                                                   int ml_row = 0 /* rows from there to its (M, L) */) {
     Merged<D> o = {-INFINITY, 0.f, {0.f, 0.f, 0.f, 0.f}};
     for (int s0 = 0; s0 < splits; s0 += 8) {
         float2 ml[8];
@@ -84,7 +85,7 @@ __device__ __forceinline__ Merged<D> merge_records(const AttnPagedParams& P, siz
 #pragma unroll
         for (int u = 0; u < 8; ++u) {
             const size_t r = rec + (size_t)min(s0 + u, splits - 1) * tm;
-            ml[u] = P.rec_ml[r];
+            ml[u] = P.rec_ml[r + ml_row];
             v[u] = *reinterpret_cast<const float4*>(P.rec + r * D + d);
         }
         float m = o.M;
@@ -159,7 +160,7 @@ __global__ __launch_bounds__(256) void merge_rows_kernel(const AttnPagedParams P
         const int per = (splits + shares - 1) / shares, s0 = min(share * per, splits), count = min(per, splits - s0);
         const int r = unit / (D / 4), d = unit % (D / 4) * 4;
         Merged<D> o = {-INFINITY, 0.f, {0.f, 0.f, 0.f, 0.f}};
-        if (share < shares && count > 0) o = merge_records<D>(P, rec + (size_t)s0 * 16 + r, 16, count, d);
+        if (share < shares && count > 0) o = merge_records<D>(P, rec + (size_t)s0 * 16 + r, 16, count, d, 8);
         if (share > 0) s_part[tid] = o;
         __syncthreads();
         if (share > 0) return;

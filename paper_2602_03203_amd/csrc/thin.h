@@ -79,8 +79,8 @@ __device__ __forceinline__ void thin_tile(const AttnPagedParams& P, int item, in
         if (split >= splits) continue;
         const int per = splits == 1 ? kt.total : scalar(divide(kt.total + splits - 1, splits)), t_begin = min(split * per, kt.total), t_end = min(t_begin + per, kt.total);
 
-        // this lane's row
-        const int my_row = r0 + min(n16, rows - 1), my_token = token_of(my_row), my_head = my_row - my_token * g;
+        // This lane's row.  ROWS: the heads a second time in the upper eight columns, of which the normaliser of the outputs is kept (below).
+        const int my_row = ROWS ? min(n16 % 8, rows - 1) : r0 + min(n16, rows - 1), my_token = token_of(my_row), my_head = my_row - my_token * g;
         const size_t q_row = ((size_t)(t.begin + my_token) * n_kv + h) * g + my_head;
         const bool lg_local = ROWS && t.n <= P.logits_lds;
         const float acc_first = ROWS && splits == 1 && tid < t.n ? P.acc[(size_t)slot * P.cap + tid] : 0.f;   // (on its way over the whole loop)
@@ -177,11 +177,18 @@ __device__ __forceinline__ void thin_tile(const AttnPagedParams& P, int item, in
         for (int lo = tile_lo, hi = tile_hi;;) {
         if (!ROWS && tid == 0) s_bad = 0;
         if constexpr (!ROWS) __syncthreads();
-        const int pos = t.first + my_token, p = n16 < rows && pos >= lo && pos <= hi ? pos : -1;   // -1: sees nothing
+        const int pos = t.first + my_token, p = ROWS || (n16 < rows && pos >= lo && pos <= hi) ? pos : -1;   // -1: sees nothing
         const int p_from = p < 0 || W.window == 0x7fffffff ? -1 : p - W.window;   // sees keys (p_from, p] and [0, min(sink, p + 1))
         const int p_sink = min(W.sink, p + 1);
         float m_run = -INFINITY, l_run = 0.f;
         tf32x4_t o[ET];
+        // The step's outputs, as those of the step without accumulation, are normalised by the weights as they meet V (bf16, head_dim 128): a row of
+        // ones more in the product (8 rows of 1000 pairs 10.0 us a step, with it 10.1; 128 of 2112 28.7 either way).  The accumulated weights by the
+        // sum of the unrounded ones.
+        constexpr bool ONES = ROWS && BF && D == 128;
+        tf32x4_t o_l = (tf32x4_t){0.f, 0.f, 0.f, 0.f};
+        T128 ones;
+        ones.u = tu32x4_t{0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u};
 #pragma unroll
         for (int e = 0; e < ET; ++e) o[e] = (tf32x4_t){0.f, 0.f, 0.f, 0.f};
 
@@ -263,11 +270,13 @@ __device__ __forceinline__ void thin_tile(const AttnPagedParams& P, int item, in
                 for (int e = 0; e < ET; ++e)
 #pragma unroll
                     for (int k = 0; k < 4; ++k) o[e][k] *= corr;
+                if constexpr (ONES) o_l[0] *= corr;   // (all four are the same sum)
             }
             T128 pr;   // bf16: the probabilities, rounded
             if constexpr (BF) {
 #pragma unroll
                 for (int w = 0; w < 4; ++w) pr.w[w] = pack_bf16(s[2 * w], s[2 * w + 1]);
+                if constexpr (ONES) o_l = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones.v, pr.v, o_l, 0, 0, 0);
             }
             if (!whole) {   // values of weight 0 must not meet the products as infinities or NaN
                 bool bad = false;
@@ -319,7 +328,7 @@ __device__ __forceinline__ void thin_tile(const AttnPagedParams& P, int item, in
         l_run = quad_sum(l_run);
         if (quad == 0) {
             s_m[wave][n16] = m_run;
-            s_l[wave][n16] = l_run;
+            s_l[wave][n16] = ONES && n16 >= 8 ? o_l[0] : l_run;   // ROWS: of the accumulated weights, and from 8 on the normaliser of the outputs
         }
         if (!ROWS || n16 < R)
 #pragma unroll
@@ -367,10 +376,13 @@ __device__ __forceinline__ void thin_tile(const AttnPagedParams& P, int item, in
             }
             if (splits > 1) {
                 *reinterpret_cast<float4*>(P.rec + (rec + r) * D + d) = make_float4(a[0], a[1], a[2], a[3]);
-                if (d == 0) P.rec_ml[rec + r] = make_float2(s_M[r], s_L[r]);
+                if (d == 0) {
+                    P.rec_ml[rec + r] = make_float2(s_M[r], s_L[r]);
+                    if constexpr (ROWS) P.rec_ml[rec + 8 + r] = make_float2(s_M[r], s_L[8 + r]);
+                }
                 continue;
             }
-            store_row<T, D>(P, ((size_t)(t.begin + tok) * n_kv + h) * g + (r0 + r - tok * g), d, a, s_M[r], s_L[r]);
+            store_row<T, D>(P, ((size_t)(t.begin + tok) * n_kv + h) * g + (r0 + r - tok * g), d, a, s_M[r], s_L[ROWS ? 8 + r : r]);
         }
         if constexpr (ROWS) {
             // the new pair joins the cache (its slot is read by nobody in this launch)

@@ -1,0 +1,84 @@
+"""Outputs of the step that accumulates its weights are those of the plain step: head_dim 128 normalised by the weights as they meet V; infinities as there."""
+import numpy as np
+import pytest
+import torch
+
+from paged_util import U
+from test_gpu_accum import Rows
+
+pytestmark = pytest.mark.gpu
+
+INF, NAN = float("inf"), float("nan")
+DT = {"bf16": torch.bfloat16, "f32": torch.float32}
+
+
+def _fk():
+    import paper_2602_03203_amd as fk
+    return fk
+
+
+@pytest.mark.parametrize("g, hkv, lens", [(1, 1, [31, 63]), (4, 2, [320, 95]), (8, 1, [128]), (4, 1, [2100, 1000]), (5, 1, [1600]), (2, 8, [64, 33] * 32)])
+def test_head_dim_128_is_normalised_by_the_rounded_weights(g, hkv, lens):
+    """Weights whose rounding to bf16 is nearly half a step up, all of them: values that are all the same come out as they are, with the sum of the same
+    rounded weights; with the sum of the unrounded ones 0.3 % off, more than the value's last bit."""
+    fk = _fk()
+    c = Rows("bf16", 128, g, hkv, lens, max(lens) + 5, 1, seed=1)
+    value = 255 / 128          # the largest below 2: half a step is 2^-8, 0.2 % of it
+    c.q.zero_()
+    c.q[..., 0] = 1
+    c.K.zero_()
+    c.K[..., 0] = -1
+    c.K[:, :, ::32] = 0        # one of every tile is the largest, so all wavefronts' and splits' maxima are the same
+    c.k.zero_()
+    c.k[..., 0] = -1
+    for b, n in enumerate(lens):
+        if n % 32 == 0:
+            c.k[:, b] = 0
+    c.V.fill_(value)
+    c.v.fill_(value)
+    c.scale = -float(np.log(0.5 * (1 + 1.1 * 2.0 ** -8)))      # the others' weight: 0.5 + 1.1 half steps, rounded to 0.5 + 2
+    s = c.dev()
+    plain = s["out"].clone()
+    K, V, pos, ln = (s[k].clone() for k in ("K", "V", "pos", "len"))
+    c.run(s)
+    fk.fk_decode_step(s["desc"], s["q"][0], K, V, pos, ln, s["k"][0], s["v"][0], s["pos_new"][0], max(lens) + 1, c.scale, plain[0], fk.new_attn_workspace(s["desc"]))
+    torch.cuda.synchronize()
+    assert (plain == value).all()
+    assert (s["out"] == value).all(), s["out"][s["out"] != value].flatten()[:4]
+    # the accumulated weights are those of the unrounded exponentials
+    w = 0.5 * (1 + 1.1 * 2.0 ** -8)
+    for b, n in enumerate(lens):
+        x = np.where(np.arange(n + 1) % 32 == 0, 1.0, w)
+        want = c.acc[b, :, :n + 1].double().numpy().copy()
+        want[:, n] = 0
+        want += g * x / x.sum()
+        assert (np.abs(s["acc"][b, :, :n + 1].double().cpu().numpy() - want) <= (2 * n + 40) * U * g * x / x.sum() + 4 * g * U * want).all()
+
+
+@pytest.mark.parametrize("dtype, D", [("bf16", 64), ("bf16", 128), ("f32", 64), ("f32", 128)])
+@pytest.mark.parametrize("n", [90, 160, 1500])
+@pytest.mark.parametrize("g", [1, 4, 7])
+def test_infinite_values(dtype, D, n, g):
+    """A pair of weight p > 0 gives p * inf = inf in its channel, every other channel is what it is without it; of cached and of new pairs."""
+    c = Rows(dtype, D, g, 2, [n, n - 3], n + 20, 8, seed=n + g)
+    c.K[0, 1, 45] = 4.0 * c.q[3, 0, g]       # the largest weight of a row: nothing is left for a remainder
+    cached = [(0, 1, 45, 17, INF), (0, 1, 46, 18, -INF), (0, 1, 47, 19, NAN), (1, 0, 5, 3, INF), (1, 0, 70, 4, -INF), (1, 0, 71, 3, INF)]
+    fresh = [(2, 0, 0, 17, INF), (2, 0, 0, 18, -INF), (3, 0, 0, 19, NAN), (5, 1, 1, 3, -INF)]
+    runs = []
+    for bad in (True, False):
+        for b, h, slot, ch, x in cached:
+            c.V[b, h, slot, ch] = x if bad else 0
+        for t, b, h, ch, x in fresh:
+            c.v[t, b, h, ch] = x if bad else 0
+        s = c.dev()
+        c.run(s)
+        torch.cuda.synchronize()
+        runs.append((s["out"].float().cpu(), s["acc"].cpu()))
+    (o, acc), (r, acc_r) = runs
+    places = [(0, b, h, ch, x) for b, h, _, ch, x in cached] + fresh
+    for t, b, h, ch, x in places:
+        got = o[t:, b, h * g:(h + 1) * g, ch]
+        assert bool(torch.isnan(got).all() if x != x else (got == x).all()), f"row ({b},{h}) channel {ch} from step {t}: {got.flatten()[:4]} for {x}"
+    for t, b, h, ch, _ in places:
+        o[t:, b, h * g:(h + 1) * g, ch] = r[t:, b, h * g:(h + 1) * g, ch]
+    assert torch.equal(o, r) and torch.equal(acc[:, :, :n], acc_r[:, :, :n])
