@@ -1,8 +1,10 @@
-"""Outputs of the step that accumulates its weights are those of the plain step: head_dim 128 normalised by the weights as they meet V; infinities as there."""
+"""Outputs of the step that accumulates its weights are those of the plain step: head_dim 64 with all bits of the weights, head_dim 128 normalised by the weights
+as they meet V; infinities as there."""
 import numpy as np
 import pytest
 import torch
 
+from oracle import paged as op
 from paged_util import U
 from test_gpu_accum import Rows
 
@@ -15,6 +17,33 @@ DT = {"bf16": torch.bfloat16, "f32": torch.float32}
 def _fk():
     import paper_2602_03203_amd as fk
     return fk
+
+
+# rows of one workgroup of eight wavefronts and of four, and of several splits
+@pytest.mark.parametrize("g, hkv, lens", [(1, 2, [0, 1, 15, 31, 32, 63, 200]), (4, 2, [1, 40, 63, 300]), (5, 1, [33, 150]), (8, 2, [20, 129]), (4, 1, [2000, 900]),
+                                          (7, 1, [1500]), (3, 2, [700, 33]), (2, 8, [90, 40, 7, 64] * 16)])
+def test_head_dim_64_keeps_all_bits_of_the_weights(g, hkv, lens):
+    c = Rows("bf16", 64, g, hkv, lens, max(lens) + 5, 2, seed=30 + g)
+    s = c.dev()
+    c.run(s)
+    torch.cuda.synchronize()
+    K, V, n = c.K.double().numpy().copy(), c.V.double().numpy().copy(), list(lens)
+    got = s["out"].double().cpu().numpy()
+    for t in range(c.steps):
+        for b in range(len(n)):
+            K[b, :, n[b]], V[b, :, n[b]] = c.k[t, b].double().numpy(), c.v[t, b].double().numpy()
+            n[b] += 1
+            m = n[b]
+            q = c.q[t, b].double().numpy()[None]
+            out, _, _, W = op.attend(q, K[b, :, :m], V[b, :, :m], np.ones(m, bool), m - 1, 0, 0, c.scale)
+            # D products a logit, exponents off by their own and the reference's error, sums of m weights (in fp32 all of it); then one rounding to bf16,
+            # half a step of the binade that the value lies in
+            mag = np.einsum("hgd,hnd->hgn", np.abs(q[0]).reshape(hkv, g, 64), np.abs(K[b, :, :m])).max(initial=0)
+            rel = 2 * np.log(2.0) * ((64 + 4) * U * mag * c.scale / np.log(2.0) + U) + (2 * m + 8) * U
+            wv = np.einsum("hgn,hnd->hgd", W[0].reshape(hkv, g, m), np.abs(V[b, :, :m])).reshape(hkv * g, 64)
+            near = np.abs(out[0]) + rel * wv + 1e-30
+            bad = np.abs(got[t, b] - out[0]) > rel * wv + 2.0 ** (np.floor(np.log2(near)) - 8)
+            assert not bad.any(), f"step {t} sequence {b}: {bad.sum()} of {bad.size} off by more than fp32 and one rounding"
 
 
 @pytest.mark.parametrize("g, hkv, lens", [(1, 1, [31, 63]), (4, 2, [320, 95]), (8, 1, [128]), (4, 1, [2100, 1000]), (5, 1, [1600]), (2, 8, [64, 33] * 32)])
