@@ -110,10 +110,11 @@ __device__ __forceinline__ Merged<D> merge_records(const AttnPagedParams& P, siz
     return o;
 }
 
-// four channels of a row from the sum of its weighted values and of its weights; 0 where nothing has been seen
-template <typename T, int D>
+// four channels of a row from the sum of its weighted values and of its weights; 0 where nothing has been seen (a row of a budgeted cache has its new
+// pair at least: where all its logits are -inf it is 0 / 0, as in the step without accumulation, and as its weights are)
+template <typename T, int D, bool ROWS>
 __device__ __forceinline__ void store_row(const AttnPagedParams& P, size_t row, int d, const float (&a)[4], float M, float L) {
-    const float inv = L == 0.f ? 0.f : 1.0f / L;
+    const float inv = !ROWS && L == 0.f ? 0.f : 1.0f / L;
     if constexpr (sizeof(T) == 2) {
         const tu32x2_t y = {pack_bf16(a[0] * inv, a[1] * inv), pack_bf16(a[2] * inv, a[3] * inv)};
         *reinterpret_cast<tu32x2_t*>(reinterpret_cast<bf16_t*>(P.out) + row * D + d) = y;
@@ -138,7 +139,7 @@ __device__ __forceinline__ void merge_tile(const AttnPagedParams& P, int item, i
         const int r = x / (D / 4), d = x % (D / 4) * 4;
         const Merged<D> o = merge_records<D>(P, rec + r, TM, splits, d);
         const int tok = divide(r0 + r, g, W.g_magic);
-        store_row<T, D>(P, ((size_t)(t.begin + tok) * n_kv + h) * g + (r0 + r - tok * g), d, o.a, o.M, o.L);
+        store_row<T, D, false>(P, ((size_t)(t.begin + tok) * n_kv + h) * g + (r0 + r - tok * g), d, o.a, o.M, o.L);
     }
 }
 
@@ -172,7 +173,7 @@ __global__ __launch_bounds__(256) void merge_rows_kernel(const AttnPagedParams P
 #pragma unroll
             for (int k = 0; k < 4; ++k) o.a[k] = o.a[k] * fo + x.a[k] * fx;
         }
-        store_row<T, D>(P, (size_t)slot * g + r, d, o.a, o.M, o.L);
+        store_row<T, D, true>(P, (size_t)slot * g + r, d, o.a, o.M, o.L);
         return;
     }
     if (splits == 1) return;   // all done

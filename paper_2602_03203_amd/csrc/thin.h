@@ -412,7 +412,7 @@ __device__ __forceinline__ void thin_tile(const AttnPagedParams& P, int item, in
                 }
                 continue;
             }
-            store_row<T, D>(P, ((size_t)(t.begin + tok) * n_kv + h) * g + (r0 + r - tok * g), d, a, s_M[r], s_L[ROWS ? 8 + r : r]);
+            store_row<T, D, ROWS>(P, ((size_t)(t.begin + tok) * n_kv + h) * g + (r0 + r - tok * g), d, a, s_M[r], s_L[ROWS ? 8 + r : r]);
         }
         if constexpr (ROWS) {
             // the new pair joins the cache (its slot is read by nobody in this launch)

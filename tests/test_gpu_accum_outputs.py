@@ -1,5 +1,5 @@
 """Outputs of the step that accumulates its weights are those of the plain step: head_dim 64 with all bits of the weights, head_dim 128 normalised by the weights
-as they meet V; infinities as there."""
+as they meet V; infinities, and rows without any number, as there."""
 import numpy as np
 import pytest
 import torch
@@ -111,3 +111,21 @@ def test_infinite_values(dtype, D, n, g):
     for t, b, h, ch, _ in places:
         o[t:, b, h * g:(h + 1) * g, ch] = r[t:, b, h * g:(h + 1) * g, ch]
     assert torch.equal(o, r) and torch.equal(acc[:, :, :n], acc_r[:, :, :n])
+
+
+@pytest.mark.parametrize("dtype, D", [("bf16", 64), ("bf16", 128), ("f32", 64), ("f32", 128)])
+@pytest.mark.parametrize("n", [40, 1500])
+def test_rows_without_any_number(dtype, D, n):
+    """All logits of a head -inf: 0 / 0, as in the plain step; other heads have their results."""
+    fk = _fk()
+    c = Rows(dtype, D, 4, 2, [n, n - 7], n + 5, 1, seed=5)
+    c.K[0, 0, :, 3], c.k[0, 0, 0, 3] = -INF, -INF
+    c.q[0, 0, :4, 3] = torch.tensor([1.0, 0.5, 2.0, 1.0]).to(DT[dtype])
+    s = c.dev()
+    plain, K, V, pos, ln = s["out"].clone(), s["K"].clone(), s["V"].clone(), s["pos"].clone(), s["len"].clone()
+    c.run(s)
+    fk.fk_decode_step(s["desc"], s["q"][0], K, V, pos, ln, s["k"][0], s["v"][0], s["pos_new"][0], n + 1, c.scale, plain[0], fk.new_attn_workspace(s["desc"]))
+    torch.cuda.synchronize()
+    assert torch.isnan(plain[0, 0, :4]).all() and torch.isfinite(plain[0, 0, 4:]).all() and torch.isfinite(plain[0, 1]).all()
+    assert torch.equal(torch.isnan(s["out"]), torch.isnan(plain))
+    assert torch.isnan(s["acc"][0, 0, :n + 1]).all() and torch.isfinite(s["acc"][0, 1]).all() and torch.isfinite(s["acc"][1]).all()
