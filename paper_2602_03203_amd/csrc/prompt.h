@@ -379,9 +379,8 @@ __device__ __forceinline__ void prompt_tile(const AttnPagedParams& P, int item, 
                 if (!mine[ct]) continue;
                 const int r = w0 + ct * 16 + n16, tok = token_of(r);
                 const size_t row = ((size_t)(t.begin + tok) * n_kv + h) * g + (r - tok * g);
-                const bool none = m_top[ct] == -INFINITY;
                 const size_t rec = ((size_t)(item - P.whole) * P.splits + split) * TM + (r - r0);
-                const float mul = splits > 1 ? f : none ? 0.f : 1.0f / l;
+                const float mul = splits > 1 ? f : l == 0.f ? 0.f : 1.0f / l;
 #pragma unroll
                 for (int e = 0; e < ET; e += BF ? 1 : 4) {
                     if constexpr (BF) {   // channels e * 16 + quad * 4 ..
@@ -400,7 +399,7 @@ __device__ __forceinline__ void prompt_tile(const AttnPagedParams& P, int item, 
                     }
                 }
                 if (quad == 0) {
-                    const float2 ml = make_float2(m_top[ct], none ? 0.f : l * f);
+                    const float2 ml = make_float2(m_top[ct], l * f);   // nothing seen: (-inf, 0); a sum that is no number stays none, whatever the maximum is
                     if (splits > 1) P.rec_ml[rec] = ml;
                     else if (P.stats) P.stats[row] = ml;
                 }
