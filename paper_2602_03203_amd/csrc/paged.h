@@ -82,6 +82,11 @@ __device__ __forceinline__ void load_to_lds(const void* from, unsigned char* to)
 }
 __device__ __forceinline__ void arrived() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }   // this wavefront's
 
+// |logits| from which they are rounded before a maximum is subtracted from them, as the few-row kernel always does; below it they are left to the fma, where an
+// exponent may be off by the rounding of the maximum, 2^-17 at most.  M and L are then the ones that the weights' exponents belong to, from whichever kernel
+// they come.  Where a tile has such logits it costs more: 2048 tokens of 16384 pairs, 8 heads of g 4, D 128, attention 501 us -> 524, weights 276 -> 312.
+static constexpr float kLargeLogit = 256.f;
+
 // ---- tiles of query rows --------------------------------------------------------------------------------------------
 // The queries of a (chunk, KV head) are rows: row r is head r % g of token r / g.  A tile is TM of them.  `slot` counts the places of a launch:
 // either place i of sequence b is slot i * batch + b (spread == false; a sequence has `per_seq` places, whose workgroups take every

@@ -4,7 +4,7 @@
 // the four wavefronts, straight into LDS (two buffers each for K and V, one barrier a tile).  While the vector units turn one tile's logits into
 // probabilities, the matrix units form the next one's: with a tile's steps one after the other a wavefront alone on its SIMD took 2.2 us a tile,
 // of which the products are 0.4.  Products and operand layouts are those of thin.h (logits K.Q^T with the keys in an order that makes a
-// lane's probabilities an operand of V^T.P^T as they are; the same 16x16 products in the same order, so that logits are the same bits
+// lane's probabilities an operand of V^T.P^T as they are; the same 16x16 products in the same order, so that they are the same bits
 // everywhere); an operand read from LDS serves two products, one for each 16 rows.
 //   in LDS a row's 16-byte chunks change places (swizzle_k, swizzle_v), so that the 16 rows of an operand lie in different banks; a load writes LDS in
 //   the order of its lanes, so each lane fetches the chunk that belongs in its place
@@ -37,7 +37,6 @@ template <typename T, int D> struct PromptCfg {
     static constexpr int TILE_BYTES = KT * CH * 16;
     static constexpr size_t LDS_BYTES = 4 * (size_t)TILE_BYTES;   // K, V, two buffers
 };
-static constexpr float kPromptHuge = 16777216.f;   // |logits| from which they are rounded before a maximum is subtracted
 
 // 16-byte chunk of a row -> its place
 template <bool BF, int CH> __device__ __forceinline__ int swizzle_k(int row) {
@@ -220,10 +219,10 @@ __device__ __forceinline__ void prompt_tile(const AttnPagedParams& P, int item, 
                 }
             };
             // a row's largest logit of a tile, and whether its reference has to move or differences would lose their bits
-            bool need = false, huge = false;
+            bool need = false, large = false;
             float m_new[CT];
             auto assess = [&](const Logits& c) {
-                need = huge = false;
+                need = large = false;
 #pragma unroll
                 for (int ct = 0; ct < CT; ++ct) {
                     float mx = c[0][ct][0];
@@ -232,7 +231,7 @@ __device__ __forceinline__ void prompt_tile(const AttnPagedParams& P, int item, 
                     const float m = attn_logit(quad_max(mx), scale);
                     m_new[ct] = m;
                     need |= m > m_ref[ct] + 8.f;
-                    huge |= fabsf(fmaxf(m, m_ref[ct])) >= kPromptHuge;   // (nothing seen: -inf as well, with nothing to lose)
+                    large |= fabsf(fmaxf(m, m_ref[ct])) >= kLargeLogit;   // (nothing seen: -inf as well, with nothing to lose)
                 }
             };
             // One tile: its logits c become weights and meet V; the next one's are formed beside them.
@@ -271,7 +270,7 @@ __device__ __forceinline__ void prompt_tile(const AttnPagedParams& P, int item, 
                 float by = scale, less[CT];
 #pragma unroll
                 for (int ct = 0; ct < CT; ++ct) less[ct] = m_ref[ct];
-                if (__any(huge)) {   // rounded before the reference is subtracted; below, there is nothing left to do
+                if (__any(large)) {   // rounded before the reference is subtracted; the fma below then has nothing left to do
                     by = 1.f;
 #pragma unroll
                     for (int ct = 0; ct < CT; ++ct) {

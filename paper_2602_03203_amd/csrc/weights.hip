@@ -4,7 +4,7 @@
 // tiles of 64, straight into LDS two tiles ahead, with their M and 1 / L, shared by the four wavefronts.  A product of 16 keys x 16 rows leaves a
 // lane with four keys of ONE row, so M and 1 / L are one register each and a pair's weight is added by one fma; the 16 lanes of a key are
 // summed once, at the end.  The order of all sums is fixed.  The products are those of the attention kernels, step by step the same ones, so that
-// logits are the same bits: beyond 2^24, where a logit's rounding is more than an exponent may be off, M still belongs to them.
+// they are the same bits; large logits are rounded before M is subtracted, as where M was found (kLargeLogit): a query's weights add up to one.
 //
 // Bound by matrix and vector instructions together: per 16 x 16 logits D / 32 products and, per lane, four times an fma, an exponential and an fma.  16
 // products and the vector work that goes with them, registers alone, two wavefronts to a SIMD, take 272 and 214 ns by themselves and 404 together; the
@@ -36,9 +36,6 @@ template <typename T, int D, bool FEW> struct WeightsCfg {   // FEW: few keys, 1
     static constexpr int NQ = QT / 16, TILE_BYTES = QT * CH * 16;
     static constexpr int LD = QT * CH / 256;              // 16-byte loads of a tile per thread
 };
-
-// |logits| from which products and maxima are subtracted as rounded numbers, not inside an fma
-static constexpr float kHugeLogit = 16777216.f;
 
 template <typename T, int D, bool FEW>
 __global__ __launch_bounds__(256, 3) void weights_kernel(const WeightsParams P) {
@@ -172,7 +169,7 @@ __global__ __launch_bounds__(256, 3) void weights_kernel(const WeightsParams P) 
                     }
                 }
                 float by = scale, less = m;
-                if (__any(fabsf(m) >= kHugeLogit)) {   // rounded before the maximum is subtracted; below, there is nothing left to do
+                if (__any(fabsf(m) >= kLargeLogit)) {   // rounded before the maximum is subtracted; the fma below then has nothing left to do
                     by = 1.f;
                     less = 0.f;
 #pragma unroll

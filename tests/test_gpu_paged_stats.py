@@ -83,3 +83,40 @@ def test_logits_of_minus_infinity_alone(dtype, D, many_rows):
     assert (stats[:40, 4:, 1] > 0).all() and (stats[40:, :, 1] > 0).all()
     acc = s["acc"].cpu()
     assert torch.isnan(acc[0, 0, :68]).all() and (acc[0, 0, 68:100] == 0).all()      # (token 7 is at position 67)
+
+
+@pytest.mark.parametrize("dtype, D", TYPES)
+@pytest.mark.parametrize("log_scale", [4, 7, 10, 14, 18, 20, 21])
+@pytest.mark.parametrize("many_rows", [True, False])
+def test_a_querys_weights_add_up_to_one(dtype, D, log_scale, many_rows):
+    """Whatever the logits' size, weights are taken against the maximum and the sum that the attention found, by the same exponents: a query's weights add up to
+    one.  Logits of up to about 2^3 times the scale here (times sqrt(64 .. 128))."""
+    chunks = [(200, 60), (333, 1), (90, 17), (70, 70)]
+    c = (_case if many_rows else Case)(dtype, D, 4, 2, 16, chunks, scale=2.0 ** log_scale / 8, seed=60 + log_scale)
+    s, out, stats = _attended(c)
+    top = np.abs(stats[..., 0]).max()
+    assert 2.0 ** log_scale < top < 2.0 ** (log_scale + 7)
+    acc, first = s["acc"].double().cpu().numpy(), c.acc.double().numpy()
+    for b, (n, m) in enumerate(chunks):
+        gained = (acc[b, :, :n].sum(axis=1) - first[b, :, :n - m].sum(axis=1)) / (4 * m)
+        # Exponents of attention and weights: the same logits, rounded or not - below 2^8 the rounding is 2^-17 at most, each side once, times ln 2; sums of n weights of
+        # 4 m queries, two steps an exponential and a reciprocal; the pairs' earlier sums, up to n of up to 1 with a rounding for each addition
+        tol = 2 * 2.0 ** -17 * np.log(2.0) + (n + 4 * m + 16) * U + 2 * n * U / (4 * m)
+        assert (np.abs(gained - 1) <= tol).all(), (b, gained - 1, tol, top)
+
+
+@pytest.mark.parametrize("dtype, D", TYPES)
+@pytest.mark.parametrize("log_scale", [7, 18, 21])
+def test_both_kernels_report_the_same(dtype, D, log_scale):
+    """One call by its bound few rows' and many rows': maxima bit for bit, sums as near as fp32 sums are."""
+    chunks = [(200, 60), (90, 17), (70, 70)]
+    few = Case(dtype, D, 4, 2, 16, chunks, scale=2.0 ** log_scale / 8, seed=70)
+    many = copy.copy(few)
+    many.max_pages = (1 << 21) // (147 * 4 // 16 * 2) // 16 + 1
+    many.table = torch.nn.functional.pad(few.table, (0, many.max_pages - few.max_pages), value=-1)
+    many.acc = torch.nn.functional.pad(few.acc, (0, (many.max_pages - few.max_pages) * 16))
+    many.max_len = many.max_pages * 16
+    (_, o1, s1), (_, o2, s2) = _attended(few), _attended(many)
+    assert (s1[..., 0] == s2[..., 0]).all()
+    # exponents below 2^8 may be off by a logit's rounding, 2^-17 at most, in either
+    assert (np.abs(s1[..., 1] - s2[..., 1]) <= s1[..., 1] * (2 * 2.0 ** -17 * np.log(2.0) + (2 * 200 + 8) * U)).all()
