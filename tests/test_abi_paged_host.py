@@ -132,3 +132,19 @@ def test_no_tokens_and_no_buffers(fklib):
     d, rows = fklib.fk_paged_desc(2, 8, 2, 128, 16, 100, 40, fklib.FK_BF16), fklib.fk_cache_desc(2, 8, 2, 128, 512, fklib.FK_BF16)
     got = calls(L, d, rows, n=0, bytes=1 << 40, q=0, out=0, stats=0, k_new=0, v_new=0)
     assert set(got.values()) == {fklib.FK_OK}
+
+
+def test_each_workspace_a_byte_short(fklib):
+    """Each call on its own: a byte less than it asks for is refused."""
+    L = fklib.lib()
+    for d in (fklib.fk_paged_desc(2, 8, 2, 128, 16, 100, 40, fklib.FK_BF16), fklib.fk_paged_desc(1, 8, 2, 64, 64, 300, 256, fklib.FK_F32)):
+        D = ctypes.byref(d)
+        rows = fklib.fk_cache_desc(2, 8, 2, 128, 512, fklib.FK_BF16)
+        for n, chunk, length in ((8, 4, 64), (200, 100, 640)):
+            need = dict(attn=L.fk_paged_attn_workspace(D, n, chunk, length), weights=L.fk_paged_weights_workspace(D, n, chunk, length))
+            for name, size in need.items():
+                assert size > 0
+                got = L.fk_paged_attn(D, p, p, p, p, p, p, n, chunk, length, 0, 0, 1.0, p, p, p, size - 1, 0) if name == "attn" else \
+                    L.fk_paged_weights(D, p, p, p, p, p, n, chunk, length, 0, 0, 1.0, p, p, p, size - 1, 0)
+                assert got == fklib.FK_ERR_WORKSPACE, (name, size, got)
+        assert calls(L, d, rows, n=8, bytes=0, skip_append=True) == dict(append=None, attn=fklib.FK_ERR_WORKSPACE, weights=fklib.FK_ERR_WORKSPACE)
