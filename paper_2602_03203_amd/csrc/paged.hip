@@ -45,13 +45,12 @@ struct CompressParams {
 };
 
 template <int CH /* 16-byte chunks of a pair's K */>
-__global__ __launch_bounds__(256) void paged_compress_kernel(const PagedParams P, const CompressParams C) {
+__device__ __forceinline__ void compress_slots(const PagedParams& P, const CompressParams& C, int row, long long (&s_src)[kCompressSlots]) {
     constexpr int U = kCompressSlots * CH / 256;
-    const int row = blockIdx.y, b = row / P.n_kv, h = row % P.n_kv, tid = threadIdx.x;
+    const int b = row / P.n_kv, h = row % P.n_kv, tid = threadIdx.x;
     const int n = pairs_of(P, b), kept = min(n, C.budget), base = blockIdx.x * kCompressSlots;
     if (blockIdx.x == 0 && tid == 0) C.len[row] = kept;
     if (base >= kept) return;
-    __shared__ long long s_src[kCompressSlots];   // pair of the pool, -1 for none
     if (tid < kCompressSlots) {
         const int j = base + tid, p = j < kept ? C.keep[(size_t)row * C.budget + j] : -1;
         long long src = -1;
@@ -84,6 +83,17 @@ __global__ __launch_bounds__(256) void paged_compress_kernel(const PagedParams P
         if (src[u] < 0) continue;
         Kr[i] = k[u];
         Vr[i] = v[u];
+    }
+}
+
+template <int CH>
+__global__ __launch_bounds__(256) void paged_compress_kernel(const PagedParams P, const CompressParams C) {
+    __shared__ long long s_src[kCompressSlots];   // pair of the pool, -1 for none
+    for (int row = blockIdx.y;;) {   // (a grid's second dimension ends at 65535)
+        compress_slots<CH>(P, C, row, s_src);
+        row += gridDim.y;
+        if (row >= P.batch * P.n_kv) break;
+        __syncthreads();
     }
 }
 
@@ -121,12 +131,11 @@ extern "C" fk_status fk_paged_compress(const fk_paged_desc* desc, const void* K,
     if (budget <= 0 || budget > rows->capacity) return FK_ERR_INVALID_ARG;
     if (!aligned16(K) || !aligned16(V) || !aligned16(K_rows) || !aligned16(V_rows)) return FK_ERR_INVALID_ARG;
     const int n_rows = desc->batch * desc->n_kv_heads;
-    if (n_rows > 65535) return FK_ERR_UNSUPPORTED;
     PagedParams P = paged_params(desc, page_table, kv_len, nullptr, 0);
     P.K = K;
     P.V = V;
     const CompressParams C = {acc, keep_idx, K_rows, V_rows, pos, len, acc_rows, budget, rows->capacity};
-    const dim3 grid((budget + kCompressSlots - 1) / kCompressSlots, n_rows);
+    const dim3 grid((budget + kCompressSlots - 1) / kCompressSlots, n_rows < 65536 ? n_rows : 65535);
     hipStream_t st = (hipStream_t)stream;
     switch (desc->head_dim * (desc->dtype == FK_F32 ? 4 : 2) / 16) {
         case 8: hipLaunchKernelGGL(paged_compress_kernel<8>, grid, dim3(256), 0, st, P, C); break;
