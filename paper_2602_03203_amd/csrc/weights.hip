@@ -37,6 +37,11 @@ template <typename T, int D, bool FEW> struct WeightsCfg {   // FEW: few keys, 1
     static constexpr int LD = QT * CH / 256;              // 16-byte loads of a tile per thread
 };
 
+// Keys k0 .. k1 - 1 of a block, older than the chunk and outside of all its windows: their sums stay as they are, and splits write no partial ones
+__device__ __forceinline__ bool nobody_sees(const PagedParams& W, int k0, int k1, int first) {
+    return W.window != 0x7fffffff && k0 >= W.sink && k1 <= first && k1 - 1 + W.window <= first;
+}
+
 template <typename T, int D, bool FEW>
 __global__ __launch_bounds__(256, 3) void weights_kernel(const WeightsParams P) {
     using C = WeightsCfg<T, D, FEW>;
@@ -55,13 +60,13 @@ __global__ __launch_bounds__(256, 3) void weights_kernel(const WeightsParams P) 
     const float scale = W.scale_log2e;
     for (int k0 = (place - b * P.blocks) * C::KEYS; k0 < n; k0 += P.blocks * C::KEYS) {
         const int k1 = min(k0 + C::KEYS, n);
+        if (nobody_sees(W, k0, k1, first)) continue;
         // tokens that see any of these keys: from position k0 on, and under a window up to the last key's reach
         int t0 = max(k0 - first, 0), t1 = nq;
         if (W.window != 0x7fffffff && k0 >= W.sink) t1 = min((long long)nq, max(0ll, (long long)k1 - 1 + W.window - first));
         const int row_lo = t0 * g, row_hi = max(t1, t0) * g;
         const int tiles = (row_hi - row_lo + QT - 1) / QT, per = scalar((tiles + P.splits - 1) / P.splits);
         const int i0 = min(split * per, tiles), i1 = min(i0 + per, tiles);
-        if (tiles == 0 && k1 <= first) continue;   // older keys, outside of all windows: their sums stay as they are
 
         const int kw = k0 + wave * (KG * 16);   // the wavefront's keys
         W128 k[KG][KS];
@@ -232,10 +237,8 @@ __global__ __launch_bounds__(256) void weights_sum_kernel(const WeightsParams P)
     const int row = blockIdx.y, b = row / W.n_kv, key = blockIdx.x * 256 + threadIdx.x;
     const int begin = chunk_begin(W, b), nq = chunk_end(W, b, begin) - begin, n = pairs_of(W, b), first = n - nq;
     if (nq == 0 || key >= n) return;
-    if (W.window != 0x7fffffff) {   // key blocks that no query sees have no partial sums
-        const int k0 = key / P.keys * P.keys, k1 = min(k0 + P.keys, n);
-        if (k0 >= W.sink && k1 <= first && k1 - 1 + W.window <= first) return;
-    }
+    const int k0 = key / P.keys * P.keys;
+    if (nobody_sees(W, k0, min(k0 + P.keys, n), first)) return;
     const size_t stride = (size_t)W.batch * W.n_kv * P.part_len;
     const float* part = P.part + (size_t)row * P.part_len + key;
     float s = 0.f;

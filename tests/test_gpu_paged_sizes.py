@@ -1,6 +1,9 @@
-"""Sizes of the paged calls at which their launches change: more rows than a grid's second dimension holds."""
+"""Sizes of the paged calls at which their launches change: more rows than a grid's second dimension holds, wide blocks of keys under a window."""
+import numpy as np
 import pytest
 import torch
+
+from paged_util import Case
 
 pytestmark = pytest.mark.gpu
 
@@ -37,3 +40,19 @@ def test_compress_more_than_65535_rows(with_acc):
     assert torch.equal(pos[:, :, :budget], torch.where(live, keep, -5)) and (pos[:, :, budget:] == -5).all()
     if with_acc:
         assert torch.equal(acc_r[:, :, :budget], torch.where(live, acc.gather(2, k), 4.0)) and (acc_r[:, :, budget:] == 4).all()
+
+
+@pytest.mark.parametrize("dtype, D, sink", [("bf16", 64, 0), ("bf16", 64, 5), ("f32", 128, 0), ("f32", 128, 5), ("bf16", 128, 300)])
+def test_wide_key_blocks_under_a_window(dtype, D, sink):
+    """Rows, pairs and queries enough for wavefronts of many keys and split queries; blocks of keys that no query reaches have no partial sums (what the workspace
+    holds there is NaN)."""
+    chunks = [(3000, 300), (2600, 1), (1500, 290)] + [(40 + 9 * b, 1 + b % 3) for b in range(29 if dtype == "bf16" else 13)]
+    c = Case(dtype, D, 8, 2, 64, chunks, 700, sink, seed=61)
+    s = c.dev()
+    c.run(s)
+    torch.cuda.synchronize()
+    assert s["wws"].numel() > 2 * s["acc"].numel() * 4      # (several splits)
+    ref, tol = c.reference()
+    c.check(s, ref, tol)
+    assert torch.equal(s["acc"][0, :, max(sink, 0) // 256 * 256 + 256:1792].cpu(), c.acc[0, :, max(sink, 0) // 256 * 256 + 256:1792])     # whole blocks behind the sinks that nobody sees
+    assert np.isfinite(s["acc"].cpu().numpy()).all()
