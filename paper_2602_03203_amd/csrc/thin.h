@@ -79,9 +79,10 @@ __device__ __forceinline__ void thin_tile(const AttnPagedParams& P, int item, in
         if (split >= splits) continue;
         const int per = splits == 1 ? kt.total : scalar(divide(kt.total + splits - 1, splits)), t_begin = min(split * per, kt.total), t_end = min(t_begin + per, kt.total);
 
-        // This lane's row.  ROWS: the heads a second time in the upper eight columns, for the second terms of their probabilities, or of which the
-        // normaliser of the outputs is kept (below).
-        const int my_row = ROWS ? min(n16 % 8, rows - 1) : r0 + min(n16, rows - 1), my_token = token_of(my_row), my_head = my_row - my_token * g;
+        // This lane's row.  Rows of a bf16 cache: the heads a second time in the upper eight columns, for the second terms of their probabilities, or of
+        // which the normaliser of the outputs is kept (below).
+        constexpr bool TWICE = ROWS && BF;
+        const int my_row = TWICE ? min(n16 % 8, rows - 1) : r0 + min(n16, rows - 1), my_token = token_of(my_row), my_head = my_row - my_token * g;
         const size_t q_row = ((size_t)(t.begin + my_token) * n_kv + h) * g + my_head;
         const bool lg_local = ROWS && t.n <= P.logits_lds;
         const float acc_first = ROWS && splits == 1 && tid < t.n ? P.acc[(size_t)slot * P.cap + tid] : 0.f;   // (on its way over the whole loop)
@@ -178,7 +179,7 @@ __device__ __forceinline__ void thin_tile(const AttnPagedParams& P, int item, in
         for (int lo = tile_lo, hi = tile_hi;;) {
         if (!ROWS && tid == 0) s_bad = 0;
         if constexpr (!ROWS) __syncthreads();
-        const int pos = t.first + my_token, p = ROWS || (n16 < rows && pos >= lo && pos <= hi) ? pos : -1;   // -1: sees nothing
+        const int pos = t.first + my_token, p = TWICE || (n16 < rows && pos >= lo && pos <= hi) ? pos : -1;   // -1: sees nothing
         const int p_from = p < 0 || W.window == 0x7fffffff ? -1 : p - W.window;   // sees keys (p_from, p] and [0, min(sink, p + 1))
         const int p_sink = min(W.sink, p + 1);
         float m_run = -INFINITY, l_run = 0.f;
@@ -352,7 +353,7 @@ __device__ __forceinline__ void thin_tile(const AttnPagedParams& P, int item, in
         l_run = quad_sum(l_run);
         if (quad == 0) {
             s_m[wave][n16] = m_run;
-            s_l[wave][n16] = ONES && n16 >= 8 ? o_l[0] : l_run;   // ROWS: of the accumulated weights, and from 8 on the normaliser of the outputs
+            s_l[wave][n16] = ONES && n16 >= 8 ? o_l[0] : l_run;   // TWICE: of the accumulated weights, and from 8 on the normaliser of the outputs
         }
         if constexpr (TERMS) {
 #pragma unroll
@@ -408,11 +409,11 @@ __device__ __forceinline__ void thin_tile(const AttnPagedParams& P, int item, in
                 *reinterpret_cast<float4*>(P.rec + (rec + r) * D + d) = make_float4(a[0], a[1], a[2], a[3]);
                 if (d == 0) {
                     P.rec_ml[rec + r] = make_float2(s_M[r], s_L[r]);
-                    if constexpr (ROWS) P.rec_ml[rec + 8 + r] = make_float2(s_M[r], s_L[8 + r]);
+                    if constexpr (ROWS) P.rec_ml[rec + 8 + r] = make_float2(s_M[r], s_L[TWICE ? 8 + r : r]);
                 }
                 continue;
             }
-            store_row<T, D, ROWS>(P, ((size_t)(t.begin + tok) * n_kv + h) * g + (r0 + r - tok * g), d, a, s_M[r], s_L[ROWS ? 8 + r : r]);
+            store_row<T, D, ROWS>(P, ((size_t)(t.begin + tok) * n_kv + h) * g + (r0 + r - tok * g), d, a, s_M[r], s_L[TWICE ? 8 + r : r]);
         }
         if constexpr (ROWS) {
             // the new pair joins the cache (its slot is read by nobody in this launch)
