@@ -91,13 +91,14 @@ struct RowsPlan {
 // Short rows, and as many rows as CUs, take a workgroup of eight wavefronts each, which adds the weights itself; others are split over 256 workgroups of
 // four, each with a tile for every wavefront or more, and the second launch, 3 us, adds them.  us a step, a row to a workgroup and split:
 //   bf16 D = 128, g = 4   8 rows of 300 8.0 and 8.9, of 1000 14.6 and 8.3; 32 of 500 9.9 and 8.3; 128 of 300 8.2 and 9.3, of 1000 16.9 and 16.8, of 2112
-//                         28 and 28; 256 of 600 16.4 and 21; D = 64  8 of 300 6.8 and 8.0, 32 of 500 7.4 and 7.3, 128 of 1000 11.4 and 11.4, of 2112 20 and 18
+//                         28 and 28; 256 of 600 16.4 and 21; D = 64 (in a graph, where a step takes 1 us more)  8 of 300 8.4 and 9.4, 32 of 500 9.2 and 9.6, 128
+//                         of 300 8.6 and 9.8, of 1000 13.4 and 13.4, of 2112 21.6 and 20.4
 //   fp32 D = 64           2 of 144 6.4 and 7.5, 8 of 300 8.2 and 7.9, 128 of 300 8.7 and 9.2, of 1000 20 and 18;  D = 128  2 of 144 9.0 and 9.2, 8 of 300
 //                         12.8 and 9.8, 128 of 300 14.1 and 14.3, of 1000 34 and 27
-// Between 128 rows and 256, us of eight wavefronts and of three splits: 152 of 2112 bf16 D = 128 29.6 and 30.7, D = 64 19.9 and 19.9, fp32 D = 64 36 and 31, 128 70
-// and 70; of 1000 fp32 D = 64 20.2 and 20.0, 128 34 and 31; 200 of 2112 bf16 36 and 41, 22 and 26, fp32 37 and 44, 82 and 92.
+// Between 128 rows and 256, us of eight wavefronts and of three splits: 152 of 2112 bf16 D = 128 29.6 and 30.7, D = 64 21.8 and 21.9, fp32 D = 64 36 and 31, 128 70
+// and 70; of 1000 fp32 D = 64 20.2 and 20.0, 128 34 and 31; 200 of 2112 bf16 36 and 41, 24 and 28, fp32 37 and 44, 82 and 92.
 // Splits: 8 rows of 4000 pairs, bf16, 8: 11.2, 16: 10.0, 32: 11.6; 32 of 2000 4: 13.4, 8: 11.8, 16: 14.1.  From 512 rows on, and fp32 with D = 128, four
-// wavefronts a row: 512 rows of 1000 43.5, eight 44.4 (fp32 87 and 92).
+// wavefronts a row: 512 rows of 1000 43.5, eight 44.4 (fp32 87 and 92; bf16 D = 64, since a probability is three terms there, 26.6 and 25.4, 1024 of 150 12.5 and 16.5).
 static RowsPlan rows_plan(const fk_cache_desc* d, int max_len) {
     const int rows = d->batch * d->n_kv_heads;
     const bool bf16 = d->dtype == FK_BF16;
