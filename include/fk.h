@@ -390,8 +390,9 @@ fk_status fk_paged_append(const fk_paged_desc *desc, void *K, void *V, const int
  * Attention of every chunk over its sequence's pairs (the chunk's own are in the cache: fk_paged_append first), single tokens included:
  *   out[t][hq][:] = sum_j 2^(s_j - M) V_j / L,  s_j = log2(e) * softmax_scale * <q[t][hq], K_j>,  M = max_j s_j,  L = sum_j 2^(s_j - M)
  * over the pairs j that the query sees.  q, out: [n_tokens][n_q_heads][head_dim]; stats (may be NULL): [n_tokens][n_q_heads][2] fp32, M and L.  A query
- * that sees nothing, or logits of -inf alone, gets zeros and (-inf, 0).  fp32 accumulation; bf16: the weights are rounded to bf16 before they meet V, L is the sum of
- * the unrounded ones.  workspace: fk_paged_attn_workspace bytes, no initialisation required; calls sharing it must not overlap in time.
+ * that sees nothing, or logits of -inf alone, gets zeros and (-inf, 0); one that is no number, or meets one, has L = NaN.  fp32 accumulation; bf16: the
+ * weights are rounded to bf16 before they meet V, L is the sum of the unrounded ones.  workspace: fk_paged_attn_workspace bytes, no initialisation
+ * required; calls sharing it must not overlap in time.
  */
 size_t fk_paged_attn_workspace(const fk_paged_desc *desc, int32_t n_tokens, int32_t max_chunk, int32_t max_len);
 fk_status fk_paged_attn(const fk_paged_desc *desc, const void *q, const void *K, const void *V, const int32_t *page_table,
