@@ -424,6 +424,117 @@ fk_status fk_paged_compress(const fk_paged_desc *desc, const void *K, const void
                             void *V_rows, int32_t *pos, int32_t *len, float *acc_rows, void *stream);
 
 /*
+ * ---- Drafted tokens: positions, attention of trees over a cache, verification, the accepted path joins the cache ----
+ *
+ * A small model drafts several tokens behind the last one, as a tree (a chain is one); one pass of the large model answers for all of them.  Only what is
+ * accepted joins the cache: a budgeted cache must not hold, score or evict for pairs that are thrown away again.  The trees of a call are packed:
+ *   q_start [batch + 1] int32   tokens q_start[b] .. q_start[b + 1] - 1 of the call are sequence b's tree (of 0 to FK_TREE_NODES nodes), ascending
+ *   parent  [n_tokens] int32    a node's parent, counted from the tree's first node and lower than its own place; others, -1 by custom, stand for none
+ * Node 0 is the root: the last token of the sequence, whose pair is not in the cache yet.  A sequence whose tree has more than FK_TREE_NODES nodes is passed
+ * over: nothing of it is written, and fk_verify_drafts accepts nothing.  The round of a layer: fk_rope, fk_tree_attn; of the model: fk_verify_drafts; of every
+ * layer then: fk_commit_drafts.
+ */
+#define FK_TREE_NODES 256
+
+/*
+ * Rotary positions.  Of every head the first rotary_dim channels turn in pairs (u, w) by the angle pos * freq_i, i = 0 .. rotary_dim / 2 - 1:
+ *   u' = magnitude * (u cos - w sin),  w' = magnitude * (u sin + w cos)
+ * with u, w = channels i and i + rotary_dim / 2 (FK_ROPE_HALF) or 2 i and 2 i + 1 (FK_ROPE_INTERLEAVED); channels from rotary_dim on are copied.  Angles are
+ * formed in 64 bits and reduced to a turn before sine and cosine are taken in fp32; results are rounded once.  inverse: the angles negated (keys turned back; the
+ * gradient of a call is the same call on the outputs' gradients with inverse flipped).
+ */
+typedef enum { FK_ROPE_HALF = 0, FK_ROPE_INTERLEAVED = 1 } fk_rope_layout;
+
+typedef struct {
+    int32_t n_q_heads;  /* query heads per token, 0: no queries */
+    int32_t n_kv_heads; /* key heads per token, 0: no keys */
+    int32_t head_dim;   /* 64 or 128 */
+    int32_t rotary_dim; /* even, 2 .. head_dim */
+    int32_t layout;     /* fk_rope_layout */
+    int32_t dtype;      /* fk_dtype of q, k and the outputs */
+    int32_t inverse;
+    float magnitude;    /* 1, or what a scaling for long contexts multiplies queries and keys by */
+    int64_t q_stride, k_stride, q_out_stride, k_out_stride; /* elements from one token's heads to the next one's, whole 16 bytes; 0: heads * head_dim */
+} fk_rope_desc;
+
+/* q [n_tokens][n_q_heads][head_dim], k [n_tokens][n_kv_heads][head_dim] with their strides, pos [n_tokens] int32 (any value), freq [rotary_dim / 2] fp64: radians per
+ * position.  q_out may be q, and k_out k, with the same strides (in place); otherwise outputs share no memory with inputs or each other. */
+fk_status fk_rope(const fk_rope_desc *desc, const void *q, const void *k, const int32_t *pos, const double *freq, int32_t n_tokens,
+                  void *q_out, void *k_out, void *stream);
+
+/* Frequencies f_i = base^(-2 i / rotary_dim), scaled for contexts `factor` times as long as trained on:
+ *   FK_ROPE_LINEAR  all divided by factor
+ *   FK_ROPE_BASE    base * factor^(rotary_dim / (rotary_dim - 2)) in the place of base: the slowest pair slows down by factor, the fastest not at all
+ *   FK_ROPE_PARTS   a pair that turns r = context * f_i / (2 pi) times over the trained context is divided by factor where r <= low, left alone where
+ *                   r >= high, and mixed linearly in r between
+ * freq: HOST memory, [rotary_dim / 2].  Parameters that a scaling does not name are not looked at. */
+typedef enum { FK_ROPE_PLAIN = 0, FK_ROPE_LINEAR = 1, FK_ROPE_BASE = 2, FK_ROPE_PARTS = 3 } fk_rope_scaling;
+fk_status fk_rope_frequencies(int32_t rotary_dim, double base, int32_t scaling, double factor, double context, double low, double high,
+                              double *freq);
+
+/*
+ * Attention of trees over the rows of a budgeted cache: a node sees the live pairs of its sequence's rows, its ancestors' pairs and its own,
+ *   out[t][hq][:] = sum_j 2^(s_j - M) V_j / L,  s_j = log2(e) * softmax_scale * <q[t][hq], K_j>,  M = max_j s_j,  L = sum_j 2^(s_j - M)
+ * k_tree, v_tree: the nodes' own pairs, [n_tokens][n_kv_heads][head_dim]; the cache is only read.  q, out: [n_tokens][n_q_heads][head_dim]; stats (may be NULL):
+ * [n_tokens][n_q_heads][2] fp32, M and L.  Logits of -inf alone give zeros and (-inf, 0); a query that is no number, or meets one, has L = NaN.  Values of
+ * pairs that a node does not see, infinities and NaN among them, do not reach its results.  fp32 accumulation; bf16: the weights are rounded to bf16 before they
+ * meet V, L is the sum of the unrounded ones (fk_paged_attn's rounding).  max_tree <= FK_TREE_NODES bounds the trees' nodes and max_len every len[r]; they only
+ * size the launch, results are right beyond them too.  workspace: fk_tree_attn_workspace bytes for the same sizes, no initialisation required; calls sharing it must not
+ * overlap in time.  FK_ERR_UNSUPPORTED: n_tokens * n_q_heads >= 2^28, n_kv_heads >= 2^16.
+ */
+size_t fk_tree_attn_workspace(const fk_cache_desc *desc, int32_t n_tokens, int32_t max_tree, int32_t max_len);
+fk_status fk_tree_attn(const fk_cache_desc *desc, const void *q, const void *K, const void *V, const int32_t *len, const void *k_tree,
+                       const void *v_tree, const int32_t *parent, const int32_t *q_start, int32_t n_tokens, int32_t max_tree,
+                       int32_t max_len, float softmax_scale, void *out, float *stats, void *workspace, size_t workspace_bytes, void *stream);
+
+/* The same over the pages of a prompt (fk_paged_attn's pool, page table and holes).  kv_len counts the pairs in the pages, none of the tree's.  A node has position
+ * p = kv_len[b] + the number of its ancestors; with window > 0 it sees, of the pairs of the pages and of its ancestors, those at positions j > p - window or
+ * j < n_sink. */
+size_t fk_paged_tree_attn_workspace(const fk_paged_desc *desc, int32_t n_tokens, int32_t max_tree, int32_t max_len);
+fk_status fk_paged_tree_attn(const fk_paged_desc *desc, const void *q, const void *K, const void *V, const int32_t *page_table,
+                             const int32_t *kv_len, const void *k_tree, const void *v_tree, const int32_t *parent, const int32_t *q_start,
+                             int32_t n_tokens, int32_t max_tree, int32_t max_len, int32_t window, int32_t n_sink, float softmax_scale,
+                             void *out, float *stats, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * Verification of drafted tokens against the large model's probabilities (speculative sampling: what comes out is distributed as the large model's own
+ * samples).  target [n_tokens][vocab] fp32: row i is the distribution of the token behind node i; draft [n_tokens][vocab] fp32: row i is the one from which the
+ * children of node i were drawn, independently of each other; tokens [n_tokens]: the nodes' tokens (the root's is not looked at); uniform [n_tokens] fp32 in
+ * [0, 1): a node's number decides about it, the root's draws the last token.  From the root on, with r = target's row of the current node, its
+ * children x in ascending order:
+ *   uniform * draft(x) < r(x): x is accepted and becomes the current node, with r = target's row again;
+ *   otherwise r becomes max(r - draft, 0), divided by its sum.
+ * draft NULL (tokens that were not drawn, the likeliest ones say): x is accepted where uniform * m < r(x), with m = 1 at first; otherwise m goes down by r(x),
+ * not below 0, and r(x) becomes 0.  When no child is left, next_token is the lowest v with r(0) + .. + r(v) > uniform * (sum of r) and r(v) > 0 - the
+ * last v with r(v) > 0 where rounding finds none; of target's row where r is 0 everywhere; -1 where that is too.  Numbers that are negative or NaN in a row of r
+ * count as 0; a token outside [0, vocab) has probability 0 in both.  Sums and comparisons are in fp64, sums in a fixed order: equal calls give equal tokens.
+ * path [n_tokens]: the accepted nodes of sequence b, the root first, from q_start[b] on, then -1; n_accepted [batch]: how many, the root among them (0 without
+ * a tree); next_token [batch] (-1 without one).
+ * workspace: fk_verify_drafts_workspace bytes, zero-filled ONCE by the caller; every call leaves its counters at zero again.  Calls sharing it must not overlap
+ * in time.  batch <= 65535, vocab < 2^30 (FK_ERR_UNSUPPORTED beyond).  One launch.
+ */
+size_t fk_verify_drafts_workspace(int32_t batch, int32_t vocab);
+fk_status fk_verify_drafts(int32_t batch, int32_t vocab, const float *target, const float *draft, const int32_t *tokens, const int32_t *parent,
+                           const int32_t *q_start, int32_t n_tokens, const float *uniform, int32_t *path, int32_t *n_accepted,
+                           int32_t *next_token, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * The accepted paths' pairs join the rows of a budgeted cache: slot len[r] + i of row r = (b, h) receives pair path[q_start[b] + i] of the tree - K, V, and
+ * pos_first[b] + i into pos - for i < n_accepted[b], then len[r] goes up by as many.  A path ends at its first entry that is no node of the tree; a row takes as
+ * many pairs as it has room for, the first ones.  acc (may be NULL): accumulated weights (fk_decode_step_acc), which start from zero in the new slots.  k_tree,
+ * v_tree, path and n_accepted as above.  The pairs must not share memory with the cache.
+ */
+fk_status fk_commit_drafts(const fk_cache_desc *desc, void *K, void *V, int32_t *pos, int32_t *len, float *acc, const void *k_tree,
+                           const void *v_tree, const int32_t *q_start, int32_t n_tokens, const int32_t *path, const int32_t *n_accepted,
+                           const int32_t *pos_first, void *stream);
+
+/* The same into pages: position kv_len[b] + i receives the i-th pair, then kv_len[b] goes up.  A pair whose place lies in a hole is not stored, and counts; a
+ * sequence takes as many pairs as its page table has room for.  Sequences may share pages that nothing is stored to. */
+fk_status fk_paged_commit_drafts(const fk_paged_desc *desc, void *K, void *V, const int32_t *page_table, int32_t *kv_len, const void *k_tree,
+                                 const void *v_tree, const int32_t *q_start, int32_t n_tokens, const int32_t *path,
+                                 const int32_t *n_accepted, void *stream);
+
+/*
  * ---- Eviction by accumulated attention weight ----
  *
  * The score that learned ones are compared with: the attention weight a pair has received so far.  Device state, owned by the caller:

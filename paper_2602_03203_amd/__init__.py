@@ -8,5 +8,7 @@ from .binding import (CacheDesc, FkError, fk_append, fk_compact, fk_decode_attn,
                       feat_heads, new_feat, new_feat_workspace, fk_golden_steps, fk_golden_scores, fk_golden_trace,
                       PagedDesc, fk_paged_append, fk_paged_attn_workspace, new_paged_attn_workspace, fk_paged_attn, fk_paged_weights_workspace,
                       new_paged_weights_workspace, fk_paged_weights, fk_paged_compress, new_acc, fk_decode_step_acc_workspace, new_acc_workspace,
-                      fk_decode_step_acc, fk_compact_acc,
+                      fk_decode_step_acc, fk_compact_acc, RopeDesc, rope_frequencies, fk_rope, fk_tree_attn_workspace, new_tree_attn_workspace, fk_tree_attn,
+                      fk_paged_tree_attn_workspace, new_paged_tree_attn_workspace, fk_paged_tree_attn, fk_verify_drafts_workspace, new_verify_workspace,
+                      fk_verify_drafts, fk_commit_drafts, fk_paged_commit_drafts,
                       fk_score_kv, fk_select_keep, fk_select_keep_workspace, fk_select_keep_ws, fk_select_keep_sampled, fk_stream_read, lib, prepare, status_string, version)

@@ -23,7 +23,8 @@ SYMBOLS = ["fk_status_string", "fk_version", "fk_append", "fk_decode_attn_worksp
            "fk_decode_step_static", "fk_score_kv", "fk_select_keep", "fk_select_keep_workspace", "fk_select_keep_ws", "fk_select_keep_sampled", "fk_compact", "fk_decode_step_feat_workspace",
            "fk_decode_step_feat", "fk_decode_window_feat", "fk_score_kv_feat", "fk_compact_feat", "fk_golden_steps", "fk_golden_scores",
            "fk_golden_trace", "fk_paged_append", "fk_paged_attn_workspace", "fk_paged_attn", "fk_paged_weights_workspace", "fk_paged_weights",
-           "fk_paged_compress", "fk_decode_step_acc_workspace", "fk_decode_step_acc", "fk_compact_acc", "fk_stream_read"]
+           "fk_paged_compress", "fk_decode_step_acc_workspace", "fk_decode_step_acc", "fk_compact_acc", "fk_rope", "fk_rope_frequencies", "fk_tree_attn_workspace", "fk_tree_attn",
+           "fk_paged_tree_attn_workspace", "fk_paged_tree_attn", "fk_verify_drafts_workspace", "fk_verify_drafts", "fk_commit_drafts", "fk_paged_commit_drafts", "fk_stream_read"]
 
 
 class fk_cache_desc(ctypes.Structure):
@@ -45,6 +46,11 @@ class fk_step_args(ctypes.Structure):
                 [(n, ctypes.c_void_p) for n in ("q", "K", "V", "pos", "len", "k_new", "v_new", "pos_new", "out", "workspace")] +
                 [("workspace_bytes", ctypes.c_size_t), ("stream", ctypes.c_void_p), ("softmax_scale", ctypes.c_float),
                  ("chunk_pos", ctypes.c_int32), ("chunk_len", ctypes.c_int32), ("feat", ctypes.c_void_p)])
+
+
+class fk_rope_desc(ctypes.Structure):
+    _fields_ = ([(n, ctypes.c_int32) for n in ("n_q_heads", "n_kv_heads", "head_dim", "rotary_dim", "layout", "dtype", "inverse")] + [("magnitude", ctypes.c_float)] +
+                [(n, ctypes.c_int64) for n in ("q_stride", "k_stride", "q_out_stride", "k_out_stride")])
 
 
 class FkError(RuntimeError):
@@ -98,6 +104,17 @@ def lib() -> ctypes.CDLL:
         L.fk_decode_step_acc_workspace.restype, L.fk_decode_step_acc_workspace.argtypes = sz, [dp]
         L.fk_decode_step_acc.restype, L.fk_decode_step_acc.argtypes = ctypes.c_int, [dp, vp, vp, vp, vp, vp, vp, vp, vp, i32, f32, vp, vp, vp, sz, vp]
         L.fk_compact_acc.restype, L.fk_compact_acc.argtypes = ctypes.c_int, [dp, vp, vp, vp, vp, vp, vp, i32, vp]
+        f64 = ctypes.c_double
+        L.fk_rope.restype, L.fk_rope.argtypes = ctypes.c_int, [ctypes.POINTER(fk_rope_desc), vp, vp, vp, vp, i32, vp, vp, vp]
+        L.fk_rope_frequencies.restype, L.fk_rope_frequencies.argtypes = ctypes.c_int, [i32, f64, i32, f64, f64, f64, f64, vp]
+        L.fk_tree_attn_workspace.restype, L.fk_tree_attn_workspace.argtypes = sz, [dp, i32, i32, i32]
+        L.fk_tree_attn.restype, L.fk_tree_attn.argtypes = ctypes.c_int, [dp, vp, vp, vp, vp, vp, vp, vp, vp, i32, i32, i32, f32, vp, vp, vp, sz, vp]
+        L.fk_paged_tree_attn_workspace.restype, L.fk_paged_tree_attn_workspace.argtypes = sz, [pp, i32, i32, i32]
+        L.fk_paged_tree_attn.restype, L.fk_paged_tree_attn.argtypes = ctypes.c_int, [pp, vp, vp, vp, vp, vp, vp, vp, vp, vp, i32, i32, i32, i32, i32, f32, vp, vp, vp, sz, vp]
+        L.fk_verify_drafts_workspace.restype, L.fk_verify_drafts_workspace.argtypes = sz, [i32, i32]
+        L.fk_verify_drafts.restype, L.fk_verify_drafts.argtypes = ctypes.c_int, [i32, i32, vp, vp, vp, vp, vp, i32, vp, vp, vp, vp, vp, sz, vp]
+        L.fk_commit_drafts.restype, L.fk_commit_drafts.argtypes = ctypes.c_int, [dp, vp, vp, vp, vp, vp, vp, vp, vp, i32, vp, vp, vp, vp]
+        L.fk_paged_commit_drafts.restype, L.fk_paged_commit_drafts.argtypes = ctypes.c_int, [pp, vp, vp, vp, vp, vp, vp, vp, i32, vp, vp, vp]
         L.fk_stream_read.restype, L.fk_stream_read.argtypes = ctypes.c_int, [vp, sz, vp, vp]
         _lib = L
     return _lib
@@ -445,6 +462,117 @@ def fk_decode_step_acc(desc: CacheDesc, q, K, V, pos, length, k_new, v_new, pos_
 
 def fk_compact_acc(desc: CacheDesc, K, V, pos, acc, length, keep_idx, budget: int, stream=None) -> None:
     _call("fk_compact_acc", ctypes.byref(desc.c()), _ptr(K), _ptr(V), _ptr(pos), _ptr(acc), _ptr(length), _ptr(keep_idx), int(budget), _stream(stream))
+
+
+@dataclass
+class RopeDesc:
+    n_q_heads: int
+    n_kv_heads: int
+    head_dim: int
+    rotary_dim: int
+    layout: str  # 'half' (channels i and i + rotary_dim / 2 turn together) | 'interleaved' (2 i and 2 i + 1)
+    dtype: str  # 'f32' | 'bf16'
+    magnitude: float = 1.0
+    inverse: bool = False
+
+    def c(self, q, k, q_out, k_out) -> fk_rope_desc:
+        return fk_rope_desc(self.n_q_heads, self.n_kv_heads, self.head_dim, self.rotary_dim, {"half": 0, "interleaved": 1}[self.layout],
+                            FK_F32 if self.dtype == "f32" else FK_BF16, 1 if self.inverse else 0, float(self.magnitude),
+                            *(self._stride(x, n) for x, n in ((q, self.n_q_heads), (k, self.n_kv_heads), (q_out, self.n_q_heads), (k_out, self.n_kv_heads))))
+
+    def _stride(self, x, heads: int) -> int:
+        """Elements from token to token of x [n_tokens, heads, head_dim], whose heads lie side by side."""
+        if x is None or x.shape[0] < 2:
+            return 0
+        return int(x.stride(0))
+
+
+def _heads_ptr(x, desc: RopeDesc, heads: int) -> int:
+    if x is None:
+        return 0
+    assert x.is_cuda and tuple(x.shape[1:]) == (heads, desc.head_dim), "queries and keys are [n_tokens, heads, head_dim] device tensors"
+    assert x.numel() == 0 or (x.stride(2) == 1 and (heads == 1 or x.stride(1) == desc.head_dim)), "a token's heads must lie side by side"
+    return x.data_ptr()
+
+
+def rope_frequencies(rotary_dim: int, base: float = 10000.0, scaling: str = "none", factor: float = 1.0, context: float = 0.0, low: float = 1.0,
+                     high: float = 32.0) -> "torch.Tensor":
+    """Radians per position of every pair of channels, fp64 [rotary_dim / 2] on the host; scaling 'none' | 'linear' | 'base' | 'parts'."""
+    freq = torch.empty(max(int(rotary_dim) // 2, 1), dtype=torch.float64)
+    _check(lib().fk_rope_frequencies(int(rotary_dim), float(base), {"none": 0, "linear": 1, "base": 2, "parts": 3}[scaling], float(factor), float(context),
+                                     float(low), float(high), freq.data_ptr()), "fk_rope_frequencies")
+    return freq
+
+
+def fk_rope(desc: RopeDesc, q, k, pos, freq, q_out, k_out, stream=None) -> None:
+    """Rotary positions of q [n_tokens, n_q_heads, D] and k [n_tokens, n_kv_heads, D]; a token's heads lie side by side, tokens any distance apart.
+    pos [n_tokens] int32; freq fp64 [rotary_dim / 2] on the device; q_out may be q, k_out may be k."""
+    some = q if q is not None else k
+    _call("fk_rope", ctypes.byref(desc.c(q, k, q_out, k_out)), _heads_ptr(q, desc, desc.n_q_heads), _heads_ptr(k, desc, desc.n_kv_heads), _ptr(pos), _ptr(freq),
+          int(some.shape[0]), _heads_ptr(q_out, desc, desc.n_q_heads), _heads_ptr(k_out, desc, desc.n_kv_heads), _stream(stream))
+
+
+def fk_tree_attn_workspace(desc: CacheDesc, n_tokens: int, max_tree: int, max_len: int) -> int:
+    return int(lib().fk_tree_attn_workspace(ctypes.byref(desc.c()), int(n_tokens), int(max_tree), int(max_len)))
+
+
+def new_tree_attn_workspace(desc: CacheDesc, n_tokens: int, max_tree: int, max_len: int) -> "torch.Tensor":
+    return torch.empty(max(fk_tree_attn_workspace(desc, n_tokens, max_tree, max_len), 16), dtype=torch.uint8, device="cuda")
+
+
+def fk_tree_attn(desc: CacheDesc, q, K, V, length, k_tree, v_tree, parent, q_start, max_tree: int, max_len: int, softmax_scale: float, out, stats,
+                 workspace, stream=None) -> None:
+    """Attention of the nodes q [n_tokens, n_q_heads, D] of drafted trees over their sequence's rows and their own ancestors (k_tree, v_tree [n_tokens,
+    n_kv_heads, D]).  stats [n_tokens, n_q_heads, 2] fp32 or None."""
+    nbytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    _call("fk_tree_attn", ctypes.byref(desc.c()), _ptr(q), _ptr(K), _ptr(V), _ptr(length), _ptr(k_tree), _ptr(v_tree), _ptr(parent), _ptr(q_start),
+          int(q.shape[0]), int(max_tree), int(max_len), float(softmax_scale), _ptr(out), _ptr(stats), _ptr(workspace), nbytes, _stream(stream))
+
+
+def fk_paged_tree_attn_workspace(desc: PagedDesc, n_tokens: int, max_tree: int, max_len: int) -> int:
+    return int(lib().fk_paged_tree_attn_workspace(ctypes.byref(desc.c()), int(n_tokens), int(max_tree), int(max_len)))
+
+
+def new_paged_tree_attn_workspace(desc: PagedDesc, n_tokens: int, max_tree: int, max_len: int) -> "torch.Tensor":
+    return torch.empty(max(fk_paged_tree_attn_workspace(desc, n_tokens, max_tree, max_len), 16), dtype=torch.uint8, device="cuda")
+
+
+def fk_paged_tree_attn(desc: PagedDesc, q, K, V, page_table, kv_len, k_tree, v_tree, parent, q_start, max_tree: int, max_len: int, window: int, n_sink: int,
+                       softmax_scale: float, out, stats, workspace, stream=None) -> None:
+    """fk_tree_attn over the pages of a prompt; kv_len counts the pairs in the pages, none of the tree's."""
+    nbytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    _call("fk_paged_tree_attn", ctypes.byref(desc.c()), _ptr(q), _ptr(K), _ptr(V), _ptr(page_table), _ptr(kv_len), _ptr(k_tree), _ptr(v_tree), _ptr(parent),
+          _ptr(q_start), int(q.shape[0]), int(max_tree), int(max_len), int(window), int(n_sink), float(softmax_scale), _ptr(out), _ptr(stats), _ptr(workspace),
+          nbytes, _stream(stream))
+
+
+def fk_verify_drafts_workspace(batch: int, vocab: int) -> int:
+    return int(lib().fk_verify_drafts_workspace(int(batch), int(vocab)))
+
+
+def new_verify_workspace(batch: int, vocab: int) -> "torch.Tensor":
+    """Zero-filled device workspace for fk_verify_drafts (its counters must start at zero)."""
+    return torch.zeros(max(fk_verify_drafts_workspace(batch, vocab), 16), dtype=torch.uint8, device="cuda")
+
+
+def fk_verify_drafts(target, draft, tokens, parent, q_start, uniform, path, n_accepted, next_token, workspace, stream=None) -> None:
+    """Which nodes of the drafted trees target's probabilities accept, and the token behind them.  target, draft [n_tokens, vocab] fp32 (draft None: tokens
+    that were not drawn); tokens, parent, path [n_tokens] int32; uniform [n_tokens] fp32; n_accepted, next_token [batch] int32."""
+    nbytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    _call("fk_verify_drafts", int(q_start.shape[0]) - 1, int(target.shape[1]), _ptr(target), _ptr(draft), _ptr(tokens), _ptr(parent), _ptr(q_start),
+          int(target.shape[0]), _ptr(uniform), _ptr(path), _ptr(n_accepted), _ptr(next_token), _ptr(workspace), nbytes, _stream(stream))
+
+
+def fk_commit_drafts(desc: CacheDesc, K, V, pos, length, acc, k_tree, v_tree, q_start, path, n_accepted, pos_first, stream=None) -> None:
+    """The accepted paths' pairs join the rows; acc (accumulated weights, zero in the new slots) may be None."""
+    _call("fk_commit_drafts", ctypes.byref(desc.c()), _ptr(K), _ptr(V), _ptr(pos), _ptr(length), _ptr(acc), _ptr(k_tree), _ptr(v_tree), _ptr(q_start),
+          int(k_tree.shape[0]), _ptr(path), _ptr(n_accepted), _ptr(pos_first), _stream(stream))
+
+
+def fk_paged_commit_drafts(desc: PagedDesc, K, V, page_table, kv_len, k_tree, v_tree, q_start, path, n_accepted, stream=None) -> None:
+    """The accepted paths' pairs join the pages; kv_len goes up by as many."""
+    _call("fk_paged_commit_drafts", ctypes.byref(desc.c()), _ptr(K), _ptr(V), _ptr(page_table), _ptr(kv_len), _ptr(k_tree), _ptr(v_tree), _ptr(q_start),
+          int(k_tree.shape[0]), _ptr(path), _ptr(n_accepted), _stream(stream))
 
 
 def fk_stream_read(src, sink, stream=None) -> None:

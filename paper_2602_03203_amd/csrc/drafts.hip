@@ -1,0 +1,458 @@
+// fk_verify_drafts: which drafted tokens the large model's probabilities accept, and the token behind them.
+// fk_commit_drafts, fk_paged_commit_drafts: the pairs of the accepted path join the cache.
+#include "paged.h"
+
+#include <algorithm>
+
+namespace fk {
+
+static constexpr int kNodes = FK_TREE_NODES;
+
+// ---------------------------------------------------------------------------------------
+// Verification.  At a node with distributions p (target) and q (draft) the first child x, drawn from q, is accepted with probability
+// min(1, p(x) / q(x)); else what is left, r = max(p - q, 0) normalised, takes the place of p for the next child, and so on: the token that
+// comes out is distributed as p whatever q is (speculative sampling, with several drafts).  Only two numbers carry from
+// rejection to rejection: with r_k = max(p - c_k q, 0) / m_k, c_0 = 0, m_0 = 1,
+//     r_k+1 ~ max(r_k - q, 0) = max(p - (c_k + m_k) q, 0) / m_k,   so   c_k+1 = c_k + m_k,   m_k+1 = sum max(p - c_k+1 q, 0).
+// A child of a likeliest-token draft (no q) is accepted with probability p(x) / m; else p(x) becomes 0 and m goes down by it.
+// Sums and comparisons in 64 bits: a 32-bit sum over a vocabulary is off by more than its smaller probabilities.
+//
+// One launch.  A sequence's vocabulary is cut into chunks, a workgroup each.  Every workgroup walks the tree (a few hundred numbers, all sent for
+// together) up to the first rejection whose sum is not known, or to the end, and sums its chunk of what is left; the last one to
+// arrive adds the chunks' sums, walks on, sums again by itself where another rejection wants it, and draws the token.
+// ---------------------------------------------------------------------------------------
+static constexpr int kVerifyThreads = 256, kVerifyWaves = kVerifyThreads / kWave, kMostChunks = 64;
+
+struct VerifyParams {
+    const float *target, *draft;
+    const int32_t *tokens, *parent, *q_start;
+    const float* uniform;
+    int32_t *path, *accepted, *next;
+    int n_tokens, batch, vocab, chunks, chunk;   // chunk: numbers of a chunk, a multiple of 4
+    double* part;        // [batch][chunks]
+    uint32_t* arrived;   // [batch], zero between calls
+};
+
+struct Tree {            // in LDS
+    float p[kNodes], q[kNodes], u[kNodes];   // target's and draft's probability of a node's token behind its parent; its number
+    int token[kNodes];
+    short parent[kNodes], path[kNodes], gone[kNodes];
+    double part[kMostChunks], wave[kVerifyWaves];
+    double c, m, left;
+    int at, depth, n_gone, tried, state, chosen, first[kVerifyWaves];
+};
+
+// A step of the walk that needs no sums, by one thread: children of `at` from `tried` on.  state 1: a sum with the new c is wanted before the next child;
+// 2: no child is left.
+__device__ __forceinline__ void walk(Tree& T, int nodes, bool drawn) {
+    int at = T.at, i = T.tried;
+    for (;; ++i) {
+        while (i < nodes && T.parent[i] != at) ++i;
+        if (i >= nodes) break;
+        const double p = T.p[i], u = T.u[i];
+        bool yes;
+        if (drawn) {
+            yes = u * T.q[i] * T.m < p - T.c * T.q[i];
+        } else {
+            bool again = false;
+            for (int k = 0; k < T.n_gone; ++k) again |= T.token[T.gone[k]] == T.token[i];
+            yes = u * T.m < (again ? 0.0 : p);
+            if (!yes && !again) {
+                T.gone[T.n_gone++] = (short)i;
+                T.m = fmax(T.m - p, 0.0);
+            }
+        }
+        if (yes) {
+            T.path[T.depth++] = (short)i;
+            at = i;
+            T.c = 0.0;
+            T.m = 1.0;
+            T.n_gone = 0;
+        } else if (drawn) {
+            T.c += T.m;
+            T.at = at;
+            T.tried = i + 1;
+            T.state = 1;
+            return;
+        }
+    }
+    T.at = at;
+    T.state = 2;
+}
+
+// what is left of number v of the vocabulary at the current node
+__device__ __forceinline__ double left_of(const Tree& T, float p, float q, bool drawn) {
+    const double r = drawn ? (double)p - T.c * (double)q : (double)p;
+    return r > 0.0 ? r : 0.0;
+}
+__device__ __forceinline__ bool is_gone(const Tree& T, int v) {
+    bool x = false;
+    for (int k = 0; k < T.n_gone; ++k) x |= T.token[T.gone[k]] == v;
+    return x;
+}
+
+__device__ __forceinline__ double wave_sum(double x) {
+#pragma unroll
+    for (int off = 32; off > 0; off >>= 1) x += __shfl_xor(x, off);
+    return x;
+}
+
+__device__ __forceinline__ double wave_scan(double x) {   // inclusive
+    const int lane = threadIdx.x & (kWave - 1);
+#pragma unroll
+    for (int off = 1; off < kWave; off <<= 1) {
+        const double o = __shfl_up(x, off);
+        if (lane >= off) x += o;
+    }
+    return x;
+}
+
+typedef float vf32x4_t __attribute__((ext_vector_type(4), aligned(4)));   // rows of an odd vocabulary start anywhere
+
+// sum over a chunk by `threads` threads, of which this is number `t`
+__device__ __forceinline__ double chunk_sum(const VerifyParams& P, const Tree& T, size_t row, int chunk, int t, int threads) {
+    const bool drawn = P.draft != nullptr;
+    const float *p = P.target + row * P.vocab, *q = drawn ? P.draft + row * P.vocab : nullptr;
+    const int begin = chunk * P.chunk, end = min(begin + P.chunk, P.vocab), whole = begin + (max(end - begin, 0) & ~3);
+    double sum = 0.0;
+    for (int v = begin + t * 4; v < whole; v += threads * 4) {
+        const vf32x4_t a = *reinterpret_cast<const vf32x4_t*>(p + v);
+        vf32x4_t b = {0.f, 0.f, 0.f, 0.f};
+        if (drawn) b = *reinterpret_cast<const vf32x4_t*>(q + v);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) sum += T.n_gone && is_gone(T, v + j) ? 0.0 : left_of(T, a[j], b[j], drawn);
+    }
+    if (whole + t < end) sum += is_gone(T, whole + t) ? 0.0 : left_of(T, p[whole + t], drawn ? q[whole + t] : 0.f, drawn);
+    return sum;
+}
+
+__global__ __launch_bounds__(kVerifyThreads) void verify_kernel(const VerifyParams P) {
+    __shared__ Tree T;
+    __shared__ bool s_last;
+    const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = tid / kWave, b = blockIdx.y, chunk = blockIdx.x;
+    const bool drawn = P.draft != nullptr;
+    const int begin = min(max(P.q_start[b], 0), P.n_tokens), nodes = min(max(P.q_start[b + 1], begin), P.n_tokens) - begin;
+    if (nodes == 0 || nodes > kNodes) {
+        if (chunk == 0 && tid == 0) {
+            P.accepted[b] = 0;
+            P.next[b] = -1;
+        }
+        return;
+    }
+    for (int i = tid; i < nodes; i += kVerifyThreads) {
+        const int up = P.parent[begin + i], x = P.tokens[begin + i];
+        const bool there = i > 0 && up >= 0 && up < i && x >= 0 && x < P.vocab;
+        const size_t at = (size_t)(begin + (there ? up : 0)) * P.vocab + (there ? x : 0);
+        const float p = P.target[at];
+        T.p[i] = there && p > 0.f ? p : 0.f;
+        T.q[i] = there && drawn ? P.draft[at] : 0.f;
+        T.u[i] = P.uniform[begin + i];
+        T.token[i] = x;
+        T.parent[i] = (short)(i > 0 && up < i ? max(up, -1) : -1);
+    }
+    if (tid == 0) {
+        T.at = 0;
+        T.depth = 1;
+        T.path[0] = 0;
+        T.n_gone = 0;
+        T.tried = 1;
+        T.c = 0.0;
+        T.m = 1.0;
+    }
+    __syncthreads();
+    if (tid == 0) walk(T, nodes, drawn);
+    __syncthreads();
+    {
+        const double sum = wave_sum(chunk_sum(P, T, begin + T.at, chunk, tid, kVerifyThreads));
+        if (lane == 0) T.wave[wave] = sum;
+        __syncthreads();
+        if (tid == 0) {
+            double all = 0.0;
+            for (int w = 0; w < kVerifyWaves; ++w) all += T.wave[w];
+            __hip_atomic_store(&P.part[(size_t)b * P.chunks + chunk], all, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            const uint32_t before = __hip_atomic_fetch_add(&P.arrived[b], 1u, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT);
+            s_last = before == (uint32_t)P.chunks - 1;
+        }
+        __syncthreads();
+        if (!s_last) return;
+    }
+    if (tid == 0) __hip_atomic_store(&P.arrived[b], 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    if (tid < P.chunks) T.part[tid] = __hip_atomic_load(&P.part[(size_t)b * P.chunks + tid], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    __syncthreads();
+    for (;;) {   // T.part holds the sums of what is left at T.at
+        if (wave == 0) {
+            const double all = wave_sum(lane < P.chunks ? T.part[lane] : 0.0);
+            if (lane == 0) {
+                if (T.state == 1) {
+                    const int depth = T.depth;
+                    T.m = all;
+                    walk(T, nodes, drawn);
+                    if (T.state == 2 && T.depth == depth) T.state = 3;   // no child was left: the sums are those to draw from
+                } else {
+                    T.state = 3;
+                }
+                if (T.state == 3 && all == 0.0) {   // nothing is left, by rounding: the target's own distribution
+                    const bool own = T.c == 0.0 && T.n_gone == 0;
+                    T.c = 0.0;
+                    T.n_gone = 0;
+                    T.state = own ? 4 : 2;
+                }
+            }
+        }
+        __syncthreads();
+        if (T.state >= 3) break;
+        for (int c = wave; c < P.chunks; c += kVerifyWaves) {
+            const double sum = wave_sum(chunk_sum(P, T, begin + T.at, c, lane, kWave));
+            if (lane == 0) T.part[c] = sum;
+        }
+        __syncthreads();
+    }
+    for (int i = tid; i < nodes; i += kVerifyThreads) P.path[begin + i] = i < T.depth ? T.path[i] : -1;
+    if (tid == 0) P.accepted[b] = T.depth;
+    if (T.state == 4) {   // no mass at all
+        if (tid == 0) P.next[b] = -1;
+        return;
+    }
+    if (wave == 0) {   // the chunk that holds the number, the last one with anything where rounding leaves it beyond all
+        const double mine = lane < P.chunks ? T.part[lane] : 0.0, incl = wave_scan(mine), want = (double)T.u[0] * __shfl(incl, kWave - 1);
+        const unsigned long long hit = __ballot(mine > 0.0 && incl > want), any = __ballot(mine > 0.0);
+        const int chosen = hit ? __ffsll((long long)hit) - 1 : 63 - __clzll((long long)any);
+        if (lane == chosen) {
+            T.chosen = chosen;
+            T.left = want - (incl - mine);
+        }
+    }
+    __syncthreads();
+    // in it: four numbers a thread at a time
+    const size_t row = (size_t)(begin + T.at) * P.vocab;
+    const int end = min((T.chosen + 1) * P.chunk, P.vocab);
+    const double want = T.left;
+    double below = 0.0;
+    int found = -1;   // of this thread: the last number with anything, or the one
+    for (int v0 = T.chosen * P.chunk;; v0 += kVerifyThreads * 4) {
+        double r[4], sum = 0.0;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int v = v0 + tid * 4 + j;
+            r[j] = 0.0;
+            if (v < end && !is_gone(T, v)) r[j] = left_of(T, P.target[row + v], drawn ? P.draft[row + v] : 0.f, drawn);
+            if (r[j] > 0.0) found = v;
+            sum += r[j];
+        }
+        const double incl = wave_scan(sum);
+        __syncthreads();
+        if (lane == kWave - 1) T.wave[wave] = incl;
+        __syncthreads();
+        double before = below + incl - sum;
+        for (int w = 0; w < wave; ++w) before += T.wave[w];
+        int one = 0x7fffffff;
+#pragma unroll
+        for (int j = 3; j >= 0; --j) {
+            double to = before;
+            for (int k = 0; k <= j; ++k) to += r[k];
+            if (r[j] > 0.0 && to > want) one = v0 + tid * 4 + j;
+        }
+        for (int w = 0; w < kVerifyWaves; ++w) below += T.wave[w];
+        const unsigned long long hit = __ballot(one != 0x7fffffff);
+        if (hit) one = __shfl(one, __ffsll((long long)hit) - 1);
+        if (lane == 0) T.first[wave] = one;
+        __syncthreads();
+        int first = 0x7fffffff;
+        for (int w = 0; w < kVerifyWaves; ++w) first = min(first, T.first[w]);
+        if (first != 0x7fffffff) {
+            if (tid == 0) P.next[b] = first;
+            return;
+        }
+        if (v0 + kVerifyThreads * 4 >= end) break;
+    }
+    // rounding has left it beyond all: the last number with anything
+#pragma unroll
+    for (int off = 32; off > 0; off >>= 1) found = max(found, __shfl_xor(found, off));
+    __syncthreads();
+    if (lane == 0) T.first[wave] = found;
+    __syncthreads();
+    if (tid == 0) {
+        for (int w = 1; w < kVerifyWaves; ++w) found = max(found, T.first[w]);
+        P.next[b] = found;
+    }
+}
+
+// ---------------------------------------------------------------------------------------
+// Commit: bound by the latency of a chain of loads (length, path, pair); every accepted pair is read and written once.
+// ---------------------------------------------------------------------------------------
+typedef unsigned int du32x4_t __attribute__((ext_vector_type(4)));
+
+struct CommitParams {
+    void *K, *V;
+    int32_t *pos, *len;          // pages: len is kv_len
+    float* acc;
+    const void *k_tree, *v_tree;
+    const int32_t *q_start, *path, *accepted, *pos_first;
+    int n_tokens, batch, n_kv, cap;
+    // pages
+    const int32_t* table;
+    int page_shift, n_pages, max_pages;
+};
+
+// nodes of the path, up to the first entry that is none; all lanes of the first wavefront
+__device__ __forceinline__ int path_length(const CommitParams& P, int b, int begin, int nodes) {
+    const int lane = threadIdx.x & (kWave - 1), n = min(max(P.accepted[b], 0), nodes);
+    for (int i0 = 0; i0 < n; i0 += kWave) {
+        const int node = i0 + lane < n ? P.path[begin + i0 + lane] : 0;
+        const unsigned long long bad = __ballot(node < 0 || node >= nodes);
+        if (bad) return i0 + __ffsll((long long)bad) - 1;
+    }
+    return n;
+}
+
+template <int CH>
+__global__ __launch_bounds__(256) void commit_rows_kernel(const CommitParams P) {
+    __shared__ int s_count;
+    const int tid = threadIdx.x, row = blockIdx.x, b = row / P.n_kv, h = row - b * P.n_kv;
+    const int begin = min(max(P.q_start[b], 0), P.n_tokens), nodes = min(max(P.q_start[b + 1], begin), P.n_tokens) - begin;
+    const int start = P.len[row];
+    if (tid < kWave) {
+        const int n = path_length(P, b, begin, nodes);
+        if (tid == 0) s_count = start < 0 ? 0 : min(n, max(P.cap - start, 0));
+    }
+    __syncthreads();
+    const int n = s_count;
+    const du32x4_t *k = reinterpret_cast<const du32x4_t*>(P.k_tree), *v = reinterpret_cast<const du32x4_t*>(P.v_tree);
+    du32x4_t *K = reinterpret_cast<du32x4_t*>(P.K), *V = reinterpret_cast<du32x4_t*>(P.V);
+    for (int x = tid; x < n * CH; x += 256) {
+        const int i = x / CH, c = x % CH;
+        const size_t from = ((size_t)(begin + P.path[begin + i]) * P.n_kv + h) * CH + c, to = ((size_t)row * P.cap + start + i) * CH + c;
+        K[to] = k[from];
+        V[to] = v[from];
+    }
+    const int first = P.pos_first[b];
+    for (int i = tid; i < n; i += 256) {
+        P.pos[(size_t)row * P.cap + start + i] = first + i;
+        if (P.acc) P.acc[(size_t)row * P.cap + start + i] = 0.f;
+    }
+    if (tid == 0 && n > 0) P.len[row] = start + n;   // (this workgroup alone reads it)
+}
+
+template <int CH>
+__global__ __launch_bounds__(1024) void commit_pages_kernel(const CommitParams P) {
+    __shared__ int s_count;
+    const int tid = threadIdx.x, b = blockIdx.x;
+    const int begin = min(max(P.q_start[b], 0), P.n_tokens), nodes = min(max(P.q_start[b + 1], begin), P.n_tokens) - begin;
+    const int start = P.len[b], most = P.max_pages << P.page_shift;
+    if (tid < kWave) {
+        const int n = path_length(P, b, begin, nodes);
+        if (tid == 0) s_count = start < 0 ? 0 : min(n, max(most - start, 0));
+    }
+    __syncthreads();
+    const int n = s_count, row = P.n_kv * CH;
+    const du32x4_t *k = reinterpret_cast<const du32x4_t*>(P.k_tree), *v = reinterpret_cast<const du32x4_t*>(P.v_tree);
+    du32x4_t *K = reinterpret_cast<du32x4_t*>(P.K), *V = reinterpret_cast<du32x4_t*>(P.V);
+    for (int x = tid; x < n * row; x += 1024) {
+        const int i = x / row, hc = x - i * row, h = hc / CH, p = start + i;
+        const int page = P.table[(size_t)b * P.max_pages + (p >> P.page_shift)];
+        if ((unsigned)page >= (unsigned)P.n_pages) continue;
+        const size_t from = (size_t)(begin + P.path[begin + i]) * row + hc;
+        const size_t to = ((((size_t)page * P.n_kv + h) << P.page_shift) + (p & ((1 << P.page_shift) - 1))) * CH + hc % CH;
+        K[to] = k[from];
+        V[to] = v[from];
+    }
+    if (tid == 0 && n > 0) P.len[b] = start + n;
+}
+
+static int verify_chunks(int vocab) { return std::min(std::max((vocab + 2047) / 2048, 1), kMostChunks); }
+
+}  // namespace fk
+
+using namespace fk;
+
+extern "C" size_t fk_verify_drafts_workspace(int32_t batch, int32_t vocab) {
+    if (batch <= 0 || vocab <= 0) return 0;
+    return ((size_t)batch * sizeof(uint32_t) + 255) / 256 * 256 + (size_t)batch * verify_chunks(vocab) * sizeof(double);
+}
+
+extern "C" fk_status fk_verify_drafts(int32_t batch, int32_t vocab, const float* target, const float* draft, const int32_t* tokens,
+                                      const int32_t* parent, const int32_t* q_start, int32_t n_tokens, const float* uniform, int32_t* path,
+                                      int32_t* n_accepted, int32_t* next_token, void* workspace, size_t workspace_bytes, void* stream) {
+    if (batch <= 0 || vocab <= 0 || n_tokens < 0) return FK_ERR_INVALID_ARG;
+    if (vocab >= (1 << 30) || batch > 65535) return FK_ERR_UNSUPPORTED;
+    if (!q_start || !n_accepted || !next_token) return FK_ERR_INVALID_ARG;
+    if (n_tokens > 0 && (!target || !tokens || !parent || !uniform || !path)) return FK_ERR_INVALID_ARG;
+    if (!workspace || workspace_bytes < fk_verify_drafts_workspace(batch, vocab) || !aligned16(workspace)) return FK_ERR_WORKSPACE;
+    VerifyParams P = {target, draft, tokens, parent, q_start, uniform, path, n_accepted, next_token, n_tokens, batch, vocab, verify_chunks(vocab), 0, nullptr, nullptr};
+    P.chunk = ((vocab + P.chunks - 1) / P.chunks + 3) / 4 * 4;
+    P.arrived = static_cast<uint32_t*>(workspace);
+    P.part = reinterpret_cast<double*>(static_cast<char*>(workspace) + ((size_t)batch * sizeof(uint32_t) + 255) / 256 * 256);
+    hipLaunchKernelGGL(verify_kernel, dim3(P.chunks, batch), dim3(kVerifyThreads), 0, (hipStream_t)stream, P);
+    return launch_status();
+}
+
+extern "C" fk_status fk_commit_drafts(const fk_cache_desc* desc, void* K, void* V, int32_t* pos, int32_t* len, float* acc, const void* k_tree,
+                                      const void* v_tree, const int32_t* q_start, int32_t n_tokens, const int32_t* path, const int32_t* n_accepted,
+                                      const int32_t* pos_first, void* stream) {
+    const fk_status s = check_desc(desc);
+    if (s != FK_OK) return s;
+    if ((int64_t)desc->batch * desc->n_kv_heads >= (1 << 24)) return FK_ERR_UNSUPPORTED;
+    if (n_tokens < 0 || !K || !V || !pos || !len || !q_start || !n_accepted || !pos_first) return FK_ERR_INVALID_ARG;
+    if (n_tokens > 0 && (!k_tree || !v_tree || !path)) return FK_ERR_INVALID_ARG;
+    if (!aligned16(K) || !aligned16(V) || !aligned16(k_tree) || !aligned16(v_tree)) return FK_ERR_INVALID_ARG;
+    if (n_tokens == 0) return FK_OK;
+    CommitParams P = {};
+    P.K = K;
+    P.V = V;
+    P.pos = pos;
+    P.len = len;
+    P.acc = acc;
+    P.k_tree = k_tree;
+    P.v_tree = v_tree;
+    P.q_start = q_start;
+    P.path = path;
+    P.accepted = n_accepted;
+    P.pos_first = pos_first;
+    P.n_tokens = n_tokens;
+    P.batch = desc->batch;
+    P.n_kv = desc->n_kv_heads;
+    P.cap = desc->capacity;
+    const dim3 grid(desc->batch * desc->n_kv_heads);
+    hipStream_t st = (hipStream_t)stream;
+    switch (desc->head_dim * (desc->dtype == FK_F32 ? 4 : 2) / 16) {
+        case 8: hipLaunchKernelGGL(commit_rows_kernel<8>, grid, dim3(256), 0, st, P); break;
+        case 16: hipLaunchKernelGGL(commit_rows_kernel<16>, grid, dim3(256), 0, st, P); break;
+        default: hipLaunchKernelGGL(commit_rows_kernel<32>, grid, dim3(256), 0, st, P); break;
+    }
+    return launch_status();
+}
+
+extern "C" fk_status fk_paged_commit_drafts(const fk_paged_desc* desc, void* K, void* V, const int32_t* page_table, int32_t* kv_len,
+                                            const void* k_tree, const void* v_tree, const int32_t* q_start, int32_t n_tokens,
+                                            const int32_t* path, const int32_t* n_accepted, void* stream) {
+    const fk_status s = check_paged(desc);
+    if (s != FK_OK) return s;
+    if (desc->n_kv_heads >= (1 << 16)) return FK_ERR_UNSUPPORTED;
+    if (n_tokens < 0 || !K || !V || !page_table || !kv_len || !q_start || !n_accepted) return FK_ERR_INVALID_ARG;
+    if (n_tokens > 0 && (!k_tree || !v_tree || !path)) return FK_ERR_INVALID_ARG;
+    if (!aligned16(K) || !aligned16(V) || !aligned16(k_tree) || !aligned16(v_tree)) return FK_ERR_INVALID_ARG;
+    if (n_tokens == 0) return FK_OK;
+    CommitParams P = {};
+    P.K = K;
+    P.V = V;
+    P.len = kv_len;
+    P.k_tree = k_tree;
+    P.v_tree = v_tree;
+    P.q_start = q_start;
+    P.path = path;
+    P.accepted = n_accepted;
+    P.n_tokens = n_tokens;
+    P.batch = desc->batch;
+    P.n_kv = desc->n_kv_heads;
+    P.table = page_table;
+    P.page_shift = __builtin_ctz(desc->page_size);
+    P.n_pages = desc->n_pages;
+    P.max_pages = desc->max_pages;
+    hipStream_t st = (hipStream_t)stream;
+    switch (desc->head_dim * (desc->dtype == FK_F32 ? 4 : 2) / 16) {
+        case 8: hipLaunchKernelGGL(commit_pages_kernel<8>, dim3(desc->batch), dim3(1024), 0, st, P); break;
+        case 16: hipLaunchKernelGGL(commit_pages_kernel<16>, dim3(desc->batch), dim3(1024), 0, st, P); break;
+        default: hipLaunchKernelGGL(commit_pages_kernel<32>, dim3(desc->batch), dim3(1024), 0, st, P); break;
+    }
+    return launch_status();
+}
