@@ -1,13 +1,12 @@
 // Attention of trees of drafted tokens over a cache: the rows of a budgeted cache or the pages of a prompt (fk_tree_attn, fk_paged_tree_attn).
 //
-// The query rows of a (tree, KV head) are its nodes times the heads of the group; a workgroup takes RB * 16 of them and a split of what they
+// The query rows of a (tree, KV head) are its nodes times the heads of the group; a workgroup takes a tile of them and a split of what they
 // see: the pairs of the cache, which all nodes see (but for a window), then the pairs of the tree, a node its ancestors' and its own.
-// Its wavefronts take tiles of KT pairs in turn, straight from memory into registers, each with its own online softmax for all rows; they are
-// merged through LDS at the end.  Products and operand layouts are those of thin.h: logits K.Q^T with the keys in an order that makes a
-// lane's probabilities an operand of V^T.P^T as they are; an operand of K or V serves a product for each 16 rows.
-// Which ancestors a node has is a bit for every node of its tree: found once per workgroup, in LDS, by walking up from it.
+// Products and operand layouts are those of thin.h: logits K.Q^T with the keys in an order that makes a lane's probabilities an operand of V^T.P^T as
+// they are.  Which ancestors a node has is a bit for every node of its tree: found once per workgroup, in LDS, by walking up from it.
 #pragma once
 #include "attn_paged.h"
+#include "prompt.h"
 #include <type_traits>
 
 namespace fk {
@@ -20,6 +19,94 @@ struct TreeParams {
     const void *k_tree, *v_tree;
 };
 
+// What a workgroup works on; false: nothing
+struct TreeWork {
+    TileOf t;
+    int h, n;                  // KV head, pairs of the cache
+    int r0, rows;              // query rows of the tile
+    int tok_lo, tok_hi;        // nodes that they belong to
+    KeyTiles old;              // tiles of the cache's pairs
+    int total, splits;         // with those of the tree
+};
+template <bool ROWS>
+__device__ __forceinline__ bool tree_work(const AttnPagedParams& P, int item, int tm, TreeWork& w) {
+    const PagedParams& W = P.view;
+    const int slot = scalar(divide(item, W.n_kv, W.kv_magic));
+    w.h = item - slot * W.n_kv;
+    if (!tile_of(W, P.grid, slot, tm, w.t)) return false;
+    if constexpr (ROWS) w.t.n = scalar(min(max(load_uniform(W.kv_len, w.t.b * W.n_kv + w.h), 0), P.cap));
+    w.n = w.t.n;
+    return true;
+}
+__device__ __forceinline__ void tree_tile_of(const AttnPagedParams& P, int tm, int kt, TreeWork& w) {
+    const PagedParams& W = P.view;
+    w.r0 = w.t.tile * tm;
+    w.rows = min(tm, w.t.nq * W.g - w.r0);
+    w.tok_lo = scalar(divide(w.r0, W.g, W.g_magic));
+    w.tok_hi = scalar(divide(w.r0 + w.rows - 1, W.g, W.g_magic));
+    w.old = key_tiles(W, w.n, w.n - 1, kt);   // (the root, at position n, sees the most under a window)
+    w.total = w.old.total + (uint32_t)(w.tok_hi + kt) / (uint32_t)kt;   // (parents come first: nobody sees a later node)
+    w.splits = scalar(splits_of(w.total, w.t.one ? P.splits : 1, P.split_shift));
+}
+
+// In LDS: of a tile's nodes, counted from its first one, whom they see of their tree
+template <int TM> struct Ancestors {
+    int16_t parent[kTreeNodes];
+    uint32_t sees[TM][kTreeNodes / 32];
+    uint32_t any[kTreeNodes / 32], all[kTreeNodes / 32];   // of a run's nodes some see, all see
+    int level[TM];             // under a window
+};
+template <int TM> __device__ __forceinline__ void find_ancestors(const TreeParams& TP, const TreeWork& w, bool windowed, Ancestors<TM>& s) {
+    const PagedParams& W = TP.a.view;
+    for (int i = threadIdx.x; i <= w.tok_hi; i += 256) {
+        const int p = TP.parent[w.t.begin + i];
+        s.parent[i] = (int16_t)(p < i ? max(p, -1) : -1);
+    }
+    __syncthreads();
+    for (int i = threadIdx.x; i <= w.tok_hi - w.tok_lo; i += 256) {
+        const int self = w.tok_lo + i;
+        int level = 0;
+        if (windowed) {
+            for (int a = s.parent[self]; a >= 0; a = s.parent[a]) ++level;
+            s.level[i] = level;
+        }
+#pragma unroll
+        for (int x = 0; x < kTreeNodes / 32; ++x) s.sees[i][x] = 0;
+        int up = 0;   // levels from the node to its ancestor
+        for (int a = self; a >= 0; a = s.parent[a], ++up)
+            if (!windowed || up < W.window || w.n + level - up < W.sink) s.sees[i][a / 32] |= 1u << a % 32;
+    }
+    __syncthreads();
+}
+// A run's nodes lo .. hi, counted from the tile's first: what they see together.  level_lo, level_hi: their levels, under a window
+template <int TM> __device__ __forceinline__ void span_of(Ancestors<TM>& s, bool windowed, int lo, int hi, int& level_lo, int& level_hi) {
+    if (threadIdx.x < kTreeNodes / 32) {
+        s.any[threadIdx.x] = 0;
+        s.all[threadIdx.x] = ~0u;
+    }
+    __syncthreads();
+    for (int i = lo * (kTreeNodes / 32) + threadIdx.x; i < (hi + 1) * (kTreeNodes / 32); i += 256) {
+        const uint32_t x = s.sees[0][i];
+        atomicOr(&s.any[i % (kTreeNodes / 32)], x);
+        atomicAnd(&s.all[i % (kTreeNodes / 32)], x);
+    }
+    level_lo = level_hi = 0;
+    if (windowed) {
+        level_lo = level_hi = s.level[lo];
+        for (int i = lo + 1; i <= hi; ++i) {
+            level_lo = min(level_lo, s.level[i]);
+            level_hi = max(level_hi, s.level[i]);
+        }
+        level_lo = scalar(level_lo);
+        level_hi = scalar(level_hi);
+    }
+    __syncthreads();
+}
+
+// ---------------------------------------------------------------------------------------------------------
+// Up to RB * 16 query rows: the wavefronts of a workgroup take tiles of KT pairs in turn, straight from memory into registers, each with its own
+// online softmax for all rows; they are merged through LDS at the end.  An operand of K or V serves a product for each 16 rows.
+// ---------------------------------------------------------------------------------------------------------
 template <typename T, int D, int RB> struct TreeCfg {
     static constexpr bool BF = sizeof(T) == 2;
     static constexpr int CH = D * (int)sizeof(T) / 16;   // 16-byte chunks of a row
@@ -33,36 +120,6 @@ template <typename T, int D, int RB> struct TreeCfg {
     // LDS: partial outputs [WAVES][TM][PART] | maxima, sums, merge weights [WAVES][TM] each | merged maxima and sums [TM] each
     static constexpr size_t LDS = sizeof(float) * ((size_t)WAVES * TM * PART + 3 * WAVES * TM + 2 * TM);
 };
-
-// What a workgroup works on; false: nothing
-struct TreeWork {
-    TileOf t;
-    int h, n;                  // KV head, pairs of the cache
-    int r0, rows;              // query rows of the tile
-    int tok_lo, tok_hi;        // nodes that they belong to
-    KeyTiles old;              // tiles of the cache's pairs
-    int total, splits;         // with those of the tree
-};
-template <bool ROWS, int TM, int KT>
-__device__ __forceinline__ bool tree_work(const AttnPagedParams& P, int item, TreeWork& w) {
-    const PagedParams& W = P.view;
-    const int slot = scalar(divide(item, W.n_kv, W.kv_magic));
-    w.h = item - slot * W.n_kv;
-    if (!tile_of(W, P.grid, slot, TM, w.t)) return false;
-    if constexpr (ROWS) w.t.n = scalar(min(max(load_uniform(W.kv_len, w.t.b * W.n_kv + w.h), 0), P.cap));
-    w.n = w.t.n;
-    return true;
-}
-template <int TM, int KT> __device__ __forceinline__ void tree_tile_of(const AttnPagedParams& P, TreeWork& w) {
-    const PagedParams& W = P.view;
-    w.r0 = w.t.tile * TM;
-    w.rows = min(TM, w.t.nq * W.g - w.r0);
-    w.tok_lo = scalar(divide(w.r0, W.g, W.g_magic));
-    w.tok_hi = scalar(divide(w.r0 + w.rows - 1, W.g, W.g_magic));
-    w.old = key_tiles(W, w.n, w.n - 1, KT);   // (the root, at position n, sees the most under a window)
-    w.total = w.old.total + (uint32_t)(w.tok_hi + KT) / (uint32_t)KT;   // (parents come first: nobody sees a later node)
-    w.splits = scalar(splits_of(w.total, w.t.one ? P.splits : 1, P.split_shift));
-}
 
 template <typename T, int D, int RB, bool ROWS>
 __device__ __forceinline__ void tree_tile(const TreeParams& TP, int item, int split) {
@@ -78,21 +135,18 @@ __device__ __forceinline__ void tree_tile(const TreeParams& TP, int item, int sp
     float (*s_o)[TM][PART] = reinterpret_cast<float (*)[TM][PART]>(smem_tree);
     float (*s_m)[TM] = reinterpret_cast<float (*)[TM]>(smem_tree + WAVES * TM * PART), (*s_l)[TM] = s_m + WAVES, (*s_w)[TM] = s_l + WAVES;
     float *s_M = s_w[WAVES], *s_L = s_M + TM;
-    __shared__ int16_t s_parent[kTreeNodes];
-    __shared__ uint32_t s_sees[TM][kTreeNodes / 32];   // nodes that the tile's nodes see
-    __shared__ int s_level[TM];
+    __shared__ Ancestors<TM> s_tree;
+    __shared__ int s_bad;   // a value that not every row of a run sees is infinite or NaN
 
     TreeWork w;
-    if (!tree_work<ROWS, TM, KT>(P, item, w)) return;
+    if (!tree_work<ROWS>(P, item, TM, w)) return;
     const TileOf& t = w.t;
     const int n = w.n, h = w.h;
     const bool windowed = !ROWS && W.window != 0x7fffffff;
-    const tu32x4_t *Kp = reinterpret_cast<const tu32x4_t*>(W.K), *Vp = reinterpret_cast<const tu32x4_t*>(W.V);
-    const tu32x4_t* k_tree = reinterpret_cast<const tu32x4_t*>(TP.k_tree) + ((size_t)t.begin * n_kv + h) * CH;
-    const tu32x4_t* v_tree = reinterpret_cast<const tu32x4_t*>(TP.v_tree) + ((size_t)t.begin * n_kv + h) * CH;
+    const size_t tree_at = ((size_t)t.begin * n_kv + h) * CH;
     const int32_t* tab = ROWS ? nullptr : scalar_ptr(W.table + (size_t)t.b * W.max_pages);
     for (; w.t.tile >= 0; w.t.tile -= w.t.step) {
-        tree_tile_of<TM, KT>(P, w);
+        tree_tile_of(P, TM, KT, w);
         if (split >= w.splits) continue;
         const int r0 = w.r0, rows = w.rows, splits = w.splits, total = w.total;
         const int per = splits == 1 ? total : scalar(divide(total + splits - 1, splits)), t_begin = min(split * per, total), t_end = min(t_begin + per, total);
@@ -113,43 +167,9 @@ __device__ __forceinline__ void tree_tile(const TreeParams& TP, int item, int sp
         }
         const float scale = W.scale_log2e;
 
-        // who sees whom
-        if (windowed || t_end > w.old.total) {
-            for (int i = tid; i <= w.tok_hi; i += WAVES * kWave) {
-                const int p = TP.parent[t.begin + i];
-                s_parent[i] = (int16_t)(p < i ? max(p, -1) : -1);
-            }
-            __syncthreads();
-            for (int i = tid; i <= w.tok_hi - w.tok_lo; i += WAVES * kWave) {
-                const int self = w.tok_lo + i;
-                int level = 0;
-                if (windowed)
-                    for (int a = s_parent[self]; a >= 0; a = s_parent[a]) ++level;
-#pragma unroll
-                for (int x = 0; x < kTreeNodes / 32; ++x) s_sees[i][x] = 0;
-                int up = 0;   // levels from the node to its ancestor
-                for (int a = self; a >= 0; a = s_parent[a], ++up)
-                    if (!windowed || up < W.window || n + level - up < W.sink) s_sees[i][a / 32] |= 1u << a % 32;
-                s_level[i] = level;
-            }
-            __syncthreads();
-        }
-        int from[RB];   // a lane's rows see pairs of the cache from here on (and the sinks)
-        int top_level = 0;
-#pragma unroll
-        for (int rb = 0; rb < RB; ++rb) from[rb] = windowed ? n + s_level[tok[rb]] - W.window + 1 : 0;
-        if (windowed) {
-#pragma unroll
-            for (int rb = 0; rb < RB; ++rb) top_level = max(top_level, s_level[tok[rb]]);
-#pragma unroll
-            for (int off = 1; off < 16; off <<= 1) top_level = max(top_level, __shfl_xor(top_level, off));
-            top_level = scalar(top_level);
-        }
-        const int all_from = windowed ? n + top_level - W.window + 1 : 0, any_from = windowed ? n - W.window + 1 : 0;
-
-        // where a tile's pairs lie: pair u at the first (u < 16) or second run + min(u, last) * stride; `hole`: a bit for each run that lies nowhere
+        // where a tile's pairs lie: pair u of run u / 16 at at[run] + min(u, last) * stride, counted in 16 bytes of K and V; a bit for each run that lies nowhere
         struct Place {
-            const tu32x4_t *k[NT], *v[NT];
+            size_t at[NT];
             int stride, last, base, holes;
             bool tree;
         };
@@ -162,10 +182,7 @@ __device__ __forceinline__ void tree_tile(const TreeParams& TP, int item, int sp
                 p.stride = n_kv * CH;
                 p.last = t.nq - 1 - p.base;
 #pragma unroll
-                for (int r = 0; r < NT; ++r) {
-                    p.k[r] = k_tree + (size_t)p.base * p.stride;
-                    p.v[r] = v_tree + (size_t)p.base * p.stride;
-                }
+                for (int r = 0; r < NT; ++r) p.at[r] = tree_at + (size_t)p.base * p.stride;
                 return p;
             }
             p.base = w.old.at(i) * KT;
@@ -173,37 +190,36 @@ __device__ __forceinline__ void tree_tile(const TreeParams& TP, int item, int sp
             p.last = ROWS ? n - 1 - p.base : KT;
 #pragma unroll
             for (int r = 0; r < NT; ++r) {
-                size_t pair;
                 if constexpr (ROWS) {
-                    pair = ((size_t)t.b * n_kv + h) * P.cap + p.base;
+                    p.at[r] = (((size_t)t.b * n_kv + h) * P.cap + p.base) * CH;
                 } else {
                     const int key = p.base + r * 16, page = load_uniform(tab, min(key >> W.page_shift, W.max_pages - 1));
                     const bool ok = page_ok(W, page);
                     if (!ok) p.holes |= 1 << r;
-                    pair = ((((size_t)(ok ? page : 0) * n_kv + h) << W.page_shift) + (key & ((1 << W.page_shift) - 1)));
+                    p.at[r] = ((((size_t)(ok ? page : 0) * n_kv + h) << W.page_shift) + (key & ((1 << W.page_shift) - 1))) * CH - r * 16 * CH;
                 }
-                p.k[r] = Kp + pair * CH - (ROWS ? 0 : r * 16 * CH);
-                p.v[r] = Vp + pair * CH - (ROWS ? 0 : r * 16 * CH);
             }
             return p;
         };
         T128 kr[NT][KS], vr[VL];
         auto load_k = [&](const Place& p) {
-            const tu32x4_t* run = NT == 2 && n16 >= 8 ? p.k[NT - 1] : p.k[0];
+            const tu32x4_t* run = static_cast<const tu32x4_t*>(p.tree ? TP.k_tree : W.K) + (!ROWS && NT == 2 && n16 >= 8 ? p.at[NT - 1] : p.at[0]);
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) {
                 const int key = BF ? n16 / 4 * 8 + nt * 4 + n16 % 4 : n16;   // with this order, a lane's logits are keys quad * 8 + u (fp32: quad * 4 + i)
-                const tu32x4_t* x = run + (size_t)(uint32_t)(min(key, p.last) * p.stride);
+                const tu32x4_t* x = run + (uint32_t)(min(key, p.last) * p.stride);
 #pragma unroll
                 for (int ks = 0; ks < KS; ++ks) kr[nt][ks].u = x[ks * 4 + quad];
             }
         };
-        auto v_run = [&](const Place& p, int quad) { return NT == 2 && quad >= 2 ? p.v[NT - 1] : p.v[0]; };
+        auto v_run = [&](const Place& p, int quad) {
+            return static_cast<const tu32x4_t*>(p.tree ? TP.v_tree : W.V) + (!ROWS && NT == 2 && quad >= 2 ? p.at[NT - 1] : p.at[0]);
+        };
         auto load_v = [&](const Place& p) {
             const tu32x4_t* run = v_run(p, quad);
 #pragma unroll
             for (int u = 0; u < (BF ? 8 : 4); ++u) {
-                const tu32x4_t* x = run + (size_t)(uint32_t)(min(quad * (BF ? 8 : 4) + u, p.last) * p.stride);
+                const tu32x4_t* x = run + (uint32_t)(min(quad * (BF ? 8 : 4) + u, p.last) * p.stride);
                 if constexpr (!BF) {
 #pragma unroll
                     for (int c = 0; c < D / 64; ++c) vr[u * (D / 64) + c].u = x[c * 16 + n16];
@@ -218,10 +234,25 @@ __device__ __forceinline__ void tree_tile(const TreeParams& TP, int item, int sp
         };
         constexpr int VW = BF && D == 64 ? 2 : 4;   // words in use of a V load
 
+        // The rows of all nodes at once.  A row gives the pairs that it does not see weight 0, which must not meet an infinity or a NaN that another row
+        // sees: where there is any, the run starts over with half of its nodes.
+        const int nodes = w.tok_hi - w.tok_lo + 1;
+        const bool some_tree = t_end > w.old.total;
+        if (windowed || some_tree) find_ancestors<TM>(TP, w, windowed, s_tree);
+        for (int lo = 0, hi = nodes - 1;;) {
+        int level_lo = 0, level_hi = 0;
+        if (tid == 0) s_bad = 0;
+        if (windowed || some_tree) span_of<TM>(s_tree, windowed, lo, hi, level_lo, level_hi);
+        else __syncthreads();
+        const int any_from = windowed ? n + level_lo - W.window + 1 : 0, all_from = windowed ? n + level_hi - W.window + 1 : 0;
+        bool mine[RB];   // this run's rows
+        int from[RB];    // they see pairs of the cache from here on (and the sinks)
         float m_run[RB], l_run[RB];
         tf32x4_t o[RB][ET];
 #pragma unroll
         for (int rb = 0; rb < RB; ++rb) {
+            mine[rb] = tok[rb] >= lo && tok[rb] <= hi;
+            from[rb] = windowed ? n + s_tree.level[tok[rb]] - W.window + 1 : 0;
             m_run[rb] = -INFINITY;
             l_run[rb] = 0.f;
 #pragma unroll
@@ -234,7 +265,7 @@ __device__ __forceinline__ void tree_tile(const TreeParams& TP, int item, int sp
             load_k(at);
             load_v(at);
         }
-        for (; i < t_end; i += WAVES) {
+        auto tile = [&](auto LAST) {   // (twice in the code: under a condition the next tile's loads would need registers of their own)
             tf32x4_t c[RB][NT];
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt)
@@ -251,9 +282,10 @@ __device__ __forceinline__ void tree_tile(const TreeParams& TP, int item, int sp
                         }
                     }
                 }
-            const bool more = i + WAVES < t_end;
-            next = place_of(more ? i + WAVES : i);
-            if (more) load_k(next);
+            if constexpr (!LAST) {
+                next = place_of(i + WAVES);
+                load_k(next);
+            }
 
             float s[RB][NT * 4];
 #pragma unroll
@@ -262,51 +294,44 @@ __device__ __forceinline__ void tree_tile(const TreeParams& TP, int item, int sp
                 for (int j = 0; j < NT * 4; ++j) s[rb][j] = attn_logit(c[rb][j / 4][j % 4], scale);
             // everything seen by every row: no masks
             const bool whole = !at.tree && at.base + KT <= n && !at.holes && (at.base >= all_from || at.base + KT <= W.sink);
-            uint32_t sees[RB];   // a bit for each of the lane's keys
-            bool bad = false;    // a value that not every row sees is infinite or NaN
             if (!whole) {
                 const int k0 = quad * (NT * 4);   // first of the lane's keys in the tile
-                if (at.tree) {
+                const bool there = !(at.holes >> (NT == 2 && quad >= 2 ? 1 : 0) & 1);   // (its keys of K and of V lie in the same run)
 #pragma unroll
-                    for (int rb = 0; rb < RB; ++rb) sees[rb] = s_sees[tok[rb]][at.base / 32] >> (at.base % 32 + k0);
-                } else {
-                    const bool there = !(at.holes >> (NT == 2 && quad >= 2 ? 1 : 0) & 1);
-#pragma unroll
-                    for (int rb = 0; rb < RB; ++rb) {
-                        sees[rb] = 0;
+                for (int rb = 0; rb < RB; ++rb) {
+                    uint32_t sees = 0;   // a bit for each of the lane's keys
+                    if (at.tree) {
+                        sees = s_tree.sees[tok[rb]][at.base / 32] >> (at.base % 32 + k0);
+                    } else {
 #pragma unroll
                         for (int j = 0; j < NT * 4; ++j) {
                             const int key = at.base + k0 + j;
-                            sees[rb] |= (uint32_t)(there & (key < n) & ((key >= from[rb]) | (key < W.sink))) << j;
+                            sees |= (uint32_t)(there & (key < n) & ((key >= from[rb]) | (key < W.sink))) << j;
                         }
                     }
+                    if (!mine[rb]) sees = 0;
+#pragma unroll
+                    for (int j = 0; j < NT * 4; ++j) s[rb][j] = sees >> j & 1 ? s[rb][j] : -INFINITY;
                 }
-#pragma unroll
-                for (int rb = 0; rb < RB; ++rb)
-#pragma unroll
-                    for (int j = 0; j < NT * 4; ++j) s[rb][j] = sees[rb] >> j & 1 ? s[rb][j] : -INFINITY;
-                // values of weight 0 must not meet the products as infinities or NaN: what nobody sees is cleared, of what some see the numbers stay
+                bool bad = false;
+                uint32_t any = ~0u, all = 0;
+                if (at.tree) {
+                    any = s_tree.any[at.base / 32] >> (at.base % 32 + k0);
+                    all = s_tree.all[at.base / 32] >> (at.base % 32 + k0);
+                }
 #pragma unroll
                 for (int x = 0; x < VL; ++x) {
-                    const int u = BF ? quad * 8 + x : quad * 4 + x / (D / 64), key = at.base + u;
-                    const bool there = !(at.holes >> (NT == 2 && quad >= 2 ? 1 : 0) & 1);
-                    const bool someone = at.tree ? u <= at.last : there & (key < n) & ((key >= any_from) | (key < W.sink));
-                    const bool everyone = !at.tree & ((key >= all_from) | (key < W.sink));
+                    const int u = BF ? x : x / (D / 64), key = at.base + k0 + u;
+                    const bool someone = at.tree ? any >> u & 1 : there & (key < n) & ((key >= any_from) | (key < W.sink));
+                    const bool everyone = at.tree ? all >> u & 1 : (key >= all_from) | (key < W.sink);
+                    const uint32_t keep = someone ? ~0u : 0u;
 #pragma unroll
                     for (int k = 0; k < VW; ++k) {
-                        uint32_t& word = vr[x].w[k];
-                        word = someone ? word : 0;
-                        if (!everyone && word_not_finite<T>(word)) {
-                            bad = true;
-                            if constexpr (BF) {
-                                if ((word & 0x7f80u) == 0x7f80u) word &= 0xffff0000u;
-                                if ((word & 0x7f800000u) == 0x7f800000u) word &= 0xffffu;
-                            } else {
-                                word = 0;
-                            }
-                        }
+                        vr[x].w[k] &= keep;
+                        bad |= !everyone & word_not_finite<T>(vr[x].w[k]);
                     }
                 }
+                if (bad && hi > lo) s_bad = 1;
             }
             T128 pr[RB];   // bf16: the probabilities, each rounded by half a step of bf16 at most; sums of them unrounded
 #pragma unroll
@@ -352,39 +377,13 @@ __device__ __forceinline__ void tree_tile(const TreeParams& TP, int item, int sp
                         for (int rb = 0; rb < RB; ++rb) o[rb][e] = __builtin_amdgcn_mfma_f32_16x16x4f32(vr[u * (D / 64) + e / 4].f[e % 4], s[rb][u], o[rb][e], 0, 0, 0);
                 }
             }
-            if (__any(bad)) {   // rare: the values taken out above, one by one, for the rows that see them
-                for (int kq = 0; kq < 4; ++kq) {
-                    const tu32x4_t* run = v_run(at, kq);
-#pragma unroll 1
-                    for (int j = 0; j < NT * 4; ++j) {
-                        const int u = kq * (NT * 4) + j;
-                        const T* x = reinterpret_cast<const T*>(run + (size_t)(uint32_t)(min(u, at.last) * at.stride));
-                        const bool everyone = !at.tree && (at.base + u >= all_from || at.base + u < W.sink);
-                        if (everyone) continue;
-#pragma unroll
-                        for (int rb = 0; rb < RB; ++rb) {
-                            float mine = s[rb][0];
-#pragma unroll
-                            for (int y = 1; y < NT * 4; ++y) mine = y == j ? s[rb][y] : mine;
-                            const float weight = __shfl(mine, kq * 16 + n16);
-                            const bool seen = __shfl((int)sees[rb], kq * 16 + n16) >> j & 1;
-#pragma unroll
-                            for (int e = 0; e < ET; ++e)
-#pragma unroll
-                                for (int k = 0; k < 4; ++k) {
-                                    const int ch = BF ? (quad * 4 + k) * ET + e : e / 4 * 64 + (quad * 4 + k) * 4 + e % 4;
-                                    float v;
-                                    if constexpr (BF) v = __uint_as_float((uint32_t)x[ch] << 16);
-                                    else v = x[ch];
-                                    if (seen && (__float_as_uint(v) & 0x7f800000u) == 0x7f800000u) o[rb][e][k] = fmaf(weight, v, o[rb][e][k]);
-                                }
-                        }
-                    }
-                }
+            if constexpr (!LAST) {
+                load_v(next);
+                at = next;
             }
-            if (more) load_v(next);
-            at = next;
-        }
+        };
+        for (; i + WAVES < t_end; i += WAVES) tile(std::false_type());
+        if (i < t_end) tile(std::true_type());
 
         // ---- merge the wavefronts ----------------------------------------------------------------------------------
 #pragma unroll
@@ -404,6 +403,11 @@ __device__ __forceinline__ void tree_tile(const TreeParams& TP, int item, int sp
                 }
         }
         __syncthreads();
+        if (scalar(s_bad)) {   // (the same for every thread)
+            hi = lo + (hi - lo) / 2;
+            __syncthreads();
+            continue;
+        }
         if (tid < TM) {
             float M = -INFINITY, L = 0.f;
 #pragma unroll
@@ -421,7 +425,8 @@ __device__ __forceinline__ void tree_tile(const TreeParams& TP, int item, int sp
         __syncthreads();
         const size_t rec = ((size_t)item * P.splits + split) * TM;
         for (int x = tid; x < rows * (D / 4); x += WAVES * kWave) {
-            const int r = x / (D / 4), d = x % (D / 4) * 4;
+            const int r = x / (D / 4), d = x % (D / 4) * 4, token = token_of(r0 + r);
+            if (token - w.tok_lo < lo || token - w.tok_lo > hi) continue;
             float a[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int y = 0; y < WAVES; ++y) {
@@ -437,10 +442,408 @@ __device__ __forceinline__ void tree_tile(const TreeParams& TP, int item, int sp
                 if (d == 0) P.rec_ml[rec + r] = make_float2(s_M[r], s_L[r]);
                 continue;
             }
-            const int token = token_of(r0 + r);
             store_row<T, D, false>(P, ((size_t)(t.begin + token) * n_kv + h) * g + (r0 + r - token * g), d, a, s_M[r], s_L[r]);
         }
-        __syncthreads();   // the LDS is the next tile's
+        __syncthreads();   // the LDS is the next run's
+        if (hi == nodes - 1) break;
+        lo = hi + 1;
+        hi = nodes - 1;
+        }
+    }
+}
+
+// ---------------------------------------------------------------------------------------------------------
+// More than 32 query rows: a wavefront owns CT * 16 of them, and the pairs pass by in tiles of KT, each read once for the four wavefronts, straight into
+// LDS (two buffers each for K and V, one barrier a tile); layouts in LDS and the order of a tile's steps - the next one's logits beside this one's
+// softmax - are those of prompt.h.
+// ---------------------------------------------------------------------------------------------------------
+template <typename T, int D, int CT_> struct WideCfg {
+    static constexpr bool BF = sizeof(T) == 2;
+    static constexpr int CT = CT_, CH = D * (int)sizeof(T) / 16, KS = CH / 4, ET = D / 16;
+    static constexpr int KT = BF ? 64 : 32;
+    static constexpr int NT = BF ? 2 : 1, BLK = 16 * NT, NB = KT / BLK, GI = KT / 16;
+    static constexpr int TM = 64 * CT;
+    static constexpr int LD = KT * CH / 256, RPU = 256 / CH;   // loads of a tile per thread and tensor; rows that one load of the workgroup covers
+    static constexpr int TILE_BYTES = KT * CH * 16;
+    static constexpr size_t LDS = 4 * (size_t)TILE_BYTES;
+};
+
+template <typename T, int D, int CT, bool ROWS>
+__device__ __forceinline__ void wide_tile(const TreeParams& TP, int item, int split) {
+    using C = WideCfg<T, D, CT>;
+    constexpr bool BF = C::BF;
+    constexpr int CH = C::CH, KS = C::KS, ET = C::ET, KT = C::KT, NT = C::NT, BLK = C::BLK, NB = C::NB, GI = C::GI, TM = C::TM, LD = C::LD, RPU = C::RPU;
+    const AttnPagedParams& P = TP.a;
+    const PagedParams& W = P.view;
+    const int tid = threadIdx.x, lane = tid & (kWave - 1), n16 = lane & 15, quad = lane >> 4, wave = scalar(tid / kWave);
+    const int n_kv = W.n_kv, g = W.g;
+    extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
+    __shared__ Ancestors<TM> s_tree;
+    __shared__ int s_bad;
+    TreeWork w;
+    if (!tree_work<ROWS>(P, item, TM, w)) return;
+    const TileOf& t = w.t;
+    const int n = w.n, h = w.h;
+    const float scale = W.scale_log2e;
+    const bool windowed = !ROWS && W.window != 0x7fffffff;
+    const int32_t* tab = ROWS ? nullptr : scalar_ptr(W.table + (size_t)t.b * W.max_pages);
+    const size_t tree_at = ((size_t)t.begin * n_kv + h) * CH * 16;
+
+    int k_at[KS];   // LDS places of this lane's operands (prompt.h)
+    {
+        const int row = BF ? n16 / 4 * 8 + n16 % 4 : n16;
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) k_at[ks] = row * CH * 16 + ((ks * 4 + quad) ^ swizzle_k<BF, CH>(row)) * 16;
+    }
+    const int v_row = BF ? quad * 8 + n16 / 4 : quad * 4;
+    auto v_at = [&](int e) { return v_row * CH * 16 + ((2 * e + n16 % 4 / 2) ^ swizzle_v<BF, CH>(v_row)) * 16 + n16 % 2 * 8; };
+    const int st_row = tid / CH, st_ch = tid % CH;
+
+    for (; w.t.tile >= 0; w.t.tile -= w.t.step) {
+        tree_tile_of(P, TM, KT, w);
+        if (split >= w.splits) continue;
+        const int r0 = w.r0, rows = w.rows, splits = w.splits, total = w.total;
+        const int per = splits == 1 ? total : scalar(divide(total + splits - 1, splits)), t_begin = min(split * per, total), t_end = min(t_begin + per, total);
+        auto token_of = [&](int r) { return divide(r, g, W.g_magic); };
+        const int w0 = r0 + wave * 16 * CT, w_rows = min(16 * CT, rows - wave * 16 * CT);   // the wavefront's rows; <= 0: none
+        int tok[CT];
+        T128 q[CT][KS];
+#pragma unroll
+        for (int ct = 0; ct < CT; ++ct) {
+            const int r = min(w0 + ct * 16 + n16, r0 + rows - 1), token = token_of(r);
+            tok[ct] = token - w.tok_lo;
+            const size_t q_row = ((size_t)(t.begin + token) * n_kv + h) * g + (r - token * g);
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks) {
+                q[ct][ks].u = reinterpret_cast<const tu32x4_t*>(W.q)[q_row * CH + ks * 4 + quad];
+                if (W.negate) q[ct][ks].u ^= BF ? 0x80008000u : 0x80000000u;
+            }
+        }
+        // The rows of all nodes at once.  A row gives the pairs that it does not see weight 0, which must not meet an infinity or a NaN that another row
+        // sees: where there is any, the run starts over with half of its nodes.
+        const int nodes = w.tok_hi - w.tok_lo + 1;
+        const bool some_tree = t_end > w.old.total;
+        if (windowed || some_tree) find_ancestors<TM>(TP, w, windowed, s_tree);
+        for (int lo = 0, hi = nodes - 1;;) {
+        int level_lo = 0, level_hi = 0;
+        if (tid == 0) s_bad = 0;
+        if (windowed || some_tree) span_of<TM>(s_tree, windowed, lo, hi, level_lo, level_hi);
+        else __syncthreads();
+        const int any_from = windowed ? n + level_lo - W.window + 1 : 0, all_from = windowed ? n + level_hi - W.window + 1 : 0;
+        bool mine[CT];   // this run's rows
+        int from[CT];    // they see pairs of the cache from here on (and the sinks)
+        float m_ref[CT], m_top[CT], l_run[CT];
+        tf32x4_t o[ET][CT];
+#pragma unroll
+        for (int ct = 0; ct < CT; ++ct) {
+            mine[ct] = tok[ct] >= lo && tok[ct] <= hi;
+            from[ct] = windowed ? n + s_tree.level[tok[ct]] - W.window + 1 : 0;
+            m_ref[ct] = m_top[ct] = -INFINITY;
+            l_run[ct] = 0.f;
+#pragma unroll
+            for (int e = 0; e < ET; ++e) o[e][ct] = (tf32x4_t){0.f, 0.f, 0.f, 0.f};
+        }
+        // where a tile's pairs lie: pair u of run u / 16 at at[run] + min(u, last) * stride bytes of K and V; a bit for each run that lies nowhere
+        struct Place {
+            size_t at[GI];
+            uint32_t stride, holes;
+            int base, last;
+            bool tree;
+        };
+        auto place_of = [&](int i) {   // (past the end: the last tile's)
+            i = min(i, t_end - 1);
+            Place p;
+            p.holes = 0;
+            p.tree = i >= w.old.total;
+            if (p.tree) {
+                p.base = (i - w.old.total) * KT;
+                p.stride = n_kv * CH * 16;
+                p.last = t.nq - 1 - p.base;
+#pragma unroll
+                for (int r = 0; r < GI; ++r) p.at[r] = tree_at + (size_t)p.base * p.stride;
+                return p;
+            }
+            p.base = w.old.at(i) * KT;
+            p.stride = CH * 16;
+            p.last = ROWS ? n - 1 - p.base : KT;
+            if constexpr (ROWS) {
+                const size_t at = (((size_t)t.b * n_kv + h) * P.cap + p.base) * CH * 16;
+#pragma unroll
+                for (int r = 0; r < GI; ++r) p.at[r] = at;
+            } else {
+                auto find = [&](int r) {
+                    const int key = p.base + r * 16, page = load_uniform(tab, min(key >> W.page_shift, W.max_pages - 1));
+                    const bool ok = page_ok(W, page);
+                    if (!ok) p.holes |= 1u << r;
+                    return ((((size_t)(ok ? page : 0) * n_kv + h) << W.page_shift) + (key & ((1 << W.page_shift) - 1))) * (CH * 16) - (size_t)r * (16 * CH * 16);
+                };
+                const size_t first = find(0);
+                if (1 << W.page_shift >= KT) {   // one page
+#pragma unroll
+                    for (int r = 0; r < GI; ++r) p.at[r] = first;
+                    if (p.holes) p.holes = (1u << GI) - 1;
+                } else {
+                    p.at[0] = first;
+#pragma unroll
+                    for (int r = 1; r < GI; ++r) p.at[r] = find(r);
+                }
+            }
+            return p;
+        };
+        auto run_of_load = [&](int u) { return RPU == 32 ? 2 * u + (wave >= 2 ? 1 : 0) : u * RPU / 16; };   // load u of this wavefront lies in one run
+        auto send = [&](bool is_k, int buf, const Place& p) {
+            const unsigned char* X = static_cast<const unsigned char*>(is_k ? (p.tree ? TP.k_tree : W.K) : (p.tree ? TP.v_tree : W.V));
+#pragma unroll
+            for (int u = 0; u < LD; ++u) {
+                const int row = st_row + u * RPU;
+                const size_t at = RPU == 32 ? (wave >= 2 ? p.at[(2 * u + 1) % GI] : p.at[2 * u % GI]) : p.at[u * RPU / 16];
+                const int ch = st_ch ^ (is_k ? swizzle_k<BF, CH>(row) : swizzle_v<BF, CH>(row));
+                load_to_lds(X + at + (uint32_t)min(row, p.last) * p.stride + (uint32_t)(ch * 16), smem + (is_k ? 0 : 2 * C::TILE_BYTES) + buf * C::TILE_BYTES + (u * 256 + wave * 64) * 16);
+            }
+        };
+        auto whole = [&](const Place& p) { return !p.tree && p.base + KT <= n && !p.holes && (p.base >= all_from || p.base + KT <= W.sink); };   // seen by every row
+        // V of a tile that not every row sees: values of weight 0 must not meet the products as infinities or NaN
+        auto clear_hidden = [&](int buf, const Place& p) {
+            bool bad = false;
+#pragma unroll
+            for (int u = 0; u < LD; ++u) {
+                const int row = st_row + u * RPU, key = p.base + row;
+                bool someone, everyone;   // (of those that someone sees)
+                if (p.tree) {
+                    someone = s_tree.any[key / 32] >> key % 32 & 1;
+                    everyone = s_tree.all[key / 32] >> key % 32 & 1;
+                } else {
+                    someone = !(p.holes >> run_of_load(u) & 1) & (key < n) & ((key >= any_from) | (key < W.sink));
+                    everyone = (key >= all_from) | (key < W.sink);
+                }
+                tu32x4_t* at = reinterpret_cast<tu32x4_t*>(smem + (2 + buf) * C::TILE_BYTES + (u * 256 + tid) * 16);
+                if (!someone) *at = tu32x4_t{0, 0, 0, 0};
+                else if (!everyone) {
+                    const tu32x4_t x = *at;
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) bad |= word_not_finite<T>(x[k]);
+                }
+            }
+            if (bad && hi > lo) s_bad = 1;
+        };
+        typedef tf32x4_t Logits[GI][CT];
+        auto products = [&](auto buf, Logits& c) {
+            const unsigned char* sk = smem + buf * C::TILE_BYTES;
+#pragma unroll
+            for (int gi = 0; gi < GI; ++gi) {
+#pragma unroll
+                for (int ct = 0; ct < CT; ++ct) c[gi][ct] = (tf32x4_t){0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int ks = 0; ks < KS; ++ks) {
+                    T128 k;
+                    k.u = *reinterpret_cast<const tu32x4_t*>(sk + k_at[ks] + (gi / NT * BLK + gi % NT * 4) * CH * 16);
+#pragma unroll
+                    for (int ct = 0; ct < CT; ++ct) {
+                        if constexpr (BF) {
+                            c[gi][ct] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k.v, q[ct][ks].v, c[gi][ct], 0, 0, 0);
+                        } else {
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) c[gi][ct] = __builtin_amdgcn_mfma_f32_16x16x4f32(k.f[e], q[ct][ks].f[e], c[gi][ct], 0, 0, 0);
+                        }
+                    }
+                }
+            }
+        };
+        bool need = false, large = false;
+        float m_new[CT];
+        auto assess = [&](const Logits& c) {   // a row's largest logit of a tile; whether its reference has to move, or differences would lose their bits
+            need = large = false;
+#pragma unroll
+            for (int ct = 0; ct < CT; ++ct) {
+                float mx = c[0][ct][0];
+#pragma unroll
+                for (int x = 1; x < GI * 4; ++x) mx = fmaxf(mx, c[x / 4][ct][x % 4]);
+                const float m = attn_logit(quad_max(mx), scale);
+                m_new[ct] = m;
+                need |= m > m_ref[ct] + 8.f;
+                large |= fabsf(fmaxf(m, m_ref[ct])) >= kLargeLogit;
+            }
+        };
+        auto step = [&](auto buf, const Place& p, Logits& c, Logits& next) {
+            if (!whole(p)) {
+#pragma unroll
+                for (int ct = 0; ct < CT; ++ct) {
+                    uint32_t sees = 0;   // a bit for each logit of the lane
+#pragma unroll
+                    for (int gi = 0; gi < GI; ++gi) {
+                        const int first = gi / NT * BLK + quad * (NT * 4) + gi % NT * 4;   // the lane's keys of product gi: first .. first + 3
+                        if (p.tree) {
+                            sees |= (s_tree.sees[tok[ct]][(p.base + first) / 32] >> (p.base + first) % 32 & 15) << gi * 4;
+                        } else {
+                            const bool there = !(p.holes >> (BF ? 2 * (gi / NT) + (quad >= 2) : gi) & 1);
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) {
+                                const int key = p.base + first + e;
+                                sees |= (uint32_t)(there & (key < n) & ((key >= from[ct]) | (key < W.sink))) << (gi * 4 + e);
+                            }
+                        }
+                    }
+                    if (!mine[ct]) sees = 0;
+#pragma unroll
+                    for (int x = 0; x < GI * 4; ++x) c[x / 4][ct][x % 4] = sees >> x & 1 ? c[x / 4][ct][x % 4] : -INFINITY;
+                }
+                assess(c);
+            }
+#pragma unroll
+            for (int ct = 0; ct < CT; ++ct) m_top[ct] = fmaxf(m_top[ct], m_new[ct]);
+            if (__any(need)) {
+#pragma unroll
+                for (int ct = 0; ct < CT; ++ct) {
+                    const float m = m_new[ct] > m_ref[ct] + 8.f ? m_new[ct] : m_ref[ct], corr = __builtin_amdgcn_exp2f(m_ref[ct] - ref_of(m));
+                    m_ref[ct] = m;
+                    l_run[ct] *= corr;
+#pragma unroll
+                    for (int e = 0; e < ET; ++e)
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) o[e][ct][k] *= corr;
+                }
+            }
+            float by = scale, less[CT];
+#pragma unroll
+            for (int ct = 0; ct < CT; ++ct) less[ct] = ref_of(m_ref[ct]);
+            if (__any(large)) {   // rounded before the reference is subtracted; the fma below then has nothing left to do
+                by = 1.f;
+#pragma unroll
+                for (int ct = 0; ct < CT; ++ct) {
+                    less[ct] = 0.f;
+#pragma unroll
+                    for (int x = 0; x < GI * 4; ++x) c[x / 4][ct][x % 4] = attn_logit(c[x / 4][ct][x % 4], scale) - ref_of(m_ref[ct]);
+                }
+            }
+            __builtin_amdgcn_s_setprio(1);
+            products(std::integral_constant<int, (buf ^ 1)>{}, next);   // (behind the last tile: of what lies there, for nobody)
+#pragma unroll
+            for (int ct = 0; ct < CT; ++ct) {
+                float sum = 0.f;
+#pragma unroll
+                for (int x = 0; x < GI * 4; ++x) {
+                    const float y = __builtin_amdgcn_exp2f(fmaf(c[x / 4][ct][x % 4], by, -less[ct]));
+                    c[x / 4][ct][x % 4] = y;
+                    sum += y;
+                }
+                l_run[ct] += sum;
+            }
+            const unsigned char* sv = smem + (2 + buf) * C::TILE_BYTES;
+#pragma unroll
+            for (int b = 0; b < NB; ++b) {
+                if constexpr (BF) {
+                    T128 pr[CT];   // rounded: each weight by half a step of bf16 at most, sums of them in fp32
+#pragma unroll
+                    for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+                        for (int x = 0; x < 4; ++x) pr[ct].w[x] = pack_bf16(c[2 * b + x / 2][ct][x % 2 * 2], c[2 * b + x / 2][ct][x % 2 * 2 + 1]);
+#pragma unroll
+                    for (int e = 0; e < ET; ++e) {
+                        T128 v;
+                        const unsigned char* at = sv + v_at(e) + b * BLK * CH * 16;
+                        const tu32x2_t v0 = read_transposed(at), v1 = read_transposed(at + 4 * CH * 16);
+                        v.u = tu32x4_t{v0.x, v0.y, v1.x, v1.y};
+#pragma unroll
+                        for (int ct = 0; ct < CT; ++ct) o[e][ct] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v.v, pr[ct].v, o[e][ct], 0, 0, 0);
+                    }
+                } else {
+#pragma unroll
+                    for (int u = 0; u < 4; ++u)
+#pragma unroll
+                        for (int cc = 0; cc < D / 64; ++cc) {
+                            T128 v;
+                            v.u = *reinterpret_cast<const tu32x4_t*>(sv + (b * BLK + v_row + u) * CH * 16 + (cc * 16 + n16) * 16);
+#pragma unroll
+                            for (int e = 0; e < 4; ++e)
+#pragma unroll
+                                for (int ct = 0; ct < CT; ++ct) o[cc * 4 + e][ct] = __builtin_amdgcn_mfma_f32_16x16x4f32(v.f[e], c[b][ct][u], o[cc * 4 + e][ct], 0, 0, 0);
+                        }
+                }
+            }
+            assess(next);
+            __builtin_amdgcn_s_setprio(0);
+        };
+
+        // K of tile i lies in buffer (i - t_begin) % 2 from two tiles ahead on, V from one tile ahead on.
+        Logits ca, cb;
+        if (t_begin < t_end) {
+            Place here = place_of(t_begin), next1 = place_of(t_begin + 1), next2 = place_of(t_begin + 2);
+            send(true, 0, here);
+            send(false, 0, here);
+            if (t_begin + 1 < t_end) send(true, 1, next1);
+            arrived();
+            __syncthreads();
+            if (w_rows > 0) {
+                products(std::integral_constant<int, 0>{}, ca);
+                assess(ca);
+            }
+            __syncthreads();
+            auto turn = [&](auto buf, int i, Logits& c, Logits& next) {
+                if (!whole(here)) {
+                    clear_hidden(buf, here);
+                    __syncthreads();
+                }
+                if (i + 2 < t_end) send(true, buf, next2);
+                if (i + 1 < t_end) send(false, buf ^ 1, next1);
+                const Place next3 = place_of(i + 3);
+                if (w_rows > 0) step(buf, here, c, next);
+                here = next1;
+                next1 = next2;
+                next2 = next3;
+                arrived();
+                __syncthreads();
+            };
+            for (int i = t_begin;;) {
+                turn(std::integral_constant<int, 0>{}, i, ca, cb);
+                if (++i == t_end) break;
+                turn(std::integral_constant<int, 1>{}, i, cb, ca);
+                if (++i == t_end) break;
+            }
+        }
+
+        if (scalar(s_bad)) {   // (the same for every thread)
+            hi = lo + (hi - lo) / 2;
+            __syncthreads();
+            continue;
+        }
+
+        // every wavefront has its rows' own
+#pragma unroll
+        for (int ct = 0; ct < CT; ++ct) {
+            const float l = quad_sum(l_run[ct]), f = __builtin_amdgcn_exp2f(m_ref[ct] - ref_of(m_top[ct]));
+            const int r = w0 + ct * 16 + n16;
+            if (r >= r0 + rows || !mine[ct]) continue;
+            const int token = token_of(r);
+            const size_t row = ((size_t)(t.begin + token) * n_kv + h) * g + (r - token * g), rec = ((size_t)item * P.splits + split) * TM + (r - r0);
+            const float mul = splits > 1 ? f : l == 0.f ? 0.f : 1.0f / l;
+#pragma unroll
+            for (int e = 0; e < ET; e += BF ? 1 : 4) {
+                if constexpr (BF) {   // channels e * 16 + quad * 4 ..
+                    const tf32x4_t a = o[e][ct] * mul;
+                    const int d = e * 16 + quad * 4;
+                    if (splits > 1) *reinterpret_cast<float4*>(P.rec + rec * D + d) = make_float4(a[0], a[1], a[2], a[3]);
+                    else *reinterpret_cast<tu32x2_t*>(reinterpret_cast<bf16_t*>(P.out) + row * D + d) = tu32x2_t{pack_bf16(a[0], a[1]), pack_bf16(a[2], a[3])};
+                } else {
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {   // e / 4 * 64 + (quad * 4 + k) * 4 ..
+                        const float4 a = make_float4(o[e][ct][k] * mul, o[e + 1][ct][k] * mul, o[e + 2][ct][k] * mul, o[e + 3][ct][k] * mul);
+                        const int d = e / 4 * 64 + (quad * 4 + k) * 4;
+                        if (splits > 1) *reinterpret_cast<float4*>(P.rec + rec * D + d) = a;
+                        else *reinterpret_cast<float4*>(reinterpret_cast<float*>(P.out) + row * D + d) = a;
+                    }
+                }
+            }
+            if (quad == 0) {
+                const float2 ml = make_float2(m_top[ct], l * f);
+                if (splits > 1) P.rec_ml[rec] = ml;
+                else if (P.stats) P.stats[row] = ml;
+            }
+        }
+        __syncthreads();   // the LDS is the next run's
+        if (hi == nodes - 1) break;
+        lo = hi + 1;
+        hi = nodes - 1;
+        }
     }
 }
 

@@ -7,21 +7,30 @@
 
 namespace fk {
 
-template <typename T, int D, int RB, bool ROWS>
-__global__ __launch_bounds__(256, RB == 1 ? 3 : RB == 2 ? 2 : 1) void tree_kernel(const TreeParams P) {
-    tree_tile<T, D, RB, ROWS>(P, blockIdx.x, blockIdx.y);
+// KIND: 1, 2: tree_tile with so many 16-row blocks; 4, 8: wide_tile with so many
+template <typename T, int D, int KIND> struct TreeKind {
+    static constexpr bool WIDE = KIND >= 4;
+    static constexpr int TM = 16 * KIND;
+    static constexpr int KT = WIDE ? WideCfg<T, D, WIDE ? KIND / 4 : 1>::KT : TreeCfg<T, D, WIDE ? 1 : KIND>::KT;
+    static constexpr size_t LDS = WIDE ? WideCfg<T, D, WIDE ? KIND / 4 : 1>::LDS : TreeCfg<T, D, WIDE ? 1 : KIND>::LDS;
+};
+
+template <typename T, int D, int KIND, bool ROWS>
+__global__ __launch_bounds__(256, KIND == 1 ? 3 : 2) void tree_kernel(const TreeParams P) {
+    if constexpr (KIND >= 4) wide_tile<T, D, KIND / 4, ROWS>(P, blockIdx.x, blockIdx.y);
+    else tree_tile<T, D, KIND, ROWS>(P, blockIdx.x, blockIdx.y);
 }
 
 // the second launch, where a tile's pairs may have been split
-template <typename T, int D, int RB, bool ROWS>
+template <typename T, int D, int KIND, bool ROWS>
 __global__ __launch_bounds__(256) void tree_merge_kernel(const AttnPagedParams P) {
-    using C = TreeCfg<T, D, RB>;
+    using C = TreeKind<T, D, KIND>;
     constexpr int TM = C::TM;
     const PagedParams& W = P.view;
     const int item = blockIdx.x, part = blockIdx.y * 16;
     TreeWork w;
-    if (!tree_work<ROWS, TM, C::KT>(P, item, w) || !w.t.one) return;   // (places that take several tiles do not split them)
-    tree_tile_of<TM, C::KT>(P, w);
+    if (!tree_work<ROWS>(P, item, TM, w) || !w.t.one) return;   // (places that take several tiles do not split them)
+    tree_tile_of(P, TM, C::KT, w);
     if (w.splits == 1) return;
     const size_t rec = (size_t)item * P.splits * TM;
     const int rows = min(16, w.rows - part);
@@ -35,18 +44,18 @@ __global__ __launch_bounds__(256) void tree_merge_kernel(const AttnPagedParams P
 
 // ---- host side ---------------------------------------------------------------------------------------------------
 struct TreePlan {
-    int rb;                    // 16-row blocks of a tile
+    int kind;                  // 16-row blocks of a tile
     TileGrid grid;
     int splits, shift;
 };
 static TreePlan tree_plan(const fk_paged_desc* d, int32_t n_tokens, int32_t max_tree, long long pairs) {
     const int g = d->n_q_heads / d->n_kv_heads, tree = std::min(std::min(max_tree, n_tokens), kTreeNodes), rows = tree * g;
-    TreePlan p = {rows <= 16 ? 1 : rows <= 32 ? 2 : 4, {}, 1, 0};
-    p.grid = tile_grid(d, n_tokens, tree, 16 * p.rb);
+    TreePlan p = {rows <= 16 ? 1 : rows <= 32 ? 2 : rows <= 64 ? 4 : 8, {}, 1, 0};
+    p.grid = tile_grid(d, n_tokens, tree, 16 * p.kind);
     p.grid.most = kTreeNodes * g;
-    const int kt_shift = d->dtype == FK_BF16 ? 5 : 4;
+    const int kt_shift = (d->dtype == FK_BF16 ? 5 : 4) + (p.kind >= 4 ? 1 : 0);
     p.shift = 8 - kt_shift;
-    const long long items = (long long)p.grid.places * d->n_kv_heads, fill = p.rb == 1 ? 768 : p.rb == 2 ? 512 : 256;
+    const long long items = (long long)p.grid.places * d->n_kv_heads, fill = p.kind == 1 ? 768 : 512;
     long long s = items < fill ? fill / items : 1;
     s = std::min(std::min(s, 16ll), (pairs + tree) >> 8);
     p.splits = (int)std::max(s, 1ll);
@@ -54,21 +63,21 @@ static TreePlan tree_plan(const fk_paged_desc* d, int32_t n_tokens, int32_t max_
 }
 static size_t tree_workspace(const fk_paged_desc* d, int32_t n_tokens, int32_t max_tree, int32_t max_len) {
     const TreePlan p = tree_plan(d, std::max(n_tokens, 1), max_tree, max_len);
-    return 16 + record_bytes((long long)p.grid.places * d->n_kv_heads, p.splits, 16 * p.rb, d->head_dim);
+    return 16 + record_bytes((long long)p.grid.places * d->n_kv_heads, p.splits, 16 * p.kind, d->head_dim);
 }
 
-template <typename T, int D, int RB, bool ROWS> static fk_status tree_start(const TreeParams& P, hipStream_t st) {
-    using C = TreeCfg<T, D, RB>;
-    auto kern = tree_kernel<T, D, RB, ROWS>;
+template <typename T, int D, int KIND, bool ROWS> static fk_status tree_start(const TreeParams& P, hipStream_t st) {
+    using C = TreeKind<T, D, KIND>;
+    auto kern = tree_kernel<T, D, KIND, ROWS>;
     static bool lds_ok[kMaxDevices] = {};
     if (!allow_dynamic_lds((const void*)kern, C::LDS, lds_ok)) return FK_ERR_LAUNCH;
     const int items = P.a.grid.places * P.a.view.n_kv;
     hipLaunchKernelGGL(kern, dim3((unsigned)items, (unsigned)P.a.splits), dim3(256), C::LDS, st, P);
-    if (P.a.splits > 1) hipLaunchKernelGGL((tree_merge_kernel<T, D, RB, ROWS>), dim3((unsigned)items, RB), dim3(256), 0, st, P.a);
+    if (P.a.splits > 1) hipLaunchKernelGGL((tree_merge_kernel<T, D, KIND, ROWS>), dim3((unsigned)items, KIND), dim3(256), 0, st, P.a);
     return launch_status();
 }
-template <typename T, int D, bool ROWS> static fk_status tree_rows_of(int rb, const TreeParams& P, hipStream_t st) {
-    return rb == 1 ? tree_start<T, D, 1, ROWS>(P, st) : rb == 2 ? tree_start<T, D, 2, ROWS>(P, st) : tree_start<T, D, 4, ROWS>(P, st);
+template <typename T, int D, bool ROWS> static fk_status tree_rows_of(int kind, const TreeParams& P, hipStream_t st) {
+    return kind == 1 ? tree_start<T, D, 1, ROWS>(P, st) : kind == 2 ? tree_start<T, D, 2, ROWS>(P, st) : kind == 4 ? tree_start<T, D, 4, ROWS>(P, st) : tree_start<T, D, 8, ROWS>(P, st);
 }
 template <bool ROWS> static fk_status tree_launch(const fk_paged_desc* d, const TreePlan& p, TreeParams& P, void* ws, hipStream_t st) {
     AttnPagedParams& A = P.a;
@@ -77,9 +86,9 @@ template <bool ROWS> static fk_status tree_launch(const fk_paged_desc* d, const 
     A.split_shift = p.shift;
     const size_t items = (size_t)p.grid.places * d->n_kv_heads;
     A.rec_ml = reinterpret_cast<float2*>(ws);
-    A.rec = reinterpret_cast<float*>(static_cast<char*>(ws) + up256(items * p.splits * 16 * p.rb * sizeof(float2)));
-    if (d->dtype == FK_F32) return d->head_dim == 64 ? tree_rows_of<float, 64, ROWS>(p.rb, P, st) : tree_rows_of<float, 128, ROWS>(p.rb, P, st);
-    return d->head_dim == 64 ? tree_rows_of<bf16_t, 64, ROWS>(p.rb, P, st) : tree_rows_of<bf16_t, 128, ROWS>(p.rb, P, st);
+    A.rec = reinterpret_cast<float*>(static_cast<char*>(ws) + up256(items * p.splits * 16 * p.kind * sizeof(float2)));
+    if (d->dtype == FK_F32) return d->head_dim == 64 ? tree_rows_of<float, 64, ROWS>(p.kind, P, st) : tree_rows_of<float, 128, ROWS>(p.kind, P, st);
+    return d->head_dim == 64 ? tree_rows_of<bf16_t, 64, ROWS>(p.kind, P, st) : tree_rows_of<bf16_t, 128, ROWS>(p.kind, P, st);
 }
 
 // what both entry points check beyond their descriptors
