@@ -454,19 +454,32 @@ __device__ __forceinline__ void tree_tile(const TreeParams& TP, int item, int sp
 
 // ---------------------------------------------------------------------------------------------------------
 // More than 32 query rows: a wavefront owns CT * 16 of them, and the pairs pass by in tiles of KT, each read once for the four wavefronts, straight into
-// LDS (two buffers each for K and V, one barrier a tile); layouts in LDS and the order of a tile's steps - the next one's logits beside this one's
-// softmax - are those of prompt.h.
+// LDS: three places each for K and V, so that a tile's loads have two turns to arrive, one barrier a turn.  Layouts in LDS and the order of a
+// turn's steps - the next tile's logits beside this one's softmax - are those of prompt.h.
 // ---------------------------------------------------------------------------------------------------------
 template <typename T, int D, int CT_> struct WideCfg {
     static constexpr bool BF = sizeof(T) == 2;
     static constexpr int CT = CT_, CH = D * (int)sizeof(T) / 16, KS = CH / 4, ET = D / 16;
-    static constexpr int KT = BF ? 64 : 32;
+    static constexpr int KT = BF && (CT == 2 || D == 64) ? 64 : 512 / CH;   // pairs of a tile
+    static constexpr int PLACES = KT * CH * 16 > 8192 ? 2 : 3;              // 64 KB of LDS at most: two workgroups on a CU
     static constexpr int NT = BF ? 2 : 1, BLK = 16 * NT, NB = KT / BLK, GI = KT / 16;
     static constexpr int TM = 64 * CT;
     static constexpr int LD = KT * CH / 256, RPU = 256 / CH;   // loads of a tile per thread and tensor; rows that one load of the workgroup covers
     static constexpr int TILE_BYTES = KT * CH * 16;
-    static constexpr size_t LDS = 4 * (size_t)TILE_BYTES;
+    static constexpr size_t LDS = 2 * PLACES * (size_t)TILE_BYTES;
 };
+
+// The wavefront's loads are there but for the latest N, and what it has read of LDS; then the workgroup's.  (__syncthreads would wait for all loads.)
+template <int N> __device__ __forceinline__ void arrived_but() {
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(N) : "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+}
+__device__ __forceinline__ void lds_barrier() {
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+}
 
 template <typename T, int D, int CT, bool ROWS>
 __device__ __forceinline__ void wide_tile(const TreeParams& TP, int item, int split) {
@@ -487,7 +500,7 @@ __device__ __forceinline__ void wide_tile(const TreeParams& TP, int item, int sp
     const float scale = W.scale_log2e;
     const bool windowed = !ROWS && W.window != 0x7fffffff;
     const int32_t* tab = ROWS ? nullptr : scalar_ptr(W.table + (size_t)t.b * W.max_pages);
-    const size_t tree_at = ((size_t)t.begin * n_kv + h) * CH * 16;
+    const size_t tree_at = ((size_t)t.begin * n_kv + h) * CH * 16, row_at = ROWS ? ((size_t)t.b * n_kv + h) * P.cap * (CH * 16) : 0;
 
     int k_at[KS];   // LDS places of this lane's operands (prompt.h)
     {
@@ -506,12 +519,10 @@ __device__ __forceinline__ void wide_tile(const TreeParams& TP, int item, int sp
         const int per = splits == 1 ? total : scalar(divide(total + splits - 1, splits)), t_begin = min(split * per, total), t_end = min(t_begin + per, total);
         auto token_of = [&](int r) { return divide(r, g, W.g_magic); };
         const int w0 = r0 + wave * 16 * CT, w_rows = min(16 * CT, rows - wave * 16 * CT);   // the wavefront's rows; <= 0: none
-        int tok[CT];
         T128 q[CT][KS];
 #pragma unroll
         for (int ct = 0; ct < CT; ++ct) {
             const int r = min(w0 + ct * 16 + n16, r0 + rows - 1), token = token_of(r);
-            tok[ct] = token - w.tok_lo;
             const size_t q_row = ((size_t)(t.begin + token) * n_kv + h) * g + (r - token * g);
 #pragma unroll
             for (int ks = 0; ks < KS; ++ks) {
@@ -530,24 +541,19 @@ __device__ __forceinline__ void wide_tile(const TreeParams& TP, int item, int sp
         if (windowed || some_tree) span_of<TM>(s_tree, windowed, lo, hi, level_lo, level_hi);
         else __syncthreads();
         const int any_from = windowed ? n + level_lo - W.window + 1 : 0, all_from = windowed ? n + level_hi - W.window + 1 : 0;
-        bool mine[CT];   // this run's rows
-        int from[CT];    // they see pairs of the cache from here on (and the sinks)
         float m_ref[CT], m_top[CT], l_run[CT];
         tf32x4_t o[ET][CT];
 #pragma unroll
         for (int ct = 0; ct < CT; ++ct) {
-            mine[ct] = tok[ct] >= lo && tok[ct] <= hi;
-            from[ct] = windowed ? n + s_tree.level[tok[ct]] - W.window + 1 : 0;
             m_ref[ct] = m_top[ct] = -INFINITY;
             l_run[ct] = 0.f;
 #pragma unroll
             for (int e = 0; e < ET; ++e) o[e][ct] = (tf32x4_t){0.f, 0.f, 0.f, 0.f};
         }
-        // where a tile's pairs lie: pair u of run u / 16 at at[run] + min(u, last) * stride bytes of K and V; a bit for each run that lies nowhere
+        // Where a tile's pairs lie.  Pages: its runs of 16 pairs, counted in such runs (so that 32 bits hold any pool), and a bit for each that lies nowhere.
         struct Place {
-            size_t at[GI];
-            uint32_t stride, holes;
-            int base, last;
+            uint32_t run[ROWS ? 1 : GI], holes;
+            int base;
             bool tree;
         };
         auto place_of = [&](int i) {   // (past the end: the last tile's)
@@ -555,56 +561,65 @@ __device__ __forceinline__ void wide_tile(const TreeParams& TP, int item, int sp
             Place p;
             p.holes = 0;
             p.tree = i >= w.old.total;
-            if (p.tree) {
-                p.base = (i - w.old.total) * KT;
-                p.stride = n_kv * CH * 16;
-                p.last = t.nq - 1 - p.base;
-#pragma unroll
-                for (int r = 0; r < GI; ++r) p.at[r] = tree_at + (size_t)p.base * p.stride;
-                return p;
-            }
-            p.base = w.old.at(i) * KT;
-            p.stride = CH * 16;
-            p.last = ROWS ? n - 1 - p.base : KT;
-            if constexpr (ROWS) {
-                const size_t at = (((size_t)t.b * n_kv + h) * P.cap + p.base) * CH * 16;
-#pragma unroll
-                for (int r = 0; r < GI; ++r) p.at[r] = at;
-            } else {
+            p.base = p.tree ? (i - w.old.total) * KT : w.old.at(i) * KT;
+            if constexpr (!ROWS) {
                 auto find = [&](int r) {
                     const int key = p.base + r * 16, page = load_uniform(tab, min(key >> W.page_shift, W.max_pages - 1));
                     const bool ok = page_ok(W, page);
                     if (!ok) p.holes |= 1u << r;
-                    return ((((size_t)(ok ? page : 0) * n_kv + h) << W.page_shift) + (key & ((1 << W.page_shift) - 1))) * (CH * 16) - (size_t)r * (16 * CH * 16);
+                    return ((uint32_t)(ok ? page : 0) * n_kv + h) << (W.page_shift - 4) | (key & ((1 << W.page_shift) - 1)) >> 4;
                 };
-                const size_t first = find(0);
+                p.run[0] = find(0);
                 if (1 << W.page_shift >= KT) {   // one page
 #pragma unroll
-                    for (int r = 0; r < GI; ++r) p.at[r] = first;
+                    for (int r = 1; r < GI; ++r) p.run[r] = p.run[0] + r;
                     if (p.holes) p.holes = (1u << GI) - 1;
                 } else {
-                    p.at[0] = first;
 #pragma unroll
-                    for (int r = 1; r < GI; ++r) p.at[r] = find(r);
+                    for (int r = 1; r < GI; ++r) p.run[r] = find(r);
                 }
             }
             return p;
         };
         auto run_of_load = [&](int u) { return RPU == 32 ? 2 * u + (wave >= 2 ? 1 : 0) : u * RPU / 16; };   // load u of this wavefront lies in one run
-        auto send = [&](bool is_k, int buf, const Place& p) {
-            const unsigned char* X = static_cast<const unsigned char*>(is_k ? (p.tree ? TP.k_tree : W.K) : (p.tree ? TP.v_tree : W.V));
+        auto send = [&](bool is_k, unsigned char* to, const Place& p) {
+            const unsigned char* X = static_cast<const unsigned char*>(is_k ? W.K : W.V);
+            to += wave * 64 * 16;
+            const int last = p.tree ? t.nq - 1 - p.base : ROWS ? n - 1 - p.base : KT;
+            if (!p.tree && (!ROWS || last >= KT - 1)) {
+                if constexpr (ROWS) X += row_at + (size_t)p.base * (CH * 16);
+#pragma unroll
+                for (int u = 0; u < LD; ++u) {
+                    const int row = st_row + u * RPU, ch = st_ch ^ (is_k ? swizzle_k<BF, CH>(row) : swizzle_v<BF, CH>(row));
+                    if constexpr (ROWS) {
+                        load_to_lds(X + (uint32_t)((row * CH + ch) * 16), to + u * 256 * 16);
+                    } else {
+                        const uint32_t run = RPU == 32 ? (wave >= 2 ? p.run[(2 * u + 1) % GI] : p.run[2 * u % GI]) : p.run[u * RPU / 16];
+                        load_to_lds(X + (size_t)run * (16 * CH * 16) + (uint32_t)((row % 16 * CH + ch) * 16), to + u * 256 * 16);
+                    }
+                }
+                return;
+            }
+            // the end of a row, or nodes: the last pair again behind the last one
+            int thread = tid;   // (opaque: or all that follows from it is kept in registers over the loop)
+            asm volatile("" : "+v"(thread));
+            const int st_row = thread / CH, st_ch = thread % CH;
+            const uint32_t stride = p.tree ? n_kv * CH * 16 : CH * 16;
+            X = p.tree ? static_cast<const unsigned char*>(is_k ? TP.k_tree : TP.v_tree) + tree_at : X + row_at;
+            X += (size_t)p.base * stride;
 #pragma unroll
             for (int u = 0; u < LD; ++u) {
-                const int row = st_row + u * RPU;
-                const size_t at = RPU == 32 ? (wave >= 2 ? p.at[(2 * u + 1) % GI] : p.at[2 * u % GI]) : p.at[u * RPU / 16];
-                const int ch = st_ch ^ (is_k ? swizzle_k<BF, CH>(row) : swizzle_v<BF, CH>(row));
-                load_to_lds(X + at + (uint32_t)min(row, p.last) * p.stride + (uint32_t)(ch * 16), smem + (is_k ? 0 : 2 * C::TILE_BYTES) + buf * C::TILE_BYTES + (u * 256 + wave * 64) * 16);
+                const int row = st_row + u * RPU, ch = st_ch ^ (is_k ? swizzle_k<BF, CH>(row) : swizzle_v<BF, CH>(row));
+                load_to_lds(X + (uint32_t)((uint32_t)min(row, last) * stride + ch * 16), to + u * 256 * 16);
             }
         };
         auto whole = [&](const Place& p) { return !p.tree && p.base + KT <= n && !p.holes && (p.base >= all_from || p.base + KT <= W.sink); };   // seen by every row
         // V of a tile that not every row sees: values of weight 0 must not meet the products as infinities or NaN
-        auto clear_hidden = [&](int buf, const Place& p) {
+        auto clear_hidden = [&](unsigned char* v, const Place& p) {
             bool bad = false;
+            int thread = tid;
+            asm volatile("" : "+v"(thread));
+            const int st_row = thread / CH;
 #pragma unroll
             for (int u = 0; u < LD; ++u) {
                 const int row = st_row + u * RPU, key = p.base + row;
@@ -616,7 +631,7 @@ __device__ __forceinline__ void wide_tile(const TreeParams& TP, int item, int sp
                     someone = !(p.holes >> run_of_load(u) & 1) & (key < n) & ((key >= any_from) | (key < W.sink));
                     everyone = (key >= all_from) | (key < W.sink);
                 }
-                tu32x4_t* at = reinterpret_cast<tu32x4_t*>(smem + (2 + buf) * C::TILE_BYTES + (u * 256 + tid) * 16);
+                tu32x4_t* at = reinterpret_cast<tu32x4_t*>(v + (u * 256 + thread) * 16);
                 if (!someone) *at = tu32x4_t{0, 0, 0, 0};
                 else if (!everyone) {
                     const tu32x4_t x = *at;
@@ -627,8 +642,7 @@ __device__ __forceinline__ void wide_tile(const TreeParams& TP, int item, int sp
             if (bad && hi > lo) s_bad = 1;
         };
         typedef tf32x4_t Logits[GI][CT];
-        auto products = [&](auto buf, Logits& c) {
-            const unsigned char* sk = smem + buf * C::TILE_BYTES;
+        auto products = [&](const unsigned char* sk, Logits& c) {
 #pragma unroll
             for (int gi = 0; gi < GI; ++gi) {
 #pragma unroll
@@ -664,26 +678,31 @@ __device__ __forceinline__ void wide_tile(const TreeParams& TP, int item, int sp
                 large |= fabsf(fmaxf(m, m_ref[ct])) >= kLargeLogit;
             }
         };
-        auto step = [&](auto buf, const Place& p, Logits& c, Logits& next) {
+        auto step = [&](const unsigned char* k_next, const unsigned char* sv, const Place& p, Logits& c, Logits& next) {
             if (!whole(p)) {
+                int at = lane;
+                asm volatile("" : "+v"(at));
+                const int quad = at >> 4, n16 = at & 15;
 #pragma unroll
                 for (int ct = 0; ct < CT; ++ct) {
                     uint32_t sees = 0;   // a bit for each logit of the lane
+                    const int tok = token_of(min(w0 + ct * 16 + n16, r0 + rows - 1)) - w.tok_lo;
+                    const int from = windowed ? n + s_tree.level[tok] - W.window + 1 : 0;   // the row sees pairs of the cache from here on (and the sinks)
 #pragma unroll
                     for (int gi = 0; gi < GI; ++gi) {
                         const int first = gi / NT * BLK + quad * (NT * 4) + gi % NT * 4;   // the lane's keys of product gi: first .. first + 3
                         if (p.tree) {
-                            sees |= (s_tree.sees[tok[ct]][(p.base + first) / 32] >> (p.base + first) % 32 & 15) << gi * 4;
+                            sees |= (s_tree.sees[tok][(p.base + first) / 32] >> (p.base + first) % 32 & 15) << gi * 4;
                         } else {
                             const bool there = !(p.holes >> (BF ? 2 * (gi / NT) + (quad >= 2) : gi) & 1);
 #pragma unroll
                             for (int e = 0; e < 4; ++e) {
                                 const int key = p.base + first + e;
-                                sees |= (uint32_t)(there & (key < n) & ((key >= from[ct]) | (key < W.sink))) << (gi * 4 + e);
+                                sees |= (uint32_t)(there & (key < n) & ((key >= from) | (key < W.sink))) << (gi * 4 + e);
                             }
                         }
                     }
-                    if (!mine[ct]) sees = 0;
+                    if (tok < lo || tok > hi) sees = 0;
 #pragma unroll
                     for (int x = 0; x < GI * 4; ++x) c[x / 4][ct][x % 4] = sees >> x & 1 ? c[x / 4][ct][x % 4] : -INFINITY;
                 }
@@ -716,7 +735,7 @@ __device__ __forceinline__ void wide_tile(const TreeParams& TP, int item, int sp
                 }
             }
             __builtin_amdgcn_s_setprio(1);
-            products(std::integral_constant<int, (buf ^ 1)>{}, next);   // (behind the last tile: of what lies there, for nobody)
+            products(k_next, next);   // (behind the last tile: of what lies there, for nobody)
 #pragma unroll
             for (int ct = 0; ct < CT; ++ct) {
                 float sum = 0.f;
@@ -728,7 +747,6 @@ __device__ __forceinline__ void wide_tile(const TreeParams& TP, int item, int sp
                 }
                 l_run[ct] += sum;
             }
-            const unsigned char* sv = smem + (2 + buf) * C::TILE_BYTES;
 #pragma unroll
             for (int b = 0; b < NB; ++b) {
                 if constexpr (BF) {
@@ -764,43 +782,61 @@ __device__ __forceinline__ void wide_tile(const TreeParams& TP, int item, int sp
             __builtin_amdgcn_s_setprio(0);
         };
 
-        // K of tile i lies in buffer (i - t_begin) % 2 from two tiles ahead on, V from one tile ahead on.
+        // Tile i lies in place (i - t_begin) % PLACES.  With three its K is sent for three turns ahead (the turn before it forms its logits) and its V two, so
+        // that the latest 2 * LD loads may still be under way at a turn's end; with two a turn's loads arrive by its end.  Every turn sends for
+        // one of each, behind the end the last tile's again.
+        constexpr bool FAR = C::PLACES == 3;
+        constexpr int UNDER_WAY = FAR ? 2 * LD : 0;
         Logits ca, cb;
         if (t_begin < t_end) {
+            unsigned char *const sk = smem, *const sv = smem + C::PLACES * C::TILE_BYTES;
             Place here = place_of(t_begin), next1 = place_of(t_begin + 1), next2 = place_of(t_begin + 2);
-            send(true, 0, here);
-            send(false, 0, here);
-            if (t_begin + 1 < t_end) send(true, 1, next1);
-            arrived();
-            __syncthreads();
+            send(true, sk, here);
+            send(false, sv, here);
+            send(true, sk + C::TILE_BYTES, next1);
+            if constexpr (FAR) {
+                send(false, sv + C::TILE_BYTES, next1);
+                send(true, sk + 2 * C::TILE_BYTES, next2);
+            }
+            arrived_but<UNDER_WAY>();
             if (w_rows > 0) {
-                products(std::integral_constant<int, 0>{}, ca);
+                products(sk, ca);
                 assess(ca);
             }
-            __syncthreads();
-            auto turn = [&](auto buf, int i, Logits& c, Logits& next) {
+            lds_barrier();
+            // the places of this tile, whose K is not needed any more, of the next one and the one after it
+            auto turn = [&](unsigned char* __restrict k_to, unsigned char* __restrict v_to, const unsigned char* __restrict k_from, unsigned char* __restrict v_from, int i, Logits& c,
+                            Logits& next) {
+                const Place next3 = FAR ? place_of(i + 3) : Place();
+                send(true, k_to, FAR ? next3 : next2);
+                send(false, v_to, FAR ? next2 : next1);
                 if (!whole(here)) {
-                    clear_hidden(buf, here);
-                    __syncthreads();
+                    clear_hidden(v_from, here);
+                    lds_barrier();
                 }
-                if (i + 2 < t_end) send(true, buf, next2);
-                if (i + 1 < t_end) send(false, buf ^ 1, next1);
-                const Place next3 = place_of(i + 3);
-                if (w_rows > 0) step(buf, here, c, next);
+                const Place after = FAR ? next3 : place_of(i + 3);
+                if (w_rows > 0) step(k_from, v_from, here, c, next);
                 here = next1;
                 next1 = next2;
-                next2 = next3;
-                arrived();
-                __syncthreads();
+                next2 = after;
+                arrived_but<UNDER_WAY>();
             };
+            uint32_t at = 0, at1 = C::TILE_BYTES, at2 = FAR ? 2 * C::TILE_BYTES : 0;
             for (int i = t_begin;;) {
-                turn(std::integral_constant<int, 0>{}, i, ca, cb);
+                turn(sk + at, sv + (FAR ? at2 : at1), sk + at1, sv + at, i, ca, cb);
                 if (++i == t_end) break;
-                turn(std::integral_constant<int, 1>{}, i, cb, ca);
+                turn(sk + at1, sv + at, sk + at2, sv + at1, i, cb, ca);
                 if (++i == t_end) break;
+                if constexpr (FAR) {   // two turns on
+                    const uint32_t x = at2;
+                    at2 = at1;
+                    at1 = at;
+                    at = x;
+                }
             }
+            arrived();   // (what is under way still for nobody)
         }
-
+        __syncthreads();
         if (scalar(s_bad)) {   // (the same for every thread)
             hi = lo + (hi - lo) / 2;
             __syncthreads();
@@ -808,12 +844,15 @@ __device__ __forceinline__ void wide_tile(const TreeParams& TP, int item, int sp
         }
 
         // every wavefront has its rows' own
+        int lane = threadIdx.x & (kWave - 1);   // (opaque, as above)
+        asm volatile("" : "+v"(lane));
+        const int n16 = lane & 15, quad = lane >> 4;
 #pragma unroll
         for (int ct = 0; ct < CT; ++ct) {
             const float l = quad_sum(l_run[ct]), f = __builtin_amdgcn_exp2f(m_ref[ct] - ref_of(m_top[ct]));
             const int r = w0 + ct * 16 + n16;
-            if (r >= r0 + rows || !mine[ct]) continue;
-            const int token = token_of(r);
+            const int token = token_of(min(r, r0 + rows - 1));
+            if (r >= r0 + rows || token - w.tok_lo < lo || token - w.tok_lo > hi) continue;
             const size_t row = ((size_t)(t.begin + token) * n_kv + h) * g + (r - token * g), rec = ((size_t)item * P.splits + split) * TM + (r - r0);
             const float mul = splits > 1 ? f : l == 0.f ? 0.f : 1.0f / l;
 #pragma unroll
