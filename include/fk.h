@@ -479,8 +479,9 @@ fk_status fk_rope_frequencies(int32_t rotary_dim, double base, int32_t scaling, 
  * [n_tokens][n_q_heads][2] fp32, M and L.  Logits of -inf alone give zeros and (-inf, 0); a query that is no number, or meets one, has L = NaN.  Values of
  * pairs that a node does not see, infinities and NaN among them, do not reach its results.  fp32 accumulation; bf16: the weights are rounded to bf16 before they
  * meet V, L is the sum of the unrounded ones (fk_paged_attn's rounding).  max_tree <= FK_TREE_NODES bounds the trees' nodes and max_len every len[r]; they only
- * size the launch, results are right beyond them too.  workspace: fk_tree_attn_workspace bytes for the same sizes, no initialisation required; calls sharing it must not
- * overlap in time.  FK_ERR_UNSUPPORTED: n_tokens * n_q_heads >= 2^28, n_kv_heads >= 2^16.
+ * size the launch, results are right beyond them too.  workspace: fk_tree_attn_workspace bytes for the same sizes, zero-filled ONCE by the caller; every call leaves its
+ * counters at zero again, and calls of any sizes (of fk_paged_tree_attn too) may take turns with one that is large enough for each; calls sharing it must not
+ * overlap in time.  One launch; the order of all sums is fixed: equal calls give equal bits.  FK_ERR_UNSUPPORTED: n_tokens * n_q_heads >= 2^28, n_kv_heads >= 2^16.
  */
 size_t fk_tree_attn_workspace(const fk_cache_desc *desc, int32_t n_tokens, int32_t max_tree, int32_t max_len);
 fk_status fk_tree_attn(const fk_cache_desc *desc, const void *q, const void *K, const void *V, const int32_t *len, const void *k_tree,

@@ -517,7 +517,8 @@ def fk_tree_attn_workspace(desc: CacheDesc, n_tokens: int, max_tree: int, max_le
 
 
 def new_tree_attn_workspace(desc: CacheDesc, n_tokens: int, max_tree: int, max_len: int) -> "torch.Tensor":
-    return torch.empty(max(fk_tree_attn_workspace(desc, n_tokens, max_tree, max_len), 16), dtype=torch.uint8, device="cuda")
+    """Zero-filled device workspace (its counters must start at zero); it serves calls with fewer tokens, smaller bounds too."""
+    return torch.zeros(max(fk_tree_attn_workspace(desc, n_tokens, max_tree, max_len), 16), dtype=torch.uint8, device="cuda")
 
 
 def fk_tree_attn(desc: CacheDesc, q, K, V, length, k_tree, v_tree, parent, q_start, max_tree: int, max_len: int, softmax_scale: float, out, stats,
@@ -534,7 +535,8 @@ def fk_paged_tree_attn_workspace(desc: PagedDesc, n_tokens: int, max_tree: int, 
 
 
 def new_paged_tree_attn_workspace(desc: PagedDesc, n_tokens: int, max_tree: int, max_len: int) -> "torch.Tensor":
-    return torch.empty(max(fk_paged_tree_attn_workspace(desc, n_tokens, max_tree, max_len), 16), dtype=torch.uint8, device="cuda")
+    """Zero-filled device workspace (its counters must start at zero); it serves calls with fewer tokens, smaller bounds too."""
+    return torch.zeros(max(fk_paged_tree_attn_workspace(desc, n_tokens, max_tree, max_len), 16), dtype=torch.uint8, device="cuda")
 
 
 def fk_paged_tree_attn(desc: PagedDesc, q, K, V, page_table, kv_len, k_tree, v_tree, parent, q_start, max_tree: int, max_len: int, window: int, n_sink: int,

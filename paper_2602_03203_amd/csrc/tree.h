@@ -17,7 +17,26 @@ struct TreeParams {
     AttnPagedParams a;         // view (rows of a budgeted cache: kv_len is len, [batch][n_kv]), out, stats, grid, splits, split_shift, rec, rec_ml, cap
     const int32_t* parent;
     const void *k_tree, *v_tree;
+    uint32_t* here;            // [items][4] splits whose records are there; zero between calls
 };
+static constexpr int kMostTreeSplits = 16;
+static constexpr int kSplitItems = 1024;   // a call with more items (a tile of rows, a KV head) splits none
+
+// Records of split tiles go from workgroup to workgroup by agent-scope relaxed atomics: loads and stores that pass the caches of the XCDs, which
+// costs nothing next to a fence that writes back and invalidates a whole L2.
+__device__ __forceinline__ void put2(float* p, float a, float b) {
+    __hip_atomic_store(reinterpret_cast<uint64_t*>(p), (uint64_t)__float_as_uint(b) << 32 | __float_as_uint(a), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ float2 get2(const float* p) {
+    const uint64_t x = __hip_atomic_load(reinterpret_cast<const uint64_t*>(p), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    return make_float2(__uint_as_float((uint32_t)x), __uint_as_float((uint32_t)(x >> 32)));
+}
+// One more split of `splits` has its record there (its stores have arrived): true for the last one, which leaves the counter at zero.  One lane's business.
+__device__ __forceinline__ bool last_one(uint32_t* here, int splits) {
+    const bool last = __hip_atomic_fetch_add(here, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == (uint32_t)splits - 1;
+    if (last) __hip_atomic_store(here, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    return last;
+}
 
 // What a workgroup works on; false: nothing
 struct TreeWork {
@@ -143,7 +162,7 @@ __device__ __forceinline__ void tree_tile(const TreeParams& TP, int item, int sp
     const TileOf& t = w.t;
     const int n = w.n, h = w.h;
     const bool windowed = !ROWS && W.window != 0x7fffffff;
-    const size_t tree_at = ((size_t)t.begin * n_kv + h) * CH;
+    const size_t tree_at = ((size_t)t.begin * n_kv + h) * CH * 16;
     const int32_t* tab = ROWS ? nullptr : scalar_ptr(W.table + (size_t)t.b * W.max_pages);
     for (; w.t.tile >= 0; w.t.tile -= w.t.step) {
         tree_tile_of(P, TM, KT, w);
@@ -153,11 +172,9 @@ __device__ __forceinline__ void tree_tile(const TreeParams& TP, int item, int sp
         auto token_of = [&](int r) { return divide(r, g, W.g_magic); };
 
         T128 q[RB][KS];
-        int tok[RB];   // of this lane's rows, counted from the tile's first
 #pragma unroll
         for (int rb = 0; rb < RB; ++rb) {
             const int r = r0 + min(rb * 16 + n16, rows - 1), token = token_of(r);
-            tok[rb] = token - w.tok_lo;
             const size_t q_row = ((size_t)(t.begin + token) * n_kv + h) * g + (r - token * g);
 #pragma unroll
             for (int ks = 0; ks < KS; ++ks) {
@@ -167,7 +184,7 @@ __device__ __forceinline__ void tree_tile(const TreeParams& TP, int item, int sp
         }
         const float scale = W.scale_log2e;
 
-        // where a tile's pairs lie: pair u of run u / 16 at at[run] + min(u, last) * stride, counted in 16 bytes of K and V; a bit for each run that lies nowhere
+        // where a tile's pairs lie: pair u of run u / 16 at at[run] + min(u, last) * stride bytes of K and V; a bit for each run that lies nowhere
         struct Place {
             size_t at[NT];
             int stride, last, base, holes;
@@ -179,54 +196,55 @@ __device__ __forceinline__ void tree_tile(const TreeParams& TP, int item, int sp
             p.holes = 0;
             if (p.tree) {
                 p.base = (i - w.old.total) * KT;
-                p.stride = n_kv * CH;
+                p.stride = n_kv * CH * 16;
                 p.last = t.nq - 1 - p.base;
 #pragma unroll
                 for (int r = 0; r < NT; ++r) p.at[r] = tree_at + (size_t)p.base * p.stride;
                 return p;
             }
             p.base = w.old.at(i) * KT;
-            p.stride = CH;
+            p.stride = CH * 16;
             p.last = ROWS ? n - 1 - p.base : KT;
 #pragma unroll
             for (int r = 0; r < NT; ++r) {
                 if constexpr (ROWS) {
-                    p.at[r] = (((size_t)t.b * n_kv + h) * P.cap + p.base) * CH;
+                    p.at[r] = (((size_t)t.b * n_kv + h) * P.cap + p.base) * CH * 16;
                 } else {
                     const int key = p.base + r * 16, page = load_uniform(tab, min(key >> W.page_shift, W.max_pages - 1));
                     const bool ok = page_ok(W, page);
                     if (!ok) p.holes |= 1 << r;
-                    p.at[r] = ((((size_t)(ok ? page : 0) * n_kv + h) << W.page_shift) + (key & ((1 << W.page_shift) - 1))) * CH - r * 16 * CH;
+                    p.at[r] = ((((size_t)(ok ? page : 0) * n_kv + h) << W.page_shift) + (key & ((1 << W.page_shift) - 1))) * CH * 16 - r * 16 * CH * 16;
                 }
             }
             return p;
         };
+        // pair u of a tile, in the first run or the second, from `lane_at` bytes on (rows: one base for all lanes and an offset of 32 bits each)
+        auto pair_at = [&](const void* cache, const void* tree, const Place& p, int u, bool second, int lane_at) {
+            const unsigned char* X = static_cast<const unsigned char*>(p.tree ? tree : cache);
+            const uint32_t off = (uint32_t)min(u, p.last) * (uint32_t)p.stride + lane_at;
+            return reinterpret_cast<const tu32x4_t*>(X + (!ROWS && NT == 2 && second ? p.at[NT - 1] : p.at[0]) + off);
+        };
         T128 kr[NT][KS], vr[VL];
         auto load_k = [&](const Place& p) {
-            const tu32x4_t* run = static_cast<const tu32x4_t*>(p.tree ? TP.k_tree : W.K) + (!ROWS && NT == 2 && n16 >= 8 ? p.at[NT - 1] : p.at[0]);
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) {
-                const int key = BF ? n16 / 4 * 8 + nt * 4 + n16 % 4 : n16;   // with this order, a lane's logits are keys quad * 8 + u (fp32: quad * 4 + i)
-                const tu32x4_t* x = run + (uint32_t)(min(key, p.last) * p.stride);
+                // with this order of keys, a lane's logits are keys quad * 8 + u (fp32: quad * 4 + i)
+                const tu32x4_t* x = pair_at(W.K, TP.k_tree, p, BF ? n16 / 4 * 8 + nt * 4 + n16 % 4 : n16, n16 >= 8, quad * 16);
 #pragma unroll
-                for (int ks = 0; ks < KS; ++ks) kr[nt][ks].u = x[ks * 4 + quad];
+                for (int ks = 0; ks < KS; ++ks) kr[nt][ks].u = x[ks * 4];
             }
         };
-        auto v_run = [&](const Place& p, int quad) {
-            return static_cast<const tu32x4_t*>(p.tree ? TP.v_tree : W.V) + (!ROWS && NT == 2 && quad >= 2 ? p.at[NT - 1] : p.at[0]);
-        };
         auto load_v = [&](const Place& p) {
-            const tu32x4_t* run = v_run(p, quad);
 #pragma unroll
             for (int u = 0; u < (BF ? 8 : 4); ++u) {
-                const tu32x4_t* x = run + (uint32_t)(min(quad * (BF ? 8 : 4) + u, p.last) * p.stride);
+                const tu32x4_t* x = pair_at(W.V, TP.v_tree, p, quad * (BF ? 8 : 4) + u, quad >= 2, n16 * (BF && D == 64 ? 8 : 16));
                 if constexpr (!BF) {
 #pragma unroll
-                    for (int c = 0; c < D / 64; ++c) vr[u * (D / 64) + c].u = x[c * 16 + n16];
+                    for (int c = 0; c < D / 64; ++c) vr[u * (D / 64) + c].u = x[c * 16];
                 } else if constexpr (D == 128) {
-                    vr[u].u = x[n16];
+                    vr[u].u = *x;
                 } else {
-                    const tu32x2_t y = reinterpret_cast<const tu32x2_t*>(x)[n16];
+                    const tu32x2_t y = *reinterpret_cast<const tu32x2_t*>(x);
                     vr[u].w[0] = y.x;
                     vr[u].w[1] = y.y;
                 }
@@ -245,14 +263,10 @@ __device__ __forceinline__ void tree_tile(const TreeParams& TP, int item, int sp
         if (windowed || some_tree) span_of<TM>(s_tree, windowed, lo, hi, level_lo, level_hi);
         else __syncthreads();
         const int any_from = windowed ? n + level_lo - W.window + 1 : 0, all_from = windowed ? n + level_hi - W.window + 1 : 0;
-        bool mine[RB];   // this run's rows
-        int from[RB];    // they see pairs of the cache from here on (and the sinks)
         float m_run[RB], l_run[RB];
         tf32x4_t o[RB][ET];
 #pragma unroll
         for (int rb = 0; rb < RB; ++rb) {
-            mine[rb] = tok[rb] >= lo && tok[rb] <= hi;
-            from[rb] = windowed ? n + s_tree.level[tok[rb]] - W.window + 1 : 0;
             m_run[rb] = -INFINITY;
             l_run[rb] = 0.f;
 #pragma unroll
@@ -295,21 +309,24 @@ __device__ __forceinline__ void tree_tile(const TreeParams& TP, int item, int sp
             // everything seen by every row: no masks
             const bool whole = !at.tree && at.base + KT <= n && !at.holes && (at.base >= all_from || at.base + KT <= W.sink);
             if (!whole) {
-                const int k0 = quad * (NT * 4);   // first of the lane's keys in the tile
+                int me = lane;
+                asm volatile("" : "+v"(me));
+                const int quad = me >> 4, n16 = me & 15, k0 = quad * (NT * 4);   // first of the lane's keys in the tile
                 const bool there = !(at.holes >> (NT == 2 && quad >= 2 ? 1 : 0) & 1);   // (its keys of K and of V lie in the same run)
 #pragma unroll
                 for (int rb = 0; rb < RB; ++rb) {
                     uint32_t sees = 0;   // a bit for each of the lane's keys
+                    const int tok = token_of(r0 + min(rb * 16 + n16, rows - 1)) - w.tok_lo, from = windowed ? n + s_tree.level[tok] - W.window + 1 : 0;
                     if (at.tree) {
-                        sees = s_tree.sees[tok[rb]][at.base / 32] >> (at.base % 32 + k0);
+                        sees = s_tree.sees[tok][at.base / 32] >> (at.base % 32 + k0);
                     } else {
 #pragma unroll
                         for (int j = 0; j < NT * 4; ++j) {
                             const int key = at.base + k0 + j;
-                            sees |= (uint32_t)(there & (key < n) & ((key >= from[rb]) | (key < W.sink))) << j;
+                            sees |= (uint32_t)(there & (key < n) & ((key >= from) | (key < W.sink))) << j;
                         }
                     }
-                    if (!mine[rb]) sees = 0;
+                    if (tok < lo || tok > hi) sees = 0;
 #pragma unroll
                     for (int j = 0; j < NT * 4; ++j) s[rb][j] = sees >> j & 1 ? s[rb][j] : -INFINITY;
                 }
@@ -386,6 +403,9 @@ __device__ __forceinline__ void tree_tile(const TreeParams& TP, int item, int sp
         if (i < t_end) tile(std::true_type());
 
         // ---- merge the wavefronts ----------------------------------------------------------------------------------
+        int tid = threadIdx.x;   // (opaque: or all that the merge derives from it is kept in registers over the loop)
+        asm volatile("" : "+v"(tid));
+        const int n16 = tid & 15, quad = (tid & (kWave - 1)) >> 4;
 #pragma unroll
         for (int rb = 0; rb < RB; ++rb) {
             const float l = quad_sum(l_run[rb]);
@@ -438,8 +458,9 @@ __device__ __forceinline__ void tree_tile(const TreeParams& TP, int item, int sp
                 a[3] = fmaf(v.w, f, a[3]);
             }
             if (splits > 1) {
-                *reinterpret_cast<float4*>(P.rec + (rec + r) * D + d) = make_float4(a[0], a[1], a[2], a[3]);
-                if (d == 0) P.rec_ml[rec + r] = make_float2(s_M[r], s_L[r]);
+                put2(P.rec + rec * D + x * 2, a[0], a[1]);   // (neighbouring lanes side by side: these stores are not gathered on their way)
+                put2(P.rec + rec * D + TM * D / 2 + x * 2, a[2], a[3]);
+                if (d == 0) put2(reinterpret_cast<float*>(P.rec_ml + rec + r), s_M[r], s_L[r]);
                 continue;
             }
             store_row<T, D, false>(P, ((size_t)(t.begin + token) * n_kv + h) * g + (r0 + r - token * g), d, a, s_M[r], s_L[r]);
@@ -449,6 +470,75 @@ __device__ __forceinline__ void tree_tile(const TreeParams& TP, int item, int sp
         lo = hi + 1;
         hi = nodes - 1;
         }
+        if (splits == 1) continue;
+        // the last workgroup to arrive adds the records up, in the order of the splits
+        int tid = threadIdx.x;
+        asm volatile("" : "+v"(tid));
+        arrived();
+        __syncthreads();
+        if (tid == 0) s_bad = last_one(TP.here + item * 4, splits);
+        __syncthreads();
+        if (!scalar(s_bad)) return;   // (a split tile is its place's only one)
+        // (in LDS, in the place of the wavefronts' own: every split's factor for a row)
+        float (*s_f)[TM] = reinterpret_cast<float (*)[TM]>(smem_tree);
+        static_assert(kMostTreeSplits <= WAVES * 16 && (size_t)kMostTreeSplits * TM <= (size_t)WAVES * TM * PART, "room for the factors");
+        const size_t rec = (size_t)item * P.splits * TM;
+        if (tid < rows) {
+            float2 ml[kMostTreeSplits];
+            float M = -INFINITY, L = 0.f;
+#pragma unroll
+            for (int u = 0; u < kMostTreeSplits; ++u) {
+                ml[u] = get2(reinterpret_cast<const float*>(P.rec_ml + rec + min(u, splits - 1) * TM + tid));
+                M = fmaxf(M, ml[u].x);   // (the copies past the end change nothing)
+            }
+            const float ref = ref_of(M);
+#pragma unroll
+            for (int u = 0; u < kMostTreeSplits; ++u) {
+                const float f = __builtin_amdgcn_exp2f(ml[u].x - ref);
+                s_f[u][tid] = f;
+                L = u < splits ? fmaf(ml[u].y, f, L) : L;
+            }
+            s_M[tid] = M;
+            s_L[tid] = L;
+        }
+        __syncthreads();
+        constexpr int UNITS = TM * (D / 4) / (WAVES * kWave);   // four channels of a row, this many a thread
+        float a[UNITS][4];
+#pragma unroll
+        for (int y = 0; y < UNITS; ++y)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) a[y][k] = 0.f;
+        for (int s0 = 0; s0 < splits; s0 += 4) {   // four records' loads in flight
+            float2 v[4][UNITS][2];
+#pragma unroll
+            for (int u = 0; u < 4; ++u)
+#pragma unroll
+                for (int y = 0; y < UNITS; ++y) {
+                    const float* from = P.rec + (rec + min(s0 + u, splits - 1) * TM) * D + min(tid + y * WAVES * kWave, rows * (D / 4) - 1) * 2;
+                    v[u][y][0] = get2(from);
+                    v[u][y][1] = get2(from + TM * D / 2);
+                }
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                if (s0 + u >= splits) break;
+#pragma unroll
+                for (int y = 0; y < UNITS; ++y) {
+                    const float f = s_f[s0 + u][min((tid + y * WAVES * kWave) / (D / 4), rows - 1)];
+                    a[y][0] = fmaf(v[u][y][0].x, f, a[y][0]);
+                    a[y][1] = fmaf(v[u][y][0].y, f, a[y][1]);
+                    a[y][2] = fmaf(v[u][y][1].x, f, a[y][2]);
+                    a[y][3] = fmaf(v[u][y][1].y, f, a[y][3]);
+                }
+            }
+        }
+#pragma unroll
+        for (int y = 0; y < UNITS; ++y) {
+            const int x = tid + y * WAVES * kWave, r = x / (D / 4), d = x % (D / 4) * 4;
+            if (r >= rows) break;
+            const int token = token_of(r0 + r);
+            store_row<T, D, false>(P, ((size_t)(t.begin + token) * n_kv + h) * g + (r0 + r - token * g), d, a[y], s_M[r], s_L[r]);
+        }
+        return;
     }
 }
 
@@ -479,6 +569,24 @@ __device__ __forceinline__ void lds_barrier() {
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
+}
+
+// a lane's share of a row: x in the layout of the products, times inv; M and L
+template <typename T, int D>
+__device__ __forceinline__ void store_wide(const AttnPagedParams& P, size_t row, int quad, const tf32x4_t (&x)[D / 16], float M, float L, float inv) {
+#pragma unroll
+    for (int e = 0; e < D / 16; e += sizeof(T) == 2 ? 1 : 4) {
+        if constexpr (sizeof(T) == 2) {   // channels e * 16 + quad * 4 ..
+            const tf32x4_t a = x[e] * inv;
+            *reinterpret_cast<tu32x2_t*>(reinterpret_cast<bf16_t*>(P.out) + row * D + e * 16 + quad * 4) = tu32x2_t{pack_bf16(a[0], a[1]), pack_bf16(a[2], a[3])};
+        } else {
+#pragma unroll
+            for (int k = 0; k < 4; ++k)   // e / 4 * 64 + (quad * 4 + k) * 4 ..
+                *reinterpret_cast<float4*>(reinterpret_cast<float*>(P.out) + row * D + e / 4 * 64 + (quad * 4 + k) * 4) =
+                    make_float4(x[e][k] * inv, x[e + 1][k] * inv, x[e + 2][k] * inv, x[e + 3][k] * inv);
+        }
+    }
+    if (P.stats && quad == 0) P.stats[row] = make_float2(M, L);
 }
 
 template <typename T, int D, int CT, bool ROWS>
@@ -843,46 +951,115 @@ __device__ __forceinline__ void wide_tile(const TreeParams& TP, int item, int sp
             continue;
         }
 
-        // every wavefront has its rows' own
+        // Every wavefront has its rows' own.  Records: its registers as they are.
         int lane = threadIdx.x & (kWave - 1);   // (opaque, as above)
         asm volatile("" : "+v"(lane));
         const int n16 = lane & 15, quad = lane >> 4;
+        const size_t rec0 = (size_t)item * P.splits * 4 + wave;   // of split 0; 4 a split on
 #pragma unroll
         for (int ct = 0; ct < CT; ++ct) {
-            const float l = quad_sum(l_run[ct]), f = __builtin_amdgcn_exp2f(m_ref[ct] - ref_of(m_top[ct]));
-            const int r = w0 + ct * 16 + n16;
-            const int token = token_of(min(r, r0 + rows - 1));
+            const float l = quad_sum(l_run[ct]);
+            const int r = w0 + ct * 16 + n16, token = token_of(min(r, r0 + rows - 1));
             if (r >= r0 + rows || token - w.tok_lo < lo || token - w.tok_lo > hi) continue;
-            const size_t row = ((size_t)(t.begin + token) * n_kv + h) * g + (r - token * g), rec = ((size_t)item * P.splits + split) * TM + (r - r0);
-            const float mul = splits > 1 ? f : l == 0.f ? 0.f : 1.0f / l;
+            if (splits > 1) {
+                const size_t rec = rec0 + (size_t)split * 4;
+                float* to = P.rec + (rec * CT + ct) * (ET * 256) + lane * 2;   // (neighbouring lanes side by side)
 #pragma unroll
-            for (int e = 0; e < ET; e += BF ? 1 : 4) {
-                if constexpr (BF) {   // channels e * 16 + quad * 4 ..
-                    const tf32x4_t a = o[e][ct] * mul;
-                    const int d = e * 16 + quad * 4;
-                    if (splits > 1) *reinterpret_cast<float4*>(P.rec + rec * D + d) = make_float4(a[0], a[1], a[2], a[3]);
-                    else *reinterpret_cast<tu32x2_t*>(reinterpret_cast<bf16_t*>(P.out) + row * D + d) = tu32x2_t{pack_bf16(a[0], a[1]), pack_bf16(a[2], a[3])};
-                } else {
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) {   // e / 4 * 64 + (quad * 4 + k) * 4 ..
-                        const float4 a = make_float4(o[e][ct][k] * mul, o[e + 1][ct][k] * mul, o[e + 2][ct][k] * mul, o[e + 3][ct][k] * mul);
-                        const int d = e / 4 * 64 + (quad * 4 + k) * 4;
-                        if (splits > 1) *reinterpret_cast<float4*>(P.rec + rec * D + d) = a;
-                        else *reinterpret_cast<float4*>(reinterpret_cast<float*>(P.out) + row * D + d) = a;
-                    }
+                for (int e = 0; e < ET; ++e) {
+                    put2(to + e * 256, o[e][ct][0], o[e][ct][1]);
+                    put2(to + e * 256 + 128, o[e][ct][2], o[e][ct][3]);
                 }
+                float* ml = reinterpret_cast<float*>(P.rec_ml) + (rec * CT + ct) * 256 + lane * 2;
+                put2(ml, m_ref[ct], m_top[ct]);
+                put2(ml + 128, l, 0.f);
+                continue;
             }
-            if (quad == 0) {
-                const float2 ml = make_float2(m_top[ct], l * f);
-                if (splits > 1) P.rec_ml[rec] = ml;
-                else if (P.stats) P.stats[row] = ml;
-            }
+            tf32x4_t x[ET];
+#pragma unroll
+            for (int e = 0; e < ET; ++e) x[e] = o[e][ct];
+            store_wide<T, D>(P, ((size_t)(t.begin + token) * n_kv + h) * g + (r - token * g), quad, x, m_top[ct], l * __builtin_amdgcn_exp2f(m_ref[ct] - ref_of(m_top[ct])),
+                             l == 0.f ? 0.f : 1.0f / l);
         }
         __syncthreads();   // the LDS is the next run's
         if (hi == nodes - 1) break;
         lo = hi + 1;
         hi = nodes - 1;
         }
+        if (splits == 1) continue;
+        // the last split's wavefront to arrive adds its rows' records up, in the order of the splits
+        if (w_rows <= 0) return;   // (a split tile is its place's only one)
+        int lane = threadIdx.x & (kWave - 1);   // (opaque, as above)
+        asm volatile("" : "+v"(lane));
+        const int n16 = lane & 15, quad = lane >> 4;
+        arrived();
+        int last = 0;
+        if (lane == 0) last = last_one(TP.here + item * 4 + wave, splits);
+        if (!scalar(__shfl(last, 0))) return;
+        const size_t rec0 = (size_t)item * P.splits * 4 + wave;
+        auto ml_of = [&](int s, int ct) { return reinterpret_cast<const float*>(P.rec_ml) + ((rec0 + (size_t)min(s, splits - 1) * 4) * CT + ct) * 256 + lane * 2; };
+        float top[CT], ref[CT], l[CT];   // largest logits, the references that the sums belong to
+        tf32x4_t x[CT][ET];
+#pragma unroll
+        for (int ct = 0; ct < CT; ++ct) {
+            top[ct] = ref[ct] = -INFINITY;
+            l[ct] = 0.f;
+#pragma unroll
+            for (int e = 0; e < ET; ++e) x[ct][e] = (tf32x4_t){0.f, 0.f, 0.f, 0.f};
+        }
+        for (int s0 = 0; s0 < splits; s0 += 8) {
+            float2 m[8][CT];
+#pragma unroll
+            for (int u = 0; u < 8; ++u)
+#pragma unroll
+                for (int ct = 0; ct < CT; ++ct) m[u][ct] = get2(ml_of(s0 + u, ct));   // (the copies past the end change nothing)
+#pragma unroll
+            for (int u = 0; u < 8; ++u)
+#pragma unroll
+                for (int ct = 0; ct < CT; ++ct) {
+                    ref[ct] = fmaxf(ref[ct], m[u][ct].x);
+                    top[ct] = fmaxf(top[ct], m[u][ct].y);
+                }
+        }
+        for (int s0 = 0; s0 < splits; s0 += 2) {   // two records' loads in flight
+            float2 v[2][CT][ET][2], m[2][CT], sum[2][CT];
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+#pragma unroll
+                for (int ct = 0; ct < CT; ++ct) {
+                    m[u][ct] = get2(ml_of(s0 + u, ct));
+                    sum[u][ct] = get2(ml_of(s0 + u, ct) + 128);
+                    const float* from = P.rec + ((rec0 + (size_t)min(s0 + u, splits - 1) * 4) * CT + ct) * (ET * 256) + lane * 2;
+#pragma unroll
+                    for (int e = 0; e < ET; ++e) {
+                        v[u][ct][e][0] = get2(from + e * 256);
+                        v[u][ct][e][1] = get2(from + e * 256 + 128);
+                    }
+                }
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                if (s0 + u >= splits) break;
+#pragma unroll
+                for (int ct = 0; ct < CT; ++ct) {
+                    const float f = __builtin_amdgcn_exp2f(m[u][ct].x - ref_of(ref[ct]));
+                    l[ct] = fmaf(sum[u][ct].x, f, l[ct]);
+#pragma unroll
+                    for (int e = 0; e < ET; ++e) {
+                        x[ct][e][0] = fmaf(v[u][ct][e][0].x, f, x[ct][e][0]);
+                        x[ct][e][1] = fmaf(v[u][ct][e][0].y, f, x[ct][e][1]);
+                        x[ct][e][2] = fmaf(v[u][ct][e][1].x, f, x[ct][e][2]);
+                        x[ct][e][3] = fmaf(v[u][ct][e][1].y, f, x[ct][e][3]);
+                    }
+                }
+            }
+        }
+#pragma unroll
+        for (int ct = 0; ct < CT; ++ct) {
+            const int r = w0 + ct * 16 + n16, token = token_of(min(r, r0 + rows - 1));
+            if (r < r0 + rows)
+                store_wide<T, D>(P, ((size_t)(t.begin + token) * n_kv + h) * g + (r - token * g), quad, x[ct], top[ct], l[ct] * __builtin_amdgcn_exp2f(ref[ct] - ref_of(top[ct])),
+                                 l[ct] == 0.f ? 0.f : 1.0f / l[ct]);
+        }
+        return;
     }
 }
 

@@ -10,36 +10,13 @@ namespace fk {
 // KIND: 1, 2: tree_tile with so many 16-row blocks; 4, 8: wide_tile with so many
 template <typename T, int D, int KIND> struct TreeKind {
     static constexpr bool WIDE = KIND >= 4;
-    static constexpr int TM = 16 * KIND;
-    static constexpr int KT = WIDE ? WideCfg<T, D, WIDE ? KIND / 4 : 1>::KT : TreeCfg<T, D, WIDE ? 1 : KIND>::KT;
     static constexpr size_t LDS = WIDE ? WideCfg<T, D, WIDE ? KIND / 4 : 1>::LDS : TreeCfg<T, D, WIDE ? 1 : KIND>::LDS;
 };
 
 template <typename T, int D, int KIND, bool ROWS>
-__global__ __launch_bounds__(256, KIND == 1 ? 3 : 2) void tree_kernel(const TreeParams P) {
+__global__ __launch_bounds__(256, KIND == 1 && D == 64 ? 3 : 2) void tree_kernel(const TreeParams P) {
     if constexpr (KIND >= 4) wide_tile<T, D, KIND / 4, ROWS>(P, blockIdx.x, blockIdx.y);
     else tree_tile<T, D, KIND, ROWS>(P, blockIdx.x, blockIdx.y);
-}
-
-// the second launch, where a tile's pairs may have been split
-template <typename T, int D, int KIND, bool ROWS>
-__global__ __launch_bounds__(256) void tree_merge_kernel(const AttnPagedParams P) {
-    using C = TreeKind<T, D, KIND>;
-    constexpr int TM = C::TM;
-    const PagedParams& W = P.view;
-    const int item = blockIdx.x, part = blockIdx.y * 16;
-    TreeWork w;
-    if (!tree_work<ROWS>(P, item, TM, w) || !w.t.one) return;   // (places that take several tiles do not split them)
-    tree_tile_of(P, TM, C::KT, w);
-    if (w.splits == 1) return;
-    const size_t rec = (size_t)item * P.splits * TM;
-    const int rows = min(16, w.rows - part);
-    for (int x = threadIdx.x; x < rows * (D / 4); x += 256) {
-        const int r = part + x / (D / 4), d = x % (D / 4) * 4;
-        const Merged<D> o = merge_records<D>(P, rec + r, TM, w.splits, d);
-        const int token = divide(w.r0 + r, W.g, W.g_magic);
-        store_row<T, D, false>(P, ((size_t)(w.t.begin + token) * W.n_kv + w.h) * W.g + (w.r0 + r - token * W.g), d, o.a, o.M, o.L);
-    }
 }
 
 // ---- host side ---------------------------------------------------------------------------------------------------
@@ -57,13 +34,19 @@ static TreePlan tree_plan(const fk_paged_desc* d, int32_t n_tokens, int32_t max_
     p.shift = 8 - kt_shift;
     const long long items = (long long)p.grid.places * d->n_kv_heads, fill = p.kind == 1 ? 768 : 512;
     long long s = items < fill ? fill / items : 1;
-    s = std::min(std::min(s, 16ll), (pairs + tree) >> 8);
-    p.splits = (int)std::max(s, 1ll);
+    s = std::min(std::min(s, (long long)kMostTreeSplits), (pairs + tree) >> 8);
+    p.splits = items > kSplitItems ? 1 : (int)std::max(s, 1ll);
     return p;
+}
+// workspace: counters, the same for every call (so that calls of any sizes may take turns with one workspace) | sums and references of records | records
+static constexpr size_t kCounterBytes = kSplitItems * 4 * sizeof(uint32_t);
+static size_t ml_bytes(const TreePlan& p, long long items) {   // wide: 16 bytes a lane and 16 rows; 8 a row
+    return p.splits > 1 ? up256((size_t)items * p.splits * 16 * p.kind * (p.kind >= 4 ? 64 : 8)) : 0;
 }
 static size_t tree_workspace(const fk_paged_desc* d, int32_t n_tokens, int32_t max_tree, int32_t max_len) {
     const TreePlan p = tree_plan(d, std::max(n_tokens, 1), max_tree, max_len);
-    return 16 + record_bytes((long long)p.grid.places * d->n_kv_heads, p.splits, 16 * p.kind, d->head_dim);
+    const long long items = (long long)p.grid.places * d->n_kv_heads;
+    return kCounterBytes + ml_bytes(p, items) + (p.splits > 1 ? (size_t)items * p.splits * 16 * p.kind * d->head_dim * sizeof(float) : 0);
 }
 
 template <typename T, int D, int KIND, bool ROWS> static fk_status tree_start(const TreeParams& P, hipStream_t st) {
@@ -73,7 +56,6 @@ template <typename T, int D, int KIND, bool ROWS> static fk_status tree_start(co
     if (!allow_dynamic_lds((const void*)kern, C::LDS, lds_ok)) return FK_ERR_LAUNCH;
     const int items = P.a.grid.places * P.a.view.n_kv;
     hipLaunchKernelGGL(kern, dim3((unsigned)items, (unsigned)P.a.splits), dim3(256), C::LDS, st, P);
-    if (P.a.splits > 1) hipLaunchKernelGGL((tree_merge_kernel<T, D, KIND, ROWS>), dim3((unsigned)items, KIND), dim3(256), 0, st, P.a);
     return launch_status();
 }
 template <typename T, int D, bool ROWS> static fk_status tree_rows_of(int kind, const TreeParams& P, hipStream_t st) {
@@ -84,9 +66,9 @@ template <bool ROWS> static fk_status tree_launch(const fk_paged_desc* d, const 
     A.grid = p.grid;
     A.splits = p.splits;
     A.split_shift = p.shift;
-    const size_t items = (size_t)p.grid.places * d->n_kv_heads;
-    A.rec_ml = reinterpret_cast<float2*>(ws);
-    A.rec = reinterpret_cast<float*>(static_cast<char*>(ws) + up256(items * p.splits * 16 * p.kind * sizeof(float2)));
+    P.here = static_cast<uint32_t*>(ws);
+    A.rec_ml = reinterpret_cast<float2*>(static_cast<char*>(ws) + kCounterBytes);
+    A.rec = reinterpret_cast<float*>(static_cast<char*>(ws) + kCounterBytes + ml_bytes(p, (long long)p.grid.places * d->n_kv_heads));
     if (d->dtype == FK_F32) return d->head_dim == 64 ? tree_rows_of<float, 64, ROWS>(p.kind, P, st) : tree_rows_of<float, 128, ROWS>(p.kind, P, st);
     return d->head_dim == 64 ? tree_rows_of<bf16_t, 64, ROWS>(p.kind, P, st) : tree_rows_of<bf16_t, 128, ROWS>(p.kind, P, st);
 }

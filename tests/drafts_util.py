@@ -128,7 +128,7 @@ class TreeCase:
             s["ws"] = fk.new_tree_attn_workspace(s["desc"], self.n_tokens, self.max_tree, self.max_len)
         s["out"] = torch.full_like(s["q"], 7.0)
         s["stats"] = torch.full((self.n_tokens, Hq, 2), 7.0, device="cuda")
-        s["ws"].fill_(255)   # contents do not matter: NaN where floats lie
+        s["ws"][16384:] = 255   # behind the counters contents do not matter: NaN where floats lie
         return s
 
     def run(self, s, stats=True, stream=None):
