@@ -20,22 +20,50 @@ __global__ __launch_bounds__(256, KIND == 1 && D == 64 ? 3 : 2) void tree_kernel
 }
 
 // ---- host side ---------------------------------------------------------------------------------------------------
+// Which kernel takes a call's tiles, by the query rows of its largest tree (us, in the order of the kinds 16, 32, 64, 128 rows; 16 sequences of 2112
+// pairs, 8 heads of g 4, D 128 where nothing else is said): 16 rows 28.6, 29.2, 29.3; 32 rows -, 32.0, 31.3, of one sequence -, 14.7, 15.5;
+// 48 rows -, -, 34.2, 40.2; 128 rows of 4 sequences -, -, 22.2, 31.2; up to 182 rows of 16, 4 heads of g 7, 4160 pairs -, -, 53, 56; up to 256 rows of 16
+// -, -, 73, 62: the last kind where its tiles are many.  fp32, where products take longer than loads: 4 sequences, 32 rows 22, 29, 36; 56 rows 33, -, 40, 59; up
+// to 128 rows 63, -, 57, 66 - the first kind, tile by tile, up to 64 rows, then the third.
 struct TreePlan {
     int kind;                  // 16-row blocks of a tile
     TileGrid grid;
     int splits, shift;
 };
+static long long items_of(const fk_paged_desc* d, const TileGrid& G) { return (long long)G.places * d->n_kv_heads; }
+
+// Splits of a tile's pairs, each 256 and more, where the items are few.  16 and 32 rows, bound by memory: up to 512 workgroups (16 rows, D 128: 128 items of 2112
+// pairs whole 31.2, in two 29.2, four 28.6; 8 items in four 13.9, eight 11.1, sixteen 12.4), D 64 up to 192 (128 items whole 18.3, in two 20.1).  Others by an
+// estimate: a turn of the loop takes `turn[k]` us with k + 1 workgroups on a CU, and records go out and come back at 4 TB/s (up to 182 rows of 4160 pairs, 192
+// items of 64 rows: whole 100, in two 68, three 61, four 53, five 67; up to 256 rows of 2112, 256 items of 128: 76, 62, 81, 77).
+static int tree_splits(const fk_paged_desc* d, int kind, long long items, long long pairs) {
+    const long long most = std::min((long long)kMostTreeSplits, pairs >> 8);
+    if (items > kSplitItems) return 1;
+    if (kind <= 2) return (int)std::max(1ll, std::min(most, (d->head_dim == 128 ? 512 : 192) / items));
+    const bool bf16 = d->dtype == FK_BF16;
+    const double wide = kind == 8 ? 2. : 1., turn[3] = {wide, wide * 1.3, wide * 1.6};   // (of as many pairs as take 0.75 us alone with 64 rows)
+    const int held = kind == 8 ? 2 : 3;   // workgroups that a CU holds
+    const double turns = (double)pairs / (kind == 8 ? 64 : 32) * d->head_dim / 128 * (kind == 8 ? 1. : .75) * (bf16 ? 1. : 4.);
+    int best = 1;
+    double least = 0;
+    for (int s = 1; s == 1 || s <= most; ++s) {
+        const long long per_cu = (items * s + 255) / 256, rest = per_cu % held;
+        const double rounds = (double)(per_cu / held) * turn[held - 1] + (rest ? turn[rest - 1] : 0.);
+        const double time = rounds * turns / s + (s == 1 ? 0. : 3 + (double)items * s * 16 * kind * d->head_dim * 8 / 4e6);
+        if (s == 1 || time < least) least = time, best = s;
+    }
+    return best;
+}
 static TreePlan tree_plan(const fk_paged_desc* d, int32_t n_tokens, int32_t max_tree, long long pairs) {
     const int g = d->n_q_heads / d->n_kv_heads, tree = std::min(std::min(max_tree, n_tokens), kTreeNodes), rows = tree * g;
-    TreePlan p = {rows <= 16 ? 1 : rows <= 32 ? 2 : rows <= 64 ? 4 : 8, {}, 1, 0};
+    TreePlan p = {};
+    if (d->dtype == FK_F32) p.kind = rows <= 64 ? 1 : 4;
+    else p.kind = rows <= 16 ? 1 : rows <= 32 ? 2 : rows <= 64 || items_of(d, tile_grid(d, n_tokens, tree, 128)) < 160 ? 4 : 8;
     p.grid = tile_grid(d, n_tokens, tree, 16 * p.kind);
     p.grid.most = kTreeNodes * g;
-    const int kt_shift = (d->dtype == FK_BF16 ? 5 : 4) + (p.kind >= 4 ? 1 : 0);
-    p.shift = 8 - kt_shift;
-    const long long items = (long long)p.grid.places * d->n_kv_heads, fill = p.kind == 1 ? 768 : 512;
-    long long s = items < fill ? fill / items : 1;
-    s = std::min(std::min(s, (long long)kMostTreeSplits), (pairs + tree) >> 8);
-    p.splits = items > kSplitItems ? 1 : (int)std::max(s, 1ll);
+    p.splits = tree_splits(d, p.kind, items_of(d, p.grid), pairs + tree);
+    const int kt = p.kind <= 2 ? (d->dtype == FK_BF16 ? 32 : 16) : d->dtype == FK_BF16 && (p.kind == 8 || d->head_dim == 64) ? 64 : d->dtype == FK_BF16 || d->head_dim == 64 ? 32 : 16;
+    p.shift = 8 - __builtin_ctz(kt);
     return p;
 }
 // workspace: counters, the same for every call (so that calls of any sizes may take turns with one workspace) | sums and references of records | records
@@ -45,7 +73,7 @@ static size_t ml_bytes(const TreePlan& p, long long items) {   // wide: 16 bytes
 }
 static size_t tree_workspace(const fk_paged_desc* d, int32_t n_tokens, int32_t max_tree, int32_t max_len) {
     const TreePlan p = tree_plan(d, std::max(n_tokens, 1), max_tree, max_len);
-    const long long items = (long long)p.grid.places * d->n_kv_heads;
+    const long long items = items_of(d, p.grid);
     return kCounterBytes + ml_bytes(p, items) + (p.splits > 1 ? (size_t)items * p.splits * 16 * p.kind * d->head_dim * sizeof(float) : 0);
 }
 
@@ -59,7 +87,11 @@ template <typename T, int D, int KIND, bool ROWS> static fk_status tree_start(co
     return launch_status();
 }
 template <typename T, int D, bool ROWS> static fk_status tree_rows_of(int kind, const TreeParams& P, hipStream_t st) {
-    return kind == 1 ? tree_start<T, D, 1, ROWS>(P, st) : kind == 2 ? tree_start<T, D, 2, ROWS>(P, st) : kind == 4 ? tree_start<T, D, 4, ROWS>(P, st) : tree_start<T, D, 8, ROWS>(P, st);
+    if constexpr (sizeof(T) == 2) {
+        if (kind == 2) return tree_start<T, D, 2, ROWS>(P, st);
+        if (kind == 8) return tree_start<T, D, 8, ROWS>(P, st);
+    }
+    return kind == 1 ? tree_start<T, D, 1, ROWS>(P, st) : tree_start<T, D, 4, ROWS>(P, st);
 }
 template <bool ROWS> static fk_status tree_launch(const fk_paged_desc* d, const TreePlan& p, TreeParams& P, void* ws, hipStream_t st) {
     AttnPagedParams& A = P.a;
@@ -68,7 +100,7 @@ template <bool ROWS> static fk_status tree_launch(const fk_paged_desc* d, const 
     A.split_shift = p.shift;
     P.here = static_cast<uint32_t*>(ws);
     A.rec_ml = reinterpret_cast<float2*>(static_cast<char*>(ws) + kCounterBytes);
-    A.rec = reinterpret_cast<float*>(static_cast<char*>(ws) + kCounterBytes + ml_bytes(p, (long long)p.grid.places * d->n_kv_heads));
+    A.rec = reinterpret_cast<float*>(static_cast<char*>(ws) + kCounterBytes + ml_bytes(p, items_of(d, p.grid)));
     if (d->dtype == FK_F32) return d->head_dim == 64 ? tree_rows_of<float, 64, ROWS>(p.kind, P, st) : tree_rows_of<float, 128, ROWS>(p.kind, P, st);
     return d->head_dim == 64 ? tree_rows_of<bf16_t, 64, ROWS>(p.kind, P, st) : tree_rows_of<bf16_t, 128, ROWS>(p.kind, P, st);
 }
