@@ -23,7 +23,7 @@ __global__ __launch_bounds__(256, KIND == 1 && D == 64 ? 3 : 2) void tree_kernel
 // Which kernel takes a call's tiles, by the query rows of its largest tree (us, in the order of the kinds 16, 32, 64, 128 rows; 16 sequences of 2112
 // pairs, 8 heads of g 4, D 128 where nothing else is said): 16 rows 28.6, 29.2, 29.3; 32 rows -, 32.0, 31.3, of one sequence -, 14.7, 15.5;
 // 48 rows -, -, 34.2, 40.2; 128 rows of 4 sequences -, -, 22.2, 31.2; up to 182 rows of 16, 4 heads of g 7, 4160 pairs -, -, 53, 56; up to 256 rows of 16
-// -, -, 73, 62: the last kind where its tiles are many.  fp32, where products take longer than loads: 4 sequences, 32 rows 22, 29, 36; 56 rows 33, -, 40, 59; up
+// -, -, 73, 62; up to 96 rows of 16 in pages, 1024 to 16384 pairs -, -, 158, 150: beyond 64 rows by the estimate below.  fp32, where products take longer than loads: 4 sequences, 32 rows 22, 29, 36; 56 rows 33, -, 40, 59; up
 // to 128 rows 63, -, 57, 66 - the first kind, tile by tile, up to 64 rows, then the third.
 struct TreePlan {
     int kind;                  // 16-row blocks of a tile
@@ -36,17 +36,16 @@ static long long items_of(const fk_paged_desc* d, const TileGrid& G) { return (l
 // pairs whole 31.2, in two 29.2, four 28.6; 8 items in four 13.9, eight 11.1, sixteen 12.4), D 64 up to 192 (128 items whole 18.3, in two 20.1).  Others by an
 // estimate: a turn of the loop takes `turn[k]` us with k + 1 workgroups on a CU, and records go out and come back at 4 TB/s (up to 182 rows of 4160 pairs, 192
 // items of 64 rows: whole 100, in two 68, three 61, four 53, five 67; up to 256 rows of 2112, 256 items of 128: 76, 62, 81, 77).
-static int tree_splits(const fk_paged_desc* d, int kind, long long items, long long pairs) {
+static int tree_splits(const fk_paged_desc* d, int kind, long long items, long long pairs, double& least) {
     const long long most = std::min((long long)kMostTreeSplits, pairs >> 8);
-    if (items > kSplitItems) return 1;
-    if (kind <= 2) return (int)std::max(1ll, std::min(most, (d->head_dim == 128 ? 512 : 192) / items));
+    least = 0;
+    if (kind <= 2) return items > kSplitItems ? 1 : (int)std::max(1ll, std::min(most, (d->head_dim == 128 ? 512 : 192) / items));
     const bool bf16 = d->dtype == FK_BF16;
     const double wide = kind == 8 ? 2. : 1., turn[3] = {wide, wide * 1.3, wide * 1.6};   // (of as many pairs as take 0.75 us alone with 64 rows)
     const int held = kind == 8 ? 2 : 3;   // workgroups that a CU holds
     const double turns = (double)pairs / (kind == 8 ? 64 : 32) * d->head_dim / 128 * (kind == 8 ? 1. : .75) * (bf16 ? 1. : 4.);
     int best = 1;
-    double least = 0;
-    for (int s = 1; s == 1 || s <= most; ++s) {
+    for (int s = 1; s == 1 || (s <= most && items <= kSplitItems); ++s) {
         const long long per_cu = (items * s + 255) / 256, rest = per_cu % held;
         const double rounds = (double)(per_cu / held) * turn[held - 1] + (rest ? turn[rest - 1] : 0.);
         const double time = rounds * turns / s + (s == 1 ? 0. : 3 + (double)items * s * 16 * kind * d->head_dim * 8 / 4e6);
@@ -57,11 +56,20 @@ static int tree_splits(const fk_paged_desc* d, int kind, long long items, long l
 static TreePlan tree_plan(const fk_paged_desc* d, int32_t n_tokens, int32_t max_tree, long long pairs) {
     const int g = d->n_q_heads / d->n_kv_heads, tree = std::min(std::min(max_tree, n_tokens), kTreeNodes), rows = tree * g;
     TreePlan p = {};
-    if (d->dtype == FK_F32) p.kind = rows <= 64 ? 1 : 4;
-    else p.kind = rows <= 16 ? 1 : rows <= 32 ? 2 : rows <= 64 || items_of(d, tile_grid(d, n_tokens, tree, 128)) < 160 ? 4 : 8;
-    p.grid = tile_grid(d, n_tokens, tree, 16 * p.kind);
+    double time = 0;
+    auto take = [&](int kind) {   // the better one
+        TreePlan x = {kind, tile_grid(d, n_tokens, tree, 16 * kind), 1, 0};
+        double t;
+        x.splits = tree_splits(d, kind, items_of(d, x.grid), pairs + tree, t);
+        if (p.kind == 0 || t < time) p = x, time = t;
+    };
+    if (d->dtype == FK_F32) {
+        take(rows <= 64 ? 1 : 4);
+    } else {
+        take(rows <= 16 ? 1 : rows <= 32 ? 2 : 4);
+        if (rows > 64) take(8);
+    }
     p.grid.most = kTreeNodes * g;
-    p.splits = tree_splits(d, p.kind, items_of(d, p.grid), pairs + tree);
     const int kt = p.kind <= 2 ? (d->dtype == FK_BF16 ? 32 : 16) : d->dtype == FK_BF16 && (p.kind == 8 || d->head_dim == 64) ? 64 : d->dtype == FK_BF16 || d->head_dim == 64 ? 32 : 16;
     p.shift = 8 - __builtin_ctz(kt);
     return p;
