@@ -17,11 +17,15 @@ static constexpr int kNodes = FK_TREE_NODES;
 // A child of a likeliest-token draft (no q) is accepted with probability p(x) / m; else p(x) becomes 0 and m goes down by it.
 // Sums and comparisons in 64 bits: a 32-bit sum over a vocabulary is off by more than its smaller probabilities.
 //
-// One launch.  A sequence's vocabulary is cut into chunks, a workgroup each.  Every workgroup walks the tree (a few hundred numbers, all sent for
-// together) up to the first rejection whose sum is not known, or to the end, and sums its chunk of what is left; the last one to
-// arrive adds the chunks' sums, walks on, sums again by itself where another rejection wants it, and draws the token.
+// One launch.  A sequence's vocabulary is cut into chunks, a workgroup each.  All of them walk the tree alike (a few hundred numbers, all sent for
+// together) up to the first rejection whose sum is not known, or to the end; each sums its chunk of what is left, tells the others, and goes on with
+// the sum of all chunks; the one whose chunk holds the last number draws the token.  Nobody has to wait: a sum that does not come in time (its
+// workgroup may not have begun) is formed by whoever misses it, in the same order, so that it is the same bits.
+// A sum on its way is two words of 32 bits of it and the call's number each: one that holds another number is not there yet.
 // ---------------------------------------------------------------------------------------
 static constexpr int kVerifyThreads = 256, kVerifyWaves = kVerifyThreads / kWave, kMostChunks = 64;
+static constexpr int kRounds = 32;         // sums of a call that are told; more, everybody forms alone
+static constexpr int kPatience = 64;       // looks at a sum that is not there, 0.5 us and more each
 
 struct VerifyParams {
     const float *target, *draft;
@@ -29,66 +33,78 @@ struct VerifyParams {
     const float* uniform;
     int32_t *path, *accepted, *next;
     int n_tokens, batch, vocab, chunks, chunk;   // chunk: numbers of a chunk, a multiple of 4
-    double* part;        // [batch][chunks]
-    uint32_t* arrived;   // [batch], zero between calls
+    uint32_t *call, *done;                       // calls on this workspace so far, workgroups of this one that are done
+    unsigned long long* told;                    // [batch][kRounds][chunks][2]
 };
 
 struct Tree {            // in LDS
     float p[kNodes], q[kNodes], u[kNodes];   // target's and draft's probability of a node's token behind its parent; its number
     int token[kNodes];
     short parent[kNodes], path[kNodes], gone[kNodes];
+    int here[kNodes];                        // rejected tokens of a chunk
     double part[kMostChunks], wave[kVerifyWaves];
-    double c, m, left;
-    int at, depth, n_gone, tried, state, chosen, first[kVerifyWaves];
+    double c, left;
+    unsigned long long missing;
+    int at, depth, n_gone, n_here, tried, state, chosen, first[kVerifyWaves];
 };
 
-// A step of the walk that needs no sums, by one thread: children of `at` from `tried` on.  state 1: a sum with the new c is wanted before the next child;
-// 2: no child is left.
-__device__ __forceinline__ void walk(Tree& T, int nodes, bool drawn) {
-    int at = T.at, i = T.tried;
-    for (;; ++i) {
-        while (i < nodes && T.parent[i] != at) ++i;
-        if (i >= nodes) break;
-        const double p = T.p[i], u = T.u[i];
-        bool yes;
-        if (drawn) {
-            yes = u * T.q[i] * T.m < p - T.c * T.q[i];
-        } else {
-            bool again = false;
-            for (int k = 0; k < T.n_gone; ++k) again |= T.token[T.gone[k]] == T.token[i];
-            yes = u * T.m < (again ? 0.0 : p);
-            if (!yes && !again) {
-                T.gone[T.n_gone++] = (short)i;
-                T.m = fmax(T.m - p, 0.0);
+// The walk as far as it needs no sums, by the first wavefront: children of `at` from `tried` on.  state 1: a sum with the new c is wanted before the next
+// child; 2: no child is left.  m: the sum of what is left (before the first child 1).  All lanes have and store the same values: what a lane reads back it has
+// written itself.
+__device__ __forceinline__ void walk(Tree& T, int nodes, bool drawn, double m) {
+    const int lane = threadIdx.x & (kWave - 1);
+    int at = T.at, from = T.tried, depth = T.depth, n_gone = T.n_gone, state = 2;
+    double c = T.c;
+    for (;;) {
+        int i = -1;
+        for (int w = from / kWave; w * kWave < nodes; ++w) {
+            const int j = w * kWave + lane;
+            const unsigned long long child = __ballot(j < nodes && j >= from && T.parent[min(j, nodes - 1)] == at);
+            if (child) {
+                i = w * kWave + __ffsll((long long)child) - 1;
+                break;
             }
         }
+        if (i < 0) break;
+        from = i + 1;
+        const double p = T.p[i], u = T.u[i];
+        bool yes, again = false;
+        if (drawn) {
+            yes = u * T.q[i] * m < p - c * T.q[i];
+        } else {
+            for (int k0 = 0; k0 < n_gone; k0 += kWave)
+                again |= __ballot(k0 + lane < n_gone && T.token[T.gone[min(k0 + lane, n_gone - 1)]] == T.token[i]) != 0;
+            yes = u * m < (again ? 0.0 : p);
+        }
         if (yes) {
-            T.path[T.depth++] = (short)i;
+            T.path[depth] = (short)i;
+            ++depth;
             at = i;
-            T.c = 0.0;
-            T.m = 1.0;
-            T.n_gone = 0;
+            c = 0.0;
+            m = 1.0;
+            n_gone = 0;
         } else if (drawn) {
-            T.c += T.m;
-            T.at = at;
-            T.tried = i + 1;
-            T.state = 1;
-            return;
+            c += m;
+            state = 1;
+            break;
+        } else if (!again) {
+            T.gone[n_gone] = (short)i;
+            ++n_gone;
+            m = fmax(m - p, 0.0);
         }
     }
     T.at = at;
-    T.state = 2;
+    T.tried = from;
+    T.depth = depth;
+    T.n_gone = n_gone;
+    T.c = c;
+    T.state = state;
 }
 
-// what is left of number v of the vocabulary at the current node
-__device__ __forceinline__ double left_of(const Tree& T, float p, float q, bool drawn) {
-    const double r = drawn ? (double)p - T.c * (double)q : (double)p;
+// what is left of a number of the vocabulary at the current node
+__device__ __forceinline__ double left_of(double c, float p, float q, bool drawn) {
+    const double r = drawn ? (double)p - c * (double)q : (double)p;
     return r > 0.0 ? r : 0.0;
-}
-__device__ __forceinline__ bool is_gone(const Tree& T, int v) {
-    bool x = false;
-    for (int k = 0; k < T.n_gone; ++k) x |= T.token[T.gone[k]] == v;
-    return x;
 }
 
 __device__ __forceinline__ double wave_sum(double x) {
@@ -96,7 +112,6 @@ __device__ __forceinline__ double wave_sum(double x) {
     for (int off = 32; off > 0; off >>= 1) x += __shfl_xor(x, off);
     return x;
 }
-
 __device__ __forceinline__ double wave_scan(double x) {   // inclusive
     const int lane = threadIdx.x & (kWave - 1);
 #pragma unroll
@@ -109,44 +124,124 @@ __device__ __forceinline__ double wave_scan(double x) {   // inclusive
 
 typedef float vf32x4_t __attribute__((ext_vector_type(4), aligned(4)));   // rows of an odd vocabulary start anywhere
 
-// sum over a chunk by `threads` threads, of which this is number `t`
-__device__ __forceinline__ double chunk_sum(const VerifyParams& P, const Tree& T, size_t row, int chunk, int t, int threads) {
-    const bool drawn = P.draft != nullptr;
-    const float *p = P.target + row * P.vocab, *q = drawn ? P.draft + row * P.vocab : nullptr;
-    const int begin = chunk * P.chunk, end = min(begin + P.chunk, P.vocab), whole = begin + (max(end - begin, 0) & ~3);
-    double sum = 0.0;
-    for (int v = begin + t * 4; v < whole; v += threads * 4) {
-        const vf32x4_t a = *reinterpret_cast<const vf32x4_t*>(p + v);
-        vf32x4_t b = {0.f, 0.f, 0.f, 0.f};
-        if (drawn) b = *reinterpret_cast<const vf32x4_t*>(q + v);
+// Four numbers of what is left, from v on; 0 from `end` on.
+struct Four {
+    double r[4];
+};
+__device__ __forceinline__ Four four_of(const Tree& T, const float* p, const float* q, int v, int end, double c) {
+    Four x;
+    vf32x4_t a = {0.f, 0.f, 0.f, 0.f}, b = a;
+    if (v + 4 <= end) {
+        a = *reinterpret_cast<const vf32x4_t*>(p + v);
+        if (q) b = *reinterpret_cast<const vf32x4_t*>(q + v);
+    } else {
 #pragma unroll
-        for (int j = 0; j < 4; ++j) sum += T.n_gone && is_gone(T, v + j) ? 0.0 : left_of(T, a[j], b[j], drawn);
+        for (int j = 0; j < 4; ++j) {
+            if (v + j >= end) break;
+            a[j] = p[v + j];
+            if (q) b[j] = q[v + j];
+        }
     }
-    if (whole + t < end) sum += is_gone(T, whole + t) ? 0.0 : left_of(T, p[whole + t], drawn ? q[whole + t] : 0.f, drawn);
-    return sum;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        x.r[j] = left_of(c, a[j], b[j], q != nullptr);
+        for (int k = 0; k < T.n_here; ++k)   // (hardly ever one)
+            if (T.here[k] == v + j) x.r[j] = 0.0;
+    }
+    return x;
+}
+
+// the rejected tokens that lie in a chunk; all threads
+__device__ __forceinline__ void find_gone(const VerifyParams& P, Tree& T, int chunk) {
+    if (threadIdx.x < kWave) {
+        const int lane = threadIdx.x;
+        int n = 0;
+        for (int k0 = 0; k0 < T.n_gone; k0 += kWave) {
+            const int x = k0 + lane < T.n_gone ? T.token[T.gone[k0 + lane]] : -1;
+            const bool in = x >= chunk * P.chunk && x < (chunk + 1) * P.chunk;
+            const unsigned long long all = __ballot(in);
+            if (in) T.here[n + __popcll(all & ((1ull << lane) - 1))] = x;
+            n += __popcll(all);
+        }
+        if (lane == 0) T.n_here = n;
+    }
+    __syncthreads();
+}
+
+// the sum of what is left in a chunk, into T.part; all threads
+__device__ __forceinline__ void sum_chunk(const VerifyParams& P, Tree& T, int begin, int chunk) {
+    const int tid = threadIdx.x, v0 = chunk * P.chunk, end = min(v0 + P.chunk, P.vocab);
+    find_gone(P, T, chunk);
+    const size_t row = (size_t)(begin + T.at) * P.vocab;
+    const float *p = P.target + row, *q = P.draft ? P.draft + row : nullptr;
+    const double c = T.c;
+    double sum = 0.0;
+    int v = v0 + tid * 4;
+    constexpr int STEP = kVerifyThreads * 4, U = 4;
+    if (T.n_here == 0) {
+        for (; v + (U - 1) * STEP + 4 <= end; v += U * STEP) {   // (all loads ahead of the sums)
+            vf32x4_t a[U], b[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                a[u] = *reinterpret_cast<const vf32x4_t*>(p + v + u * STEP);
+                b[u] = vf32x4_t{0.f, 0.f, 0.f, 0.f};
+                if (q) b[u] = *reinterpret_cast<const vf32x4_t*>(q + v + u * STEP);
+            }
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                double r[4];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) r[j] = left_of(c, a[u][j], b[u][j], q != nullptr);
+                sum += (r[0] + r[1]) + (r[2] + r[3]);
+            }
+        }
+    }
+    for (; v < end; v += STEP) {
+        const Four x = four_of(T, p, q, v, end, c);
+        sum += (x.r[0] + x.r[1]) + (x.r[2] + x.r[3]);
+    }
+    sum = wave_sum(sum);
+    if (tid % kWave == 0) T.wave[tid / kWave] = sum;
+    __syncthreads();
+    if (tid == 0) {
+        double all = 0.0;
+        for (int w = 0; w < kVerifyWaves; ++w) all += T.wave[w];
+        T.part[chunk] = all;
+    }
+    __syncthreads();
 }
 
 __global__ __launch_bounds__(kVerifyThreads) void verify_kernel(const VerifyParams P) {
     __shared__ Tree T;
-    __shared__ bool s_last;
     const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = tid / kWave, b = blockIdx.y, chunk = blockIdx.x;
     const bool drawn = P.draft != nullptr;
+    const uint32_t call = P.chunks > 1 ? __hip_atomic_load(P.call, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) + 1 : 0;
+    // the last one to be done with it: the next call, of whatever sizes, has another number
+    auto be_done = [&]() {
+        if (P.chunks == 1 || tid != 0) return;
+        if (__hip_atomic_fetch_add(P.done, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == (uint32_t)(P.chunks * P.batch) - 1) {
+            __hip_atomic_store(P.done, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            __hip_atomic_store(P.call, call, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        }
+    };
     const int begin = min(max(P.q_start[b], 0), P.n_tokens), nodes = min(max(P.q_start[b + 1], begin), P.n_tokens) - begin;
     if (nodes == 0 || nodes > kNodes) {
         if (chunk == 0 && tid == 0) {
             P.accepted[b] = 0;
             P.next[b] = -1;
         }
+        be_done();
         return;
     }
     for (int i = tid; i < nodes; i += kVerifyThreads) {
         const int up = P.parent[begin + i], x = P.tokens[begin + i];
+        const float u = P.uniform[begin + i];
         const bool there = i > 0 && up >= 0 && up < i && x >= 0 && x < P.vocab;
         const size_t at = (size_t)(begin + (there ? up : 0)) * P.vocab + (there ? x : 0);
-        const float p = P.target[at];
+        const float p = P.target[at], q = drawn ? P.draft[at] : 0.f;
         T.p[i] = there && p > 0.f ? p : 0.f;
-        T.q[i] = there && drawn ? P.draft[at] : 0.f;
-        T.u[i] = P.uniform[begin + i];
+        T.q[i] = there ? q : 0.f;
+        T.u[i] = u;
         T.token[i] = x;
         T.parent[i] = (short)(i > 0 && up < i ? max(up, -1) : -1);
     }
@@ -157,41 +252,46 @@ __global__ __launch_bounds__(kVerifyThreads) void verify_kernel(const VerifyPara
         T.n_gone = 0;
         T.tried = 1;
         T.c = 0.0;
-        T.m = 1.0;
     }
     __syncthreads();
-    if (tid == 0) walk(T, nodes, drawn);
+    if (wave == 0) walk(T, nodes, drawn, 1.0);
     __syncthreads();
-    {
-        const double sum = wave_sum(chunk_sum(P, T, begin + T.at, chunk, tid, kVerifyThreads));
-        if (lane == 0) T.wave[wave] = sum;
-        __syncthreads();
-        if (tid == 0) {
-            double all = 0.0;
-            for (int w = 0; w < kVerifyWaves; ++w) all += T.wave[w];
-            __hip_atomic_store(&P.part[(size_t)b * P.chunks + chunk], all, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-            const uint32_t before = __hip_atomic_fetch_add(&P.arrived[b], 1u, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT);
-            s_last = before == (uint32_t)P.chunks - 1;
+    for (int round = 0;; ++round) {
+        // the sums of what is left at T.at, chunk by chunk
+        sum_chunk(P, T, begin, chunk);
+        if (P.chunks > 1) {
+            unsigned long long* told = P.told + ((size_t)b * kRounds + min(round, kRounds - 1)) * P.chunks * 2;
+            if (wave == 0) {
+                if (round < kRounds && lane < 2) {
+                    const uint64_t bits = (uint64_t)__double_as_longlong(T.part[chunk]);
+                    __hip_atomic_store(told + chunk * 2 + lane, (unsigned long long)call << 32 | (uint32_t)(bits >> (32 * lane)), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+                }
+                bool here = lane >= P.chunks || lane == chunk;
+                for (int look = 0; round < kRounds && look < kPatience; ++look) {
+                    if (!here) {
+                        const unsigned long long lo = __hip_atomic_load(told + lane * 2, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+                        const unsigned long long hi = __hip_atomic_load(told + lane * 2 + 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+                        if ((uint32_t)(lo >> 32) == call && (uint32_t)(hi >> 32) == call) {
+                            T.part[lane] = __longlong_as_double((long long)((uint64_t)(uint32_t)hi << 32 | (uint32_t)lo));
+                            here = true;
+                        }
+                    }
+                    if (__all(here)) break;
+                    __builtin_amdgcn_s_sleep(2);
+                }
+                const unsigned long long missing = __ballot(!here);
+                if (lane == 0) T.missing = missing;
+            }
+            __syncthreads();
+            for (unsigned long long missing = T.missing; missing; missing &= missing - 1) sum_chunk(P, T, begin, __ffsll((long long)missing) - 1);
         }
-        __syncthreads();
-        if (!s_last) return;
-    }
-    if (tid == 0) __hip_atomic_store(&P.arrived[b], 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    if (tid < P.chunks) T.part[tid] = __hip_atomic_load(&P.part[(size_t)b * P.chunks + tid], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    __syncthreads();
-    for (;;) {   // T.part holds the sums of what is left at T.at
         if (wave == 0) {
             const double all = wave_sum(lane < P.chunks ? T.part[lane] : 0.0);
+            const int depth = T.depth, was = T.state;
+            if (was == 1) walk(T, nodes, drawn, all);
             if (lane == 0) {
-                if (T.state == 1) {
-                    const int depth = T.depth;
-                    T.m = all;
-                    walk(T, nodes, drawn);
-                    if (T.state == 2 && T.depth == depth) T.state = 3;   // no child was left: the sums are those to draw from
-                } else {
-                    T.state = 3;
-                }
-                if (T.state == 3 && all == 0.0) {   // nothing is left, by rounding: the target's own distribution
+                if (was != 1 || (T.state == 2 && T.depth == depth)) T.state = 3;   // no child was left: the sums are those to draw from
+                if (T.state == 3 && all == 0.0) {                                  // nothing is left, by rounding: the target's own distribution
                     const bool own = T.c == 0.0 && T.n_gone == 0;
                     T.c = 0.0;
                     T.n_gone = 0;
@@ -201,18 +301,14 @@ __global__ __launch_bounds__(kVerifyThreads) void verify_kernel(const VerifyPara
         }
         __syncthreads();
         if (T.state >= 3) break;
-        for (int c = wave; c < P.chunks; c += kVerifyWaves) {
-            const double sum = wave_sum(chunk_sum(P, T, begin + T.at, c, lane, kWave));
-            if (lane == 0) T.part[c] = sum;
-        }
-        __syncthreads();
     }
-    for (int i = tid; i < nodes; i += kVerifyThreads) P.path[begin + i] = i < T.depth ? T.path[i] : -1;
-    if (tid == 0) P.accepted[b] = T.depth;
-    if (T.state == 4) {   // no mass at all
-        if (tid == 0) P.next[b] = -1;
-        return;
+    be_done();
+    if (chunk == 0) {
+        for (int i = tid; i < nodes; i += kVerifyThreads) P.path[begin + i] = i < T.depth ? T.path[i] : -1;
+        if (tid == 0) P.accepted[b] = T.depth;
+        if (tid == 0 && T.state == 4) P.next[b] = -1;   // no mass at all
     }
+    if (T.state == 4) return;
     if (wave == 0) {   // the chunk that holds the number, the last one with anything where rounding leaves it beyond all
         const double mine = lane < P.chunks ? T.part[lane] : 0.0, incl = wave_scan(mine), want = (double)T.u[0] * __shfl(incl, kWave - 1);
         const unsigned long long hit = __ballot(mine > 0.0 && incl > want), any = __ballot(mine > 0.0);
@@ -223,35 +319,35 @@ __global__ __launch_bounds__(kVerifyThreads) void verify_kernel(const VerifyPara
         }
     }
     __syncthreads();
+    if (T.chosen != chunk) return;
     // in it: four numbers a thread at a time
+    find_gone(P, T, chunk);
     const size_t row = (size_t)(begin + T.at) * P.vocab;
-    const int end = min((T.chosen + 1) * P.chunk, P.vocab);
-    const double want = T.left;
+    const float *p = P.target + row, *q = drawn ? P.draft + row : nullptr;
+    const int end = min((chunk + 1) * P.chunk, P.vocab);
+    const double want = T.left, c = T.c;
     double below = 0.0;
-    int found = -1;   // of this thread: the last number with anything, or the one
-    for (int v0 = T.chosen * P.chunk;; v0 += kVerifyThreads * 4) {
-        double r[4], sum = 0.0;
+    int found = -1;   // of this thread: the last number with anything
+    for (int v0 = chunk * P.chunk;; v0 += kVerifyThreads * 4) {
+        const int v = v0 + tid * 4;
+        const Four x = four_of(T, p, q, v, end, c);
+        double to[4];
+        to[0] = x.r[0];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const int v = v0 + tid * 4 + j;
-            r[j] = 0.0;
-            if (v < end && !is_gone(T, v)) r[j] = left_of(T, P.target[row + v], drawn ? P.draft[row + v] : 0.f, drawn);
-            if (r[j] > 0.0) found = v;
-            sum += r[j];
-        }
-        const double incl = wave_scan(sum);
+        for (int j = 1; j < 4; ++j) to[j] = to[j - 1] + x.r[j];
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            if (x.r[j] > 0.0) found = v + j;
+        const double incl = wave_scan(to[3]);
         __syncthreads();
         if (lane == kWave - 1) T.wave[wave] = incl;
         __syncthreads();
-        double before = below + incl - sum;
+        double before = below + incl - to[3];
         for (int w = 0; w < wave; ++w) before += T.wave[w];
         int one = 0x7fffffff;
 #pragma unroll
-        for (int j = 3; j >= 0; --j) {
-            double to = before;
-            for (int k = 0; k <= j; ++k) to += r[k];
-            if (r[j] > 0.0 && to > want) one = v0 + tid * 4 + j;
-        }
+        for (int j = 3; j >= 0; --j)
+            if (x.r[j] > 0.0 && before + to[j] > want) one = v + j;
         for (int w = 0; w < kVerifyWaves; ++w) below += T.wave[w];
         const unsigned long long hit = __ballot(one != 0x7fffffff);
         if (hit) one = __shfl(one, __ffsll((long long)hit) - 1);
@@ -359,15 +455,17 @@ __global__ __launch_bounds__(1024) void commit_pages_kernel(const CommitParams P
     if (tid == 0 && n > 0) P.len[b] = start + n;
 }
 
-static int verify_chunks(int vocab) { return std::min(std::max((vocab + 2047) / 2048, 1), kMostChunks); }
+// Chunks of 2048 numbers and more, up to 512 workgroups, two to a CU: all at work at once as a rule.
+static int verify_chunks(int batch, int vocab) { return std::max(1, std::min(std::min(512 / batch, vocab / 2048), kMostChunks)); }
 
 }  // namespace fk
 
 using namespace fk;
 
 extern "C" size_t fk_verify_drafts_workspace(int32_t batch, int32_t vocab) {
-    if (batch <= 0 || vocab <= 0) return 0;
-    return ((size_t)batch * sizeof(uint32_t) + 255) / 256 * 256 + (size_t)batch * verify_chunks(vocab) * sizeof(double);
+    if (batch <= 0 || vocab <= 0 || batch > 65535) return 0;
+    const int chunks = verify_chunks(batch, vocab);
+    return 256 + (chunks > 1 ? (size_t)batch * kRounds * chunks * 2 * sizeof(unsigned long long) : 0);
 }
 
 extern "C" fk_status fk_verify_drafts(int32_t batch, int32_t vocab, const float* target, const float* draft, const int32_t* tokens,
@@ -378,10 +476,11 @@ extern "C" fk_status fk_verify_drafts(int32_t batch, int32_t vocab, const float*
     if (!q_start || !n_accepted || !next_token) return FK_ERR_INVALID_ARG;
     if (n_tokens > 0 && (!target || !tokens || !parent || !uniform || !path)) return FK_ERR_INVALID_ARG;
     if (!workspace || workspace_bytes < fk_verify_drafts_workspace(batch, vocab) || !aligned16(workspace)) return FK_ERR_WORKSPACE;
-    VerifyParams P = {target, draft, tokens, parent, q_start, uniform, path, n_accepted, next_token, n_tokens, batch, vocab, verify_chunks(vocab), 0, nullptr, nullptr};
+    VerifyParams P = {target, draft, tokens, parent, q_start, uniform, path, n_accepted, next_token, n_tokens, batch, vocab, verify_chunks(batch, vocab), 0, nullptr, nullptr, nullptr};
     P.chunk = ((vocab + P.chunks - 1) / P.chunks + 3) / 4 * 4;
-    P.arrived = static_cast<uint32_t*>(workspace);
-    P.part = reinterpret_cast<double*>(static_cast<char*>(workspace) + ((size_t)batch * sizeof(uint32_t) + 255) / 256 * 256);
+    P.call = static_cast<uint32_t*>(workspace);
+    P.done = P.call + 1;
+    P.told = reinterpret_cast<unsigned long long*>(static_cast<char*>(workspace) + 256);
     hipLaunchKernelGGL(verify_kernel, dim3(P.chunks, batch), dim3(kVerifyThreads), 0, (hipStream_t)stream, P);
     return launch_status();
 }
