@@ -3,6 +3,7 @@
 #include "paged.h"
 
 #include <algorithm>
+#include <type_traits>
 
 namespace fk {
 
@@ -124,11 +125,11 @@ __device__ __forceinline__ double wave_scan(double x) {   // inclusive
 
 typedef float vf32x4_t __attribute__((ext_vector_type(4), aligned(4)));   // rows of an odd vocabulary start anywhere
 
-// Four numbers of what is left, from v on; 0 from `end` on.
+// Four numbers of what is left, from v on; 0 from `end` on and where `gone` has a bit.
 struct Four {
     double r[4];
 };
-__device__ __forceinline__ Four four_of(const Tree& T, const float* p, const float* q, int v, int end, double c) {
+__device__ __forceinline__ Four four_of(const float* p, const float* q, int v, int end, double c, uint32_t gone) {
     Four x;
     vf32x4_t a = {0.f, 0.f, 0.f, 0.f}, b = a;
     if (v + 4 <= end) {
@@ -143,12 +144,18 @@ __device__ __forceinline__ Four four_of(const Tree& T, const float* p, const flo
         }
     }
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        x.r[j] = left_of(c, a[j], b[j], q != nullptr);
-        for (int k = 0; k < T.n_here; ++k)   // (hardly ever one)
-            if (T.here[k] == v + j) x.r[j] = 0.0;
-    }
+    for (int j = 0; j < 4; ++j) x.r[j] = gone >> j & 1 ? 0.0 : left_of(c, a[j], b[j], q != nullptr);
     return x;
+}
+// A bit for each rejected token among this thread's numbers v, v + 1, v + 2, v + 3, then those kStep on, sixteen times.
+static constexpr int kStep = kVerifyThreads * 4;
+__device__ __forceinline__ unsigned long long gone_of(const Tree& T, int v) {
+    unsigned long long bits = 0;
+    for (int k = 0; k < T.n_here; ++k) {
+        const int x = T.here[k] - v;
+        if (x >= 0 && x < 16 * kStep && x % kStep < 4) bits |= 1ull << (x / kStep * 4 + x % kStep);
+    }
+    return bits;
 }
 
 // the rejected tokens that lie in a chunk; all threads
@@ -176,30 +183,41 @@ __device__ __forceinline__ void sum_chunk(const VerifyParams& P, Tree& T, int be
     const float *p = P.target + row, *q = P.draft ? P.draft + row : nullptr;
     const double c = T.c;
     double sum = 0.0;
-    int v = v0 + tid * 4;
-    constexpr int STEP = kVerifyThreads * 4, U = 4;
-    if (T.n_here == 0) {
-        for (; v + (U - 1) * STEP + 4 <= end; v += U * STEP) {   // (all loads ahead of the sums)
-            vf32x4_t a[U], b[U];
+    auto add = [&](auto SOME) {   // SOME: tokens that do not count
+        for (int first = v0 + tid * 4; first < end; first += 16 * kStep) {
+            const unsigned long long gone = SOME ? gone_of(T, first) : 0;
+            constexpr int U = 4;
+            for (int g0 = 0; g0 < 16; g0 += U) {   // (all loads of a turn ahead of its sums)
+                const int v = first + g0 * kStep;
+                if (v >= end) break;
+                const uint32_t bits = (uint32_t)(gone >> (g0 * 4));
+                if (v + (U - 1) * kStep + 4 <= end) {
+                    vf32x4_t a[U], b[U];
 #pragma unroll
-            for (int u = 0; u < U; ++u) {
-                a[u] = *reinterpret_cast<const vf32x4_t*>(p + v + u * STEP);
-                b[u] = vf32x4_t{0.f, 0.f, 0.f, 0.f};
-                if (q) b[u] = *reinterpret_cast<const vf32x4_t*>(q + v + u * STEP);
-            }
+                    for (int u = 0; u < U; ++u) {
+                        a[u] = *reinterpret_cast<const vf32x4_t*>(p + v + u * kStep);
+                        b[u] = vf32x4_t{0.f, 0.f, 0.f, 0.f};
+                        if (q) b[u] = *reinterpret_cast<const vf32x4_t*>(q + v + u * kStep);
+                    }
 #pragma unroll
-            for (int u = 0; u < U; ++u) {
-                double r[4];
+                    for (int u = 0; u < U; ++u) {
+                        double r[4];
 #pragma unroll
-                for (int j = 0; j < 4; ++j) r[j] = left_of(c, a[u][j], b[u][j], q != nullptr);
-                sum += (r[0] + r[1]) + (r[2] + r[3]);
+                        for (int j = 0; j < 4; ++j) r[j] = SOME && bits >> (u * 4 + j) & 1 ? 0.0 : left_of(c, a[u][j], b[u][j], q != nullptr);
+                        sum += (r[0] + r[1]) + (r[2] + r[3]);
+                    }
+                } else {
+                    Four x[U];
+#pragma unroll
+                    for (int u = 0; u < U; ++u) x[u] = four_of(p, q, v + u * kStep, end, c, bits >> (u * 4));
+#pragma unroll
+                    for (int u = 0; u < U; ++u) sum += (x[u].r[0] + x[u].r[1]) + (x[u].r[2] + x[u].r[3]);
+                }
             }
         }
-    }
-    for (; v < end; v += STEP) {
-        const Four x = four_of(T, p, q, v, end, c);
-        sum += (x.r[0] + x.r[1]) + (x.r[2] + x.r[3]);
-    }
+    };
+    if (T.n_here == 0) add(std::false_type());
+    else add(std::true_type());
     sum = wave_sum(sum);
     if (tid % kWave == 0) T.wave[tid / kWave] = sum;
     __syncthreads();
@@ -328,9 +346,11 @@ __global__ __launch_bounds__(kVerifyThreads) void verify_kernel(const VerifyPara
     const double want = T.left, c = T.c;
     double below = 0.0;
     int found = -1;   // of this thread: the last number with anything
-    for (int v0 = chunk * P.chunk;; v0 += kVerifyThreads * 4) {
+    unsigned long long gone = 0;
+    for (int v0 = chunk * P.chunk, turn = 0;; v0 += kStep, ++turn) {
         const int v = v0 + tid * 4;
-        const Four x = four_of(T, p, q, v, end, c);
+        if (turn % 16 == 0) gone = gone_of(T, v);
+        const Four x = four_of(p, q, v, end, c, (uint32_t)(gone >> (turn % 16 * 4)));
         double to[4];
         to[0] = x.r[0];
 #pragma unroll
@@ -359,7 +379,7 @@ __global__ __launch_bounds__(kVerifyThreads) void verify_kernel(const VerifyPara
             if (tid == 0) P.next[b] = first;
             return;
         }
-        if (v0 + kVerifyThreads * 4 >= end) break;
+        if (v0 + kStep >= end) break;
     }
     // rounding has left it beyond all: the last number with anything
 #pragma unroll

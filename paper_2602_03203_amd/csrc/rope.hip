@@ -5,13 +5,11 @@
 // they become 32 bits (off by 2^-25 of a turn at most).  A workgroup takes a few tokens: sine and cosine once for every pair
 // of channels, in LDS, then all heads of these tokens pass by, 16 bytes a thread and load.
 // Bound by the memory system: every element is read and written once.
-#include "fk_common.h"
+#include "paged.h"
 
 #include <cmath>
 
 namespace fk {
-
-typedef unsigned int ru32x4_t __attribute__((ext_vector_type(4)));
 
 struct RopeParams {
     const void *q, *k;
@@ -19,25 +17,106 @@ struct RopeParams {
     const int32_t* pos;
     const double* freq;
     long long q_stride, k_stride, qo_stride, ko_stride;   // elements from token to token
-    int n_tokens, hq, heads, dim, rot, tokens /* of a workgroup */, parts /* workgroups of the same tokens: each takes a share of the heads */;
+    int n_tokens, hq, heads, dim, rot, tokens;            // tokens: of a workgroup
+    uint32_t token_magic, unit_magic, pair_magic;         // for divisions by a token's units, a head's, the pairs of channels
     float magnitude;
     bool inverse, half, q_copy, k_copy;                   // copy: the channels behind the rotated ones go into another tensor
 };
 
 template <typename T> __device__ __forceinline__ void store16(T* p, const float* f) {
-    if constexpr (sizeof(T) == 2) *reinterpret_cast<ru32x4_t*>(p) = ru32x4_t{pack_bf16(f[0], f[1]), pack_bf16(f[2], f[3]), pack_bf16(f[4], f[5]), pack_bf16(f[6], f[7])};
+    if constexpr (sizeof(T) == 2) *reinterpret_cast<uint4*>(p) = make_uint4(pack_bf16(f[0], f[1]), pack_bf16(f[2], f[3]), pack_bf16(f[4], f[5]), pack_bf16(f[6], f[7]));
     else *reinterpret_cast<float4*>(p) = make_float4(f[0], f[1], f[2], f[3]);
 }
 __device__ __forceinline__ float load_in(const float* p) { return *p; }
 __device__ __forceinline__ float load_in(const bf16_t* p) { return __uint_as_float((uint32_t)*p << 16); }
 
-// VEC: whole 16-byte groups turn together; otherwise a thread turns one pair of channels or copies one channel
+// VEC: whole 16-byte groups turn together; otherwise a thread turns one pair of channels or copies one channel.  A thread's units are two turns' loads ahead
+// of their stores.
 template <typename T, bool VEC>
 __global__ __launch_bounds__(256) void rope_kernel(const RopeParams P) {
     extern __shared__ float2 s_turn[];   // [tokens][rot / 2] (cos, sin) times the magnitude
-    const int tid = threadIdx.x, pairs = P.rot / 2, t0 = blockIdx.x / P.parts * P.tokens, part = blockIdx.x % P.parts, tokens = min(P.tokens, P.n_tokens - t0);
+    constexpr int N = VEC ? Vec16<T>::N : 1, U = VEC ? 4 : 1;
+    const int tid = threadIdx.x, pairs = P.rot / 2, t0 = blockIdx.x * P.tokens, tokens = min(P.tokens, P.n_tokens - t0);
+    // units of a head: those that turn, then those that are copied
+    const int turning = VEC ? (P.half ? pairs / N : P.rot / N) : pairs, units = turning + (P.q_copy || P.k_copy ? (P.dim - P.rot) / N : 0);
+    const int per_token = P.heads * units, all = tokens * per_token;
+    struct Unit {
+        T* y;
+        int t, u;              // u < 0: nothing to do
+        uint4 a, b;
+    };
+    auto fetch = [&](int i) {
+        Unit x;
+        x.u = -1;
+        if (i >= all) return x;
+        const int t = divide(i, per_token, P.token_magic), r = i - t * per_token, h = divide(r, units, P.unit_magic), u = r - h * units;
+        const bool is_q = h < P.hq;
+        if (u >= turning && !(is_q ? P.q_copy : P.k_copy)) return x;
+        const size_t token = (size_t)(t0 + t);
+        const T* from = is_q ? reinterpret_cast<const T*>(P.q) + token * P.q_stride + (size_t)h * P.dim : reinterpret_cast<const T*>(P.k) + token * P.k_stride + (size_t)(h - P.hq) * P.dim;
+        x.y = is_q ? reinterpret_cast<T*>(P.q_out) + token * P.qo_stride + (size_t)h * P.dim : reinterpret_cast<T*>(P.k_out) + token * P.ko_stride + (size_t)(h - P.hq) * P.dim;
+        x.t = t;
+        x.u = u;
+        if constexpr (VEC) {
+            const int d = u < turning ? u * N : P.rot + (u - turning) * N;
+            x.a = *reinterpret_cast<const uint4*>(from + d);
+            if (P.half && u < turning) x.b = *reinterpret_cast<const uint4*>(from + d + pairs);
+        } else {
+            const int a = u >= turning ? P.rot + u - turning : P.half ? u : 2 * u;
+            x.a.x = __float_as_uint(load_in(from + a));
+            if (u < turning) x.b.x = __float_as_uint(load_in(from + (P.half ? a + pairs : a + 1)));
+        }
+        return x;
+    };
+    auto finish = [&](const Unit& x) {
+        if (x.u < 0) return;
+        const float2* turn = s_turn + x.t * pairs;
+        if constexpr (VEC) {
+            if (x.u >= turning) {
+                *reinterpret_cast<uint4*>(x.y + P.rot + (x.u - turning) * N) = x.a;
+                return;
+            }
+            float v[N], w[N];
+            Vec16<T>::unpack(x.a, v);
+            if (P.half) {
+                Vec16<T>::unpack(x.b, w);
+#pragma unroll
+                for (int j = 0; j < N; ++j) {
+                    const float2 cs = turn[x.u * N + j];
+                    const float a = v[j] * cs.x - w[j] * cs.y;
+                    w[j] = v[j] * cs.y + w[j] * cs.x;
+                    v[j] = a;
+                }
+                store16(x.y + x.u * N, v);
+                store16(x.y + pairs + x.u * N, w);
+            } else {
+#pragma unroll
+                for (int j = 0; j < N; j += 2) {
+                    const float2 cs = turn[x.u * (N / 2) + j / 2];
+                    const float a = v[j] * cs.x - v[j + 1] * cs.y;
+                    v[j + 1] = v[j] * cs.y + v[j + 1] * cs.x;
+                    v[j] = a;
+                }
+                store16(x.y + x.u * N, v);
+            }
+        } else {
+            const float v = __uint_as_float(x.a.x);
+            if (x.u >= turning) {
+                store_out(x.y + P.rot + x.u - turning, v);   // (exact: it comes from there)
+                return;
+            }
+            const float w = __uint_as_float(x.b.x);
+            const int a = P.half ? x.u : 2 * x.u, b = P.half ? a + pairs : a + 1;
+            const float2 cs = turn[x.u];
+            store_out(x.y + a, v * cs.x - w * cs.y);
+            store_out(x.y + b, v * cs.y + w * cs.x);
+        }
+    };
+    Unit x[U];
+#pragma unroll
+    for (int k = 0; k < U; ++k) x[k] = fetch(tid + k * 256);   // (on their way while the angles are formed)
     for (int i = tid; i < tokens * pairs; i += 256) {
-        const int t = i / pairs;
+        const int t = divide(i, pairs, P.pair_magic);
         double turns = (double)P.pos[t0 + t] * (P.freq[i - t * pairs] * 0.15915494309189535);
         turns -= rint(turns);
         float s, c;
@@ -45,55 +124,13 @@ __global__ __launch_bounds__(256) void rope_kernel(const RopeParams P) {
         s_turn[i] = make_float2(c * P.magnitude, (P.inverse ? -s : s) * P.magnitude);
     }
     __syncthreads();
-    constexpr int N = VEC ? Vec16<T>::N : 1;
-    // units of a head: those that turn, then those that are copied
-    const int turning = VEC ? (P.half ? pairs / N : P.rot / N) : pairs, units = turning + (P.q_copy || P.k_copy ? (P.dim - P.rot) / N : 0);
-    const int first = P.heads * part / P.parts, heads = P.heads * (part + 1) / P.parts - first;
-    const int all = tokens * heads * units;
-    for (int i = tid; i < all; i += 256) {
-        const int u = i % units, th = i / units, h = first + th % heads, t = th / heads;
-        const bool is_q = h < P.hq;
-        const T* x = (is_q ? reinterpret_cast<const T*>(P.q) + (t0 + t) * P.q_stride : reinterpret_cast<const T*>(P.k) + (t0 + t) * P.k_stride) + (size_t)(is_q ? h : h - P.hq) * P.dim;
-        T* y = (is_q ? reinterpret_cast<T*>(P.q_out) + (t0 + t) * P.qo_stride : reinterpret_cast<T*>(P.k_out) + (t0 + t) * P.ko_stride) + (size_t)(is_q ? h : h - P.hq) * P.dim;
-        const float2* turn = s_turn + t * pairs;
-        if (u >= turning) {
-            if (!(is_q ? P.q_copy : P.k_copy)) continue;
-            const int d = P.rot + (u - turning) * N;
-            if constexpr (VEC) *reinterpret_cast<ru32x4_t*>(y + d) = *reinterpret_cast<const ru32x4_t*>(x + d);
-            else y[d] = x[d];
-            continue;
-        }
-        if constexpr (!VEC) {
-            const int a = P.half ? u : 2 * u, b = P.half ? u + pairs : a + 1;
-            const float v = load_in(x + a), w = load_in(x + b);
-            const float2 cs = turn[u];
-            store_out(y + a, v * cs.x - w * cs.y);
-            store_out(y + b, v * cs.y + w * cs.x);
-        } else if (P.half) {
-            float v[N], w[N];
-            Vec16<T>::unpack(*reinterpret_cast<const uint4*>(x + u * N), v);
-            Vec16<T>::unpack(*reinterpret_cast<const uint4*>(x + pairs + u * N), w);
+    for (int i = tid;;) {
 #pragma unroll
-            for (int j = 0; j < N; ++j) {
-                const float2 cs = turn[u * N + j];
-                const float a = v[j] * cs.x - w[j] * cs.y;
-                w[j] = v[j] * cs.y + w[j] * cs.x;
-                v[j] = a;
-            }
-            store16(y + u * N, v);
-            store16(y + pairs + u * N, w);
-        } else {
-            float v[N];
-            Vec16<T>::unpack(*reinterpret_cast<const uint4*>(x + u * N), v);
+        for (int k = 0; k < U; ++k) finish(x[k]);
+        i += U * 256;
+        if (i >= all) break;
 #pragma unroll
-            for (int j = 0; j < N; j += 2) {
-                const float2 cs = turn[u * (N / 2) + j / 2];
-                const float a = v[j] * cs.x - v[j + 1] * cs.y;
-                v[j + 1] = v[j] * cs.y + v[j + 1] * cs.x;
-                v[j] = a;
-            }
-            store16(y + u * N, v);
-        }
+        for (int k = 0; k < U; ++k) x[k] = fetch(i + k * 256);
     }
 }
 
@@ -161,9 +198,12 @@ extern "C" fk_status fk_rope(const fk_rope_desc* d, const void* q, const void* k
     P.q_copy = q != q_out;
     P.k_copy = k != k_out;
     P.tokens = n_tokens >= 2048 ? 4 : 1;
-    P.parts = 1;
     const bool vec = (P.half ? P.rot / 2 : P.rot) * es % 16 == 0;
-    const dim3 grid((unsigned)((n_tokens + P.tokens - 1) / P.tokens) * P.parts);
+    const int n = vec ? 16 / es : 1, turning = vec && !P.half ? P.rot / n : P.rot / 2 / n, units = turning + (P.q_copy || P.k_copy ? (P.dim - P.rot) / n : 0);
+    P.token_magic = magic_of(P.heads * units);
+    P.unit_magic = magic_of(units);
+    P.pair_magic = magic_of(P.rot / 2);
+    const dim3 grid((unsigned)((n_tokens + P.tokens - 1) / P.tokens));
     const size_t lds = (size_t)P.tokens * P.rot / 2 * sizeof(float2);
     hipStream_t st = (hipStream_t)stream;
     if (d->dtype == FK_F32) {
