@@ -32,13 +32,13 @@ __device__ __forceinline__ float load_in(const bf16_t* p) { return __uint_as_flo
 
 // VEC: whole 16-byte groups turn together; otherwise a thread turns one pair of channels or copies one channel.  A thread's units are two turns' loads ahead
 // of their stores.
-template <typename T, bool VEC>
+template <typename T, bool VEC, bool HALF>
 __global__ __launch_bounds__(256) void rope_kernel(const RopeParams P) {
     extern __shared__ float2 s_turn[];   // [tokens][rot / 2] (cos, sin) times the magnitude
-    constexpr int N = VEC ? Vec16<T>::N : 1, U = VEC ? 4 : 1;
+    constexpr int N = VEC ? Vec16<T>::N : 1, U = !VEC ? 2 : HALF ? 4 : 8;   // units of a thread under way: eight loads
     const int tid = threadIdx.x, pairs = P.rot / 2, t0 = blockIdx.x * P.tokens, tokens = min(P.tokens, P.n_tokens - t0);
     // units of a head: those that turn, then those that are copied
-    const int turning = VEC ? (P.half ? pairs / N : P.rot / N) : pairs, units = turning + (P.q_copy || P.k_copy ? (P.dim - P.rot) / N : 0);
+    const int turning = VEC ? (HALF ? pairs / N : P.rot / N) : pairs, units = turning + (P.q_copy || P.k_copy ? (P.dim - P.rot) / N : 0);
     const int per_token = P.heads * units, all = tokens * per_token;
     struct Unit {
         T* y;
@@ -60,11 +60,11 @@ __global__ __launch_bounds__(256) void rope_kernel(const RopeParams P) {
         if constexpr (VEC) {
             const int d = u < turning ? u * N : P.rot + (u - turning) * N;
             x.a = *reinterpret_cast<const uint4*>(from + d);
-            if (P.half && u < turning) x.b = *reinterpret_cast<const uint4*>(from + d + pairs);
+            if (HALF && u < turning) x.b = *reinterpret_cast<const uint4*>(from + d + pairs);
         } else {
-            const int a = u >= turning ? P.rot + u - turning : P.half ? u : 2 * u;
+            const int a = u >= turning ? P.rot + u - turning : HALF ? u : 2 * u;
             x.a.x = __float_as_uint(load_in(from + a));
-            if (u < turning) x.b.x = __float_as_uint(load_in(from + (P.half ? a + pairs : a + 1)));
+            if (u < turning) x.b.x = __float_as_uint(load_in(from + (HALF ? a + pairs : a + 1)));
         }
         return x;
     };
@@ -78,7 +78,7 @@ __global__ __launch_bounds__(256) void rope_kernel(const RopeParams P) {
             }
             float v[N], w[N];
             Vec16<T>::unpack(x.a, v);
-            if (P.half) {
+            if constexpr (HALF) {
                 Vec16<T>::unpack(x.b, w);
 #pragma unroll
                 for (int j = 0; j < N; ++j) {
@@ -106,7 +106,7 @@ __global__ __launch_bounds__(256) void rope_kernel(const RopeParams P) {
                 return;
             }
             const float w = __uint_as_float(x.b.x);
-            const int a = P.half ? x.u : 2 * x.u, b = P.half ? a + pairs : a + 1;
+            const int a = HALF ? x.u : 2 * x.u, b = HALF ? a + pairs : a + 1;
             const float2 cs = turn[x.u];
             store_out(x.y + a, v * cs.x - w * cs.y);
             store_out(x.y + b, v * cs.y + w * cs.x);
@@ -206,12 +206,8 @@ extern "C" fk_status fk_rope(const fk_rope_desc* d, const void* q, const void* k
     const dim3 grid((unsigned)((n_tokens + P.tokens - 1) / P.tokens));
     const size_t lds = (size_t)P.tokens * P.rot / 2 * sizeof(float2);
     hipStream_t st = (hipStream_t)stream;
-    if (d->dtype == FK_F32) {
-        if (vec) hipLaunchKernelGGL((rope_kernel<float, true>), grid, dim3(256), lds, st, P);
-        else hipLaunchKernelGGL((rope_kernel<float, false>), grid, dim3(256), lds, st, P);
-    } else {
-        if (vec) hipLaunchKernelGGL((rope_kernel<bf16_t, true>), grid, dim3(256), lds, st, P);
-        else hipLaunchKernelGGL((rope_kernel<bf16_t, false>), grid, dim3(256), lds, st, P);
-    }
+    auto kern = d->dtype == FK_F32 ? (vec ? (P.half ? rope_kernel<float, true, true> : rope_kernel<float, true, false>) : P.half ? rope_kernel<float, false, true> : rope_kernel<float, false, false>)
+                                   : (vec ? (P.half ? rope_kernel<bf16_t, true, true> : rope_kernel<bf16_t, true, false>) : P.half ? rope_kernel<bf16_t, false, true> : rope_kernel<bf16_t, false, false>);
+    hipLaunchKernelGGL(kern, grid, dim3(256), lds, st, P);
     return launch_status();
 }
