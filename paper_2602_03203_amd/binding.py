@@ -492,6 +492,7 @@ def _heads_ptr(x, desc: RopeDesc, heads: int) -> int:
         return 0
     assert x.is_cuda and tuple(x.shape[1:]) == (heads, desc.head_dim), "queries and keys are [n_tokens, heads, head_dim] device tensors"
     assert x.numel() == 0 or (x.stride(2) == 1 and (heads == 1 or x.stride(1) == desc.head_dim)), "a token's heads must lie side by side"
+    assert x.shape[0] < 2 or x.stride(0) >= heads * desc.head_dim, "tokens must not share memory"
     return x.data_ptr()
 
 
@@ -508,6 +509,7 @@ def fk_rope(desc: RopeDesc, q, k, pos, freq, q_out, k_out, stream=None) -> None:
     """Rotary positions of q [n_tokens, n_q_heads, D] and k [n_tokens, n_kv_heads, D]; a token's heads lie side by side, tokens any distance apart.
     pos [n_tokens] int32; freq fp64 [rotary_dim / 2] on the device; q_out may be q, k_out may be k."""
     some = q if q is not None else k
+    assert freq.dtype == torch.float64 and freq.numel() >= desc.rotary_dim // 2, "freq is fp64 [rotary_dim / 2]"
     _call("fk_rope", ctypes.byref(desc.c(q, k, q_out, k_out)), _heads_ptr(q, desc, desc.n_q_heads), _heads_ptr(k, desc, desc.n_kv_heads), _ptr(pos), _ptr(freq),
           int(some.shape[0]), _heads_ptr(q_out, desc, desc.n_q_heads), _heads_ptr(k_out, desc, desc.n_kv_heads), _stream(stream))
 

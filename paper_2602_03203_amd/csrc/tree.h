@@ -252,6 +252,14 @@ __device__ __forceinline__ void tree_tile(const TreeParams& TP, int item, int sp
         };
         constexpr int VW = BF && D == 64 ? 2 : 4;   // words in use of a V load
 
+        Place at, next;
+        auto begin = [&]() {
+            if (t_begin + wave >= t_end) return;
+            at = place_of(t_begin + wave);
+            load_k(at);
+            load_v(at);
+        };
+        begin();   // (on their way while the ancestors are found)
         // The rows of all nodes at once.  A row gives the pairs that it does not see weight 0, which must not meet an infinity or a NaN that another row
         // sees: where there is any, the run starts over with half of its nodes.
         const int nodes = w.tok_hi - w.tok_lo + 1;
@@ -272,13 +280,7 @@ __device__ __forceinline__ void tree_tile(const TreeParams& TP, int item, int sp
 #pragma unroll
             for (int e = 0; e < ET; ++e) o[rb][e] = (tf32x4_t){0.f, 0.f, 0.f, 0.f};
         }
-        Place at, next;
         int i = t_begin + wave;
-        if (i < t_end) {
-            at = place_of(i);
-            load_k(at);
-            load_v(at);
-        }
         auto tile = [&](auto LAST) {   // (twice in the code: under a condition the next tile's loads would need registers of their own)
             tf32x4_t c[RB][NT];
 #pragma unroll
@@ -426,6 +428,7 @@ __device__ __forceinline__ void tree_tile(const TreeParams& TP, int item, int sp
         if (scalar(s_bad)) {   // (the same for every thread)
             hi = lo + (hi - lo) / 2;
             __syncthreads();
+            begin();
             continue;
         }
         if (tid < TM) {
@@ -469,6 +472,7 @@ __device__ __forceinline__ void tree_tile(const TreeParams& TP, int item, int sp
         if (hi == nodes - 1) break;
         lo = hi + 1;
         hi = nodes - 1;
+        begin();
         }
         if (splits == 1) continue;
         // the last workgroup to arrive adds the records up, in the order of the splits

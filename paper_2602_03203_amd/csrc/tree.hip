@@ -38,14 +38,14 @@ static long long items_of(const fk_paged_desc* d, const TileGrid& G) { return (l
 // items of 64 rows: whole 100, in two 68, three 61, four 53, five 67; up to 256 rows of 2112, 256 items of 128: 76, 62, 81, 77).
 static int tree_splits(const fk_paged_desc* d, int kind, long long items, long long pairs, double& least) {
     const long long most = std::min((long long)kMostTreeSplits, pairs >> 8);
-    least = 0;
-    if (kind <= 2) return items > kSplitItems ? 1 : (int)std::max(1ll, std::min(most, (d->head_dim == 128 ? 512 : 192) / items));
     const bool bf16 = d->dtype == FK_BF16;
+    least = 0;
+    if (kind <= 2) return items > kSplitItems ? 1 : (int)std::max(1ll, std::min(most, (bf16 ? d->head_dim == 128 ? 512 : 192 : 256) / items));
     const double wide = kind == 8 ? 2. : 1., turn[3] = {wide, wide * 1.3, wide * 1.6};   // (of as many pairs as take 0.75 us alone with 64 rows)
     const int held = kind == 8 ? 2 : 3;   // workgroups that a CU holds
     const double turns = (double)pairs / (kind == 8 ? 64 : 32) * d->head_dim / 128 * (kind == 8 ? 1. : .75) * (bf16 ? 1. : 4.);
     int best = 1;
-    for (int s = 1; s == 1 || (s <= most && items <= kSplitItems); ++s) {
+    for (int s = 1; s == 1 || (s <= most && items <= kSplitItems && items * s * kind <= 1 << 15 /* a quarter of a GiB of records */); ++s) {
         const long long per_cu = (items * s + 255) / 256, rest = per_cu % held;
         const double rounds = (double)(per_cu / held) * turn[held - 1] + (rest ? turn[rest - 1] : 0.);
         const double time = rounds * turns / s + (s == 1 ? 0. : 3 + (double)items * s * 16 * kind * d->head_dim * 8 / 4e6);

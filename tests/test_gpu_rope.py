@@ -165,3 +165,16 @@ def test_other_stream_and_graph():
         g.replay()
         torch.cuda.synchronize()
         assert torch.equal(want[0], got[0]) and torch.equal(want[1], got[1])
+
+
+def test_refused():
+    """Tokens that share memory, heads that do not lie side by side, frequencies in 32 bits."""
+    fk = _fk()
+    q, pos, freq = torch.randn((6, 4, 64), device="cuda"), torch.arange(6, dtype=torch.int32, device="cuda"), fk.rope_frequencies(64).cuda()
+    desc = fk.RopeDesc(4, 0, 64, 64, "half", "f32")
+    for x, f in ((q[:1].expand(6, -1, -1), freq), (q.transpose(0, 1).contiguous().transpose(0, 1), freq), (q, freq.float()), (q, freq[:31])):
+        with pytest.raises(AssertionError):
+            fk.fk_rope(desc, x, None, pos, f, torch.empty_like(q), None)
+    with pytest.raises(fk.FkError):   # in place, but the outputs' tokens lie closer together
+        wide = torch.randn((6, 8, 64), device="cuda")
+        fk.fk_rope(desc, wide[:, :4], None, pos, freq, wide.view(-1)[:6 * 4 * 64].view(6, 4, 64), None)

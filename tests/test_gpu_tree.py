@@ -232,3 +232,37 @@ def test_pairs_beyond_32_bit_offsets():
         c.run(s)
         torch.cuda.synchronize()
         c.check(s, *c.reference())
+
+
+def test_rows_beyond_32_bit_offsets():
+    """Rows that begin 2^31 elements into the cache."""
+    import paper_2602_03203_amd as fk
+    D, H, cap = 128, 3, 1 << 23
+    K = torch.zeros((1, H, cap, D), dtype=torch.bfloat16, device="cuda")
+    V = torch.zeros_like(K)
+    for g, nodes, n in ((4, 3, 3000), (4, 7, 1025), (4, 15, 2000), (1, 256, 700), (8, 256, 300)):
+        c = TreeCase("bf16", D, g, H, [(n, tree(nodes, 1))], seed=nodes)
+        K[:, :, :c.cap], V[:, :, :c.cap] = c.K.cuda(), c.V.cuda()
+        s = c.dev()
+        s["K"], s["V"], s["desc"] = K, V, fk.CacheDesc(1, H * g, H, D, cap, "bf16")
+        s["ws"] = fk.new_tree_attn_workspace(s["desc"], c.n_tokens, c.max_tree, c.max_len)
+        c.run(s)
+        torch.cuda.synchronize()
+        c.check(s, *c.reference(), f"{nodes} nodes")
+
+
+def test_calls_of_any_sizes_share_a_workspace():
+    """Rows and pages, few and many splits, in turns: the counters are where every call looks for them."""
+    cases = [TreeCase("bf16", 128, 4, 2, [(3000, tree(4, 1)), (2500, tree(3))], 0, seed=1), TreeCase("bf16", 128, 4, 1, [(4000, tree(50, 2))], 64, seed=2),
+             TreeCase("f32", 64, 8, 1, [(900, tree(40, 3)), (100, tree(8)), (2000, tree(2))], 0, seed=3), TreeCase("bf16", 64, 4, 4, [(1500, tree(33, 4))], 16, seed=4)]
+    devs = [c.dev() for c in cases]
+    ws = torch.zeros(max(s["ws"].numel() for s in devs), dtype=torch.uint8, device="cuda")
+    refs = [c.reference() for c in cases]
+    for turn in range(3):
+        for c, s in zip(cases, devs):
+            s["ws"] = ws
+            s["out"].fill_(7)
+            c.run(s)
+        torch.cuda.synchronize()
+        for i, (c, s, r) in enumerate(zip(cases, devs, refs)):
+            c.check(s, *r, f"turn {turn} case {i}")

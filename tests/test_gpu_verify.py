@@ -178,3 +178,30 @@ def test_rows_beyond_32_bit_offsets():
     path, acc, nxt = torch.zeros(n, **i32), torch.zeros(1, **i32), torch.zeros(1, **i32)
     fk.fk_verify_drafts(target, None, tokens, parent, q_start, torch.full((n,), 0.5, device="cuda"), path, acc, nxt, fk.new_verify_workspace(1, V))
     assert acc.item() == 2 and nxt.item() == V - 2 and path[n - 2:].tolist() == [0, 1]
+
+
+def test_calls_of_any_sizes_share_a_workspace():
+    """Other batches and vocabularies in turns: a sum of an earlier call is never taken for one of this call."""
+    import paper_2602_03203_amd as fk
+    cases = [Trees([tree(20, s, depth=2, fan=20) for s in range(b)], v, drawn, 1.5, seed=b) for b, v, drawn in ((3, 9001, True), (7, 40000, True), (1, 130001, True), (5, 9001, False), (2, 5000, True))]
+    devs = [c.dev() for c in cases]
+    ws = torch.zeros(max(d[9].numel() for d in devs), dtype=torch.uint8, device="cuda")
+    for turn in range(4):
+        for d in devs:
+            for x in d[6:9]:
+                x.fill_(-9)
+            fk.fk_verify_drafts(*d[:9], ws)
+        torch.cuda.synchronize()
+        for i, (c, d) in enumerate(zip(cases, devs)):
+            c.check(d, f"turn {turn} case {i}")
+
+
+def test_more_rejections_than_sums_are_told():
+    """Sixty children of one node, all rejected: the first sums are shared, the others everybody forms."""
+    c = Trees([[-1] + [0] * 60 for _ in range(3)], 20000, True, 0.3, seed=4)
+    c.uniform[:] = 1 - 2.0 ** -24
+    d = c.go()
+    assert d[7].max().item() >= 1
+    c.tokens[:] = 5   # (and the same token every time, which the draft likes better than the target)
+    c.target[:, 5] *= 0.5
+    c.go()
