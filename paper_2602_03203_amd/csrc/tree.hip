@@ -35,12 +35,14 @@ static long long items_of(const fk_paged_desc* d, const TileGrid& G) { return (l
 // Splits of a tile's pairs, each 256 and more, where the items are few.  16 and 32 rows, bound by memory: up to 512 workgroups (16 rows, D 128: 128 items of 2112
 // pairs whole 31.2, in two 29.2, four 28.6; 8 items in four 13.9, eight 11.1, sixteen 12.4), D 64 up to 192 (128 items whole 18.3, in two 20.1).  Others by an
 // estimate: a turn of the loop takes `turn[k]` us with k + 1 workgroups on a CU, and records go out and come back at 4 TB/s (up to 182 rows of 4160 pairs, 192
-// items of 64 rows: whole 100, in two 68, three 61, four 53, five 67; up to 256 rows of 2112, 256 items of 128: 76, 62, 81, 77).
-static int tree_splits(const fk_paged_desc* d, int kind, long long items, long long pairs, double& least) {
-    const long long most = std::min((long long)kMostTreeSplits, pairs >> 8);
+// items of 64 rows: whole 100, in two 68, three 61, four 53, five 67; up to 256 rows of 2112, 256 items of 128: 76, 62, 81, 77).  Sequences in pages differ in
+// length as a rule, which only the device knows: up to twice as many splits, of 512 pairs and more, even them out (16 sequences of 1024 to 16384 pairs, 8 heads: 16 rows
+// in four 127, eight 113; 32 rows 133 and 121; up to 96 rows 159 and 152).
+static int tree_splits(const fk_paged_desc* d, int kind, long long items, long long pairs, bool uneven, double& least) {
+    const long long most = std::min((long long)kMostTreeSplits, pairs >> (uneven ? 9 : 8)), places = uneven ? 1024 : 512;
     const bool bf16 = d->dtype == FK_BF16;
     least = 0;
-    if (kind <= 2) return items > kSplitItems ? 1 : (int)std::max(1ll, std::min(most, (bf16 ? d->head_dim == 128 ? 512 : 192 : 256) / items));
+    if (kind <= 2) return items > kSplitItems ? 1 : (int)std::max(1ll, std::min(most, (bf16 ? d->head_dim == 128 ? places : places * 3 / 8 : places / 2) / items));
     const double wide = kind == 8 ? 2. : 1., turn[3] = {wide, wide * 1.3, wide * 1.6};   // (of as many pairs as take 0.75 us alone with 64 rows)
     const int held = kind == 8 ? 2 : 3;   // workgroups that a CU holds
     const double turns = (double)pairs / (kind == 8 ? 64 : 32) * d->head_dim / 128 * (kind == 8 ? 1. : .75) * (bf16 ? 1. : 4.);
@@ -51,16 +53,18 @@ static int tree_splits(const fk_paged_desc* d, int kind, long long items, long l
         const double time = rounds * turns / s + (s == 1 ? 0. : 3 + (double)items * s * 16 * kind * d->head_dim * 8 / 4e6);
         if (s == 1 || time < least) least = time, best = s;
     }
+    if (uneven && items <= kSplitItems / 2) best = (int)std::max((long long)best, std::min(most, places / items));
     return best;
 }
-static TreePlan tree_plan(const fk_paged_desc* d, int32_t n_tokens, int32_t max_tree, long long pairs) {
+// uneven: sequences in pages, several of them
+static TreePlan tree_plan(const fk_paged_desc* d, int32_t n_tokens, int32_t max_tree, long long pairs, bool uneven) {
     const int g = d->n_q_heads / d->n_kv_heads, tree = std::min(std::min(max_tree, n_tokens), kTreeNodes), rows = tree * g;
     TreePlan p = {};
     double time = 0;
     auto take = [&](int kind) {   // the better one
         TreePlan x = {kind, tile_grid(d, n_tokens, tree, 16 * kind), 1, 0};
         double t;
-        x.splits = tree_splits(d, kind, items_of(d, x.grid), pairs + tree, t);
+        x.splits = tree_splits(d, kind, items_of(d, x.grid), pairs + tree, uneven, t);
         if (p.kind == 0 || t < time) p = x, time = t;
     };
     if (d->dtype == FK_F32) {
@@ -71,7 +75,7 @@ static TreePlan tree_plan(const fk_paged_desc* d, int32_t n_tokens, int32_t max_
     }
     p.grid.most = kTreeNodes * g;
     const int kt = p.kind <= 2 ? (d->dtype == FK_BF16 ? 32 : 16) : d->dtype == FK_BF16 && (p.kind == 8 || d->head_dim == 64) ? 64 : d->dtype == FK_BF16 || d->head_dim == 64 ? 32 : 16;
-    p.shift = 8 - __builtin_ctz(kt);
+    p.shift = (uneven ? 9 : 8) - __builtin_ctz(kt);
     return p;
 }
 // workspace: counters, the same for every call (so that calls of any sizes may take turns with one workspace) | sums and references of records | records
@@ -79,8 +83,8 @@ static constexpr size_t kCounterBytes = kSplitItems * 4 * sizeof(uint32_t);
 static size_t ml_bytes(const TreePlan& p, long long items) {   // wide: 16 bytes a lane and 16 rows; 8 a row
     return p.splits > 1 ? up256((size_t)items * p.splits * 16 * p.kind * (p.kind >= 4 ? 64 : 8)) : 0;
 }
-static size_t tree_workspace(const fk_paged_desc* d, int32_t n_tokens, int32_t max_tree, int32_t max_len) {
-    const TreePlan p = tree_plan(d, std::max(n_tokens, 1), max_tree, max_len);
+static size_t tree_workspace(const fk_paged_desc* d, int32_t n_tokens, int32_t max_tree, int32_t max_len, bool uneven) {
+    const TreePlan p = tree_plan(d, std::max(n_tokens, 1), max_tree, max_len, uneven);
     const long long items = items_of(d, p.grid);
     return kCounterBytes + ml_bytes(p, items) + (p.splits > 1 ? (size_t)items * p.splits * 16 * p.kind * d->head_dim * sizeof(float) : 0);
 }
@@ -152,7 +156,7 @@ static fk_status check_rows(const fk_cache_desc* desc, int32_t n_tokens, int32_t
 extern "C" size_t fk_tree_attn_workspace(const fk_cache_desc* desc, int32_t n_tokens, int32_t max_tree, int32_t max_len) {
     if (check_rows(desc, n_tokens, max_tree, max_len) != FK_OK) return 0;
     const fk_paged_desc d = as_paged(desc);
-    return tree_workspace(&d, n_tokens, max_tree, max_len);
+    return tree_workspace(&d, n_tokens, max_tree, max_len, false);
 }
 
 extern "C" fk_status fk_tree_attn(const fk_cache_desc* desc, const void* q, const void* K, const void* V, const int32_t* len, const void* k_tree,
@@ -178,7 +182,7 @@ extern "C" fk_status fk_tree_attn(const fk_cache_desc* desc, const void* q, cons
     P.parent = parent;
     P.k_tree = k_tree;
     P.v_tree = v_tree;
-    return tree_launch<true>(&d, tree_plan(&d, n_tokens, max_tree, max_len), P, workspace, (hipStream_t)stream);
+    return tree_launch<true>(&d, tree_plan(&d, n_tokens, max_tree, max_len, false), P, workspace, (hipStream_t)stream);
 }
 
 static fk_status check_pages(const fk_paged_desc* desc, int32_t n_tokens, int32_t max_tree, int32_t max_len) {
@@ -190,7 +194,7 @@ static fk_status check_pages(const fk_paged_desc* desc, int32_t n_tokens, int32_
 
 extern "C" size_t fk_paged_tree_attn_workspace(const fk_paged_desc* desc, int32_t n_tokens, int32_t max_tree, int32_t max_len) {
     if (check_pages(desc, n_tokens, max_tree, max_len) != FK_OK) return 0;
-    return tree_workspace(desc, n_tokens, max_tree, max_len);
+    return tree_workspace(desc, n_tokens, max_tree, max_len, desc->batch > 1);
 }
 
 extern "C" fk_status fk_paged_tree_attn(const fk_paged_desc* desc, const void* q, const void* K, const void* V, const int32_t* page_table,
@@ -217,5 +221,5 @@ extern "C" fk_status fk_paged_tree_attn(const fk_paged_desc* desc, const void* q
     P.parent = parent;
     P.k_tree = k_tree;
     P.v_tree = v_tree;
-    return tree_launch<false>(desc, tree_plan(desc, n_tokens, max_tree, max_len), P, workspace, (hipStream_t)stream);
+    return tree_launch<false>(desc, tree_plan(desc, n_tokens, max_tree, max_len, desc->batch > 1), P, workspace, (hipStream_t)stream);
 }
