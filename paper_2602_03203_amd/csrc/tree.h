@@ -563,6 +563,12 @@ template <typename T, int D, int CT_> struct WideCfg {
     static constexpr size_t LDS = 2 * PLACES * (size_t)TILE_BYTES;
 };
 
+// load_to_lds of pairs that nobody else reads: not kept (up to 96 rows of 16 sequences of 4000 pairs in pages: 87 -> 79 us; beside a second tile of rows, which
+// reads them too, 225 -> 234)
+__device__ __forceinline__ void load_once_to_lds(const void* from, unsigned char* to) {
+    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)from, (__attribute__((address_space(3))) void*)to, 16, 0, 2);
+}
+
 // The wavefront's loads are there but for the latest N, and what it has read of LDS; then the workgroup's.  (__syncthreads would wait for all loads.)
 template <int N> __device__ __forceinline__ void arrived_but() {
     asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(N) : "memory");
@@ -593,7 +599,7 @@ __device__ __forceinline__ void store_wide(const AttnPagedParams& P, size_t row,
     if (P.stats && quad == 0) P.stats[row] = make_float2(M, L);
 }
 
-template <typename T, int D, int CT, bool ROWS>
+template <typename T, int D, int CT, bool ROWS, bool ONCE>
 __device__ __forceinline__ void wide_tile(const TreeParams& TP, int item, int split) {
     using C = WideCfg<T, D, CT>;
     constexpr bool BF = C::BF;
@@ -703,12 +709,13 @@ __device__ __forceinline__ void wide_tile(const TreeParams& TP, int item, int sp
 #pragma unroll
                 for (int u = 0; u < LD; ++u) {
                     const int row = st_row + u * RPU, ch = st_ch ^ (is_k ? swizzle_k<BF, CH>(row) : swizzle_v<BF, CH>(row));
-                    if constexpr (ROWS) {
-                        load_to_lds(X + (uint32_t)((row * CH + ch) * 16), to + u * 256 * 16);
-                    } else {
+                    const unsigned char* from = X + (uint32_t)((row * CH + ch) * 16);
+                    if constexpr (!ROWS) {
                         const uint32_t run = RPU == 32 ? (wave >= 2 ? p.run[(2 * u + 1) % GI] : p.run[2 * u % GI]) : p.run[u * RPU / 16];
-                        load_to_lds(X + (size_t)run * (16 * CH * 16) + (uint32_t)((row % 16 * CH + ch) * 16), to + u * 256 * 16);
+                        from = X + (size_t)run * (16 * CH * 16) + (uint32_t)((row % 16 * CH + ch) * 16);
                     }
+                    if constexpr (ONCE) load_once_to_lds(from, to + u * 256 * 16);
+                    else load_to_lds(from, to + u * 256 * 16);
                 }
                 return;
             }

@@ -13,9 +13,10 @@ template <typename T, int D, int KIND> struct TreeKind {
     static constexpr size_t LDS = WIDE ? WideCfg<T, D, WIDE ? KIND / 4 : 1>::LDS : TreeCfg<T, D, WIDE ? 1 : KIND>::LDS;
 };
 
-template <typename T, int D, int KIND, bool ROWS>
+// ONCE: one tile of rows for every tree, nobody else reads its pairs
+template <typename T, int D, int KIND, bool ROWS, bool ONCE>
 __global__ __launch_bounds__(256, KIND == 1 && D == 64 ? 3 : 2) void tree_kernel(const TreeParams P) {
-    if constexpr (KIND >= 4) wide_tile<T, D, KIND / 4, ROWS>(P, blockIdx.x, blockIdx.y);
+    if constexpr (KIND >= 4) wide_tile<T, D, KIND / 4, ROWS, ONCE>(P, blockIdx.x, blockIdx.y);
     else tree_tile<T, D, KIND, ROWS>(P, blockIdx.x, blockIdx.y);
 }
 
@@ -89,9 +90,9 @@ static size_t tree_workspace(const fk_paged_desc* d, int32_t n_tokens, int32_t m
     return kCounterBytes + ml_bytes(p, items) + (p.splits > 1 ? (size_t)items * p.splits * 16 * p.kind * d->head_dim * sizeof(float) : 0);
 }
 
-template <typename T, int D, int KIND, bool ROWS> static fk_status tree_start(const TreeParams& P, hipStream_t st) {
+template <typename T, int D, int KIND, bool ROWS, bool ONCE> static fk_status tree_start(const TreeParams& P, hipStream_t st) {
     using C = TreeKind<T, D, KIND>;
-    auto kern = tree_kernel<T, D, KIND, ROWS>;
+    auto kern = tree_kernel<T, D, KIND, ROWS, ONCE>;
     static bool lds_ok[kMaxDevices] = {};
     if (!allow_dynamic_lds((const void*)kern, C::LDS, lds_ok)) return FK_ERR_LAUNCH;
     const int items = P.a.grid.places * P.a.view.n_kv;
@@ -100,10 +101,12 @@ template <typename T, int D, int KIND, bool ROWS> static fk_status tree_start(co
 }
 template <typename T, int D, bool ROWS> static fk_status tree_rows_of(int kind, const TreeParams& P, hipStream_t st) {
     if constexpr (sizeof(T) == 2) {
-        if (kind == 2) return tree_start<T, D, 2, ROWS>(P, st);
-        if (kind == 8) return tree_start<T, D, 8, ROWS>(P, st);
+        const bool once = !P.a.grid.spread && P.a.grid.per_seq == 1;
+        if (kind == 2) return tree_start<T, D, 2, ROWS, false>(P, st);
+        if (kind == 8) return once ? tree_start<T, D, 8, ROWS, true>(P, st) : tree_start<T, D, 8, ROWS, false>(P, st);
+        if (kind == 4 && once) return tree_start<T, D, 4, ROWS, true>(P, st);
     }
-    return kind == 1 ? tree_start<T, D, 1, ROWS>(P, st) : tree_start<T, D, 4, ROWS>(P, st);
+    return kind == 1 ? tree_start<T, D, 1, ROWS, false>(P, st) : tree_start<T, D, 4, ROWS, false>(P, st);
 }
 template <bool ROWS> static fk_status tree_launch(const fk_paged_desc* d, const TreePlan& p, TreeParams& P, void* ws, hipStream_t st) {
     AttnPagedParams& A = P.a;
