@@ -124,7 +124,9 @@ template <int TM> __device__ __forceinline__ void span_of(Ancestors<TM>& s, bool
 
 // ---------------------------------------------------------------------------------------------------------
 // Up to RB * 16 query rows: the wavefronts of a workgroup take tiles of KT pairs in turn, straight from memory into registers, each with its own
-// online softmax for all rows; they are merged through LDS at the end.  An operand of K or V serves a product for each 16 rows.
+// online softmax for all rows; they are merged through LDS at the end.  An operand of K or V serves a product for each 16 rows.  K and V of the next tile
+// are sent off when this one's products have read theirs.  Bound by the memory system: 4 nodes for each of 16 sequences of 2112 pairs, 8 heads of g 4, D 128
+// (142 MB) 27.4 us, 8 nodes 30.6; one sequence, whose splits hold 256 pairs each, by the latency of its loads and of the merge: 11.3.
 // ---------------------------------------------------------------------------------------------------------
 template <typename T, int D, int RB> struct TreeCfg {
     static constexpr bool BF = sizeof(T) == 2;
@@ -550,6 +552,12 @@ __device__ __forceinline__ void tree_tile(const TreeParams& TP, int item, int sp
 // More than 32 query rows: a wavefront owns CT * 16 of them, and the pairs pass by in tiles of KT, each read once for the four wavefronts, straight into
 // LDS: three places each for K and V, so that a tile's loads have two turns to arrive, one barrier a turn.  Layouts in LDS and the order of a
 // turn's steps - the next tile's logits beside this one's softmax - are those of prompt.h.
+// The compiler, which sees loads into LDS and reads of it, has to be told that they are of different places (the __restrict pointers of `turn`), or it waits for
+// all loads before the first read: with that, and two places instead of three, up to 256 rows over 2112 pairs took 70 us, so 62 to 67 by the box.
+// Bound by a turn's chain of LDS reads, products and exponentials, with two or three wavefronts a SIMD to fill its gaps (a turn of 64 pairs for 128 rows takes
+// 2.0 us with the CU to itself, 2.7 beside another workgroup; the products are 0.4): 64 nodes for each of 16 sequences of 16384 pairs, 8 heads of g 4, D 128, 356 us,
+// 773 TFLOP/s.  Matrix cores are busy a third of the time, LDS and vector units as long each; tiles of 32 pairs for 128 rows took 403 us.  Smaller calls spend as long
+// on a workgroup's start and the merge: 12 nodes over 16 rows of 2112 pairs 33 us, of which the pairs' way from memory is 22.
 // ---------------------------------------------------------------------------------------------------------
 template <typename T, int D, int CT_> struct WideCfg {
     static constexpr bool BF = sizeof(T) == 2;
@@ -656,8 +664,7 @@ __device__ __forceinline__ void wide_tile(const TreeParams& TP, int item, int sp
         for (int lo = 0, hi = nodes - 1;;) {
         int level_lo = 0, level_hi = 0;
         if (tid == 0) s_bad = 0;
-        if (windowed || some_tree) span_of<TM>(s_tree, windowed, lo, hi, level_lo, level_hi);
-        else __syncthreads();
+        if (windowed || some_tree) span_of<TM>(s_tree, windowed, lo, hi, level_lo, level_hi);   // (otherwise no barrier here: the first tiles' is ahead of the flag's use)
         const int any_from = windowed ? n + level_lo - W.window + 1 : 0, all_from = windowed ? n + level_hi - W.window + 1 : 0;
         float m_ref[CT], m_top[CT], l_run[CT];
         tf32x4_t o[ET][CT];
