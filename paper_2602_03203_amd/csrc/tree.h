@@ -104,10 +104,11 @@ template <int TM> __device__ __forceinline__ void span_of(Ancestors<TM>& s, bool
         s.all[threadIdx.x] = ~0u;
     }
     __syncthreads();
-    for (int i = lo * (kTreeNodes / 32) + threadIdx.x; i < (hi + 1) * (kTreeNodes / 32); i += 256) {
-        const uint32_t x = s.sees[0][i];
-        atomicOr(&s.any[i % (kTreeNodes / 32)], x);
-        atomicAnd(&s.all[i % (kTreeNodes / 32)], x);
+    constexpr int WORDS = kTreeNodes / 32;
+    for (int i = lo * WORDS + threadIdx.x; i < (hi + 1) * WORDS; i += 256) {
+        const uint32_t x = s.sees[i / WORDS][i % WORDS];
+        atomicOr(&s.any[i % WORDS], x);
+        atomicAnd(&s.all[i % WORDS], x);
     }
     level_lo = level_hi = 0;
     if (windowed) {
@@ -553,7 +554,7 @@ __device__ __forceinline__ void tree_tile(const TreeParams& TP, int item, int sp
 // LDS: three places each for K and V, so that a tile's loads have two turns to arrive, one barrier a turn.  Layouts in LDS and the order of a
 // turn's steps - the next tile's logits beside this one's softmax - are those of prompt.h.
 // The compiler, which sees loads into LDS and reads of it, has to be told that they are of different places (the __restrict pointers of `turn`), or it waits for
-// all loads before the first read: with that, and two places instead of three, up to 256 rows over 2112 pairs took 70 us, so 62 to 67 by the box.
+// all loads before the first read: with that, and two places instead of three, up to 256 rows over 2112 pairs took 70 us, so 61 to 67 from card to card.
 // Bound by a turn's chain of LDS reads, products and exponentials, with two or three wavefronts a SIMD to fill its gaps (a turn of 64 pairs for 128 rows takes
 // 2.0 us with the CU to itself, 2.7 beside another workgroup; the products are 0.4): 64 nodes for each of 16 sequences of 16384 pairs, 8 heads of g 4, D 128, 356 us,
 // 773 TFLOP/s.  Matrix cores are busy a third of the time, LDS and vector units as long each; tiles of 32 pairs for 128 rows took 403 us.  Smaller calls spend as long
