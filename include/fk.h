@@ -500,9 +500,9 @@ fk_status fk_paged_tree_attn(const fk_paged_desc *desc, const void *q, const voi
 /*
  * Verification of drafted tokens against the large model's probabilities (speculative sampling: what comes out is distributed as the large model's own
  * samples).  target [n_tokens][vocab] fp32: row i is the distribution of the token behind node i; draft [n_tokens][vocab] fp32: row i is the one from which the
- * children of node i were drawn, independently of each other; tokens [n_tokens]: the nodes' tokens (the root's is not looked at); uniform [n_tokens] fp32 in
- * [0, 1): a node's number decides about it, the root's draws the last token.  From the root on, with r = target's row of the current node, its
- * children x in ascending order:
+ * children of node i were drawn, independently of each other (rows of nodes without children are not looked at); tokens [n_tokens]: the nodes' tokens (the root's
+ * is not looked at); uniform [n_tokens] fp32 in [0, 1): a node's number decides about it, the root's draws the last token.  From the root on, with r = target's
+ * row of the current node, its children x in ascending order:
  *   uniform * draft(x) < r(x): x is accepted and becomes the current node, with r = target's row again;
  *   otherwise r becomes max(r - draft, 0), divided by its sum.
  * draft NULL (tokens that were not drawn, the likeliest ones say): x is accepted where uniform * m < r(x), with m = 1 at first; otherwise m goes down by r(x),

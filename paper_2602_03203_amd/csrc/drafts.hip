@@ -105,7 +105,7 @@ __device__ __forceinline__ void walk(Tree& T, int nodes, bool drawn, double m) {
     T.state = state;
 }
 
-// what is left of a number of the vocabulary at the current node
+// what is left of a number of the vocabulary at the current node; drawn: tokens of the draft have been rejected there
 __device__ __forceinline__ double left_of(double c, float p, float q, bool drawn) {
     const double r = drawn ? (double)p - c * (double)q : (double)p;
     return r > 0.0 ? r : 0.0;
@@ -161,6 +161,10 @@ __device__ __forceinline__ unsigned long long gone_of(const Tree& T, int v) {
     return bits;
 }
 
+// The draft's row as far as it plays a part: with nothing rejected (c = 0) what is left is the target's row whatever the draft holds - nobody drew from the row
+// of a node without children, which may not have been filled, and 0 times an infinity or a NaN is no 0.  The same for all threads of a sequence.
+__device__ __forceinline__ const float* draft_of(const VerifyParams& P, const Tree& T, size_t row) { return P.draft && T.c != 0.0 ? P.draft + row : nullptr; }
+
 // the rejected tokens that lie in a chunk; all threads
 __device__ __forceinline__ void find_gone(const VerifyParams& P, Tree& T, int chunk) {
     if (threadIdx.x < kWave) {
@@ -183,7 +187,7 @@ __device__ __forceinline__ void sum_chunk(const VerifyParams& P, Tree& T, int be
     const int tid = threadIdx.x, v0 = chunk * P.chunk, end = min(v0 + P.chunk, P.vocab);
     find_gone(P, T, chunk);
     const size_t row = (size_t)(begin + T.at) * P.vocab;
-    const float *p = P.target + row, *q = P.draft ? P.draft + row : nullptr;
+    const float *p = P.target + row, *q = draft_of(P, T, row);
     const double c = T.c;
     double sum = 0.0;
     auto add = [&](auto SOME) {   // SOME: tokens that do not count
@@ -344,7 +348,7 @@ __global__ __launch_bounds__(kVerifyThreads) void verify_kernel(const VerifyPara
     // in it: four numbers a thread at a time
     find_gone(P, T, chunk);
     const size_t row = (size_t)(begin + T.at) * P.vocab;
-    const float *p = P.target + row, *q = drawn ? P.draft + row : nullptr;
+    const float *p = P.target + row, *q = draft_of(P, T, row);
     const int end = min((chunk + 1) * P.chunk, P.vocab);
     const double want = T.left, c = T.c;
     double below = 0.0;

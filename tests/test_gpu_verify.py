@@ -205,3 +205,26 @@ def test_more_rejections_than_sums_are_told():
     c.tokens[:] = 5   # (and the same token every time, which the draft likes better than the target)
     c.target[:, 5] *= 0.5
     c.go()
+
+
+@pytest.mark.parametrize("vocab", [130, 5003, 40001])
+def test_draft_rows_that_play_no_part(vocab):
+    """Nobody drew from the row of a node without children, which may hold anything; nor does a draft's row count where nothing was rejected, or where nothing is left of r
+    and the target's own row takes its place."""
+    c = Trees([[-1], [-1], [-1, 0, 0, 1], [-1, 0, 1, 2], [-1, 0], [-1, -1], tree(30, 1, depth=3)], vocab, seed=vocab, sharp=1.0)
+    s, p, q = c.q_start, c.target, c.draft
+    with_children = {s[b] + x for b, t in enumerate(c.trees) for x in t if x >= 0}
+    leaves = [i for i in range(c.n) if i not in with_children]
+    q[leaves] = np.nan
+    q[leaves[::2], ::3] = np.inf
+    q[leaves[::3], 1::2] = -np.inf
+    c.uniform[s[3]:s[4]] = 0.0                           # a chain, all accepted: its leaf's row is the target's
+    keep = int(c.tokens[s[4] + 1])
+    q[s[4]] = 2 * p[s[4]]                                # nothing is left: the target's own row, infinities of the draft or not
+    q[s[4], [x for x in range(0, vocab, 7) if x != keep]] = np.inf
+    c.uniform[s[4] + 1] = 0.75
+    for u in (0.0, 0.3, 0.999):
+        c.uniform[s[:-1]] = u
+        path, count, following = c.reference()
+        assert count[3] == 4 and count[4] == 1 and (following >= 0).all()
+        c.go(f"u {u}")
