@@ -477,8 +477,8 @@ fk_status fk_rope_frequencies(int32_t rotary_dim, double base, int32_t scaling, 
  *   out[t][hq][:] = sum_j 2^(s_j - M) V_j / L,  s_j = log2(e) * softmax_scale * <q[t][hq], K_j>,  M = max_j s_j,  L = sum_j 2^(s_j - M)
  * k_tree, v_tree: the nodes' own pairs, [n_tokens][n_kv_heads][head_dim]; the cache is only read.  q, out: [n_tokens][n_q_heads][head_dim]; stats (may be NULL):
  * [n_tokens][n_q_heads][2] fp32, M and L.  Logits of -inf alone give zeros and (-inf, 0); a query that is no number, or meets one, has L = NaN.  Values of
- * pairs that a node does not see, infinities and NaN among them, do not reach its results.  fp32 accumulation; bf16: the weights are rounded to bf16 before they
- * meet V, L is the sum of the unrounded ones (fk_paged_attn's rounding).  max_tree <= FK_TREE_NODES bounds the trees' nodes and max_len every len[r]; they only
+ * pairs that a node does not see, infinities and NaN among them, do not reach its results.  fp32 accumulation; bf16: a weight meets V as two bf16 terms, off
+ * by 2^-15 of it at most, L is the sum of the unrounded ones.  max_tree <= FK_TREE_NODES bounds the trees' nodes and max_len every len[r]; they only
  * size the launch, results are right beyond them too.  workspace: fk_tree_attn_workspace bytes for the same sizes, zero-filled ONCE by the caller; every call leaves its
  * counters at zero again, and calls of any sizes (of fk_paged_tree_attn too) may take turns with one that is large enough for each; calls sharing it must not
  * overlap in time.  One launch; the order of all sums is fixed: equal calls give equal bits.  FK_ERR_UNSUPPORTED: n_tokens * n_q_heads >= 2^28, n_kv_heads >= 2^16.

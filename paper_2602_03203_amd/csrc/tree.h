@@ -38,6 +38,15 @@ __device__ __forceinline__ bool last_one(uint32_t* here, int splits) {
     return last;
 }
 
+// bf16: a weight meets V as two terms, the first cut off and the second the rest, rounded: 2^-15 of it off at most (one term is off by up to 2^-8, alike for equal weights,
+// which no average takes away).  Sums of weights are those of the unrounded ones.  The rest is taken 2^-20 too large, so that both terms of a weight above 0 (from 2^-106 on) are
+// above 0 and an infinity among the values stays one.  Up to 64 query rows cost 1 % by it (12 nodes for each of 16 sequences of 2112 pairs, 8 heads of g 4, D 128: 32.6 -> 32.9 us, of g 7
+// and 26 nodes 52 -> 56), 128 rows a fifth (64 nodes 60 -> 72).
+__device__ __forceinline__ void two_terms(float a, float b, uint32_t& first, uint32_t& second) {
+    first = __builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x07060302u);
+    second = pack_bf16(fmaf(a, 1.f + 0x1p-20f, -__uint_as_float(__float_as_uint(a) & 0xffff0000u)), fmaf(b, 1.f + 0x1p-20f, -__uint_as_float(__float_as_uint(b) & 0xffff0000u)));
+}
+
 // What a workgroup works on; false: nothing
 struct TreeWork {
     TileOf t;
@@ -355,7 +364,7 @@ __device__ __forceinline__ void tree_tile(const TreeParams& TP, int item, int sp
                 }
                 if (bad && hi > lo) s_bad = 1;
             }
-            T128 pr[RB];   // bf16: the probabilities, each rounded by half a step of bf16 at most; sums of them unrounded
+            T128 pr[RB], pr2[RB];   // bf16: the probabilities' two terms
 #pragma unroll
             for (int rb = 0; rb < RB; ++rb) {
                 float mx = s[rb][0];
@@ -380,7 +389,7 @@ __device__ __forceinline__ void tree_tile(const TreeParams& TP, int item, int sp
                 }
                 if constexpr (BF) {
 #pragma unroll
-                    for (int x = 0; x < 4; ++x) pr[rb].w[x] = pack_bf16(s[rb][2 * x], s[rb][2 * x + 1]);
+                    for (int x = 0; x < 4; ++x) two_terms(s[rb][2 * x], s[rb][2 * x + 1], pr[rb].w[x], pr2[rb].w[x]);
                 }
             }
 #pragma unroll
@@ -392,6 +401,8 @@ __device__ __forceinline__ void tree_tile(const TreeParams& TP, int item, int sp
                     for (int x = 0; x < 4; ++x) vb.w[x] = __builtin_amdgcn_perm(vr[2 * x + 1].w[e >> 1], vr[2 * x].w[e >> 1], sel);
 #pragma unroll
                     for (int rb = 0; rb < RB; ++rb) o[rb][e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vb.v, pr[rb].v, o[rb][e], 0, 0, 0);
+#pragma unroll
+                    for (int rb = 0; rb < RB; ++rb) o[rb][e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vb.v, pr2[rb].v, o[rb][e], 0, 0, 0);
                 } else {
 #pragma unroll
                     for (int u = 0; u < 4; ++u)
@@ -877,19 +888,25 @@ __device__ __forceinline__ void wide_tile(const TreeParams& TP, int item, int sp
 #pragma unroll
             for (int b = 0; b < NB; ++b) {
                 if constexpr (BF) {
-                    T128 pr[CT];   // rounded: each weight by half a step of bf16 at most, sums of them in fp32
+                    T128 pr[CT], pr2[CT];
 #pragma unroll
                     for (int ct = 0; ct < CT; ++ct)
 #pragma unroll
-                        for (int x = 0; x < 4; ++x) pr[ct].w[x] = pack_bf16(c[2 * b + x / 2][ct][x % 2 * 2], c[2 * b + x / 2][ct][x % 2 * 2 + 1]);
+                        for (int x = 0; x < 4; ++x) two_terms(c[2 * b + x / 2][ct][x % 2 * 2], c[2 * b + x / 2][ct][x % 2 * 2 + 1], pr[ct].w[x], pr2[ct].w[x]);
+                    constexpr int EE = CT == 1 ? 4 : 1;   // channel tiles at a time: no product waits for the one before it (D 64, 64 nodes 48.0 -> 43.6 us)
 #pragma unroll
-                    for (int e = 0; e < ET; ++e) {
-                        T128 v;
-                        const unsigned char* at = sv + v_at(e) + b * BLK * CH * 16;
-                        const tu32x2_t v0 = read_transposed(at), v1 = read_transposed(at + 4 * CH * 16);
-                        v.u = tu32x4_t{v0.x, v0.y, v1.x, v1.y};
+                    for (int e0 = 0; e0 < ET; e0 += EE) {
+                        T128 v[EE];
 #pragma unroll
-                        for (int ct = 0; ct < CT; ++ct) o[e][ct] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v.v, pr[ct].v, o[e][ct], 0, 0, 0);
+                        for (int e = 0; e < EE; ++e) {
+                            const unsigned char* at = sv + v_at(e0 + e) + b * BLK * CH * 16;
+                            const tu32x2_t v0 = read_transposed(at), v1 = read_transposed(at + 4 * CH * 16);
+                            v[e].u = tu32x4_t{v0.x, v0.y, v1.x, v1.y};
+                        }
+#pragma unroll
+                        for (int k = 0; k < 2 * CT; ++k)
+#pragma unroll
+                            for (int e = 0; e < EE; ++e) o[e0 + e][k % CT] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v[e].v, k < CT ? pr[k % CT].v : pr2[k % CT].v, o[e0 + e][k % CT], 0, 0, 0);
                     }
                 } else {
 #pragma unroll

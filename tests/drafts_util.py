@@ -88,7 +88,8 @@ class TreeCase:
                 t0 = int(self.q_start[b])
                 yield b, parent, slice(t0, t0 + len(parent))
 
-    def reference(self):
+    def reference(self, weight=UB):
+        """weight: how far a bf16 weight may be off as it meets V, relative."""
         Hq = self.H * self.g
         ref = dict(out=np.full((self.n_tokens, Hq, self.D), 7.0), M=np.full((self.n_tokens, Hq), 7.0), L=np.full((self.n_tokens, Hq), 7.0))
         tol = {k: np.zeros_like(v) for k, v in ref.items()}
@@ -109,8 +110,8 @@ class TreeCase:
             d = (self.D + 4) * U * mag * abs(self.scale) / np.log(2.0) + U
             rel = 2 * np.log(2.0) * d + (2 * n + 8) * U
             half = U if self.dtype == "f32" else UB
-            # bf16: every weight is rounded before it meets V (half a step), and the result once more
-            tol["out"][tok] = (rel[:, :, None] + (0 if self.dtype == "f32" else UB)) * wv + half * np.abs(out) * (1 + rel[:, :, None] + half) + 1e-30
+            # bf16: every weight is rounded before it meets V, and the result once more (half a step); two terms of a weight are twice as many products to sum
+            tol["out"][tok] = (rel[:, :, None] + (0 if self.dtype == "f32" else weight + n * U)) * wv + half * np.abs(out) * (1 + rel[:, :, None] + half) + 1e-30
             tol["M"][tok], tol["L"][tok] = d, rel * L
         return ref, tol
 

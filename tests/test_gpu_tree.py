@@ -3,7 +3,7 @@ import numpy as np
 import pytest
 import torch
 
-from drafts_util import TreeCase, tree
+from drafts_util import UB, TreeCase, tree
 
 pytestmark = pytest.mark.gpu
 
@@ -266,3 +266,55 @@ def test_calls_of_any_sizes_share_a_workspace():
         torch.cuda.synchronize()
         for i, (c, s, r) in enumerate(zip(cases, devs, refs)):
             c.check(s, *r, f"turn {turn} case {i}")
+
+
+# two terms of bf16 for a weight: the first cut off, by a step of bf16 (2^-7 of it) at most, the second off by half a step (2^-8) of that rest; the rest is 2^-20 of the
+# weight too large, which is rounded with it
+TWO_TERMS = 2.0 ** -15 + 2.0 ** -19
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("g, nodes, page", [(4, 4, 0), (4, 8, 16), (8, 4, 0), (4, 12, 0), (1, 50, 32), (4, 40, 0), (8, 30, 16)])
+def test_equal_weights_next_to_a_larger_one(D, g, nodes, page):
+    """All pairs but one have the same weight, which rounds down by nearly half a step of bf16: an error that no average takes away."""
+    w = (1 + 0.97 * UB) / 8
+    c = TreeCase("bf16", D, g, 1, [(250, tree(nodes, depth=0)), (100, tree(nodes, 1))], page, scale=-float(np.log(w)), seed=nodes)
+    c.q[:], c.K[:], c.k_tree[:] = 0, 0, 0
+    c.q[..., 0], c.K[..., 0], c.k_tree[..., 0] = 1, -1, -1
+    gen = torch.Generator().manual_seed(D)
+    c.V[:] = torch.rand(D, generator=gen).add_(0.5).to(c.dt)   # alike for all pairs but the first of a row
+    c.v_tree[:] = c.V[(0,) * (c.V.dim() - 1)]
+    for b in range(2):
+        c.K[c.slot(b, 0, 0)], c.V[c.slot(b, 0, 0)] = 0, 0
+    s = c.dev()
+    c.run(s)
+    torch.cuda.synchronize()
+    c.check(s, *c.reference(TWO_TERMS))
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("g, nodes, lens, page, window", [(4, 4, (300, 33), 0, 0), (7, 3, (300, 129), 16, 0), (4, 8, (65, 200), 0, 0), (4, 12, (1100, 700), 0, 0), (4, 16, (300, 17), 64, 100),
+                                                          (7, 26, (800,), 0, 0), (8, 30, (900, 64), 32, 0), (1, 200, (64, 600), 0, 0), (4, 3, (2500,), 0, 0), (2, 15, (0, 1), 16, 0)])
+def test_weights_keep_sixteen_bits(D, g, nodes, lens, page, window):
+    c = TreeCase("bf16", D, g, 2, [(n, tree(nodes, n)) for n in lens], page, window, 4 if window else 0, seed=nodes)
+    s = c.dev()
+    c.run(s)
+    torch.cuda.synchronize()
+    c.check(s, *c.reference(TWO_TERMS))
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("g, nodes, page", [(4, 4, 0), (4, 8, 16), (4, 12, 0), (8, 30, 16), (4, 64, 0)])
+def test_infinite_values_of_equal_weights(D, g, nodes, page):
+    """All weights are 1, whose second term has nothing to hold: infinities that are seen stay infinities of their sign, in the cache and on a node's way."""
+    c = TreeCase("bf16", D, g, 1, [(250, tree(nodes, depth=0)), (90, tree(nodes, 1)), (700, tree(nodes, 2))], page, seed=nodes)
+    c.q[:] = 0
+    for b, j in ((0, 3), (1, 89), (2, 600)):
+        c.V[c.slot(b, 0, j)][7], c.V[c.slot(b, 0, j)][D - 1] = float("inf"), -float("inf")
+    c.v_tree[int(c.q_start[1]) + nodes // 2, 0, 20] = float("inf")
+    ref = c.reference(TWO_TERMS)
+    assert np.isinf(ref[0]["out"]).any() and not np.isnan(ref[0]["out"]).any()
+    s = c.dev()
+    c.run(s)
+    torch.cuda.synchronize()
+    c.check(s, *ref)
