@@ -464,6 +464,25 @@ def fk_compact_acc(desc: CacheDesc, K, V, pos, acc, length, keep_idx, budget: in
     _call("fk_compact_acc", ctypes.byref(desc.c()), _ptr(K), _ptr(V), _ptr(pos), _ptr(acc), _ptr(length), _ptr(keep_idx), int(budget), _stream(stream))
 
 
+def _buf(t, dtype, n: int, what: str) -> int:
+    """_ptr of a buffer of at least n elements of this type: a position or a token in 64 bits, a row too few would be misread or read past its end."""
+    if t is None:
+        return 0
+    assert t.dtype == dtype, f"{what} is {dtype}, not {t.dtype}"
+    assert t.numel() >= n, f"{what} holds {n} elements, not {t.numel()}"
+    return _ptr(t)
+
+
+def _torch_dtype(desc):
+    return torch.float32 if desc.dtype == "f32" else torch.bfloat16
+
+
+def _nodes(desc, x, n: int, heads: int, what: str) -> int:
+    """_buf of the heads of n tokens and more."""
+    assert x is None or x.numel() == x.shape[0] * heads * desc.head_dim, f"{what} is [n_tokens, {heads}, {desc.head_dim}], not {tuple(x.shape)}"
+    return _buf(x, _torch_dtype(desc), n * heads * desc.head_dim, what)
+
+
 @dataclass
 class RopeDesc:
     n_q_heads: int
@@ -487,9 +506,11 @@ class RopeDesc:
         return int(x.stride(0))
 
 
-def _heads_ptr(x, desc: RopeDesc, heads: int) -> int:
+def _heads_ptr(x, desc: RopeDesc, heads: int, n_tokens: int) -> int:
     if x is None:
         return 0
+    assert x.dtype == _torch_dtype(desc), f"queries and keys are {_torch_dtype(desc)}, not {x.dtype}"
+    assert x.shape[0] == n_tokens, f"queries, keys and outputs are of {n_tokens} tokens each, not {x.shape[0]}"
     assert x.is_cuda and tuple(x.shape[1:]) == (heads, desc.head_dim), "queries and keys are [n_tokens, heads, head_dim] device tensors"
     assert x.numel() == 0 or (x.stride(2) == 1 and (heads == 1 or x.stride(1) == desc.head_dim)), "a token's heads must lie side by side"
     assert x.shape[0] < 2 or x.stride(0) >= heads * desc.head_dim, "tokens must not share memory"
@@ -508,10 +529,10 @@ def rope_frequencies(rotary_dim: int, base: float = 10000.0, scaling: str = "non
 def fk_rope(desc: RopeDesc, q, k, pos, freq, q_out, k_out, stream=None) -> None:
     """Rotary positions of q [n_tokens, n_q_heads, D] and k [n_tokens, n_kv_heads, D]; a token's heads lie side by side, tokens any distance apart.
     pos [n_tokens] int32; freq fp64 [rotary_dim / 2] on the device; q_out may be q, k_out may be k."""
-    some = q if q is not None else k
+    n = int((q if q is not None else k).shape[0])
     assert freq.dtype == torch.float64 and freq.numel() >= desc.rotary_dim // 2, "freq is fp64 [rotary_dim / 2]"
-    _call("fk_rope", ctypes.byref(desc.c(q, k, q_out, k_out)), _heads_ptr(q, desc, desc.n_q_heads), _heads_ptr(k, desc, desc.n_kv_heads), _ptr(pos), _ptr(freq),
-          int(some.shape[0]), _heads_ptr(q_out, desc, desc.n_q_heads), _heads_ptr(k_out, desc, desc.n_kv_heads), _stream(stream))
+    _call("fk_rope", ctypes.byref(desc.c(q, k, q_out, k_out)), _heads_ptr(q, desc, desc.n_q_heads, n), _heads_ptr(k, desc, desc.n_kv_heads, n),
+          _buf(pos, torch.int32, n, "pos"), _ptr(freq), n, _heads_ptr(q_out, desc, desc.n_q_heads, n), _heads_ptr(k_out, desc, desc.n_kv_heads, n), _stream(stream))
 
 
 def fk_tree_attn_workspace(desc: CacheDesc, n_tokens: int, max_tree: int, max_len: int) -> int:
@@ -528,8 +549,11 @@ def fk_tree_attn(desc: CacheDesc, q, K, V, length, k_tree, v_tree, parent, q_sta
     """Attention of the nodes q [n_tokens, n_q_heads, D] of drafted trees over their sequence's rows and their own ancestors (k_tree, v_tree [n_tokens,
     n_kv_heads, D]).  stats [n_tokens, n_q_heads, 2] fp32 or None."""
     nbytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
-    _call("fk_tree_attn", ctypes.byref(desc.c()), _ptr(q), _ptr(K), _ptr(V), _ptr(length), _ptr(k_tree), _ptr(v_tree), _ptr(parent), _ptr(q_start),
-          int(q.shape[0]), int(max_tree), int(max_len), float(softmax_scale), _ptr(out), _ptr(stats), _ptr(workspace), nbytes, _stream(stream))
+    n, cache = int(q.shape[0]), desc.batch * desc.n_kv_heads * desc.capacity * desc.head_dim
+    _call("fk_tree_attn", ctypes.byref(desc.c()), _nodes(desc, q, n, desc.n_q_heads, "q"), _buf(K, _torch_dtype(desc), cache, "K"), _buf(V, _torch_dtype(desc), cache, "V"),
+          _buf(length, torch.int32, desc.batch * desc.n_kv_heads, "length"), _nodes(desc, k_tree, n, desc.n_kv_heads, "k_tree"), _nodes(desc, v_tree, n, desc.n_kv_heads, "v_tree"),
+          _buf(parent, torch.int32, n, "parent"), _buf(q_start, torch.int32, desc.batch + 1, "q_start"), n, int(max_tree), int(max_len), float(softmax_scale),
+          _nodes(desc, out, n, desc.n_q_heads, "out"), _buf(stats, torch.float32, n * desc.n_q_heads * 2, "stats"), _ptr(workspace), nbytes, _stream(stream))
 
 
 def fk_paged_tree_attn_workspace(desc: PagedDesc, n_tokens: int, max_tree: int, max_len: int) -> int:
@@ -545,9 +569,12 @@ def fk_paged_tree_attn(desc: PagedDesc, q, K, V, page_table, kv_len, k_tree, v_t
                        softmax_scale: float, out, stats, workspace, stream=None) -> None:
     """fk_tree_attn over the pages of a prompt; kv_len counts the pairs in the pages, none of the tree's."""
     nbytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
-    _call("fk_paged_tree_attn", ctypes.byref(desc.c()), _ptr(q), _ptr(K), _ptr(V), _ptr(page_table), _ptr(kv_len), _ptr(k_tree), _ptr(v_tree), _ptr(parent),
-          _ptr(q_start), int(q.shape[0]), int(max_tree), int(max_len), int(window), int(n_sink), float(softmax_scale), _ptr(out), _ptr(stats), _ptr(workspace),
-          nbytes, _stream(stream))
+    n, pool = int(q.shape[0]), desc.n_pages * desc.n_kv_heads * desc.page_size * desc.head_dim
+    _call("fk_paged_tree_attn", ctypes.byref(desc.c()), _nodes(desc, q, n, desc.n_q_heads, "q"), _buf(K, _torch_dtype(desc), pool, "K"), _buf(V, _torch_dtype(desc), pool, "V"),
+          _buf(page_table, torch.int32, desc.batch * desc.max_pages, "page_table"), _buf(kv_len, torch.int32, desc.batch, "kv_len"),
+          _nodes(desc, k_tree, n, desc.n_kv_heads, "k_tree"), _nodes(desc, v_tree, n, desc.n_kv_heads, "v_tree"), _buf(parent, torch.int32, n, "parent"),
+          _buf(q_start, torch.int32, desc.batch + 1, "q_start"), n, int(max_tree), int(max_len), int(window), int(n_sink), float(softmax_scale),
+          _nodes(desc, out, n, desc.n_q_heads, "out"), _buf(stats, torch.float32, n * desc.n_q_heads * 2, "stats"), _ptr(workspace), nbytes, _stream(stream))
 
 
 def fk_verify_drafts_workspace(batch: int, vocab: int) -> int:
@@ -563,20 +590,30 @@ def fk_verify_drafts(target, draft, tokens, parent, q_start, uniform, path, n_ac
     """Which nodes of the drafted trees target's probabilities accept, and the token behind them.  target, draft [n_tokens, vocab] fp32 (draft None: tokens
     that were not drawn); tokens, parent, path [n_tokens] int32; uniform [n_tokens] fp32; n_accepted, next_token [batch] int32."""
     nbytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
-    _call("fk_verify_drafts", int(q_start.shape[0]) - 1, int(target.shape[1]), _ptr(target), _ptr(draft), _ptr(tokens), _ptr(parent), _ptr(q_start),
-          int(target.shape[0]), _ptr(uniform), _ptr(path), _ptr(n_accepted), _ptr(next_token), _ptr(workspace), nbytes, _stream(stream))
+    (n, vocab), batch, i32 = target.shape, int(q_start.shape[0]) - 1, torch.int32
+    assert draft is None or draft.shape == target.shape, f"draft is of target's shape {tuple(target.shape)}, not {tuple(draft.shape)}"
+    _call("fk_verify_drafts", batch, int(vocab), _buf(target, torch.float32, n * vocab, "target"), _buf(draft, torch.float32, n * vocab, "draft"), _buf(tokens, i32, n, "tokens"),
+          _buf(parent, i32, n, "parent"), _buf(q_start, i32, batch + 1, "q_start"), int(n), _buf(uniform, torch.float32, n, "uniform"), _buf(path, i32, n, "path"),
+          _buf(n_accepted, i32, batch, "n_accepted"), _buf(next_token, i32, batch, "next_token"), _ptr(workspace), nbytes, _stream(stream))
 
 
 def fk_commit_drafts(desc: CacheDesc, K, V, pos, length, acc, k_tree, v_tree, q_start, path, n_accepted, pos_first, stream=None) -> None:
     """The accepted paths' pairs join the rows; acc (accumulated weights, zero in the new slots) may be None."""
-    _call("fk_commit_drafts", ctypes.byref(desc.c()), _ptr(K), _ptr(V), _ptr(pos), _ptr(length), _ptr(acc), _ptr(k_tree), _ptr(v_tree), _ptr(q_start),
-          int(k_tree.shape[0]), _ptr(path), _ptr(n_accepted), _ptr(pos_first), _stream(stream))
+    rows, n, i32 = desc.batch * desc.n_kv_heads, int(k_tree.shape[0]), torch.int32
+    slots = rows * desc.capacity
+    _call("fk_commit_drafts", ctypes.byref(desc.c()), _buf(K, _torch_dtype(desc), slots * desc.head_dim, "K"), _buf(V, _torch_dtype(desc), slots * desc.head_dim, "V"),
+          _buf(pos, i32, slots, "pos"), _buf(length, i32, rows, "length"), _buf(acc, torch.float32, slots, "acc"), _nodes(desc, k_tree, n, desc.n_kv_heads, "k_tree"),
+          _nodes(desc, v_tree, n, desc.n_kv_heads, "v_tree"), _buf(q_start, i32, desc.batch + 1, "q_start"), n, _buf(path, i32, n, "path"),
+          _buf(n_accepted, i32, desc.batch, "n_accepted"), _buf(pos_first, i32, desc.batch, "pos_first"), _stream(stream))
 
 
 def fk_paged_commit_drafts(desc: PagedDesc, K, V, page_table, kv_len, k_tree, v_tree, q_start, path, n_accepted, stream=None) -> None:
     """The accepted paths' pairs join the pages; kv_len goes up by as many."""
-    _call("fk_paged_commit_drafts", ctypes.byref(desc.c()), _ptr(K), _ptr(V), _ptr(page_table), _ptr(kv_len), _ptr(k_tree), _ptr(v_tree), _ptr(q_start),
-          int(k_tree.shape[0]), _ptr(path), _ptr(n_accepted), _stream(stream))
+    n, i32, pool = int(k_tree.shape[0]), torch.int32, desc.n_pages * desc.n_kv_heads * desc.page_size * desc.head_dim
+    _call("fk_paged_commit_drafts", ctypes.byref(desc.c()), _buf(K, _torch_dtype(desc), pool, "K"), _buf(V, _torch_dtype(desc), pool, "V"),
+          _buf(page_table, i32, desc.batch * desc.max_pages, "page_table"), _buf(kv_len, i32, desc.batch, "kv_len"), _nodes(desc, k_tree, n, desc.n_kv_heads, "k_tree"),
+          _nodes(desc, v_tree, n, desc.n_kv_heads, "v_tree"), _buf(q_start, i32, desc.batch + 1, "q_start"), n, _buf(path, i32, n, "path"),
+          _buf(n_accepted, i32, desc.batch, "n_accepted"), _stream(stream))
 
 
 def fk_stream_read(src, sink, stream=None) -> None:

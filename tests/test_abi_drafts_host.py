@@ -157,3 +157,61 @@ def test_commit(fklib, change, code):
     if not only_rows:
         assert got[1] == code
     assert calls(0) == (0, 0)
+
+
+def _wrapped(F, name, change):
+    """Runs the wrapper of a call, which must not get as far as the library, on buffers of the right types and sizes but for those in `change`."""
+    import torch
+
+    class Device(torch.Tensor):   # (host memory that nothing follows)
+        is_cuda = True
+    B, H, g, D, n, vocab, cap, page = 2, 2, 4, 64, 5, 11, 32, 16
+    bf, f32, i32 = torch.bfloat16, torch.float32, torch.int32
+    z = lambda *s, dtype=i32: torch.zeros(s, dtype=dtype).as_subclass(Device)   # noqa: E731
+    rows, pages = F.CacheDesc(B, H * g, H, D, cap, "bf16"), F.PagedDesc(B, H * g, H, D, page, 3, 2, "bf16")
+    in_rows = dict(K=z(B, H, cap, D, dtype=bf), V=z(B, H, cap, D, dtype=bf))
+    in_pages = dict(K=z(3, H, page, D, dtype=bf), V=z(3, H, page, D, dtype=bf), page_table=z(B, 2), kv_len=z(B))
+    tree = dict(k_tree=z(n, H, D, dtype=bf), v_tree=z(n, H, D, dtype=bf))
+    nodes, paths = dict(parent=z(n), q_start=z(B + 1)), dict(q_start=z(B + 1), path=z(n), n_accepted=z(B))
+    attend = dict(q=z(n, H * g, D, dtype=bf), out=z(n, H * g, D, dtype=bf), stats=z(n, H * g, 2, dtype=f32), workspace=None, max_tree=3, max_len=16, softmax_scale=1.0)
+    calls = dict(
+        fk_rope=dict(desc=F.RopeDesc(H * g, H, D, D, "half", "bf16"), q=attend["q"], k=tree["k_tree"], pos=z(n), freq=z(D // 2, dtype=torch.float64), q_out=attend["out"],
+                     k_out=tree["v_tree"]),
+        fk_tree_attn=dict(desc=rows, length=z(B, H), **in_rows, **tree, **nodes, **attend),
+        fk_paged_tree_attn=dict(desc=pages, window=0, n_sink=0, **in_pages, **tree, **nodes, **attend),
+        fk_verify_drafts=dict(target=z(n, vocab, dtype=f32), draft=z(n, vocab, dtype=f32), tokens=z(n), uniform=z(n, dtype=f32), path=z(n), n_accepted=z(B), next_token=z(B),
+                              workspace=None, **nodes),
+        fk_commit_drafts=dict(desc=rows, pos=z(B, H, cap), length=z(B, H), acc=z(B, H, cap, dtype=f32), pos_first=z(B), **in_rows, **tree, **paths),
+        fk_paged_commit_drafts=dict(desc=pages, **in_pages, **tree, **paths))
+    a = calls[name]
+    for k, make in change.items():
+        assert k in a
+        a[k] = make(a[k])
+    getattr(F, name)(**a, stream=type("Stream", (), dict(cuda_stream=0)))
+
+
+SHORT = dict(fk_rope=["k", "pos", "q_out", "k_out"], fk_tree_attn=["K", "V", "length", "k_tree", "v_tree", "parent", "q_start", "out", "stats"],
+             fk_paged_tree_attn=["K", "V", "page_table", "kv_len", "k_tree", "v_tree", "parent", "q_start", "out", "stats"],
+             fk_verify_drafts=["draft", "tokens", "parent", "uniform", "path", "n_accepted", "next_token"],
+             fk_commit_drafts=["K", "V", "pos", "length", "acc", "v_tree", "q_start", "path", "n_accepted", "pos_first"],
+             fk_paged_commit_drafts=["K", "V", "page_table", "kv_len", "v_tree", "q_start", "path", "n_accepted"])
+ONLY_TYPE = dict(fk_rope=["q"], fk_tree_attn=["q"], fk_paged_tree_attn=["q"], fk_verify_drafts=["target", "q_start"], fk_commit_drafts=["k_tree"], fk_paged_commit_drafts=["k_tree"])
+
+
+@pytest.mark.parametrize("name", sorted(SHORT))
+def test_buffers_of_another_type_or_too_few_are_refused(fklib, name, monkeypatch):
+    """What torch gives by itself - tokens and positions in 64 bits, probabilities in bf16 - and rows too few are named, not misread."""
+    import torch
+    import paper_2602_03203_amd as F
+    reached = []
+    monkeypatch.setattr(fklib, "_call", lambda call, *args: reached.append(call))
+    _wrapped(F, name, {})
+    assert reached == [name]
+    other = {torch.int32: torch.int64, torch.float32: torch.bfloat16, torch.bfloat16: torch.float16}
+    for what in SHORT[name] + ONLY_TYPE[name]:
+        with pytest.raises(AssertionError, match="not torch"):
+            _wrapped(F, name, {what: lambda x: x.to(other[x.dtype])})
+    for what in SHORT[name]:
+        with pytest.raises(AssertionError, match="not"):
+            _wrapped(F, name, {what: lambda x: x[:-1].contiguous()})
+    assert reached == [name]
