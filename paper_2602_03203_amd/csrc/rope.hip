@@ -178,9 +178,8 @@ extern "C" fk_status fk_rope(const fk_rope_desc* d, const void* q, const void* k
     if ((P.q_stride | P.qo_stride | P.k_stride | P.ko_stride) * es % 16) return FK_ERR_INVALID_ARG;
     if (n_tokens > 0 && (!pos || !freq || (d->n_q_heads && (!q || !q_out)) || (d->n_kv_heads && (!k || !k_out)))) return FK_ERR_INVALID_ARG;
     if (!aligned16(q) || !aligned16(k) || !aligned16(q_out) || !aligned16(k_out) || (reinterpret_cast<uintptr_t>(freq) & 7)) return FK_ERR_INVALID_ARG;
-    if ((q == q_out && P.q_stride != P.qo_stride) || (k == k_out && P.k_stride != P.ko_stride)) {
-        if ((q && q == q_out && d->n_q_heads) || (k && k == k_out && d->n_kv_heads)) return FK_ERR_INVALID_ARG;
-    }
+    if (d->n_q_heads && q && q == q_out && P.q_stride != P.qo_stride) return FK_ERR_INVALID_ARG;
+    if (d->n_kv_heads && k && k == k_out && P.k_stride != P.ko_stride) return FK_ERR_INVALID_ARG;
     if (n_tokens == 0) return FK_OK;
     P.q = q;
     P.k = k;

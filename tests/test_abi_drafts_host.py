@@ -40,6 +40,16 @@ def test_rope(fklib, change, code):
     assert fklib.lib().fk_rope(None, p, p, p, p, 0, p, p, 0) == INVALID
 
 
+def test_strides_in_place_are_each_tensors_own(fklib):
+    """Strides of heads that a call has none of do not matter; of those it has, each in place keeps its own."""
+    L, F = fklib.lib(), fklib
+    assert rope(L, F, n_q_heads=0, q=0, qo=0, q_stride=128) == 0 and rope(L, F, n_q_heads=0, q_out_stride=128) == 0     # keys in place, no queries
+    assert rope(L, F, n_kv_heads=0, k=0, ko=0, k_stride=128) == 0 and rope(L, F, n_kv_heads=0, k_out_stride=128) == 0   # the other way round
+    assert rope(L, F, q_stride=2048, qo=2 * p) == 0 and rope(L, F, k_stride=2048, ko=2 * p) == 0                        # keys in place, queries elsewhere
+    assert rope(L, F, q_stride=2048) == INVALID and rope(L, F, k_out_stride=2048) == INVALID
+    assert rope(L, F, q_stride=2048, q_out_stride=2048, k_stride=512, k_out_stride=512) == 0
+
+
 def test_frequencies(fklib):
     import paper_2602_03203_amd as fk
     r, base = 128, 1e6
