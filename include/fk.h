@@ -479,8 +479,9 @@ fk_status fk_rope_frequencies(int32_t rotary_dim, double base, int32_t scaling, 
  * [n_tokens][n_q_heads][2] fp32, M and L.  Logits of -inf alone give zeros and (-inf, 0); a query that is no number, or meets one, has L = NaN.  Values of
  * pairs that a node does not see, infinities and NaN among them, do not reach its results.  fp32 accumulation; bf16: a weight meets V as two bf16 terms, off
  * by 2^-15 of it at most, L is the sum of the unrounded ones.  max_tree <= FK_TREE_NODES bounds the trees' nodes and max_len every len[r]; they only
- * size the launch, results are right beyond them too.  workspace: fk_tree_attn_workspace bytes for the same sizes, zero-filled ONCE by the caller; every call leaves its
- * counters at zero again, and calls of any sizes (of fk_paged_tree_attn too) may take turns with one that is large enough for each; calls sharing it must not
+ * size the launch, results are right beyond them too.  workspace: fk_tree_attn_workspace bytes for these sizes or larger ones (what serves a call serves every call of
+ * the descriptor with as many tokens or fewer and such bounds or lower ones), zero-filled ONCE by the caller; every call leaves its counters at zero again, and
+ * calls of any sizes (of fk_paged_tree_attn too) may take turns with one that is large enough for each; calls sharing it must not
  * overlap in time.  One launch; the order of all sums is fixed: equal calls give equal bits.  FK_ERR_UNSUPPORTED: n_tokens * n_q_heads >= 2^28, n_kv_heads >= 2^16.
  */
 size_t fk_tree_attn_workspace(const fk_cache_desc *desc, int32_t n_tokens, int32_t max_tree, int32_t max_len);

@@ -540,7 +540,7 @@ def fk_tree_attn_workspace(desc: CacheDesc, n_tokens: int, max_tree: int, max_le
 
 
 def new_tree_attn_workspace(desc: CacheDesc, n_tokens: int, max_tree: int, max_len: int) -> "torch.Tensor":
-    """Zero-filled device workspace (its counters must start at zero); it serves calls with fewer tokens, smaller bounds too."""
+    """Zero-filled device workspace (its counters must start at zero); it serves the desc's calls with fewer tokens and lower bounds too."""
     return torch.zeros(max(fk_tree_attn_workspace(desc, n_tokens, max_tree, max_len), 16), dtype=torch.uint8, device="cuda")
 
 
@@ -561,7 +561,7 @@ def fk_paged_tree_attn_workspace(desc: PagedDesc, n_tokens: int, max_tree: int, 
 
 
 def new_paged_tree_attn_workspace(desc: PagedDesc, n_tokens: int, max_tree: int, max_len: int) -> "torch.Tensor":
-    """Zero-filled device workspace (its counters must start at zero); it serves calls with fewer tokens, smaller bounds too."""
+    """Zero-filled device workspace (its counters must start at zero); it serves the desc's calls with fewer tokens and lower bounds too."""
     return torch.zeros(max(fk_paged_tree_attn_workspace(desc, n_tokens, max_tree, max_len), 16), dtype=torch.uint8, device="cuda")
 
 

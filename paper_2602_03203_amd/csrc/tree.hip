@@ -39,7 +39,8 @@ static long long items_of(const fk_paged_desc* d, const TileGrid& G) { return (l
 // items of 64 rows: whole 100, in two 68, three 61, four 53, five 67; up to 256 rows of 2112, 256 items of 128: 76, 62, 81, 77).  Sequences in pages differ in
 // length as a rule, which only the device knows: up to twice as many splits, of 512 pairs and more, even them out (16 sequences of 1024 to 16384 pairs, 8 heads: 16 rows
 // in four 127, eight 113; 32 rows 133 and 121; up to 96 rows 159 and 152).
-static int tree_splits(const fk_paged_desc* d, int kind, long long items, long long pairs, bool uneven, double& least) {
+// bound: the most splits of which rounding can make the estimate choose, for fewer pairs too (a split more costs records and saves turns: more pairs, more splits).
+static int tree_splits(const fk_paged_desc* d, int kind, long long items, long long pairs, bool uneven, double& least, bool bound = false) {
     const long long most = std::min((long long)kMostTreeSplits, pairs >> (uneven ? 9 : 8)), places = uneven ? 1024 : 512;
     const bool bf16 = d->dtype == FK_BF16;
     least = 0;
@@ -47,13 +48,20 @@ static int tree_splits(const fk_paged_desc* d, int kind, long long items, long l
     const double wide = kind == 8 ? 2. : 1., turn[3] = {wide, wide * 1.3, wide * 1.6};   // (of as many pairs as take 0.75 us alone with 64 rows)
     const int held = kind == 8 ? 2 : 3;   // workgroups that a CU holds
     const double turns = (double)pairs / (kind == 8 ? 64 : 32) * d->head_dim / 128 * (kind == 8 ? 1. : .75) * (bf16 ? 1. : 4.);
-    int best = 1;
-    for (int s = 1; s == 1 || (s <= most && items <= kSplitItems && items * s * kind <= 1 << 15 /* a quarter of a GiB of records */); ++s) {
+    auto allowed = [&](int s) { return s == 1 || (s <= most && items <= kSplitItems && items * s * kind <= 1 << 15 /* a quarter of a GiB of records */); };
+    auto time_of = [&](int s) {
         const long long per_cu = (items * s + 255) / 256, rest = per_cu % held;
         const double rounds = (double)(per_cu / held) * turn[held - 1] + (rest ? turn[rest - 1] : 0.);
-        const double time = rounds * turns / s + (s == 1 ? 0. : 3 + (double)items * s * 16 * kind * d->head_dim * 8 / 4e6);
+        return rounds * turns / s + (s == 1 ? 0. : 3 + (double)items * s * 16 * kind * d->head_dim * 8 / 4e6);
+    };
+    int best = 1;
+    for (int s = 1; allowed(s); ++s) {
+        const double time = time_of(s);
         if (s == 1 || time < least) least = time, best = s;
     }
+    if (bound)
+        for (int s = best + 1; allowed(s); ++s)
+            if (time_of(s) <= least * (1 + 1e-9)) best = s;
     if (uneven && items <= kSplitItems / 2) best = (int)std::max((long long)best, std::min(most, places / items));
     return best;
 }
@@ -81,13 +89,40 @@ static TreePlan tree_plan(const fk_paged_desc* d, int32_t n_tokens, int32_t max_
 }
 // workspace: counters, the same for every call (so that calls of any sizes may take turns with one workspace) | sums and references of records | records
 static constexpr size_t kCounterBytes = kSplitItems * 4 * sizeof(uint32_t);
-static size_t ml_bytes(const TreePlan& p, long long items) {   // wide: 16 bytes a lane and 16 rows; 8 a row
-    return p.splits > 1 ? up256((size_t)items * p.splits * 16 * p.kind * (p.kind >= 4 ? 64 : 8)) : 0;
+static size_t ml_bytes(int kind, long long items, int splits) {   // wide: 16 bytes a lane and 16 rows; 8 a row
+    return splits > 1 ? up256((size_t)items * splits * 16 * kind * (kind >= 4 ? 64 : 8)) : 0;
 }
+static size_t need_of(const fk_paged_desc* d, int kind, long long items, int splits) {
+    return kCounterBytes + ml_bytes(kind, items, splits) + (splits > 1 ? (size_t)items * splits * 16 * kind * d->head_dim * sizeof(float) : 0);
+}
+static size_t need_of(const fk_paged_desc* d, const TreePlan& p) { return need_of(d, p.kind, items_of(d, p.grid), p.splits); }
+// The most that a call of these sizes or smaller ones needs - fewer items are split more often, and go to other kernels: every kind and number of places that
+// tree_plan and tile_grid can come to.
 static size_t tree_workspace(const fk_paged_desc* d, int32_t n_tokens, int32_t max_tree, int32_t max_len, bool uneven) {
-    const TreePlan p = tree_plan(d, std::max(n_tokens, 1), max_tree, max_len, uneven);
-    const long long items = items_of(d, p.grid);
-    return kCounterBytes + ml_bytes(p, items) + (p.splits > 1 ? (size_t)items * p.splits * 16 * p.kind * d->head_dim * sizeof(float) : 0);
+    const long long g = d->n_q_heads / d->n_kv_heads, tokens = std::max(n_tokens, 1), tree = std::min<long long>(std::min<long long>(max_tree, tokens), kTreeNodes), rows = tree * g;
+    size_t most = kCounterBytes;
+    auto look = [&](int kind, long long least_rows, long long most_rows) {   // the kind takes trees of more than least_rows query rows, up to most_rows
+        if (rows <= least_rows) return;
+        const long long tm = 16 * kind, per_seq = (std::min(rows, most_rows) + tm - 1) / tm, spread = tokens * g / tm + d->batch;
+        auto with = [&](long long places) {
+            double t;
+            const long long items = places * d->n_kv_heads;
+            most = std::max(most, need_of(d, kind, items, tree_splits(d, kind, items, max_len + tree, uneven, t, true)));
+        };
+        for (long long i = 1; i <= per_seq && i * d->batch <= 2 * spread && i * d->batch * d->n_kv_heads <= kSplitItems; ++i) with(i * d->batch);
+        for (long long x = d->batch; x <= spread && 2 * x < per_seq * d->batch && x * d->n_kv_heads <= kSplitItems; ++x) with(x);
+    };
+    const long long all = kTreeNodes * g;
+    if (d->dtype == FK_F32) {
+        look(1, 0, 64);
+        look(4, 64, all);
+    } else {
+        look(1, 0, 16);
+        look(2, 16, 32);
+        look(4, 32, all);
+        look(8, 64, all);
+    }
+    return most;
 }
 
 template <typename T, int D, int KIND, bool ROWS, bool ONCE> static fk_status tree_start(const TreeParams& P, hipStream_t st) {
@@ -115,7 +150,7 @@ template <bool ROWS> static fk_status tree_launch(const fk_paged_desc* d, const 
     A.split_shift = p.shift;
     P.here = static_cast<uint32_t*>(ws);
     A.rec_ml = reinterpret_cast<float2*>(static_cast<char*>(ws) + kCounterBytes);
-    A.rec = reinterpret_cast<float*>(static_cast<char*>(ws) + kCounterBytes + ml_bytes(p, items_of(d, p.grid)));
+    A.rec = reinterpret_cast<float*>(static_cast<char*>(ws) + kCounterBytes + ml_bytes(p.kind, items_of(d, p.grid), p.splits));
     if (d->dtype == FK_F32) return d->head_dim == 64 ? tree_rows_of<float, 64, ROWS>(p.kind, P, st) : tree_rows_of<float, 128, ROWS>(p.kind, P, st);
     return d->head_dim == 64 ? tree_rows_of<bf16_t, 64, ROWS>(p.kind, P, st) : tree_rows_of<bf16_t, 128, ROWS>(p.kind, P, st);
 }
@@ -170,7 +205,8 @@ extern "C" fk_status fk_tree_attn(const fk_cache_desc* desc, const void* q, cons
     const fk_paged_desc d = as_paged(desc);
     s = check_trees(&d, q, K, V, len, k_tree, v_tree, parent, q_start, n_tokens, max_tree, out, stats);
     if (s != FK_OK) return s;
-    if (!workspace || workspace_bytes < fk_tree_attn_workspace(desc, n_tokens, max_tree, max_len) || !aligned16(workspace)) return FK_ERR_WORKSPACE;
+    const TreePlan plan = tree_plan(&d, std::max(n_tokens, 1), max_tree, max_len, false);
+    if (!workspace || workspace_bytes < need_of(&d, plan) || !aligned16(workspace)) return FK_ERR_WORKSPACE;
     if (n_tokens == 0) return FK_OK;
     TreeParams P = {};
     P.a.view = paged_params(&d, nullptr, len, q_start, n_tokens);
@@ -185,7 +221,7 @@ extern "C" fk_status fk_tree_attn(const fk_cache_desc* desc, const void* q, cons
     P.parent = parent;
     P.k_tree = k_tree;
     P.v_tree = v_tree;
-    return tree_launch<true>(&d, tree_plan(&d, n_tokens, max_tree, max_len, false), P, workspace, (hipStream_t)stream);
+    return tree_launch<true>(&d, plan, P, workspace, (hipStream_t)stream);
 }
 
 static fk_status check_pages(const fk_paged_desc* desc, int32_t n_tokens, int32_t max_tree, int32_t max_len) {
@@ -209,7 +245,8 @@ extern "C" fk_status fk_paged_tree_attn(const fk_paged_desc* desc, const void* q
     if (s == FK_OK) s = check_trees(desc, q, K, V, kv_len, k_tree, v_tree, parent, q_start, n_tokens, max_tree, out, stats);
     if (s != FK_OK) return s;
     if (!page_table || window < 0 || n_sink < 0) return FK_ERR_INVALID_ARG;
-    if (!workspace || workspace_bytes < fk_paged_tree_attn_workspace(desc, n_tokens, max_tree, max_len) || !aligned16(workspace)) return FK_ERR_WORKSPACE;
+    const TreePlan plan = tree_plan(desc, std::max(n_tokens, 1), max_tree, max_len, desc->batch > 1);
+    if (!workspace || workspace_bytes < need_of(desc, plan) || !aligned16(workspace)) return FK_ERR_WORKSPACE;
     if (n_tokens == 0) return FK_OK;
     TreeParams P = {};
     P.a.view = paged_params(desc, page_table, kv_len, q_start, n_tokens);
@@ -224,5 +261,5 @@ extern "C" fk_status fk_paged_tree_attn(const fk_paged_desc* desc, const void* q
     P.parent = parent;
     P.k_tree = k_tree;
     P.v_tree = v_tree;
-    return tree_launch<false>(desc, tree_plan(desc, n_tokens, max_tree, max_len, desc->batch > 1), P, workspace, (hipStream_t)stream);
+    return tree_launch<false>(desc, plan, P, workspace, (hipStream_t)stream);
 }

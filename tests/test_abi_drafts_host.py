@@ -123,6 +123,29 @@ def test_workspaces_of_trees(fklib):
     assert none["rows"] == none["pages"] == 0   # no tokens: nothing to do
 
 
+@pytest.mark.parametrize("batch, g, hkv, D, dtype", [(16, 4, 8, 128, "bf16"), (16, 7, 4, 64, "bf16"), (1, 8, 1, 128, "bf16"), (64, 1, 1, 128, "bf16"), (5, 3, 2, 64, "f32"), (90, 4, 1, 128, "f32"),
+                                                     (3, 5, 40, 128, "bf16"), (200, 2, 8, 64, "bf16")])
+def test_a_workspace_serves_smaller_calls(fklib, batch, g, hkv, D, dtype):
+    """Fewer tiles are split more often and go to other kernels: what serves a call serves every one with fewer tokens, smaller trees, shorter rows."""
+    import random
+    rng = random.Random(batch)
+    rows, pages = fklib.CacheDesc(batch, g * hkv, hkv, D, 40000, dtype), fklib.PagedDesc(batch, g * hkv, hkv, D, 64, 1000, 625, dtype)
+    log = lambda lo, hi: int(round(lo * (hi / lo) ** rng.random()))   # noqa: E731
+    for size, desc in ((fklib.fk_tree_attn_workspace, rows), (fklib.fk_paged_tree_attn_workspace, pages)):
+        needs = {}
+        for _ in range(12):
+            tree = log(1, 256)
+            n, length = log(tree, tree * batch), log(1, 40000)
+            whole = size(desc, n, tree, length)
+            for _ in range(120):
+                t, m, k = log(1, tree), log(1, n), log(1, length)
+                needs[m, t, k] = size(desc, m, t, k)
+                assert needs[m, t, k] <= whole, f"{(m, t, k)} needs {needs[m, t, k]}, {(n, tree, length)} has {whole}"
+        assert len(set(needs.values())) > 3 or batch * hkv > 1024   # (sizes do differ, but where so many tiles are never split)
+    if (batch, g, hkv, D, dtype) == (16, 4, 8, 128, "bf16"):
+        assert fklib.fk_tree_attn_workspace(rows, 4096, 256, 4096) >= fklib.fk_tree_attn_workspace(rows, 1024, 64, 4096) > 1 << 20
+
+
 def verify(F, **other):
     a = dict(batch=2, vocab=1000, target=p, draft=p, tokens=p, parent=p, q_start=p, n=8, uniform=p, path=p, accepted=p, next=p, ws=p, bytes=0)
     a.update(other)

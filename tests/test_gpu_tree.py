@@ -318,3 +318,38 @@ def test_infinite_values_of_equal_weights(D, g, nodes, page):
     c.run(s)
     torch.cuda.synchronize()
     c.check(s, *ref)
+
+
+@pytest.mark.parametrize("dtype, D, page", [("bf16", 128, 0), ("bf16", 64, 64), ("f32", 64, 0)])
+def test_one_workspace_for_smaller_calls(dtype, D, page):
+    """Allocated once for the largest trees, which split nothing, it serves smaller ones, which do: the same bits as with a workspace of their own."""
+    import paper_2602_03203_amd as fk
+    B, H, g, cap = 16, 8, 4, 2048
+    dt = torch.float32 if dtype == "f32" else torch.bfloat16
+    gen = torch.Generator(device="cuda").manual_seed(D)
+    r = lambda *s: torch.randn(s, generator=gen, device="cuda").to(dt)   # noqa: E731
+    i32 = dict(dtype=torch.int32, device="cuda")
+    K, V = (r(B * cap // page, H, page, D) if page else r(B, H, cap, D) for _ in range(2))
+    if page:
+        desc, size = fk.PagedDesc(B, H * g, H, D, page, K.shape[0], cap // page, dtype), fk.fk_paged_tree_attn_workspace
+        where = (torch.arange(K.shape[0], **i32).reshape(B, -1), torch.full((B,), cap, **i32))
+    else:
+        desc, size, where = fk.CacheDesc(B, H * g, H, D, cap, dtype), fk.fk_tree_attn_workspace, (torch.full((B, H), cap, **i32),)
+    most = torch.zeros(size(desc, B * 256, 256, cap), dtype=torch.uint8, device="cuda")
+    for nodes, max_len in ((64, cap), (256, cap), (8, cap), (30, cap), (1, 1200), (16, cap), (100, cap)):
+        n = B * nodes
+        parent = torch.tensor([p for b in range(B) for p in tree(nodes, b)], **i32)
+        q_start = torch.arange(0, n + 1, nodes, **i32)
+        q, kt, vt = r(n, H * g, D), r(n, H, D), r(n, H, D)
+        outs = []
+        for ws in (most, torch.zeros(size(desc, n, nodes, max_len), dtype=torch.uint8, device="cuda")):
+            out, stats = torch.full_like(q, 7), torch.full((n, H * g, 2), 7.0, device="cuda")
+            tail = (out, stats, ws)
+            if page:
+                fk.fk_paged_tree_attn(desc, q, K, V, *where, kt, vt, parent, q_start, nodes, max_len, 0, 0, D ** -0.5, *tail)
+            else:
+                fk.fk_tree_attn(desc, q, K, V, *where, kt, vt, parent, q_start, nodes, max_len, D ** -0.5, *tail)
+            outs.append((out, stats))
+        torch.cuda.synchronize()
+        assert torch.equal(outs[0][0], outs[1][0]) and torch.equal(outs[0][1], outs[1][1]) and torch.isfinite(outs[0][1]).all(), f"{nodes} nodes"
+    assert not most[:16384].any()   # the counters are at zero again
