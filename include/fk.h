@@ -430,9 +430,9 @@ fk_status fk_paged_compress(const fk_paged_desc *desc, const void *K, const void
  * accepted joins the cache: a budgeted cache must not hold, score or evict for pairs that are thrown away again.  The trees of a call are packed:
  *   q_start [batch + 1] int32   tokens q_start[b] .. q_start[b + 1] - 1 of the call are sequence b's tree (of 0 to FK_TREE_NODES nodes), ascending
  *   parent  [n_tokens] int32    a node's parent, counted from the tree's first node and lower than its own place; others, -1 by custom, stand for none
- * Node 0 is the root: the last token of the sequence, whose pair is not in the cache yet.  A sequence whose tree has more than FK_TREE_NODES nodes is passed
- * over: nothing of it is written, and fk_verify_drafts accepts nothing.  The round of a layer: fk_rope, fk_tree_attn; of the model: fk_verify_drafts; of every
- * layer then: fk_commit_drafts.
+ * Node 0 is the root: the last token of the sequence, whose pair is not in the cache yet.  A tree of more than FK_TREE_NODES nodes is passed over by the attention,
+ * which writes nothing of it, and by fk_verify_drafts, which accepts nothing; the commits take a path's pairs out of any number of nodes.  The round of a layer:
+ * fk_rope, fk_tree_attn; of the model: fk_verify_drafts; of every layer then: fk_commit_drafts.
  */
 #define FK_TREE_NODES 256
 

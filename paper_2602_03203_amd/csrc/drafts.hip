@@ -443,8 +443,8 @@ __global__ __launch_bounds__(256) void commit_rows_kernel(const CommitParams P) 
     const int n = s_count;
     const du32x4_t *k = reinterpret_cast<const du32x4_t*>(P.k_tree), *v = reinterpret_cast<const du32x4_t*>(P.v_tree);
     du32x4_t *K = reinterpret_cast<du32x4_t*>(P.K), *V = reinterpret_cast<du32x4_t*>(P.V);
-    for (int x = tid; x < n * CH; x += 256) {
-        const int i = x / CH, c = x % CH;
+    const int c = tid % CH;
+    for (int i = tid / CH; i < n; i += 256 / CH) {
         const size_t from = ((size_t)(begin + P.path[begin + i]) * P.n_kv + h) * CH + c, to = ((size_t)row * P.cap + start + i) * CH + c;
         K[to] = k[from];
         V[to] = v[from];
@@ -471,8 +471,13 @@ __global__ __launch_bounds__(1024) void commit_pages_kernel(const CommitParams P
     const int n = s_count, row = P.n_kv * CH;
     const du32x4_t *k = reinterpret_cast<const du32x4_t*>(P.k_tree), *v = reinterpret_cast<const du32x4_t*>(P.v_tree);
     du32x4_t *K = reinterpret_cast<du32x4_t*>(P.K), *V = reinterpret_cast<du32x4_t*>(P.V);
-    for (int x = tid; x < n * row; x += 1024) {
-        const int i = x / row, hc = x - i * row, h = hc / CH, p = start + i;
+    // pair i of the path, 16 bytes hc of all its heads (together more than 32 bits count)
+    for (int i = tid / row, hc = tid % row; i < n; i += 1024 / row, hc += 1024 % row) {
+        if (hc >= row) {
+            hc -= row;
+            if (++i >= n) break;
+        }
+        const int h = hc / CH, p = start + i;
         const int page = P.table[(size_t)b * P.max_pages + (p >> P.page_shift)];
         if ((unsigned)page >= (unsigned)P.n_pages) continue;
         const size_t from = (size_t)(begin + P.path[begin + i]) * row + hc;

@@ -113,6 +113,24 @@ def test_many_rows():
     assert torch.equal(K[:, :, 1], kt) and (ln == 2).all() and torch.equal(pos[:, 0, 1], q_start[:B]) and (K[:, :, 0] == 0).all()
 
 
+def test_paths_of_more_than_32_bits_of_chunks():
+    """Commits take paths of any length: 4097 nodes of 65535 heads are more 16-byte chunks than 32 bits count.  All places but the last lie in holes."""
+    import paper_2602_03203_amd as fk
+    n, H, D, page = 4097, 65535, 64, 16
+    i32 = dict(dtype=torch.int32, device="cuda")
+    kt = torch.empty((n, H, D), dtype=torch.bfloat16, device="cuda")
+    kt[-1] = torch.randn((H, D), device="cuda").bfloat16()
+    K, V = (torch.zeros((1, H, page, D), dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    table = torch.full((1, n // page + 1), -1, **i32)
+    table[0, -1] = 0
+    length = torch.zeros(1, **i32)
+    fk.fk_paged_commit_drafts(fk.PagedDesc(1, H, H, D, page, 1, n // page + 1, "bf16"), K, V, table, length, kt, kt, torch.tensor([0, n], **i32), torch.full((n,), n - 1, **i32),
+                              torch.tensor([n], **i32))
+    assert length.item() == n
+    for x in (K, V):
+        assert torch.equal(x[0, :, 0], kt[-1]) and not x[0, :, 1:].any()
+
+
 @pytest.mark.parametrize("dtype, D", [("bf16", 128), ("f32", 64), ("bf16", 64)])
 def test_a_round_is_the_steps_of_its_tokens(dtype, D):
     """Two rounds of drafts: positions, attention, verification, commit.  The cache holds what decode steps of the accepted tokens would have left, and the path's
