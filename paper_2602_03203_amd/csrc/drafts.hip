@@ -24,11 +24,11 @@ static constexpr int kNodes = FK_TREE_NODES;
 // workgroup may not have begun) is formed by whoever misses it, in the same order, so that it is the same bits.
 // A sum on its way is two words of 32 bits of it and the call's number each: one that holds another number is not there yet.
 // Bound by latencies, one after the other: sequence, nodes, their probabilities, the row, the others' sums, the chunk's numbers (16 chains of 4 drafted tokens, 32000
-// numbers: 11.6 us), and another 3 us for every further sum (16 trees of 17 to 33 nodes, 131072 numbers: 24 us; one workgroup alone, which then
-// summed whole rows, took 234).
+// numbers: 11.2 us), and another 3 us for every further sum (16 trees of 17 to 33 nodes, 131072 numbers: 25 us; one workgroup alone, which then
+// summed whole rows, took 234; 4 nodes with 200 children each, all rejected: 0.6 ms, and 10.7 while the first 32 sums alone were told).
 // ---------------------------------------------------------------------------------------
 static constexpr int kVerifyThreads = 256, kVerifyWaves = kVerifyThreads / kWave, kMostChunks = 64;
-static constexpr int kRounds = 32;         // sums of a call that are told; more, everybody forms alone
+static constexpr int kRounds = kNodes + 1; // sums of a sequence: one for every rejected node, the last token's, and the target's own where nothing is left
 static constexpr int kPatience = 64;       // looks at a sum that is not there, 0.5 us and more each
 
 struct VerifyParams {
@@ -285,14 +285,14 @@ __global__ __launch_bounds__(kVerifyThreads) void verify_kernel(const VerifyPara
         // the sums of what is left at T.at, chunk by chunk
         sum_chunk(P, T, begin, chunk);
         if (P.chunks > 1) {
-            unsigned long long* told = P.told + ((size_t)b * kRounds + min(round, kRounds - 1)) * P.chunks * 2;
+            unsigned long long* told = P.told + ((size_t)b * kRounds + round) * P.chunks * 2;
             if (wave == 0) {
-                if (round < kRounds && lane < 2) {
+                if (lane < 2) {
                     const uint64_t bits = (uint64_t)__double_as_longlong(T.part[chunk]);
                     __hip_atomic_store(told + chunk * 2 + lane, (unsigned long long)call << 32 | (uint32_t)(bits >> (32 * lane)), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
                 }
                 bool here = lane >= P.chunks || lane == chunk;
-                for (int look = 0; round < kRounds && look < kPatience; ++look) {
+                for (int look = 0; look < kPatience; ++look) {
                     if (!here) {
                         const unsigned long long lo = __hip_atomic_load(told + lane * 2, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
                         const unsigned long long hi = __hip_atomic_load(told + lane * 2 + 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);

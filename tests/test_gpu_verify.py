@@ -228,3 +228,33 @@ def test_draft_rows_that_play_no_part(vocab):
         path, count, following = c.reference()
         assert count[3] == 4 and count[4] == 1 and (following >= 0).all()
         c.go(f"u {u}")
+
+
+@pytest.mark.parametrize("vocab", [700, 5003, 40001])
+def test_many_rejections_before_an_acceptance(vocab):
+    """Sixty different children of the root, then two hundred, are rejected before one is accepted or none is: c and m, carried from sum to sum, decide about each one behind them."""
+    rng = np.random.default_rng(vocab)
+    wide = [60, 200, 60, 200, 60, 200]
+    c = Trees([[-1] + [0] * (n + 20) for n in wide], vocab, True, seed=vocab)
+    c.uniform[:] = rng.random(c.n)
+    for b, n in enumerate(wide):
+        s = int(c.q_start[b])
+        picked = rng.permutation(vocab)[:n + 20]
+        likely, others = picked[:n], picked[n:]   # the draft likes the first ones far better than the target, the others a little
+        p, q = rng.dirichlet(np.ones(vocab)), rng.random(vocab)
+        share = 0.9 / n
+        p[likely] = 0.1 * share * rng.random(n)
+        p /= p.sum()
+        q = p * np.exp(2 * rng.standard_normal(vocab)) * 0.7 / n
+        q[likely] = share
+        c.target[s], c.draft[s] = p, q / q.sum()
+        c.tokens[s + 1:s + 1 + n], c.tokens[s + 1 + n:s + 21 + n] = likely, others
+        c.uniform[s + 1:s + 1 + n] = 0.9 + 0.09 * rng.random(n)
+        if b >= 4:
+            c.target[s, others] = 0   # nobody is accepted
+    path, count, _ = c.reference()
+    rejected = [int(path[s + 1]) - 1 if k > 1 else n + 20 for s, k, n in zip(c.q_start, count, wide)]
+    assert min(rejected[::2]) >= 60 and min(rejected[1::2]) >= 200 and 2 in count and (count[4:] == 1).all() and max(r - n for r, n in zip(rejected[:4], wide)) > 0, rejected
+    d = c.go()
+    if vocab > 4096:   # every workgroup's sums of every rejection are told, two words each, and none is formed by everybody again
+        assert int(d[9][256:].view(torch.int64).count_nonzero()) >= 2 * 2 * sum(rejected)
