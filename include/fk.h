@@ -512,8 +512,8 @@ fk_status fk_paged_tree_attn(const fk_paged_desc *desc, const void *q, const voi
  * count as 0; a token outside [0, vocab) has probability 0 in both.  Sums and comparisons are in fp64, sums in a fixed order: equal calls give equal tokens.
  * path [n_tokens]: the accepted nodes of sequence b, the root first, from q_start[b] on, then -1; n_accepted [batch]: how many, the root among them (0 without
  * a tree); next_token [batch] (-1 without one).
- * workspace: fk_verify_drafts_workspace bytes, zero-filled ONCE by the caller and from then on only handed to this call; it may serve calls of any sizes that it
- * is large enough for.  Calls sharing it must not overlap in time.  batch <= 65535, vocab < 2^30 (FK_ERR_UNSUPPORTED beyond).  One launch.
+ * workspace: fk_verify_drafts_workspace bytes for these sizes or larger ones, zero-filled ONCE by the caller and from then on only handed to this call, of any
+ * sizes that it is large enough for.  Calls sharing it must not overlap in time.  batch <= 65535, vocab < 2^30 (FK_ERR_UNSUPPORTED beyond).  One launch.
  */
 size_t fk_verify_drafts_workspace(int32_t batch, int32_t vocab);
 fk_status fk_verify_drafts(int32_t batch, int32_t vocab, const float *target, const float *draft, const int32_t *tokens, const int32_t *parent,

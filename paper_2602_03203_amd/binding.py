@@ -582,7 +582,7 @@ def fk_verify_drafts_workspace(batch: int, vocab: int) -> int:
 
 
 def new_verify_workspace(batch: int, vocab: int) -> "torch.Tensor":
-    """Zero-filled device workspace for fk_verify_drafts (its counters must start at zero)."""
+    """Zero-filled device workspace for fk_verify_drafts (its counters must start at zero); it serves smaller batches and vocabularies too."""
     return torch.zeros(max(fk_verify_drafts_workspace(batch, vocab), 16), dtype=torch.uint8, device="cuda")
 
 

@@ -497,8 +497,9 @@ using namespace fk;
 
 extern "C" size_t fk_verify_drafts_workspace(int32_t batch, int32_t vocab) {
     if (batch <= 0 || vocab <= 0 || batch > 65535) return 0;
-    const int chunks = verify_chunks(batch, vocab);
-    return 256 + (chunks > 1 ? (size_t)batch * kRounds * chunks * 2 * sizeof(unsigned long long) : 0);
+    // (a smaller batch has more chunks: the most workgroups of as many sequences or fewer)
+    const int chunks = std::min(vocab / 2048, kMostChunks);
+    return 256 + (chunks > 1 ? (size_t)std::min<int64_t>(512, (int64_t)batch * chunks) * kRounds * 2 * sizeof(unsigned long long) : 0);
 }
 
 extern "C" fk_status fk_verify_drafts(int32_t batch, int32_t vocab, const float* target, const float* draft, const int32_t* tokens,

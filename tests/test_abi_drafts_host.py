@@ -164,6 +164,16 @@ def test_verify(fklib, change, code):
     assert fklib.lib().fk_verify_drafts_workspace(0, 1000) == 0 and fklib.lib().fk_verify_drafts_workspace(2, 0) == 0
 
 
+def test_a_workspace_of_verification_serves_smaller_calls(fklib):
+    """Fewer sequences are cut into more chunks."""
+    size = fklib.fk_verify_drafts_workspace
+    for batch in (1, 2, 7, 16, 64, 255, 256, 257, 512, 513, 65535):
+        for vocab in (1, 2048, 4095, 4096, 32000, 131072, (1 << 30) - 1):
+            whole = size(batch, vocab)
+            assert all(size(b, v) <= whole for b in (1, 3, 8, 100, 256, 500, batch) for v in (5, 4096, 50257, 131072, vocab) if b <= batch and v <= vocab), (batch, vocab)
+    assert size(512, 131072) >= 256 + 512 * 16   # (eight sequences of 64 chunks at least have a place for a sum each)
+
+
 @pytest.mark.parametrize("change, code", [(dict(K=0), INVALID), (dict(V=0), INVALID), (dict(pos=0), INVALID), (dict(len=0), INVALID), (dict(kt=0), INVALID), (dict(vt=0), INVALID),
                                           (dict(q_start=0), INVALID), (dict(n=-1), INVALID), (dict(path=0), INVALID), (dict(accepted=0), INVALID), (dict(first=0), INVALID),
                                           (dict(table=0), INVALID), (dict(K=p + 8), INVALID), (dict(vt=p + 8), INVALID), (dict(head_dim=96), UNSUPPORTED), (dict(dtype=5), UNSUPPORTED),
