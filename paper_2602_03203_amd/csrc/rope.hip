@@ -31,6 +31,11 @@ template <typename T> __device__ __forceinline__ void store16(T* p, const float*
 __device__ __forceinline__ float load_in(const float* p) { return *p; }
 __device__ __forceinline__ float load_in(const bf16_t* p) { return __uint_as_float((uint32_t)*p << 16); }
 
+template <typename T> __device__ __forceinline__ T copy_of(uint32_t x) {   // what load_in's bits came from, a NaN's own ones among them
+    if constexpr (sizeof(T) == 2) return (T)(x >> 16);
+    else return __uint_as_float(x);
+}
+
 // VEC: whole 16-byte groups turn together; otherwise a thread turns one pair of channels or copies one channel.  A thread's units are two turns' loads ahead
 // of their stores.
 template <typename T, bool VEC, bool HALF>
@@ -103,7 +108,7 @@ __global__ __launch_bounds__(256) void rope_kernel(const RopeParams P) {
         } else {
             const float v = __uint_as_float(x.a.x);
             if (x.u >= turning) {
-                store_out(x.y + P.rot + x.u - turning, v);   // (exact: it comes from there)
+                x.y[P.rot + x.u - turning] = copy_of<T>(x.a.x);
                 return;
             }
             const float w = __uint_as_float(x.b.x);

@@ -178,3 +178,17 @@ def test_refused():
     with pytest.raises(fk.FkError):   # in place, but the outputs' tokens lie closer together
         wide = torch.randn((6, 8, 64), device="cuda")
         fk.fk_rope(desc, wide[:, :4], None, pos, freq, wide.view(-1)[:6 * 4 * 64].view(6, 4, 64), None)
+
+
+@pytest.mark.parametrize("rot, layout", [(50, "half"), (50, "interleaved"), (64, "half"), (6, "interleaved")])
+def test_channels_that_do_not_turn_keep_their_bits(rot, layout):
+    """Every bf16 there is, NaN of all kinds among them, behind the rotated channels: copied as they are, whatever the width of the loads."""
+    fk = _fk()
+    D, n = 128, 2 ** 16 // (128 - 64) + 1
+    k = torch.ones((n, 1, D), dtype=torch.bfloat16, device="cuda")
+    x = k.view(torch.int16)
+    x[..., rot:] = torch.arange(n * (D - rot), device="cuda").remainder(2 ** 16).sub(2 ** 15).to(torch.int16).reshape(n, 1, D - rot)
+    assert x[..., rot:].unique().numel() == 2 ** 16
+    out = torch.empty_like(k)
+    fk.fk_rope(fk.RopeDesc(0, 1, D, rot, layout, "bf16"), None, k, torch.arange(n, dtype=torch.int32, device="cuda"), fk.rope_frequencies(rot).cuda(), None, out)
+    assert torch.equal(out.view(torch.int16)[..., rot:], x[..., rot:])
