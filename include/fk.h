@@ -523,8 +523,8 @@ fk_status fk_verify_drafts(int32_t batch, int32_t vocab, const float *target, co
 /*
  * The accepted paths' pairs join the rows of a budgeted cache: slot len[r] + i of row r = (b, h) receives pair path[q_start[b] + i] of the tree - K, V, and
  * pos_first[b] + i into pos - for i < n_accepted[b], then len[r] goes up by as many.  A path ends at its first entry that is no node of the tree; a row takes as
- * many pairs as it has room for, the first ones.  acc (may be NULL): accumulated weights (fk_decode_step_acc), which start from zero in the new slots.  k_tree,
- * v_tree, path and n_accepted as above.  The pairs must not share memory with the cache.
+ * many pairs as it has room for, the first ones.  acc (may be NULL): accumulated weights (fk_decode_step_acc), which start from zero in the new slots and stay as they
+ * are in the others.  k_tree, v_tree, path and n_accepted as above.  The pairs must not share memory with the cache.
  */
 fk_status fk_commit_drafts(const fk_cache_desc *desc, void *K, void *V, int32_t *pos, int32_t *len, float *acc, const void *k_tree,
                            const void *v_tree, const int32_t *q_start, int32_t n_tokens, const int32_t *path, const int32_t *n_accepted,

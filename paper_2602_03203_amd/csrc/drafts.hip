@@ -402,7 +402,7 @@ __global__ __launch_bounds__(kVerifyThreads) void verify_kernel(const VerifyPara
 
 // ---------------------------------------------------------------------------------------
 // Commit: bound by the latency of a chain of loads (length, path, pair); every accepted pair is read and written once.  A workgroup owns a row, or all
-// heads of a sequence in pages: it alone reads and sets the length.  16 sequences, 8 heads, paths of up to 8 nodes: 3.4 us.
+// heads of a sequence in pages: it alone reads and sets the length.  16 sequences, 8 heads, paths of up to 8 nodes: 3.2 us.
 // ---------------------------------------------------------------------------------------
 typedef unsigned int du32x4_t __attribute__((ext_vector_type(4)));
 

@@ -4,8 +4,9 @@
 // positions have no fraction left in 32 bits (from 2^23 radians on), so they are formed in 64, in turns, and reduced to half a turn before
 // they become 32 bits (off by 2^-25 of a turn at most).  A workgroup takes a few tokens: sine and cosine once for every pair
 // of channels, in LDS, then all heads of these tokens pass by, 16 bytes a thread and load.
-// Bound by the memory system: every element is read and written once.  65000 tokens of 40 heads of 128 channels (1.33 GB) 245 to 253 us, 5.3 TB/s (a copy of 2 GiB 4.9);
-// 4096 tokens 15 us; 16 tokens 4.0, a launch and two loads one after the other.
+// Bound by the memory system: every element is read and written once.  65000 tokens of 40 heads of 128 channels (1.33 GB) 253 us, 5.3 TB/s (a copy of 2 GiB 4.9);
+// 4096 tokens 15 us; 16 tokens 3.8, a launch and two loads one after the other.  Where rotated channels are no whole 16-byte groups (50 of 128) a thread takes a pair of channels or
+// copies one, 2 or 4 bytes a load, bound by the number of its loads: 16384 tokens 177 us (interleaved 173), 66 where all 128 turn.
 #include "paged.h"
 
 #include <cmath>

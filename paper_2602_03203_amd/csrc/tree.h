@@ -23,7 +23,9 @@ static constexpr int kMostTreeSplits = 16;
 static constexpr int kSplitItems = 1024;   // a call with more items (a tile of rows, a KV head) splits none
 
 // Records of split tiles go from workgroup to workgroup by agent-scope relaxed atomics: loads and stores that pass the caches of the XCDs, which
-// costs nothing next to a fence that writes back and invalidates a whole L2.
+// costs nothing next to a fence that writes back and invalidates a whole L2.  None is needed for these words: a wavefront waits for its stores (vmcnt 0: they are where every
+// XCD sees them) before its workgroup's counter goes up, and the last one sends its loads when the counter's answer is there, for none of which a cache is asked.  That is an
+// order of gfx950's own, with the waits as they stand here; the language promises it for acquire and release alone.
 __device__ __forceinline__ void put2(float* p, float a, float b) {
     __hip_atomic_store(reinterpret_cast<uint64_t*>(p), (uint64_t)__float_as_uint(b) << 32 | __float_as_uint(a), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
@@ -40,8 +42,8 @@ __device__ __forceinline__ bool last_one(uint32_t* here, int splits) {
 
 // bf16: a weight meets V as two terms, the first cut off and the second the rest, rounded: 2^-15 of it off at most (one term is off by up to 2^-8, alike for equal weights,
 // which no average takes away).  Sums of weights are those of the unrounded ones.  The rest is taken 2^-20 too large, so that both terms of a weight above 0 (from 2^-106 on) are
-// above 0 and an infinity among the values stays one.  Up to 64 query rows cost 1 % by it (12 nodes for each of 16 sequences of 2112 pairs, 8 heads of g 4, D 128: 32.6 -> 32.9 us, of g 7
-// and 26 nodes 52 -> 56), 128 rows a fifth (64 nodes 60 -> 72).
+// above 0 and an infinity among the values stays one.  With one term and two: 4 nodes for each of 16 sequences of 2112 pairs, 8 heads of g 4, D 128, 27.4 us either way, 12 nodes 32.7
+// and 33.0, 64 nodes 60 and 70, D 64 40.3 and 40.5; 26 nodes of g 7 over 4160 pairs 53 and 57.
 __device__ __forceinline__ void two_terms(float a, float b, uint32_t& first, uint32_t& second) {
     first = __builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x07060302u);
     second = pack_bf16(fmaf(a, 1.f + 0x1p-20f, -__uint_as_float(__float_as_uint(a) & 0xffff0000u)), fmaf(b, 1.f + 0x1p-20f, -__uint_as_float(__float_as_uint(b) & 0xffff0000u)));
@@ -136,7 +138,7 @@ template <int TM> __device__ __forceinline__ void span_of(Ancestors<TM>& s, bool
 // Up to RB * 16 query rows: the wavefronts of a workgroup take tiles of KT pairs in turn, straight from memory into registers, each with its own
 // online softmax for all rows; they are merged through LDS at the end.  An operand of K or V serves a product for each 16 rows.  K and V of the next tile
 // are sent off when this one's products have read theirs.  Bound by the memory system: 4 nodes for each of 16 sequences of 2112 pairs, 8 heads of g 4, D 128
-// (142 MB) 27.4 us, 8 nodes 30.6; one sequence, whose splits hold 256 pairs each, by the latency of its loads and of the merge: 11.3.
+// (139 MB) 27.4 us, 8 nodes 30.6; one sequence, whose splits hold 256 pairs each, by the latency of its loads and of the merge: 11.6.
 // ---------------------------------------------------------------------------------------------------------
 template <typename T, int D, int RB> struct TreeCfg {
     static constexpr bool BF = sizeof(T) == 2;
@@ -565,10 +567,10 @@ __device__ __forceinline__ void tree_tile(const TreeParams& TP, int item, int sp
 // LDS: three places each for K and V, so that a tile's loads have two turns to arrive, one barrier a turn.  Layouts in LDS and the order of a
 // turn's steps - the next tile's logits beside this one's softmax - are those of prompt.h.
 // The compiler, which sees loads into LDS and reads of it, has to be told that they are of different places (the __restrict pointers of `turn`), or it waits for
-// all loads before the first read: with that, and two places instead of three, up to 256 rows over 2112 pairs took 70 us, so 61 to 67 from card to card.
+// all loads before the first read.
 // Bound by a turn's chain of LDS reads, products and exponentials, with two or three wavefronts a SIMD to fill its gaps (a turn of 64 pairs for 128 rows takes
-// 2.0 us with the CU to itself, 2.7 beside another workgroup; the products are 0.4): 64 nodes for each of 16 sequences of 16384 pairs, 8 heads of g 4, D 128, 356 us,
-// 773 TFLOP/s.  Matrix cores are busy a third of the time, LDS and vector units as long each; tiles of 32 pairs for 128 rows took 403 us.  Smaller calls spend as long
+// 2.1 us with the CU to itself, 3.1 beside another workgroup; the products are 0.64): 64 nodes for each of 16 sequences of 16384 pairs, 8 heads of g 4, D 128, 417 us,
+// 660 TFLOP/s.  Matrix cores are busy a third of the time, vector units as long.  Smaller calls spend as long
 // on a workgroup's start and the merge: 12 nodes over 16 rows of 2112 pairs 33 us, of which the pairs' way from memory is 22.
 // ---------------------------------------------------------------------------------------------------------
 template <typename T, int D, int CT_> struct WideCfg {

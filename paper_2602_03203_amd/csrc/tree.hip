@@ -22,10 +22,10 @@ __global__ __launch_bounds__(256, KIND == 1 && D == 64 ? 3 : 2) void tree_kernel
 
 // ---- host side ---------------------------------------------------------------------------------------------------
 // Which kernel takes a call's tiles, by the query rows of its largest tree (us, in the order of the kinds 16, 32, 64, 128 rows; 16 sequences of 2112
-// pairs, 8 heads of g 4, D 128 where nothing else is said): 16 rows 28.6, 29.2, 29.3; 32 rows -, 32.0, 31.3, of one sequence -, 14.7, 15.5;
-// 48 rows -, -, 34.2, 40.2; 128 rows of 4 sequences -, -, 22.2, 31.2; up to 182 rows of 16, 4 heads of g 7, 4160 pairs -, -, 53, 56; up to 256 rows of 16
-// -, -, 73, 62; up to 96 rows of 16 in pages, 1024 to 16384 pairs -, -, 158, 150: beyond 64 rows by the estimate below.  fp32, where products take longer than loads: 4 sequences, 32 rows 22, 29, 36; 56 rows 33, -, 40, 59; up
-// to 128 rows 63, -, 57, 66 - the first kind, tile by tile, up to 64 rows, then the third.
+// pairs, 8 heads of g 4, D 128 where nothing else is said): 16 rows 27.6, 28.8, 29.4, 43.0; 32 rows 33.9, 30.5, 31.9, 43.2, of one sequence 11.7, 15.0, 16.3, 25.0;
+// 48 rows 51.6, 39.8, 32.9, 48.7; up to 128 rows of 4 sequences 28.4, 23.5, 21.6, 33.4; up to 182 rows of 16, 4 heads of g 7, 4160 pairs 117, 84, 57, 63; up to 256 rows of 16
+// 167, 99, 73, 71; up to 96 rows of 16 in pages, 1024 to 16384 pairs 355, 221, 183, 158: beyond 64 rows by the estimate below.  fp32, where products take longer than loads:
+// 4 sequences, 32 rows 21.9 and, of the third kind, 34.5; 56 rows 32.3 and 38.1; up to 128 rows 51.1 and 52.8 - the first kind, tile by tile, up to 64 rows, then the third.
 struct TreePlan {
     int kind;                  // 16-row blocks of a tile
     TileGrid grid;
@@ -34,11 +34,11 @@ struct TreePlan {
 static long long items_of(const fk_paged_desc* d, const TileGrid& G) { return (long long)G.places * d->n_kv_heads; }
 
 // Splits of a tile's pairs, each 256 and more, where the items are few.  16 and 32 rows, bound by memory: up to 512 workgroups (16 rows, D 128: 128 items of 2112
-// pairs whole 31.2, in two 29.2, four 28.6; 8 items in four 13.9, eight 11.1, sixteen 12.4), D 64 up to 192 (128 items whole 18.3, in two 20.1).  Others by an
+// pairs whole 32.1, in two 28.5, four 27.7, eight 32.1; 8 items in four 14.1, eight 11.6), D 64 up to 192 (128 items whole 17.9, in two 17.8, four 16.7, eight 20.1).  Others by an
 // estimate: a turn of the loop takes `turn[k]` us with k + 1 workgroups on a CU, and records go out and come back at 4 TB/s (up to 182 rows of 4160 pairs, 192
-// items of 64 rows: whole 100, in two 68, three 61, four 53, five 67; up to 256 rows of 2112, 256 items of 128: 76, 62, 81, 77).  Sequences in pages differ in
+// items of 64 rows: whole 109, in two 72, three 69, four 57, six 73; up to 256 rows of 2112, 256 items of 128: 87, 71, 96, 89).  Sequences in pages differ in
 // length as a rule, which only the device knows: up to twice as many splits, of 512 pairs and more, even them out (16 sequences of 1024 to 16384 pairs, 8 heads: 16 rows
-// in four 127, eight 113; 32 rows 133 and 121; up to 96 rows 159 and 152).
+// in four 126, eight 111; 32 rows 132 and 119; up to 96 rows 173 and 158).
 // bound: the most splits of which rounding can make the estimate choose, for fewer pairs too (a split more costs records and saves turns: more pairs, more splits).
 static int tree_splits(const fk_paged_desc* d, int kind, long long items, long long pairs, bool uneven, double& least, bool bound = false) {
     const long long most = std::min((long long)kMostTreeSplits, pairs >> (uneven ? 9 : 8)), places = uneven ? 1024 : 512;
